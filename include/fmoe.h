@@ -14,7 +14,8 @@
  *    library only borrows them for the duration of the enqueued work.
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All work is
  *    enqueued asynchronously on it; no call synchronises with the host and no hot call
- *    (route / prune / permute / expert_ffn / combine / layer_forward) allocates memory.
+ *    (route / select_experts and its backward / prune / permute / expert_ffn / combine / layer_forward / quantize_weights
+ *    / dequantize_weights) allocates memory.
  *    Scratch comes from a caller-provided workspace sized by fmoe_workspace_bytes().  A hot call
  *    is a sequence of kernel launches and nothing else (no memset, no copy), so it can be
  *    captured into a HIP graph on `stream` and replayed.
@@ -98,6 +99,25 @@ typedef struct {
   double L_v;              /* vision tokens before pruning                                        */
 } fmoe_flops_model;
 
+/* Routing from logits (fmoe_select_experts). */
+typedef struct {
+  int32_t score;        /* 0: softmax over the experts; 1: sigmoid of each logit                          */
+  int32_t n_groups;     /* groups of E / n_groups neighbouring experts: 1 .. 16, a divisor of E; 1 = off  */
+  int32_t topk_groups;  /* groups of a token whose experts it may list: 1 .. n_groups                     */
+  int32_t group_score;  /* a group's score: 0 its largest key, 1 the sum of its two largest keys          */
+  float gate_scale;     /* factor of every gate, finite                                                   */
+} fmoe_select_params;
+
+/* A matrix [rows, K] (K the length of the reduction) in 4 bits: codes [rows, K/2] bytes, element 2i in the low
+ * half of byte i and element 2i+1 in the high half; scales [rows, ceil(K/32)] bytes, one for 32 neighbours of a row (the
+ * last group of a row may be shorter).  A code c stands for (c < 8 ? 1 : -1) * {0, 0.5, 1, 1.5, 2, 3, 4, 6}[c % 8], a
+ * scale byte e for 2^(e - 127) (255: NaN), the element for their product. */
+#define FMOE_QUANT_GROUP 32
+typedef struct {
+  const void* codes;
+  const uint8_t* scales;
+} fmoe_quant_tensor;
+
 typedef struct fmoe_ctx fmoe_ctx;
 
 /* Library version string, static storage. */
@@ -157,6 +177,32 @@ int fmoe_set_weights(fmoe_ctx* ctx, const void* router_w, const float* router_bi
                      const void* w_gate, const void* w_up, const void* w_down,
                      const void* ws_gate, const void* ws_up, const void* ws_down, void* stream);
 
+/* fmoe_set_weights with the expert matrices in 4 bits (fmoe_quant_tensor; bf16 contexts, else FMOE_ERR_UNSUPPORTED).
+ * router_w and router_bias as there; w_gate, w_up [E,S_m,H], w_down [E,H,S_m], ws_gate, ws_up [N_s,S_s,H], ws_down
+ * [N_s,H,S_s]: the last dimension is the one of the groups.  codes 16-byte aligned, scales at any address.  From then on
+ * fmoe_expert_ffn, fmoe_layer_forward and fmoe_stack_forward run on these weights, until one of the two calls registers
+ * others.  An element is a bf16 number exactly: the results are those of a bf16 context that is given the
+ * dequantized matrices, bit for bit.  (Elements that fp32 cannot hold, 2^128 and more, count as infinite.)
+ * The library keeps private copies in matrix-core operand order (4.25 bits a weight, padded as those of
+ * fmoe_set_weights; allocated by the first call, freed by fmoe_destroy): the caller's expert tensors may be freed or
+ * changed once the stream has drained. */
+int fmoe_set_weights_quant(fmoe_ctx* ctx, const void* router_w, const float* router_bias,
+                           const fmoe_quant_tensor* w_gate, const fmoe_quant_tensor* w_up,
+                           const fmoe_quant_tensor* w_down, const fmoe_quant_tensor* ws_gate,
+                           const fmoe_quant_tensor* ws_up, const fmoe_quant_tensor* ws_down, void* stream);
+
+/* Weights to 4 bits and back (no context: the current device).  w [rows, K] of `dtype` (fmoe_dtype), K % 8 == 0; codes
+ * and scales as in fmoe_quant_tensor; w and codes 16-byte aligned.
+ * fmoe_quantize_weights: with a the largest magnitude of a group, its scale is 2^(floor(log2 a) - 2) if saturate != 0
+ * (magnitudes above 6 scales, up to 8, become 6), else the least power of two with a <= 6 scales; at least 2^-126, and 1
+ * for a group of zeros.  Every element becomes the nearest code, ties the even one, with its sign.  A group that
+ * holds an infinity or NaN gets codes 0 and scale byte 255.
+ * fmoe_dequantize_weights: w = code * scale, exact in both types (beyond fp32's range: infinite). */
+int fmoe_quantize_weights(const void* w, int32_t dtype, int64_t rows, int32_t K, int32_t saturate, void* codes,
+                          uint8_t* scales, void* stream);
+int fmoe_dequantize_weights(const void* codes, const uint8_t* scales, int64_t rows, int32_t K, int32_t dtype, void* w,
+                            void* stream);
+
 /* Bytes of workspace that any hot call needs for up to max_tokens tokens in up to max_seqs
  * sequences with this context (for the Kmax current at the time of the call). [host] */
 size_t fmoe_workspace_bytes(const fmoe_ctx* ctx, int32_t max_tokens, int32_t max_seqs);
@@ -170,6 +216,33 @@ size_t fmoe_workspace_bytes(const fmoe_ctx* ctx, int32_t max_tokens, int32_t max
  * topk_gate [T,Kmax] fp32: P_j / sum of the listed P (or P_j if renormalize == 0), pad 0. */
 int fmoe_route(fmoe_ctx* ctx, const void* x, const uint8_t* is_visual, int32_t T, float* probs,
                int32_t* topk_idx, float* topk_gate, void* stream);
+
+/* Experts of each token from its router logits, for routers other than Eq.1-3: scores by softmax or sigmoid, a bias that
+ * takes part in the choice and not in the gates (load balance), groups of experts.  Needs no weights.
+ * logits [T,E] of logits_dtype (fmoe_dtype).  An expert with logit -inf or NaN is masked for the token; +inf counts
+ * as the largest finite fp32 number.  is_visual [T] or NULL (every token is text).  select_bias [E] fp32 or NULL; an expert
+ * with bias -inf or NaN is masked for every token (its logit still counts in the softmax).
+ * score s = softmax over the unmasked logits, or 1 / (1 + exp(-z)); key = s + select_bias in 64 bits, without
+ * select_bias the order of the logits.  With n_groups > 1 a token's experts come from its topk_groups groups of highest
+ * group_score (in 64 bits; ties: lower group).
+ * topk_idx [T,Kmax]: the k experts (k_visual / k_text of the context) of largest key, ordered by (key descending,
+ * index ascending), padded with -1 where k or the unmasked experts end.
+ * topk_gate [T,Kmax]: gate_scale * s / (sum of the listed s) with the context's renormalize, else gate_scale * s; 0 in
+ * padding.  The quotient is taken in logarithms: it is right also where the scores themselves underflow.
+ * scores [T,E] fp32 or NULL: s, 0 where the logit is masked (fmoe_prune takes them as probs).
+ * The outputs feed fmoe_permute and fmoe_combine as those of fmoe_route do.  fmoe_set_selection has no effect here. */
+int fmoe_select_experts(fmoe_ctx* ctx, const fmoe_select_params* params, const void* logits, int32_t logits_dtype,
+                        const uint8_t* is_visual, const float* select_bias, int32_t T, float* scores,
+                        int32_t* topk_idx, float* topk_gate, void* stream);
+
+/* Gradient of fmoe_select_experts with respect to the logits; the choice of experts is a constant, select_bias has none.
+ * logits, logits_dtype, params and the context's renormalize as in the forward call; topk_idx [T,Kmax] its output (distinct
+ * experts in a row; entries outside 0 .. E-1 are empty).  d_gate [T,Kmax] fp32: gradient of topk_gate (not
+ * looked at in empty places).  d_scores [T,E] fp32 or NULL: gradient of scores.
+ * d_logits [T,E] of logits_dtype, every element written; 0 for masked experts. */
+int fmoe_select_experts_backward(fmoe_ctx* ctx, const fmoe_select_params* params, const void* logits,
+                                 int32_t logits_dtype, const int32_t* topk_idx, const float* d_gate,
+                                 const float* d_scores, int32_t T, void* d_logits, void* stream);
 
 /* Sec. 3.2: window redundancy scores, budget, drop, compaction -- per sequence.
  * probs [T,E] fp32 from fmoe_route; cu_seqlens [B+1] int32 (cu[0] = 0, cu[B] = T; T > 0 with

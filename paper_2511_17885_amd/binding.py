@@ -17,6 +17,8 @@ LIB_PATH = os.path.join(_HERE, "libfmoe.so")
 
 FMOE_F32, FMOE_BF16 = 0, 1
 TOPK, RANDOMK, MINK = 0, 1, 2   # fmoe_set_selection strategies
+SOFTMAX, SIGMOID = 0, 1         # scores of fmoe_select_experts
+QUANT_GROUP = 32                # weights that share a scale (fmoe_quant_tensor)
 EXPORTS = ["fmoe_version", "fmoe_last_error", "fmoe_create", "fmoe_destroy", "fmoe_set_topk",
            "fmoe_set_selection",
            "fmoe_set_weights", "fmoe_workspace_bytes", "fmoe_route", "fmoe_prune", "fmoe_permute",
@@ -24,7 +26,8 @@ EXPORTS = ["fmoe_version", "fmoe_last_error", "fmoe_create", "fmoe_destroy", "fm
            "fmoe_profile_slots", "fmoe_profile_name", "fmoe_profile_read", "fmoe_adjacent_similarity",
            "fmoe_magnitude_stability", "fmoe_row_cosine", "fmoe_gate_cosine", "fmoe_flops_ratios",
            "fmoe_kept_counts", "fmoe_stage_retention", "fmoe_stack_plan", "fmoe_stack_workspace_bytes",
-           "fmoe_stack_forward", "fmoe_permute_noalloc", "fmoe_set_ffn_shape"]
+           "fmoe_stack_forward", "fmoe_permute_noalloc", "fmoe_set_ffn_shape", "fmoe_set_weights_quant",
+           "fmoe_quantize_weights", "fmoe_dequantize_weights", "fmoe_select_experts", "fmoe_select_experts_backward"]
 
 
 class FmoeConfig(C.Structure):
@@ -48,6 +51,15 @@ class FmoePruneParams(C.Structure):
 
 class FmoeLayerPlan(C.Structure):
     _fields_ = [("k_text", C.c_int32), ("k_visual", C.c_int32), ("prune", FmoePruneParams)]
+
+
+class FmoeSelectParams(C.Structure):
+    _fields_ = [("score", C.c_int32), ("n_groups", C.c_int32), ("topk_groups", C.c_int32), ("group_score", C.c_int32),
+                ("gate_scale", C.c_float)]
+
+
+class FmoeQuantTensor(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)]
 
 
 class FmoeError(RuntimeError):
@@ -78,6 +90,13 @@ def load():
     lib.fmoe_set_selection.argtypes = [vp, i32, i32, C.c_uint64]
     lib.fmoe_set_ffn_shape.argtypes = [vp, i32]
     lib.fmoe_set_weights.argtypes = [vp] + [vp] * 8 + [vp]
+    qt = C.POINTER(FmoeQuantTensor)
+    lib.fmoe_set_weights_quant.argtypes = [vp, vp, vp, qt, qt, qt, qt, qt, qt, vp]
+    lib.fmoe_quantize_weights.argtypes = [vp, i32, C.c_int64, i32, i32, vp, vp, vp]
+    lib.fmoe_dequantize_weights.argtypes = [vp, vp, C.c_int64, i32, i32, vp, vp]
+    sp = C.POINTER(FmoeSelectParams)
+    lib.fmoe_select_experts.argtypes = [vp, sp, vp, i32, vp, vp, i32, vp, vp, vp, vp]
+    lib.fmoe_select_experts_backward.argtypes = [vp, sp, vp, i32, vp, vp, vp, i32, vp, vp]
     lib.fmoe_workspace_bytes.argtypes = [vp, i32, i32]
     lib.fmoe_workspace_bytes.restype = sz
     lib.fmoe_route.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp]
@@ -135,6 +154,53 @@ def _stream():
 def prune_params(retention=1.0, window=1, alpha=1.0, gamma=0.0, sim_mode=0, prune_mode=1, merge_mode=0):
     return FmoePruneParams(float(retention), int(window), float(alpha), float(gamma), int(sim_mode),
                            int(prune_mode), int(merge_mode))
+
+
+def select_params(score="softmax", n_groups=1, topk_groups=1, group_score=0, gate_scale=1.0):
+    """Routing of fmoe_select_experts.  score: "softmax" / "sigmoid" (or SOFTMAX / SIGMOID)."""
+    score = {"softmax": SOFTMAX, "sigmoid": SIGMOID}.get(score, score)
+    return FmoeSelectParams(int(score), int(n_groups), int(topk_groups), int(group_score), float(gate_scale))
+
+
+def _float_type(t, what):
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{what} must be float32 or bfloat16, not {t.dtype}")
+    return FMOE_BF16 if t.dtype == torch.bfloat16 else FMOE_F32
+
+
+def _expect(t, what, dtype, shape):
+    """The library takes plain pointers: a tensor of another type or shape would be read past its end."""
+    if t is None:
+        return
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+
+
+def quantize_weights(w, saturate=True):
+    """Weights [..., K] (float32 or bfloat16) to 4 bits in groups of 32 along K (fmoe_quantize_weights).  Returns (codes
+    [..., K/2] uint8, scales [..., ceil(K/32)] uint8)."""
+    dtype = _float_type(w, "w")
+    if not w.is_contiguous():
+        raise ValueError("w must be contiguous")
+    K = w.shape[-1]
+    codes = torch.empty((*w.shape[:-1], K // 2), dtype=torch.uint8, device=w.device)
+    scales = torch.empty((*w.shape[:-1], (K + QUANT_GROUP - 1) // QUANT_GROUP), dtype=torch.uint8, device=w.device)
+    with torch.cuda.device(w.device):
+        _check(load().fmoe_quantize_weights(_ptr(w), dtype, w.numel() // max(K, 1), K, int(bool(saturate)), _ptr(codes),
+                                            _ptr(scales), _stream()))
+    return codes, scales
+
+
+def dequantize_weights(codes, scales, dtype=torch.bfloat16):
+    """The weights [..., K] that codes [..., K/2] and scales [..., ceil(K/32)] stand for (fmoe_dequantize_weights)."""
+    K = codes.shape[-1] * 2
+    _expect(codes, "codes", torch.uint8, codes.shape)
+    _expect(scales, "scales", torch.uint8, (*codes.shape[:-1], (K + QUANT_GROUP - 1) // QUANT_GROUP))
+    w = torch.empty((*codes.shape[:-1], K), dtype=dtype, device=codes.device)
+    with torch.cuda.device(w.device):
+        _check(load().fmoe_dequantize_weights(_ptr(codes), _ptr(scales), w.numel() // max(K, 1), K,
+                                              _float_type(w, "w"), _ptr(w), _stream()))
+    return w
 
 
 class FMoE:
@@ -199,6 +265,27 @@ class FMoE:
             torch.cuda.current_stream().synchronize()
             self._weights = (router_bias,)
 
+    def set_weights_quant(self, router_w, router_bias, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None):
+        """fmoe_set_weights_quant: every expert matrix as (codes, scales) (quantize_weights).  The context copies them; the
+        pairs may be dropped at any time (the binding holds on to the router alone)."""
+        c = self.cfg
+        E, H, S, N, Ss = c.n_experts, c.d_model, c.d_ffn, c.n_shared, c.d_ffn_shared
+        _expect(router_w, "router_w", self.torch_dtype, (E, H))
+        _expect(router_bias, "router_bias", torch.float32, (E,))
+        names = ("w_gate", "w_up", "w_down", "ws_gate", "ws_up", "ws_down")
+        shapes = ((E, S, H), (E, S, H), (E, H, S), (N, Ss, H), (N, Ss, H), (N, H, Ss))
+        pairs = (w_gate, w_up, w_down, ws_gate, ws_up, ws_down)
+        tensors = []
+        for pair, name, (g, n, K) in zip(pairs, names, shapes):
+            if pair is None:
+                tensors.append(None)
+                continue
+            _expect(pair[0], f"codes of {name}", torch.uint8, (g, n, K // 2))
+            _expect(pair[1], f"scales of {name}", torch.uint8, (g, n, (K + QUANT_GROUP - 1) // QUANT_GROUP))
+            tensors.append(C.byref(FmoeQuantTensor(pair[0].data_ptr(), pair[1].data_ptr())))
+        self._weights = (router_w, router_bias)
+        _check(self.lib.fmoe_set_weights_quant(self._ctx, _ptr(router_w), _ptr(router_bias), *tensors, _stream()))
+
     def workspace_bytes(self, max_tokens, max_seqs=1):
         return int(self.lib.fmoe_workspace_bytes(self._ctx, max_tokens, max_seqs))
 
@@ -234,6 +321,34 @@ class FMoE:
         _check(self.lib.fmoe_route(self._ctx, _ptr(x), _ptr(is_visual), T, _ptr(probs), _ptr(idx),
                                    _ptr(gate), _stream()))
         return probs, idx[:, :self.kmax], gate[:, :self.kmax]
+
+    def select_experts(self, params, logits, is_visual=None, select_bias=None, want_scores=False):
+        """fmoe_select_experts on logits [T, E] (float32 or bfloat16).  Returns (scores or None, topk_idx, topk_gate)."""
+        T = logits.shape[0]
+        K = max(self.kmax, 1)
+        dtype = _float_type(logits, "logits")
+        _expect(logits, "logits", logits.dtype, (T, self.E))
+        _expect(is_visual, "is_visual", torch.uint8, (T,))
+        _expect(select_bias, "select_bias", torch.float32, (self.E,))
+        scores = self._f32(T, self.E) if want_scores else None
+        idx, gate = self._i32(T, K), self._f32(T, K)
+        _check(self.lib.fmoe_select_experts(self._ctx, C.byref(params), _ptr(logits), dtype, _ptr(is_visual),
+                                            _ptr(select_bias), T, _ptr(scores), _ptr(idx), _ptr(gate), _stream()))
+        return scores, idx[:, :self.kmax], gate[:, :self.kmax]
+
+    def select_experts_backward(self, params, logits, topk_idx, d_gate, d_scores=None):
+        """fmoe_select_experts_backward: the gradient of the logits from those of topk_gate [T, kmax] and, if given, of
+        scores [T, E]."""
+        T = logits.shape[0]
+        dtype = _float_type(logits, "logits")
+        _expect(logits, "logits", logits.dtype, (T, self.E))
+        _expect(topk_idx, "topk_idx", torch.int32, (T, self.kmax))
+        _expect(d_gate, "d_gate", torch.float32, (T, self.kmax))
+        _expect(d_scores, "d_scores", torch.float32, (T, self.E))
+        d_logits = torch.empty_like(logits)
+        _check(self.lib.fmoe_select_experts_backward(self._ctx, C.byref(params), _ptr(logits), dtype, _ptr(topk_idx),
+                                                     _ptr(d_gate), _ptr(d_scores), T, _ptr(d_logits), _stream()))
+        return d_logits
 
     def prune(self, params, probs, is_visual, cu_seqlens, attn=None, want_scores=False, x=None):
         """Returns (kept_idx, new_cu_seqlens, scores or None); with window merging (params.gamma > 0,

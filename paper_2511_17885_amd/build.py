@@ -24,6 +24,9 @@ SOURCES = {
     "prune.hip": ["-ffp-contract=off"],
     "permute.hip": [],
     "ffn.hip": [],
+    "ffn_quant.hip": [],
+    "select.hip": [],
+    "quant.hip": [],
     "combine.hip": [],
     "diag.hip": [],
     "stack.hip": [],

@@ -1,7 +1,8 @@
 // C-ABI entry points: argument validation, workspace carve-up, kernel sequencing.
-// No entry point other than fmoe_set_weights (private router copy; packed expert weights of bf16
-// contexts) allocates device memory, and none synchronises with the host.
+// No entry point other than fmoe_set_weights and fmoe_set_weights_quant (private router copy; packed expert weights of
+// bf16 contexts) allocates device memory, and none synchronises with the host.
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -66,6 +67,40 @@ int check_prune(const fmoe_prune_params* p) {
     return fmoe_fail(FMOE_ERR_INVALID_ARG, "prune: sim_mode %d", p->sim_mode);
   if (p->prune_mode < 0 || p->prune_mode > 2)
     return fmoe_fail(FMOE_ERR_INVALID_ARG, "prune: prune_mode %d", p->prune_mode);
+  return FMOE_OK;
+}
+
+int check_select(const fmoe_ctx* ctx, const fmoe_select_params* p, int32_t logits_dtype, const char* who) {
+  const int E = ctx->cfg.n_experts;
+  if (p->score != 0 && p->score != 1)
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: score %d is neither 0 (softmax) nor 1 (sigmoid)", who, p->score);
+  if (p->n_groups < 1 || E % p->n_groups != 0)
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: n_groups %d does not divide E = %d", who, p->n_groups, E);
+  if (p->n_groups > FMOE_MAX_GROUPS)
+    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "%s: n_groups %d > %d", who, p->n_groups, FMOE_MAX_GROUPS);
+  if (p->topk_groups < 1 || p->topk_groups > p->n_groups)
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: topk_groups %d outside 1..%d", who, p->topk_groups, p->n_groups);
+  if (p->group_score != 0 && p->group_score != 1)
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: group_score %d is neither 0 (largest) nor 1 (sum of two)", who, p->group_score);
+  if (!std::isfinite(p->gate_scale)) return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: gate_scale is not finite", who);
+  if (logits_dtype != FMOE_F32 && logits_dtype != FMOE_BF16)
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: dtype %d is neither FMOE_F32 nor FMOE_BF16", who, logits_dtype);
+  return FMOE_OK;
+}
+
+// Arguments of the two conversions of weights in 4 bits
+int check_quant(const void* w, int32_t dtype, int64_t rows, int32_t K, const void* codes, const uint8_t* scales,
+                const char* who) {
+  if (dtype != FMOE_F32 && dtype != FMOE_BF16)
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: dtype %d is neither FMOE_F32 nor FMOE_BF16", who, dtype);
+  if (rows < 0 || K <= 0) return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: rows %lld, K %d", who, (long long)rows, K);
+  if (K % 8) return fmoe_fail(FMOE_ERR_UNSUPPORTED, "%s: K %d is not a multiple of 8", who, K);
+  if (K > (1 << 24) || rows > ((int64_t)1 << 40) / K)
+    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "%s: %lld x %d elements", who, (long long)rows, K);
+  if (rows == 0) return FMOE_OK;
+  if (!w || !codes || !scales) return fmoe_fail(FMOE_ERR_NULL_PTR, "%s: w / codes / scales is NULL", who);
+  if (!aligned16(w) || !aligned16(codes))
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: w / codes not 16-byte aligned", who);
   return FMOE_OK;
 }
 
@@ -179,6 +214,8 @@ void fmoe_destroy(fmoe_ctx* ctx) {
   void* packed[4] = {ctx->pk_gate_up, ctx->pk_down, ctx->pk_sgate_up, ctx->pk_sdown};
   for (void* p : packed)
     if (p) (void)hipFree(p);
+  for (void* p : ctx->pq)
+    if (p) (void)hipFree(p);
   delete ctx;
 }
 
@@ -217,6 +254,22 @@ int fmoe_set_ffn_shape(fmoe_ctx* ctx, int32_t shape) {
   return FMOE_OK;
 }
 
+namespace {
+// The router's part of registering weights; the context has none until the caller has registered the rest.
+int set_router(fmoe_ctx* ctx, const void* router_w, const float* router_bias, hipStream_t stream) {
+  ctx->weights_set = false;
+  ctx->router_w = router_w;
+  if (!ctx->router_wp) {
+    FMOE_HIP_CHECK(hipSetDevice(ctx->device));
+    FMOE_HIP_CHECK(hipMalloc(reinterpret_cast<void**>(&ctx->router_wp), router_pack_floats(ctx) * sizeof(float)));
+  }
+  const int rc = launch_pack_router(ctx, router_w, ctx->router_wp, stream);
+  if (rc != FMOE_OK) return rc;
+  ctx->router_bias = router_bias;
+  return FMOE_OK;
+}
+}  // namespace
+
 int fmoe_set_weights(fmoe_ctx* ctx, const void* router_w, const float* router_bias,
                      const void* w_gate, const void* w_up, const void* w_down, const void* ws_gate,
                      const void* ws_up, const void* ws_down, void* stream) {
@@ -233,15 +286,8 @@ int fmoe_set_weights(fmoe_ctx* ctx, const void* router_w, const float* router_bi
   const void* ptrs[] = {router_w, router_bias, w_gate, w_up, w_down, ws_gate, ws_up, ws_down};
   for (const void* p : ptrs)
     if (p && !aligned16(p)) return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_set_weights: pointer %p not 16-byte aligned", p);
-  ctx->weights_set = false;
-  ctx->router_w = router_w;
-  if (!ctx->router_wp) {
-    FMOE_HIP_CHECK(hipSetDevice(ctx->device));
-    FMOE_HIP_CHECK(hipMalloc(reinterpret_cast<void**>(&ctx->router_wp), router_pack_floats(ctx) * sizeof(float)));
-  }
-  rc = launch_pack_router(ctx, router_w, ctx->router_wp, static_cast<hipStream_t>(stream));
-  if (rc != FMOE_OK) return rc;
-  ctx->router_bias = router_bias;
+  if ((rc = set_router(ctx, router_w, router_bias, static_cast<hipStream_t>(stream))) != FMOE_OK) return rc;
+  ctx->quant = false;
   ctx->w_gate = w_gate; ctx->w_up = w_up; ctx->w_down = w_down;
   ctx->ws_gate = ws_gate; ctx->ws_up = ws_up; ctx->ws_down = ws_down;
   if (ctx->cfg.dtype == FMOE_BF16) {
@@ -254,6 +300,53 @@ int fmoe_set_weights(fmoe_ctx* ctx, const void* router_w, const float* router_bi
   }
   ctx->weights_set = true;
   return FMOE_OK;
+}
+
+int fmoe_set_weights_quant(fmoe_ctx* ctx, const void* router_w, const float* router_bias,
+                           const fmoe_quant_tensor* w_gate, const fmoe_quant_tensor* w_up,
+                           const fmoe_quant_tensor* w_down, const fmoe_quant_tensor* ws_gate,
+                           const fmoe_quant_tensor* ws_up, const fmoe_quant_tensor* ws_down, void* stream) {
+  int rc = check_ctx(ctx, false);
+  if (rc != FMOE_OK) return rc;
+  if (ctx->cfg.dtype != FMOE_BF16)
+    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "fmoe_set_weights_quant: 4-bit weights need a bf16 context");
+  const bool has_shared = ctx->cfg.n_shared > 0;
+  if (!has_shared && (ws_gate || ws_up || ws_down))
+    return fmoe_fail(FMOE_ERR_BAD_SHAPE, "fmoe_set_weights_quant: shared-expert weights given but n_shared = 0");
+  const fmoe_quant_tensor* const w[6] = {w_gate, w_up, w_down, ws_gate, ws_up, ws_down};
+  for (int i = 0; i < (has_shared ? 6 : 3); ++i) {
+    if (!w[i] || !w[i]->codes || !w[i]->scales)
+      return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_set_weights_quant: a weight matrix, its codes or its scales are NULL");
+    if (!aligned16(w[i]->codes))
+      return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_set_weights_quant: codes %p not 16-byte aligned", w[i]->codes);
+  }
+  if (!router_w) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_set_weights_quant: router_w is NULL");
+  if (!aligned16(router_w) || !aligned16(router_bias))
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_set_weights_quant: router_w / router_bias not 16-byte aligned");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((rc = set_router(ctx, router_w, router_bias, s)) != FMOE_OK) return rc;
+  for (int i = 0; i < 4; ++i) {
+    const size_t bytes = fmoe_quant_bytes(ctx, i, nullptr);
+    if (bytes && !ctx->pq[i]) FMOE_HIP_CHECK(hipMalloc(&ctx->pq[i], bytes));
+  }
+  if ((rc = launch_pack_quant(ctx, w, s)) != FMOE_OK) return rc;
+  ctx->quant = true;
+  ctx->weights_set = true;
+  return FMOE_OK;
+}
+
+int fmoe_quantize_weights(const void* w, int32_t dtype, int64_t rows, int32_t K, int32_t saturate, void* codes,
+                          uint8_t* scales, void* stream) {
+  const int rc = check_quant(w, dtype, rows, K, codes, scales, "fmoe_quantize_weights");
+  if (rc != FMOE_OK || rows == 0) return rc;
+  return launch_quantize(w, dtype, rows, K, saturate != 0, codes, scales, static_cast<hipStream_t>(stream));
+}
+
+int fmoe_dequantize_weights(const void* codes, const uint8_t* scales, int64_t rows, int32_t K, int32_t dtype, void* w,
+                            void* stream) {
+  const int rc = check_quant(w, dtype, rows, K, codes, scales, "fmoe_dequantize_weights");
+  if (rc != FMOE_OK || rows == 0) return rc;
+  return launch_dequantize(codes, scales, rows, K, dtype, w, static_cast<hipStream_t>(stream));
 }
 
 size_t fmoe_workspace_bytes(const fmoe_ctx* ctx, int32_t max_tokens, int32_t max_seqs) {
@@ -273,6 +366,42 @@ int fmoe_route(fmoe_ctx* ctx, const void* x, const uint8_t* is_visual, int32_t T
   if (!aligned16(x)) return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_route: x not 16-byte aligned");
   return launch_route(ctx, x, is_visual, T, probs, topk_idx, topk_gate, fmoe_ordinals_job{},
                       static_cast<hipStream_t>(stream));
+}
+
+int fmoe_select_experts(fmoe_ctx* ctx, const fmoe_select_params* params, const void* logits, int32_t logits_dtype,
+                        const uint8_t* is_visual, const float* select_bias, int32_t T, float* scores,
+                        int32_t* topk_idx, float* topk_gate, void* stream) {
+  int rc = check_ctx(ctx, false);
+  if (rc != FMOE_OK) return rc;
+  if (!params) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_select_experts: params is NULL");
+  if ((rc = check_select(ctx, params, logits_dtype, "fmoe_select_experts")) != FMOE_OK) return rc;
+  if ((rc = check_tokens(T)) != FMOE_OK) return rc;
+  if (T == 0) return FMOE_OK;
+  if (!logits) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_select_experts: logits is NULL");
+  if (ctx->kmax > 0 && (!topk_idx || !topk_gate))
+    return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_select_experts: topk_idx / topk_gate is NULL");
+  if (!aligned16(logits) || !aligned16(scores) || !aligned16(select_bias))
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_select_experts: logits / scores / select_bias not 16-byte aligned");
+  return launch_select(ctx, params, logits, logits_dtype, is_visual, select_bias, T, scores, topk_idx, topk_gate,
+                       static_cast<hipStream_t>(stream));
+}
+
+int fmoe_select_experts_backward(fmoe_ctx* ctx, const fmoe_select_params* params, const void* logits,
+                                 int32_t logits_dtype, const int32_t* topk_idx, const float* d_gate,
+                                 const float* d_scores, int32_t T, void* d_logits, void* stream) {
+  int rc = check_ctx(ctx, false);
+  if (rc != FMOE_OK) return rc;
+  if (!params) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_select_experts_backward: params is NULL");
+  if ((rc = check_select(ctx, params, logits_dtype, "fmoe_select_experts_backward")) != FMOE_OK) return rc;
+  if ((rc = check_tokens(T)) != FMOE_OK) return rc;
+  if (T == 0) return FMOE_OK;
+  if (!logits || !d_logits) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_select_experts_backward: logits / d_logits is NULL");
+  if (ctx->kmax > 0 && (!topk_idx || !d_gate))
+    return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_select_experts_backward: topk_idx / d_gate is NULL");
+  if (!aligned16(logits) || !aligned16(d_scores) || !aligned16(d_logits))
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_select_experts_backward: logits / d_scores / d_logits not 16-byte aligned");
+  return launch_select_backward(ctx, params, logits, logits_dtype, topk_idx, d_gate, d_scores, T, d_logits,
+                                static_cast<hipStream_t>(stream));
 }
 
 int fmoe_prune(fmoe_ctx* ctx, const fmoe_prune_params* params, const float* probs,

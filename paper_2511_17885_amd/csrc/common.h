@@ -10,6 +10,7 @@
 #define FMOE_MAX_EXPERTS 256
 #define FMOE_MAX_TOPK 16
 #define FMOE_MAX_WINDOW 64
+#define FMOE_MAX_GROUPS 16       // expert groups in fmoe_select_experts
 #define FMOE_PERM_BLOCK 256   // kept positions per block in the permutation kernels
 #define FMOE_ROUTE_DISPATCH_TOKENS 16   // tokens up to which the router's one block does the dispatch too
 #define FMOE_TILE_M 64        // rows per grouped-GEMM tile (tile list granularity)
@@ -65,6 +66,8 @@ struct fmoe_ctx {
   const void *ws_gate, *ws_up, *ws_down;
   // bf16 contexts: private copies of the expert weights in matrix-core operand order (ffn.hip)
   void *pk_gate_up, *pk_down, *pk_sgate_up, *pk_sdown;
+  void* pq[4];               // the same of 4-bit weights (ffn_quant.hip): gate/up, down, shared gate/up, shared down
+  bool quant;                // the weights in force are the 4-bit ones
   bool weights_set;
   int sel_strategy, sel_k_base;   // selection-strategy ablation (fmoe_set_selection); 0 = off
   unsigned long long sel_seed;
@@ -128,6 +131,11 @@ struct fmoe_ffn_geom {
 fmoe_ffn_geom fmoe_geom(const fmoe_ctx* ctx, int n_cap);
 size_t fmoe_packed_bytes(const fmoe_ctx* ctx, int which);   // 0 gate/up, 1 down, 2 shared gate/up, 3 shared down
 int launch_pack_experts(fmoe_ctx* ctx, hipStream_t stream);
+// bytes of the packed 4-bit weights of matrix `which` (as above) and, if asked for, how many of them are codes
+size_t fmoe_quant_bytes(const fmoe_ctx* ctx, int which, size_t* codes);
+int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStream_t stream);
+int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* perm_src, void* y,
+                  void* y_shared, char* base, const fmoe_ws_layout& L, const fmoe_ffn_geom& geo, hipStream_t stream);
 
 // ---- kernel launchers (each returns a fmoe_status; all work goes to `stream`)
 size_t router_pack_floats(const fmoe_ctx* ctx);
@@ -206,6 +214,18 @@ int launch_expert_ffn(const fmoe_ctx* ctx, const void* x, const int32_t* kept_id
 int launch_combine(const fmoe_ctx* ctx, const void* y, const void* y_shared, const int32_t* inv_perm,
                    const float* topk_gate, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,
                    int n_expected, const void* residual, void* out, hipStream_t stream);
+
+// ---- routing from logits (select.hip), weights in 4 bits (quant.hip)
+int launch_select(const fmoe_ctx* ctx, const fmoe_select_params* p, const void* logits, int dtype,
+                  const uint8_t* is_visual, const float* bias, int T, float* scores, int32_t* topk_idx,
+                  float* topk_gate, hipStream_t stream);
+int launch_select_backward(const fmoe_ctx* ctx, const fmoe_select_params* p, const void* logits, int dtype,
+                           const int32_t* topk_idx, const float* d_gate, const float* d_scores, int T, void* d_logits,
+                           hipStream_t stream);
+int launch_quantize(const void* w, int dtype, long long rows, int K, int saturate, void* codes, uint8_t* scales,
+                    hipStream_t stream);
+int launch_dequantize(const void* codes, const uint8_t* scales, long long rows, int K, int dtype, void* w,
+                      hipStream_t stream);
 
 // ---- diagnostics (diag.hip)
 int launch_adjacent_similarity(const float* probs, const uint8_t* is_visual, const int32_t* cu, int B, int T,

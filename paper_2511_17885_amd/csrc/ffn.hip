@@ -1572,7 +1572,9 @@ int launch_expert_ffn(const fmoe_ctx* ctx, const void* x, const int32_t* kept_id
                        reinterpret_cast<int32_t*>(base + L.tile_count));
   }
   int rc;
-  if (c.dtype == FMOE_BF16)
+  if (ctx->quant)
+    rc = run_ffn_quant(ctx, x, kept_idx, n_cap, perm_src, y, y_shared, base, L, geo, stream);
+  else if (c.dtype == FMOE_BF16)
     rc = run_ffn_bf16(ctx, x, kept_idx, n_cap, perm_src, y, y_shared, base, L, geo, stream);
   else
     rc = run_ffn_f32(ctx, x, kept_idx, n_cap, perm_src, y, y_shared, base, L, geo, stream);

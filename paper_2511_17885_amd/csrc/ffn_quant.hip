@@ -1,0 +1,329 @@
+// The expert FFNs of Eq.4 with weights in 4 bits (quant.hip: +-{0, .5, 1, 1.5, 2, 3, 4, 6} times a power of two per 32
+// values along the reduction), activations in bf16.
+//
+// A weight is a bf16 number exactly, so the products are those of the bf16 kernels: a wavefront turns eight codes into an
+// operand of v_mfma_f32_16x16x32_bf16 by four conversion instructions that apply the scale as well, and the matrix
+// instruction does the rest, in the same order of k.  A context with 4-bit weights gives the same bits as a bf16 context
+// that is given the dequantized ones.
+//
+// Packing (fmoe_set_weights_quant, matrix-core operand order as in ffn.hip): of a column block (16 features, gate and up;
+// or 32 output features) and a k tile of 64, lane l has one 16-byte unit: word 2s + f = the eight codes of k step s and
+// fragment f that the bf16 packing holds as 16 bytes.  The scales of a k tile, the same four of each column, are a word,
+// and four k tiles' words are one 16-byte unit per column: 17 bits per four weights in two linear streams.
+
+#include "ffn_dev.h"
+
+namespace {
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+struct QuantProblem {
+  StreamProblem s;            // Bp: codes, group_stride in 16-byte units
+  const u32x4_t* Sp;          // scales
+  long long scale_stride;     // 16-byte units between groups
+};
+
+struct QuantArgs {
+  QuantProblem p0, p1;        // routed experts; shared group (tile.group >= E)
+  int E;
+  const fmoe_tile* tiles;
+  const int32_t* n_tiles;     // device
+  int cols;                   // work items per tile entry in this launch
+};
+
+__host__ __device__ inline int quant_tiles(int K) { return (K + SBK - 1) / SBK; }
+__host__ __device__ inline int quant_scale_tiles(int K) { return (quant_tiles(K) + 3) / 4; }
+
+// Eight codes times the scale in byte I of `scales`.
+template <int I>
+__device__ __forceinline__ bf16x8_t dequantize(uint32_t codes, uint32_t scales) {
+  const uint32_t e = (I == 0 ? scales << 23 : I == 1 ? scales << 15 : I == 2 ? scales << 7 : scales >> 1) & 0x7f800000u;
+  const float s = __uint_as_float(e);
+  const u32x4_t v = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3))};
+  return __builtin_bit_cast(bf16x8_t, v);
+}
+
+// One wavefront, one column block, sixteen rows: codes, scales and rows straight into registers in matrix order, no LDS and
+// no barrier.  Rows past the tile reuse its last one, row indices are clamped as in gather_offsets.
+constexpr int THIN_ROWS = 16;
+constexpr int THIN_SLOTS = 8;   // k tiles (64 wide) in flight
+
+template <bool SWIGLU>
+__device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, const fmoe_tile& tile, int group, int cb) {
+  constexpr int S = THIN_SLOTS;
+  static_assert(S % 4 == 0, "a unit of scales serves four k tiles");
+  const StreamProblem& P = Q.s;
+  const int lane = threadIdx.x;
+  const int K = P.K, N = P.N;
+  const int NT = quant_tiles(K), NT4 = quant_scale_tiles(K);
+  const __amdgpu_buffer_rsrc_t b_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<u32x4_t*>(P.Bp) + (size_t)group * P.group_stride + (size_t)(cb >> 2) * NT * 256 + (cb & 3) * 64, 0,
+      0xffffffff, 0x00020000);
+  const __amdgpu_buffer_rsrc_t s_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<u32x4_t*>(Q.Sp) + (size_t)group * Q.scale_stride + (size_t)(cb >> 2) * NT4 * 64 + (cb & 3) * 16, 0,
+      0xffffffff, 0x00020000);
+  const __amdgpu_buffer_rsrc_t a_rsrc =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(P.A), 0, 0xffffffff, 0x00020000);
+  const uint32_t lane16 = (uint32_t)lane * 16u, column16 = (uint32_t)(lane & 15) * 16u;
+  const int kq = (lane >> 4) * 8;
+  u32x4_t breg[S], sreg[S / 4], areg[S][2];
+  auto load_b = [&](int slot, int t) {   // past the last tile the last one again
+    breg[slot] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane16, (t < NT ? t : NT - 1) * 4096, 0);
+  };
+  auto load_s = [&](int slot, int t4) {
+    sreg[slot] = __builtin_amdgcn_raw_buffer_load_b128(s_rsrc, column16, (t4 < NT4 ? t4 : NT4 - 1) * 1024, 0);
+  };
+  uint32_t a_row;   // byte offset of the lane's row
+  auto load_a = [&](int slot, int t) {   // k past K re-reads the row's end, where the packed weights are zero
+    const int k0 = (t < NT ? t : NT - 1) * SBK;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int k = k0 + s * 32 + kq;
+      areg[slot][s] = __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, a_row + (uint32_t)(k < K ? k : K - 8) * 2u, 0, 0);
+    }
+  };
+  const uint32_t a_max_row = 0xffffffffu / ((uint32_t)P.lda * 2u) - 1u;
+  int src = tile.row0 + ((lane & 15) < tile.rows ? (lane & 15) : tile.rows - 1);
+  if (P.map1) src = P.map1[src];
+  if (P.map1 && P.map1_limit > 0) src = src < 0 ? 0 : (src >= P.map1_limit ? P.map1_limit - 1 : src);
+  if (P.map2) src = P.map2[src];
+  a_row = ((uint32_t)src < a_max_row ? (uint32_t)src : a_max_row) * (uint32_t)P.lda * 2u;
+#pragma unroll
+  for (int t = 0; t < S; ++t) {
+    if (t % 4 == 0) load_s(t / 4, t / 4);
+    load_b(t, t);
+    load_a(t, t);
+  }
+
+  f32x4_t acc[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
+  auto multiply = [&](int slot) {
+    const uint32_t sc = sreg[slot / 4][slot % 4];
+    const bf16x8_t a0 = __builtin_bit_cast(bf16x8_t, areg[slot][0]), a1 = __builtin_bit_cast(bf16x8_t, areg[slot][1]);
+    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, dequantize<0>(breg[slot][0], sc), acc[0], 0, 0, 0);
+    acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, dequantize<1>(breg[slot][1], sc), acc[1], 0, 0, 0);
+    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, dequantize<2>(breg[slot][2], sc), acc[0], 0, 0, 0);
+    acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, dequantize<3>(breg[slot][3], sc), acc[1], 0, 0, 0);
+  };
+  int t0 = 0;
+  for (; t0 + S <= NT; t0 += S) {
+#pragma unroll
+    for (int u = 0; u < S; ++u) {
+      multiply(u);
+      load_b(u, t0 + u + S);
+      load_a(u, t0 + u + S);
+      if (u % 4 == 3) load_s(u / 4, (t0 + S) / 4 + u / 4);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < S - 1; ++u)
+    if (t0 + u < NT) multiply(u);   // uniform
+  // accumulator register v of lane l: row 4*(l/16) + v, column l%16
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const int row = 4 * (lane >> 4) + v;
+    if (row >= tile.rows) continue;
+    bf16_t* crow = P.C + (size_t)(tile.row0 + row) * P.ldc;
+    if (SWIGLU) {
+      const int col = cb * 16 + (lane & 15);
+      if (col < N) crow[col] = f32_to_bf16(silu_mul_bf16(acc[0][v], acc[1][v]));
+    } else {
+      const int col = cb * 32 + (lane & 15);
+      if (col < N) crow[col] = f32_to_bf16(acc[0][v]);
+      if (col + 16 < N) crow[col + 16] = f32_to_bf16(acc[1][v]);
+    }
+  }
+}
+
+// field by field, so that the descriptors stay in scalar registers
+__device__ __forceinline__ QuantProblem select_problem(const QuantArgs& a, bool shared) {
+  QuantProblem Q;
+#define FMOE_SEL(f) Q.f = shared ? a.p1.f : a.p0.f
+  FMOE_SEL(s.A); FMOE_SEL(s.lda); FMOE_SEL(s.map1); FMOE_SEL(s.map2); FMOE_SEL(s.map1_limit); FMOE_SEL(s.Bp);
+  FMOE_SEL(s.group_stride); FMOE_SEL(s.nbw); FMOE_SEL(s.ks); FMOE_SEL(s.C); FMOE_SEL(s.ldc); FMOE_SEL(s.N);
+  FMOE_SEL(s.K); FMOE_SEL(s.n_col_tiles); FMOE_SEL(s.a_group_off); FMOE_SEL(s.c_group_off); FMOE_SEL(Sp);
+  FMOE_SEL(scale_stride);
+#undef FMOE_SEL
+  return Q;
+}
+
+// Item -> (tile entry, column block), a.cols = column blocks per entry in the launch.
+template <bool SWIGLU>
+__global__ __launch_bounds__(64, 2) void ffn_quant_thin_kernel(QuantArgs a) {
+  const int ti = (int)blockIdx.x / a.cols;
+  if (ti >= *a.n_tiles) return;
+  fmoe_tile tile = load_entry(a.tiles, ti);
+  take_row_tile(tile, tile.rt, SBM);
+  const bool shared = tile.group >= a.E;
+  QuantProblem Q = select_problem(a, shared);
+  const int cb = tile.col0 * 4 + ((int)blockIdx.x - ti * a.cols);
+  if (cb >= Q.s.nbw) return;
+  const int group = shared ? tile.group - a.E : tile.group;
+  if (shared) {   // per-shared-expert slices of the hidden buffer / output (down GEMM)
+    Q.s.A += (size_t)group * Q.s.a_group_off;
+    Q.s.C += (size_t)group * Q.s.c_group_off;
+  }
+  for (int left = tile.rows; left > 0; left -= THIN_ROWS, tile.row0 += THIN_ROWS) {
+    tile.rows = left < THIN_ROWS ? left : THIN_ROWS;
+    thin_quant_tile<SWIGLU>(Q, tile, group, cb);
+  }
+}
+
+// Source rows [group][n][k]: codes two to a byte, scales one byte per 32 k.  PAIR: gate and up (fragments 0 and 1), else
+// fragment f = features 16f..16f+15 of the column block.  Past N and K the codes are 0 and the scales 1.
+template <bool PAIR>
+__global__ __launch_bounds__(256) void pack_quant_kernel(const uint32_t* __restrict__ codes0, const uint8_t* __restrict__ scales0,
+                                                         const uint32_t* __restrict__ codes1, const uint8_t* __restrict__ scales1,
+                                                         u32x4_t* __restrict__ dst, u32x4_t* __restrict__ dst_scales, int G,
+                                                         int N, int K, int nbt) {
+  const int NT = quant_tiles(K), NT4 = quant_scale_tiles(K), KG = (K + FMOE_QUANT_GROUP - 1) / FMOE_QUANT_GROUP;
+  const size_t total = (size_t)G * nbt * NT * 256, total_scales = (size_t)G * nbt * NT4 * 64;
+  for (size_t u = (size_t)blockIdx.x * blockDim.x + threadIdx.x; u < total + total_scales;
+       u += (size_t)gridDim.x * blockDim.x) {
+    const bool scales = u >= total;
+    size_t q = scales ? u - total : u;
+    const int lane = scales ? (int)(q & 15) : (int)(q & 63);
+    const int w = (int)(scales ? q >> 4 : q >> 6) & 3;
+    q >>= scales ? 6 : 8;
+    const int kt = (int)(q % (scales ? NT4 : NT));
+    q /= scales ? NT4 : NT;
+    const int b = (int)(q % nbt) * 4 + w, g = (int)(q / nbt);
+    u32x4_t v = {0u, 0u, 0u, 0u};
+    if (!scales) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {   // k step i/2, fragment i%2
+        const int f = i & 1, n = PAIR ? b * 16 + (lane & 15) : b * 32 + f * 16 + (lane & 15);
+        const int k = kt * SBK + (i >> 1) * 32 + 8 * (lane >> 4);
+        if (n < N && k < K) v[i] = (PAIR && f ? codes1 : codes0)[(((size_t)g * N + n) * K + k) >> 3];
+      }
+      dst[u] = v;
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int f = i & 1, n = PAIR ? b * 16 + lane : b * 32 + f * 16 + lane;
+          const int kg = (kt * 4 + t) * 2 + (i >> 1);
+          uint32_t s = 127u;
+          if (n < N && kg < KG) s = (PAIR && f ? scales1 : scales0)[((size_t)g * N + n) * KG + kg];
+          v[t] |= s << (8 * i);
+        }
+      dst_scales[u - total] = v;
+    }
+  }
+}
+
+// 16-byte units of one packed group: column tiles (of four column blocks) times k tiles
+inline size_t code_units(int nbw, int K) { return (size_t)((nbw + 3) / 4) * quant_tiles(K) * 256; }
+inline size_t scale_units(int nbw, int K) { return (size_t)((nbw + 3) / 4) * quant_scale_tiles(K) * 64; }
+
+struct PackedMatrix {
+  int groups, nbw, N, K;
+};
+// 0 gate/up, 1 down, 2 shared gate/up, 3 shared down
+PackedMatrix packed_matrix(const fmoe_config& c, int which) {
+  const int Ft = c.n_shared * c.d_ffn_shared;
+  switch (which) {
+    case 0: return {c.n_experts, (c.d_ffn + 15) / 16, c.d_ffn, c.d_model};
+    case 1: return {c.n_experts, (c.d_model + 31) / 32, c.d_model, c.d_ffn};
+    case 2: return {Ft > 0 ? 1 : 0, (Ft + 15) / 16, Ft, c.d_model};
+    default: return {Ft > 0 ? c.n_shared : 0, (c.d_model + 31) / 32, c.d_model, Ft > 0 ? c.d_ffn_shared : 8};
+  }
+}
+
+}  // namespace
+
+size_t fmoe_quant_bytes(const fmoe_ctx* ctx, int which, size_t* codes) {
+  const PackedMatrix m = packed_matrix(ctx->cfg, which);
+  const size_t c = (size_t)m.groups * code_units(m.nbw, m.K) * 16;
+  if (codes) *codes = c;
+  return c + (size_t)m.groups * scale_units(m.nbw, m.K) * 16;
+}
+
+int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStream_t stream) {
+  for (int which = 0; which < 4; ++which) {
+    const PackedMatrix m = packed_matrix(ctx->cfg, which);
+    if (m.groups == 0) continue;
+    const bool pair = (which & 1) == 0;
+    const fmoe_quant_tensor* a = w[which == 0 ? 0 : which == 1 ? 2 : which == 2 ? 3 : 5];
+    const fmoe_quant_tensor* b = pair ? w[which == 0 ? 1 : 4] : nullptr;
+    size_t codes;
+    const size_t threads = fmoe_quant_bytes(ctx, which, &codes) / 16;
+    char* const base = static_cast<char*>(ctx->pq[which]);
+    const size_t blocks = threads / 256 + 1;
+    const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536)), block(256);
+#define FMOE_PACK(PAIR)                                                                                                 \
+  hipLaunchKernelGGL(pack_quant_kernel<PAIR>, grid, block, 0, stream, static_cast<const uint32_t*>(a->codes), a->scales, \
+                     PAIR ? static_cast<const uint32_t*>(b->codes) : nullptr, PAIR ? b->scales : nullptr,               \
+                     reinterpret_cast<u32x4_t*>(base), reinterpret_cast<u32x4_t*>(base + codes), m.groups, m.N, m.K,    \
+                     (m.nbw + 3) / 4)
+    if (pair) FMOE_PACK(true);
+    else FMOE_PACK(false);
+#undef FMOE_PACK
+  }
+  FMOE_HIP_CHECK(hipGetLastError());
+  return FMOE_OK;
+}
+
+int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* perm_src, void* y,
+                  void* y_shared, char* base, const fmoe_ws_layout& L, const fmoe_ffn_geom& geo, hipStream_t stream) {
+  const fmoe_config& c = ctx->cfg;
+  const int d = c.d_model, E = c.n_experts, F = c.d_ffn;
+  const int Ft = c.n_shared * c.d_ffn_shared;
+  if ((size_t)n_cap * ctx->kmax * F * 2 > 0xffffffffull || (size_t)n_cap * Ft * 2 > 0xffffffffull)
+    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "expert FFN: a hidden buffer of %d rows exceeds 4 GiB", n_cap);
+  int32_t* tile_count = reinterpret_cast<int32_t*>(base + L.tile_count);
+  auto problem = [&](int which) {
+    const PackedMatrix m = packed_matrix(c, which);
+    QuantProblem q{};
+    if (m.groups == 0) return q;
+    size_t codes;
+    (void)fmoe_quant_bytes(ctx, which, &codes);
+    const char* packed = static_cast<const char*>(ctx->pq[which]);
+    q.s.Bp = reinterpret_cast<const u32x4_t*>(packed);
+    q.Sp = reinterpret_cast<const u32x4_t*>(packed + codes);
+    q.s.nbw = m.nbw; q.s.N = m.N; q.s.K = m.K;
+    q.s.group_stride = (long long)code_units(m.nbw, m.K);
+    q.scale_stride = (long long)scale_units(m.nbw, m.K);
+    return q;
+  };
+  QuantArgs g1{}, g2{};
+  g1.E = g2.E = E;
+  g1.tiles = reinterpret_cast<fmoe_tile*>(base + L.tiles);
+  g2.tiles = reinterpret_cast<fmoe_tile*>(base + L.tiles2);
+  g1.n_tiles = tile_count;
+  g2.n_tiles = tile_count + 1;
+  g1.p0 = problem(0); g1.p1 = problem(2); g2.p0 = problem(1); g2.p1 = problem(3);
+  {
+    StreamProblem &p = g1.p0.s, &q = g1.p1.s;
+    p.A = q.A = static_cast<const bf16_t*>(x); p.lda = q.lda = d;
+    p.map1 = perm_src; p.map1_limit = n_cap;
+    p.map2 = q.map2 = kept_idx;
+    p.C = reinterpret_cast<bf16_t*>(base + L.h); p.ldc = F; p.n_col_tiles = geo.cols1;
+    q.C = reinterpret_cast<bf16_t*>(base + L.h_shared); q.ldc = Ft; q.n_col_tiles = geo.scols1;
+  }
+  {
+    StreamProblem &p = g2.p0.s, &q = g2.p1.s;
+    p.A = reinterpret_cast<const bf16_t*>(base + L.h); p.lda = F;
+    p.C = static_cast<bf16_t*>(y); p.ldc = d; p.n_col_tiles = geo.cols2;
+    q.A = reinterpret_cast<const bf16_t*>(base + L.h_shared); q.lda = Ft; q.a_group_off = c.d_ffn_shared;
+    q.C = static_cast<bf16_t*>(y_shared); q.ldc = d; q.c_group_off = (long long)n_cap * d; q.n_col_tiles = geo.scols2;
+  }
+  // tile entries the lists can have (geo.tile_cap allows for one of every expert)
+  const long long row_cap = (long long)n_cap * ctx->kmax;
+  const int all = geo.tile_cap - (row_cap < E ? E - (int)row_cap : 0);
+  const unsigned entries = (unsigned)(all > 0 ? all : 0);
+  g1.cols = geo.cols1 * 4;
+  g2.cols = geo.cols2 * 4;
+  {
+    fmoe_prof_scope prof(ctx, SLOT_GEMM1, stream);
+    hipLaunchKernelGGL(ffn_quant_thin_kernel<true>, dim3(entries * g1.cols), dim3(64), 0, stream, g1);
+  }
+  {
+    fmoe_prof_scope prof(ctx, SLOT_GEMM2, stream);
+    hipLaunchKernelGGL(ffn_quant_thin_kernel<false>, dim3(entries * g2.cols), dim3(64), 0, stream, g2);
+  }
+  return FMOE_OK;
+}

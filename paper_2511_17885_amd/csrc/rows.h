@@ -34,4 +34,23 @@ __device__ __forceinline__ int row_min(int v) {
   v = min(v, row_rotate<2>(v));
   return min(v, row_rotate<1>(v));
 }
+// The same in 64 bits.
+template <int ROT>
+__device__ __forceinline__ double row_rotate(double v) {
+  const int lo = row_rotate<ROT>(__double2loint(v)), hi = row_rotate<ROT>(__double2hiint(v));
+  return __hiloint2double(hi, lo);
+}
+__device__ __forceinline__ double row_sum_butterfly(double v) {
+  v = v + row_rotate<8>(v);
+  v = v + row_rotate<4>(v);
+  v = v + row_rotate<2>(v);
+  return v + row_rotate<1>(v);
+}
+__device__ __forceinline__ double larger(double v, double o) { return (o > v) ? o : v; }
+__device__ __forceinline__ double row_max(double v) {
+  v = larger(v, row_rotate<8>(v));
+  v = larger(v, row_rotate<4>(v));
+  v = larger(v, row_rotate<2>(v));
+  return larger(v, row_rotate<1>(v));
+}
 #endif
