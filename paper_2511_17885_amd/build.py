@@ -34,10 +34,13 @@ SOURCES = {
 }
 
 
+HAND_PLACED = ("ffn.hip", "ffn_quant.hip")   # files whose kernels name accumulation registers themselves
+
+
 def check_accumulation_registers(asm_path):
-    """The dense-shape expert GEMM kernels (ffn_dense_kernel) keep their accumulators in accumulation
+    """The dense-shape expert GEMM kernels (ffn_dense_kernel, ffn_quant_dense_kernel) keep their accumulators in accumulation
     registers that the kernel names itself, which the compiler's register allocator does not see.  This
-    reads the device assembly the compiler wrote for ffn.hip and fails if, inside those kernels, the
+    reads the device assembly the compiler wrote for their file and fails if, inside those kernels, the
     compiler placed anything of its own in an accumulation register (any a<N> operand outside the
     kernel's own inline-assembly blocks), or spilled a register (their LDS reads are inline assembly and
     land later than the compiler believes)."""
@@ -45,7 +48,7 @@ def check_accumulation_registers(asm_path):
     inside = in_asm = False
     kernels = 0
     for n, line in enumerate(open(asm_path), 1):
-        if re.match(r"^_ZN\S*ffn_dense_kernel\S*:", line):
+        if re.match(r"^_ZN\S*(ffn_dense_kernel|ffn_quant_dense_kernel)\S*:", line):
             inside, in_asm = True, False
             kernels += 1
             name = line.split(":")[0]
@@ -64,15 +67,47 @@ def check_accumulation_registers(asm_path):
             raise RuntimeError(f"{asm_path}:{n}: the compiler uses an accumulation register inside {name}, which "
                                f"keeps hand-placed accumulators there: {line.strip()}")
     if kernels == 0:
-        raise RuntimeError(f"{asm_path}: no ffn_dense_kernel found to check")
+        raise RuntimeError(f"{asm_path}: no dense-shape kernel found to check")
     return kernels
+
+
+def check_pending_reads(asm_path):
+    """Some kernels start LDS reads in one inline-assembly block and wait for them in a later one; the compiler takes their
+    registers as written at once.  This reads the device assembly and fails if an instruction of the compiler's own
+    touches such a register before the wait."""
+    import re
+
+    def registers(text):
+        found = set()
+        for m in re.finditer(r"\bv(?:\[(\d+):(\d+)\]|(\d+)\b)", text):
+            lo = int(m.group(1) or m.group(3))
+            found.update(range(lo, int(m.group(2) or lo) + 1))
+        return found
+
+    in_asm, pending, reads = False, set(), 0
+    for n, line in enumerate(open(asm_path), 1):
+        code = line.split(";")[0].strip()
+        if "ASMSTART" in line:
+            in_asm = True
+        elif "ASMEND" in line:
+            in_asm = False
+        elif line.startswith(".Lfunc_end"):
+            pending = set()
+        elif code.startswith("s_waitcnt") and "lgkmcnt(0)" in code:
+            pending = set()
+        elif in_asm and code.startswith("ds_read"):
+            pending |= registers(code.split(",")[0])
+            reads += 1
+        elif not in_asm and pending and code and not code.startswith(".") and registers(code) & pending:
+            raise RuntimeError(f"{asm_path}:{n}: the compiler touches a register that an LDS read has not reached yet: {code}")
+    return reads
 
 
 def _compile(name, extra, verbose):
     src = os.path.join(CSRC, name)
     obj = os.path.join(OBJ, name.replace(".hip", ".o"))
     cmd = ["hipcc", "-c", src, "-o", obj] + COMMON + extra
-    if name == "ffn.hip":
+    if name in HAND_PLACED:
         cmd.append("-save-temps=obj")   # keeps the device assembly beside the object, for the check below
     if verbose:
         print(" ".join(cmd), flush=True)
@@ -83,8 +118,10 @@ def _compile(name, extra, verbose):
         raise RuntimeError(f"hipcc failed on {name}:\n{err}")
     if err.strip() and verbose:
         print(err, flush=True)
-    if name == "ffn.hip":
-        check_accumulation_registers(os.path.join(OBJ, "ffn-hip-amdgcn-amd-amdhsa-gfx950.s"))
+    if name in HAND_PLACED:
+        asm = os.path.join(OBJ, name.replace(".hip", "-hip-amdgcn-amd-amdhsa-gfx950.s"))
+        check_accumulation_registers(asm)
+        check_pending_reads(asm)
     return obj
 
 

@@ -29,6 +29,7 @@ struct QuantArgs {
   const fmoe_tile* tiles;
   const int32_t* n_tiles;     // device
   int cols;                   // work items per tile entry in this launch
+  int cols_entry;             // column tiles per tile entry
 };
 
 __host__ __device__ inline int quant_tiles(int K) { return (K + SBK - 1) / SBK; }
@@ -36,14 +37,13 @@ __host__ __device__ inline int quant_scale_tiles(int K) { return (quant_tiles(K)
 
 // Eight codes times the scale in byte I of `scales`.
 template <int I>
-__device__ __forceinline__ bf16x8_t dequantize(uint32_t codes, uint32_t scales) {
+__device__ __forceinline__ u32x4_t dequantize(uint32_t codes, uint32_t scales) {
   const uint32_t e = (I == 0 ? scales << 23 : I == 1 ? scales << 15 : I == 2 ? scales << 7 : scales >> 1) & 0x7f800000u;
   const float s = __uint_as_float(e);
-  const u32x4_t v = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3))};
-  return __builtin_bit_cast(bf16x8_t, v);
+  return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3))};
 }
 
 // One wavefront, one column block, sixteen rows: codes, scales and rows straight into registers in matrix order, no LDS and
@@ -102,10 +102,10 @@ __device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, const fmo
   auto multiply = [&](int slot) {
     const uint32_t sc = sreg[slot / 4][slot % 4];
     const bf16x8_t a0 = __builtin_bit_cast(bf16x8_t, areg[slot][0]), a1 = __builtin_bit_cast(bf16x8_t, areg[slot][1]);
-    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, dequantize<0>(breg[slot][0], sc), acc[0], 0, 0, 0);
-    acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, dequantize<1>(breg[slot][1], sc), acc[1], 0, 0, 0);
-    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, dequantize<2>(breg[slot][2], sc), acc[0], 0, 0, 0);
-    acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, dequantize<3>(breg[slot][3], sc), acc[1], 0, 0, 0);
+    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, __builtin_bit_cast(bf16x8_t, dequantize<0>(breg[slot][0], sc)), acc[0], 0, 0, 0);
+    acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, __builtin_bit_cast(bf16x8_t, dequantize<1>(breg[slot][1], sc)), acc[1], 0, 0, 0);
+    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, __builtin_bit_cast(bf16x8_t, dequantize<2>(breg[slot][2], sc)), acc[0], 0, 0, 0);
+    acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, __builtin_bit_cast(bf16x8_t, dequantize<3>(breg[slot][3], sc)), acc[1], 0, 0, 0);
   };
   int t0 = 0;
   for (; t0 + S <= NT; t0 += S) {
@@ -135,6 +135,171 @@ __device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, const fmo
       if (col + 16 < N) crow[col + 16] = f32_to_bf16(acc[1][v]);
     }
   }
+}
+
+// One work item of a workgroup: a tile of up to 128 rows (NAB live bands of 32) times NCB column tiles, column block w of
+// each for wavefront w.  Rows go through a ring of four LDS stages as in ffn.hip; codes and scales into registers, three k
+// tiles ahead; a k tile is one barrier.  Every load is unconditional (past the end the last tile again), so the number of
+// loads in flight at a wait is a compile-time constant.  Row blocks are taken two at a time, the next pair's operands
+// requested from LDS before the present pair's products.
+template <bool SWIGLU, int NAB, int NCB>
+__device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_tile& tile, int group, int ct0, int ct_limit,
+                                           bf16_t* As) {
+  constexpr int NRB = 2 * NAB;
+  constexpr int STAGES = 4, AHEAD = 3;
+  const StreamProblem& P = Q.s;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int K = P.K;
+  const int NT = quant_tiles(K), NT4 = quant_scale_tiles(K);
+  const int col_tiles = (P.nbw + 3) / 4;
+
+  const __amdgpu_buffer_rsrc_t b_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<u32x4_t*>(P.Bp) + (size_t)group * P.group_stride, 0, 0xffffffff, 0x00020000);
+  const __amdgpu_buffer_rsrc_t s_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<u32x4_t*>(Q.Sp) + (size_t)group * Q.scale_stride, 0, 0xffffffff, 0x00020000);
+  const __amdgpu_buffer_rsrc_t a_rsrc =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(P.A), 0, 0xffffffff, 0x00020000);
+  uint32_t bbase[NCB], sbase[NCB];   // scalar
+#pragma unroll
+  for (int j = 0; j < NCB; ++j) {    // column tiles past the packing: the last one again, never stored
+    const uint32_t ct = (uint32_t)(ct0 + j < col_tiles ? ct0 + j : col_tiles - 1);
+    bbase[j] = (ct * (uint32_t)NT * 256u + (uint32_t)wave * 64u) * 16u;
+    sbase[j] = (ct * (uint32_t)NT4 * 64u + (uint32_t)wave * 16u) * 16u;
+  }
+  const uint32_t lane16 = (uint32_t)lane * 16u, column16 = (uint32_t)(lane & 15) * 16u;
+  const int a_kc = ((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) * 8;
+
+  u32x4_t breg[STAGES][NCB], scales[NCB], next_scales[NCB];
+  uint32_t a_src[NAB];
+  auto loadB1 = [&](int slot, int t, int j) {
+    breg[slot][j] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane16, bbase[j] + (uint32_t)(t < NT ? t : NT - 1) * 4096u, 0);
+  };
+  auto loadS1 = [&](int t4, int j) {
+    return __builtin_amdgcn_raw_buffer_load_b128(s_rsrc, column16, sbase[j] + (uint32_t)(t4 < NT4 ? t4 : NT4 - 1) * 1024u, 0);
+  };
+  auto loadA1 = [&](int stage, int t, int it) {   // k past K re-reads the row's end, where the packed weights are zero
+    const int k = (t < NT ? t : NT - 1) * SBK + a_kc;
+    const int kk = k < K ? k : K - 8;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        a_rsrc, FMOE_LPTR(As + stage * (SBM * SBK) + (32 * it + 8 * wave) * SBK), 16,
+        a_src[it] + (uint32_t)kk * 2u, 0, 0, 0);
+  };
+  const uint32_t lds0 = (uint32_t)(uintptr_t)FMOE_LPTR(As);
+  const uint32_t frag_row = lds0 + (uint32_t)(lane & 15) * (SBK * 2);
+  const uint32_t frag_a0 = frag_row + (uint32_t)(((lane >> 4)) ^ ((lane & 15) >> 1)) * 16;
+  const uint32_t frag_a1 = frag_row + (uint32_t)(((lane >> 4) + 4) ^ ((lane & 15) >> 1)) * 16;
+
+  // prologue: weights between the two loads of the row indices, then the first activations
+  int src[NAB];
+  gather_first<NAB>(P, tile, src);
+  order_loads();
+#pragma unroll
+  for (int j = 0; j < NCB; ++j) scales[j] = loadS1(0, j);
+#pragma unroll
+  for (int t = 0; t < AHEAD; ++t)
+#pragma unroll
+    for (int j = 0; j < NCB; ++j) loadB1(t, t, j);
+  order_loads();
+  gather_offsets<NAB>(P, src, a_src);
+#pragma unroll
+  for (int t = 0; t < AHEAD; ++t) {
+#pragma unroll
+    for (int it = 0; it < NAB; ++it) loadA1(t, t, it);
+    order_loads();
+  }
+  FMOE_WAIT_VM((AHEAD - 1) * NAB);   // the first tile's rows; later ones have as many newer loads as in the steady state
+
+  // Accumulators: the compiler's with one column tile, hand-placed ones with two (number (j*NRB + rb)*2 + f), which it would
+  // put in part into scratch memory
+  constexpr bool NAMED = NCB == 2;
+  f32x4_t acc[NAMED ? 1 : NRB][2];
+  if constexpr (NAMED) {
+    dense_claim_acc();
+  } else {
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) acc[rb][0] = acc[rb][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  u32x4_t fa[2][2];
+  u32x4_t fb[NCB][2];
+  // k tile t = base + U: products, and the loads of tile t + AHEAD (with U == 0 the next four tiles' scales)
+  auto ktile = [&](auto uc, int t) {
+    constexpr int U = decltype(uc)::value;
+    constexpr int PER_TILE = NAB + NCB;
+    constexpr int NL = PER_TILE + (U == 0 ? NCB : 0);   // loads this tile issues
+    // loads newer than this tile's rows: those of the two tiles before (the scales count where they are sure to be among them)
+    FMOE_WAIT_VM((AHEAD - 1) * PER_TILE + (U == 2 ? NCB : 0));
+    block_barrier();   // every wavefront's share of the tile is in LDS; all are done with the tile before
+    constexpr int off = U * (SBM * SBK * 2);
+    lds_issue_frags_at<2, off>(frag_a0, fa[0]);
+    static_for<0, 2 * NAB>([&](auto pc) {
+      constexpr int p = decltype(pc)::value, s = p / NAB, h = p % NAB, cur = p & 1, nxt = cur ^ 1;
+      if constexpr (h == 0) {
+#pragma unroll
+        for (int j = 0; j < NCB; ++j) {
+          uint32_t c0 = breg[U][j][2 * s], c1 = breg[U][j][2 * s + 1];
+          if constexpr (NAMED) asm volatile("" : "+v"(c0), "+v"(c1));   // not converted earlier: there are no registers for it
+          fb[j][0] = dequantize<2 * s>(c0, scales[j][U]);
+          fb[j][1] = dequantize<2 * s + 1>(c1, scales[j][U]);
+          // a conversion's result must not be read by the very next instruction, and the compiler does not see that the
+          // hand-placed matrix instructions do
+          if constexpr (NAMED) asm volatile("s_nop 0" : "+v"(fb[j][0]), "+v"(fb[j][1]));
+        }
+      }
+      lds_settle_frags<2>(fa[cur]);
+      if constexpr (h + 1 < NAB) lds_issue_frags_at<2, off + (h + 1) * 4096>(s ? frag_a1 : frag_a0, fa[nxt]);
+      else if constexpr (s == 0) lds_issue_frags_at<2, off>(frag_a1, fa[nxt]);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {   // load i of the tile goes out with pair i * (2 NAB) / NL
+        if ((i * 2 * NAB) / NL != p) continue;
+        if (i < NAB) loadA1((U + AHEAD) % STAGES, t + AHEAD, i);
+        else if (i < PER_TILE) loadB1((U + AHEAD) % STAGES, t + AHEAD, i - NAB);
+        else next_scales[i - PER_TILE] = loadS1(t / 4 + 1, i - PER_TILE);
+      }
+      static_for<0, NCB>([&](auto jc) {
+        constexpr int j = decltype(jc)::value;
+        const bf16x8_t b0 = __builtin_bit_cast(bf16x8_t, fb[j][0]), b1 = __builtin_bit_cast(bf16x8_t, fb[j][1]);
+        static_for<0, 2>([&](auto rc) {
+          constexpr int rb = 2 * h + decltype(rc)::value;
+          const bf16x8_t a8 = __builtin_bit_cast(bf16x8_t, fa[cur][decltype(rc)::value]);
+          if constexpr (NAMED) {
+            mfma_at<(j * NRB + rb) * 2>(a8, b0);
+            mfma_at<(j * NRB + rb) * 2 + 1>(a8, b1);
+          } else {
+            acc[rb][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a8, b0, acc[rb][0], 0, 0, 0);
+            acc[rb][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a8, b1, acc[rb][1], 0, 0, 0);
+          }
+        });
+      });
+    });
+    if constexpr (U == 3) {
+#pragma unroll
+      for (int j = 0; j < NCB; ++j) scales[j] = next_scales[j];
+    }
+  };
+  int t0 = 0;
+  for (; t0 + 4 <= NT; t0 += 4) static_for<0, 4>([&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
+  const int left = NT - t0;   // uniform
+  if (left == 1) {
+    static_for<0, 1>([&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
+  } else if (left == 2) {
+    static_for<0, 2>([&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
+  } else if (left == 3) {
+    static_for<0, 3>([&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
+  }
+  FMOE_WAIT_VM(0);   // the loads issued past the end have landed before the ring is reused
+  // the last matrix instructions have retired before hand-placed accumulators are read, see ffn.hip
+  if constexpr (NAMED) asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
+  static_for<0, NCB>([&](auto jc) {
+    constexpr int j = decltype(jc)::value;
+    if (ct0 + j < ct_limit)   // uniform
+      store_tile<SWIGLU, NAB, STAGES>(P, tile, ct0 + j, [&](auto rbc, auto fc) {
+        constexpr int rb = decltype(rbc)::value, f = decltype(fc)::value;
+        if constexpr (NAMED) return read_acc<(j * NRB + rb) * 2 + f>();
+        else return acc[rb][f];
+      }, As);
+  });
 }
 
 // field by field, so that the descriptors stay in scalar registers
@@ -169,6 +334,51 @@ __global__ __launch_bounds__(64, 2) void ffn_quant_thin_kernel(QuantArgs a) {
     tile.rows = left < THIN_ROWS ? left : THIN_ROWS;
     thin_quant_tile<SWIGLU>(Q, tile, group, cb);
   }
+}
+
+// The work item of a workgroup, dealt out as deal.h says; column tiles are taken NCB at a time (a.cols = such groups per tile
+// entry).
+template <bool SWIGLU, int NCB>
+__device__ __forceinline__ void quant_item(const QuantArgs& a, bf16_t* As) {
+  int nt_launch, strip_cols;
+  bool single;
+  const int ti = dense_entry((int)blockIdx.x, a.n_tiles[0], a.n_tiles[2], a.cols, nt_launch, single, strip_cols);
+  if (ti < 0) return;
+  fmoe_tile tile = load_entry(a.tiles, ti);
+  const bool shared = tile.group >= a.E;
+  QuantProblem Q = select_problem(a, shared);
+  // column tiles this entry really has, and groups of NCB of them
+  const int ct_here = (Q.s.n_col_tiles - tile.col0 < a.cols_entry) ? (Q.s.n_col_tiles - tile.col0) : a.cols_entry;
+  const int c_eff = (ct_here + NCB - 1) / NCB;
+  if (nt_launch >= c_eff) return;
+  int row_tile = tile.rt;
+  if (tile.nrt > 1) dense_run_order(tile.rt, tile.nrt, c_eff, strip_cols, row_tile, nt_launch);
+  take_row_tile(tile, row_tile, SBM);
+  const int ct0 = tile.col0 + nt_launch * NCB;
+  const int ct_limit = tile.col0 + ct_here;
+  const int group = shared ? tile.group - a.E : tile.group;
+  if (shared) {
+    Q.s.A += (size_t)group * Q.s.a_group_off;
+    Q.s.C += (size_t)group * Q.s.c_group_off;
+  }
+  switch ((tile.rows + 31) >> 5) {   // live 32-row bands of the tile, uniform per block
+    case 1: quant_tile<SWIGLU, 1, NCB>(Q, tile, group, ct0, ct_limit, As); break;
+    case 2: quant_tile<SWIGLU, 2, NCB>(Q, tile, group, ct0, ct_limit, As); break;
+    case 3: quant_tile<SWIGLU, 3, NCB>(Q, tile, group, ct0, ct_limit, As); break;
+    default: quant_tile<SWIGLU, 4, NCB>(Q, tile, group, ct0, ct_limit, As); break;
+  }
+}
+
+// One column tile an item (few rows an expert), two (many); by name, since the build looks at the second one's registers.
+template <bool SWIGLU>
+__global__ __launch_bounds__(256, 2) void ffn_quant_stream_kernel(QuantArgs a) {
+  __shared__ __align__(16) bf16_t As[4 * SBM * SBK];
+  quant_item<SWIGLU, 1>(a, As);
+}
+template <bool SWIGLU>
+__global__ __launch_bounds__(256, 2) void ffn_quant_dense_kernel(QuantArgs a) {
+  __shared__ __align__(16) bf16_t As[4 * SBM * SBK];
+  quant_item<SWIGLU, 2>(a, As);
 }
 
 // Source rows [group][n][k]: codes two to a byte, scales one byte per 32 k.  PAIR: gate and up (fragments 0 and 1), else
@@ -311,19 +521,34 @@ int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, i
     q.A = reinterpret_cast<const bf16_t*>(base + L.h_shared); q.lda = Ft; q.a_group_off = c.d_ffn_shared;
     q.C = static_cast<bf16_t*>(y_shared); q.ldc = d; q.c_group_off = (long long)n_cap * d; q.n_col_tiles = geo.scols2;
   }
-  // tile entries the lists can have (geo.tile_cap allows for one of every expert)
-  const long long row_cap = (long long)n_cap * ctx->kmax;
-  const int all = geo.tile_cap - (row_cap < E ? E - (int)row_cap : 0);
+  g1.cols = g1.cols_entry = geo.cols1;
+  g2.cols = g2.cols_entry = geo.cols2;
+  // at most THIN_ROWS tokens: no tile has more rows, and the weight stream wants the finest work items
+  const bool thin = n_cap <= THIN_ROWS && ctx->ffn_shape == 0;
+  const bool dense = !thin && geo.dense;
+  // tile entries the lists of a thin call can have (geo.tile_cap allows for one of every expert)
+  const int row_cap = n_cap * ctx->kmax;
+  const int all = geo.tile_cap - (row_cap < E ? E - row_cap : 0);
   const unsigned entries = (unsigned)(all > 0 ? all : 0);
-  g1.cols = geo.cols1 * 4;
-  g2.cols = geo.cols2 * 4;
+  auto launch = [&](auto swiglu, QuantArgs g) {
+    constexpr bool S = decltype(swiglu)::value;
+    if (thin) {
+      g.cols *= 4;
+      hipLaunchKernelGGL(ffn_quant_thin_kernel<S>, dim3(entries * g.cols), dim3(64), 0, stream, g);
+    } else if (dense) {
+      g.cols = (g.cols + 1) / 2;
+      hipLaunchKernelGGL(ffn_quant_dense_kernel<S>, dim3(dense_blocks(geo.tile_cap, g.cols)), dim3(256), 0, stream, g);
+    } else {
+      hipLaunchKernelGGL(ffn_quant_stream_kernel<S>, dim3(dense_blocks(geo.tile_cap, g.cols)), dim3(256), 0, stream, g);
+    }
+  };
   {
-    fmoe_prof_scope prof(ctx, SLOT_GEMM1, stream);
-    hipLaunchKernelGGL(ffn_quant_thin_kernel<true>, dim3(entries * g1.cols), dim3(64), 0, stream, g1);
+    fmoe_prof_scope prof(ctx, dense ? SLOT_GEMM1_DENSE : SLOT_GEMM1, stream);
+    launch(std::true_type{}, g1);
   }
   {
-    fmoe_prof_scope prof(ctx, SLOT_GEMM2, stream);
-    hipLaunchKernelGGL(ffn_quant_thin_kernel<false>, dim3(entries * g2.cols), dim3(64), 0, stream, g2);
+    fmoe_prof_scope prof(ctx, dense ? SLOT_GEMM2_DENSE : SLOT_GEMM2, stream);
+    launch(std::false_type{}, g2);
   }
   return FMOE_OK;
 }

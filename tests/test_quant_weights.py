@@ -565,3 +565,17 @@ def test_binding_refuses_tensors_that_do_not_fit():
         m.set_weights_quant(router.float(), None, *good)
     with pytest.raises(ValueError):
         m.set_weights_quant(router, torch.zeros(3), *good)
+
+
+def test_build_check_catches_registers_used_before_an_lds_read_has_landed(tmp_path):
+    from paper_2511_17885_amd import build
+    issue = "\t;;#ASMSTART\n\tds_read_b128 v[4:7], v1 offset:64\n\t;;#ASMEND\n"
+    wait = "\t;;#ASMSTART\n\ts_waitcnt lgkmcnt(0)\n\t;;#ASMEND\n"
+    use = "\tv_mov_b32_e32 v9, v6\n"
+    p = tmp_path / "a.s"
+    p.write_text("k:\n" + issue + "\tv_add_u32 v8, v3, v10\n\tv_mfma_f32_16x16x32_bf16 a[4:7], v[12:15], v[16:19], 0\n" + wait + use)
+    assert build.check_pending_reads(str(p)) == 1
+    for early in (use, "\tv_mfma_f32_16x16x32_bf16 a[0:3], v[2:5], v[16:19], 0\n", "\tglobal_load_dwordx4 v[7:10], v[20:21], off\n"):
+        p.write_text("k:\n" + issue + early + wait)
+        with pytest.raises(RuntimeError, match="has not reached"):
+            build.check_pending_reads(str(p))
