@@ -6,6 +6,7 @@ been built, loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -144,11 +145,12 @@ def _ptr(t: Optional[torch.Tensor]):
     if t is None:
         return None
     assert t.is_contiguous()
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # the raw handle: the stream object around it takes 2.5 us to make, a third of a small call
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def prune_params(retention=1.0, window=1, alpha=1.0, gamma=0.0, sim_mode=0, prune_mode=1, merge_mode=0):
@@ -176,6 +178,13 @@ def _expect(t, what, dtype, shape):
         raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
 
 
+def _on(device):
+    """Makes the device of a call without a context the current one, where it is not (1.3 us)."""
+    if device.type == "cuda" and device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
 def quantize_weights(w, saturate=True):
     """Weights [..., K] (float32 or bfloat16) to 4 bits in groups of 32 along K (fmoe_quantize_weights).  Returns (codes
     [..., K/2] uint8, scales [..., ceil(K/32)] uint8)."""
@@ -185,7 +194,7 @@ def quantize_weights(w, saturate=True):
     K = w.shape[-1]
     codes = torch.empty((*w.shape[:-1], K // 2), dtype=torch.uint8, device=w.device)
     scales = torch.empty((*w.shape[:-1], (K + QUANT_GROUP - 1) // QUANT_GROUP), dtype=torch.uint8, device=w.device)
-    with torch.cuda.device(w.device):
+    with _on(w.device):
         _check(load().fmoe_quantize_weights(_ptr(w), dtype, w.numel() // max(K, 1), K, int(bool(saturate)), _ptr(codes),
                                             _ptr(scales), _stream()))
     return codes, scales
@@ -197,7 +206,7 @@ def dequantize_weights(codes, scales, dtype=torch.bfloat16):
     _expect(codes, "codes", torch.uint8, codes.shape)
     _expect(scales, "scales", torch.uint8, (*codes.shape[:-1], (K + QUANT_GROUP - 1) // QUANT_GROUP))
     w = torch.empty((*codes.shape[:-1], K), dtype=dtype, device=codes.device)
-    with torch.cuda.device(w.device):
+    with _on(w.device):
         _check(load().fmoe_dequantize_weights(_ptr(codes), _ptr(scales), w.numel() // max(K, 1), K,
                                               _float_type(w, "w"), _ptr(w), _stream()))
     return w
@@ -334,7 +343,9 @@ class FMoE:
         idx, gate = self._i32(T, K), self._f32(T, K)
         _check(self.lib.fmoe_select_experts(self._ctx, C.byref(params), _ptr(logits), dtype, _ptr(is_visual),
                                             _ptr(select_bias), T, _ptr(scores), _ptr(idx), _ptr(gate), _stream()))
-        return scores, idx[:, :self.kmax], gate[:, :self.kmax]
+        if self.kmax == 0:
+            idx, gate = idx[:, :0], gate[:, :0]
+        return scores, idx, gate
 
     def select_experts_backward(self, params, logits, topk_idx, d_gate, d_scores=None):
         """fmoe_select_experts_backward: the gradient of the logits from those of topk_gate [T, kmax] and, if given, of

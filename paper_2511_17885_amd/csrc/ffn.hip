@@ -1563,7 +1563,7 @@ int launch_expert_ffn(const fmoe_ctx* ctx, const void* x, const int32_t* kept_id
   if (n_cap == 0 || (row_cap == 0 && !has_shared)) return FMOE_OK;
   char* base = static_cast<char*>(ws);
   const fmoe_ffn_geom geo = fmoe_geom(ctx, n_cap);
-  if (!tiles_ready) {
+  if (!tiles_ready && !(ctx->quant && quant_ffn_is_thin(ctx, n_cap))) {
     fmoe_prof_scope prof(ctx, SLOT_TILES, stream);
     hipLaunchKernelGGL(build_tiles_kernel, dim3(1), dim3(256), 0, stream, expert_offsets, c.n_experts,
                        row_cap, n_cap, n_dev, c.n_shared, geo,
@@ -1573,7 +1573,7 @@ int launch_expert_ffn(const fmoe_ctx* ctx, const void* x, const int32_t* kept_id
   }
   int rc;
   if (ctx->quant)
-    rc = run_ffn_quant(ctx, x, kept_idx, n_cap, perm_src, y, y_shared, base, L, geo, stream);
+    rc = run_ffn_quant(ctx, x, kept_idx, n_cap, n_dev, expert_offsets, perm_src, y, y_shared, base, L, geo, stream);
   else if (c.dtype == FMOE_BF16)
     rc = run_ffn_bf16(ctx, x, kept_idx, n_cap, perm_src, y, y_shared, base, L, geo, stream);
   else

@@ -47,85 +47,95 @@ __device__ __forceinline__ u32x4_t dequantize(uint32_t codes, uint32_t scales) {
 }
 
 // One wavefront, one column block, sixteen rows: codes, scales and rows straight into registers in matrix order, no LDS and
-// no barrier.  Rows past the tile reuse its last one, row indices are clamped as in gather_offsets.
+// no barrier, for calls of at most THIN_ROWS tokens, where the weights are all there is to move.  Rows past the tile reuse
+// its last one, row indices are clamped as in gather_offsets.
+constexpr int THIN_HINT = 0;
 constexpr int THIN_ROWS = 16;
-constexpr int THIN_SLOTS = 8;   // k tiles (64 wide) in flight
+constexpr int THIN_SLOTS = 8;    // k tiles (64 wide) of codes in flight
+constexpr int THIN_A_SLOTS = 8;   // and of rows, which come from L2
 
 template <bool SWIGLU>
-__device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, const fmoe_tile& tile, int group, int cb) {
-  constexpr int S = THIN_SLOTS;
-  static_assert(S % 4 == 0, "a unit of scales serves four k tiles");
+__device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, int row0, int rows, int group, int cb) {
+  constexpr int S = THIN_SLOTS, SA = THIN_A_SLOTS;
+  static_assert(S % 4 == 0 && S % SA == 0, "a unit of scales serves four k tiles");
   const StreamProblem& P = Q.s;
   const int lane = threadIdx.x;
   const int K = P.K, N = P.N;
   const int NT = quant_tiles(K), NT4 = quant_scale_tiles(K);
+  // The streams' descriptors end with the column block: loads past the last k tile return zeros and fetch nothing
   const __amdgpu_buffer_rsrc_t b_rsrc = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<u32x4_t*>(P.Bp) + (size_t)group * P.group_stride + (size_t)(cb >> 2) * NT * 256 + (cb & 3) * 64, 0,
-      0xffffffff, 0x00020000);
+      const_cast<u32x4_t*>(P.Bp) + (size_t)group * P.group_stride + (size_t)cb * NT * 64, 0, NT * 1024, 0x00020000);
   const __amdgpu_buffer_rsrc_t s_rsrc = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<u32x4_t*>(Q.Sp) + (size_t)group * Q.scale_stride + (size_t)(cb >> 2) * NT4 * 64 + (cb & 3) * 16, 0,
-      0xffffffff, 0x00020000);
+      const_cast<u32x4_t*>(Q.Sp) + (size_t)group * Q.scale_stride + (size_t)cb * NT4 * 16, 0, NT4 * 256, 0x00020000);
   const __amdgpu_buffer_rsrc_t a_rsrc =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(P.A), 0, 0xffffffff, 0x00020000);
   const uint32_t lane16 = (uint32_t)lane * 16u, column16 = (uint32_t)(lane & 15) * 16u;
   const int kq = (lane >> 4) * 8;
-  u32x4_t breg[S], sreg[S / 4], areg[S][2];
-  auto load_b = [&](int slot, int t) {   // past the last tile the last one again
-    breg[slot] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane16, (t < NT ? t : NT - 1) * 4096, 0);
-  };
+  u32x4_t breg[S], sreg[S / 4], areg[SA][2];
+  auto load_b = [&](int slot, int t) { breg[slot] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane16 + (uint32_t)t * 1024u, 0, THIN_HINT); };
   auto load_s = [&](int slot, int t4) {
-    sreg[slot] = __builtin_amdgcn_raw_buffer_load_b128(s_rsrc, column16, (t4 < NT4 ? t4 : NT4 - 1) * 1024, 0);
+    sreg[slot] = __builtin_amdgcn_raw_buffer_load_b128(s_rsrc, column16 + (uint32_t)t4 * 256u, 0, 0);
   };
   uint32_t a_row;   // byte offset of the lane's row
   auto load_a = [&](int slot, int t) {   // k past K re-reads the row's end, where the packed weights are zero
-    const int k0 = (t < NT ? t : NT - 1) * SBK;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const int k = k0 + s * 32 + kq;
+      const int k = t * SBK + s * 32 + kq;
       areg[slot][s] = __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, a_row + (uint32_t)(k < K ? k : K - 8) * 2u, 0, 0);
     }
   };
+  // the weights do not need the row indices (two dependent loads)
   const uint32_t a_max_row = 0xffffffffu / ((uint32_t)P.lda * 2u) - 1u;
-  int src = tile.row0 + ((lane & 15) < tile.rows ? (lane & 15) : tile.rows - 1);
+  int src = row0 + ((lane & 15) < rows ? (lane & 15) : rows - 1);
   if (P.map1) src = P.map1[src];
-  if (P.map1 && P.map1_limit > 0) src = src < 0 ? 0 : (src >= P.map1_limit ? P.map1_limit - 1 : src);
-  if (P.map2) src = P.map2[src];
-  a_row = ((uint32_t)src < a_max_row ? (uint32_t)src : a_max_row) * (uint32_t)P.lda * 2u;
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int t = 0; t < S; ++t) {
     if (t % 4 == 0) load_s(t / 4, t / 4);
     load_b(t, t);
-    load_a(t, t);
   }
+  __builtin_amdgcn_sched_barrier(0);
+  if (P.map1 && P.map1_limit > 0) src = src < 0 ? 0 : (src >= P.map1_limit ? P.map1_limit - 1 : src);
+  if (P.map2) src = P.map2[src];
+  a_row = ((uint32_t)src < a_max_row ? (uint32_t)src : a_max_row) * (uint32_t)P.lda * 2u;
+#pragma unroll
+  for (int t = 0; t < SA; ++t) load_a(t, t);
+  __builtin_amdgcn_sched_barrier(0);
 
   f32x4_t acc[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
   auto multiply = [&](int slot) {
     const uint32_t sc = sreg[slot / 4][slot % 4];
-    const bf16x8_t a0 = __builtin_bit_cast(bf16x8_t, areg[slot][0]), a1 = __builtin_bit_cast(bf16x8_t, areg[slot][1]);
+    const bf16x8_t a0 = __builtin_bit_cast(bf16x8_t, areg[slot % SA][0]), a1 = __builtin_bit_cast(bf16x8_t, areg[slot % SA][1]);
     acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, __builtin_bit_cast(bf16x8_t, dequantize<0>(breg[slot][0], sc)), acc[0], 0, 0, 0);
     acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, __builtin_bit_cast(bf16x8_t, dequantize<1>(breg[slot][1], sc)), acc[1], 0, 0, 0);
     acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, __builtin_bit_cast(bf16x8_t, dequantize<2>(breg[slot][2], sc)), acc[0], 0, 0, 0);
     acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, __builtin_bit_cast(bf16x8_t, dequantize<3>(breg[slot][3], sc)), acc[1], 0, 0, 0);
   };
   int t0 = 0;
-  for (; t0 + S <= NT; t0 += S) {
+  for (; t0 + S <= NT; t0 += S) {   // no exit inside, so that the waits can count on the rings' order
 #pragma unroll
     for (int u = 0; u < S; ++u) {
       multiply(u);
+      __builtin_amdgcn_sched_barrier(0);
       load_b(u, t0 + u + S);
-      load_a(u, t0 + u + S);
+      load_a(u % SA, t0 + u + SA);
       if (u % 4 == 3) load_s(u / 4, (t0 + S) / 4 + u / 4);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
+  // fewer than S tiles are left, all of their codes on the way
 #pragma unroll
-  for (int u = 0; u < S - 1; ++u)
-    if (t0 + u < NT) multiply(u);   // uniform
+  for (int u = 0; u < S - 1; ++u) {
+    if (t0 + u >= NT) break;   // uniform
+    multiply(u);
+    if (u + SA < S - 1) load_a(u % SA, t0 + u + SA);
+  }
   // accumulator register v of lane l: row 4*(l/16) + v, column l%16
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
     const int row = 4 * (lane >> 4) + v;
-    if (row >= tile.rows) continue;
-    bf16_t* crow = P.C + (size_t)(tile.row0 + row) * P.ldc;
+    if (row >= rows) continue;
+    bf16_t* crow = P.C + (size_t)(row0 + row) * P.ldc;
     if (SWIGLU) {
       const int col = cb * 16 + (lane & 15);
       if (col < N) crow[col] = f32_to_bf16(silu_mul_bf16(acc[0][v], acc[1][v]));
@@ -163,9 +173,9 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
   uint32_t bbase[NCB], sbase[NCB];   // scalar
 #pragma unroll
   for (int j = 0; j < NCB; ++j) {    // column tiles past the packing: the last one again, never stored
-    const uint32_t ct = (uint32_t)(ct0 + j < col_tiles ? ct0 + j : col_tiles - 1);
-    bbase[j] = (ct * (uint32_t)NT * 256u + (uint32_t)wave * 64u) * 16u;
-    sbase[j] = (ct * (uint32_t)NT4 * 64u + (uint32_t)wave * 16u) * 16u;
+    const uint32_t cb = (uint32_t)(ct0 + j < col_tiles ? ct0 + j : col_tiles - 1) * 4u + (uint32_t)wave;
+    bbase[j] = cb * (uint32_t)NT * 1024u;
+    sbase[j] = cb * (uint32_t)NT4 * 256u;
   }
   const uint32_t lane16 = (uint32_t)lane * 16u, column16 = (uint32_t)(lane & 15) * 16u;
   const int a_kc = ((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) * 8;
@@ -173,10 +183,10 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
   u32x4_t breg[STAGES][NCB], scales[NCB], next_scales[NCB];
   uint32_t a_src[NAB];
   auto loadB1 = [&](int slot, int t, int j) {
-    breg[slot][j] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane16, bbase[j] + (uint32_t)(t < NT ? t : NT - 1) * 4096u, 0);
+    breg[slot][j] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane16, bbase[j] + (uint32_t)(t < NT ? t : NT - 1) * 1024u, 0);
   };
   auto loadS1 = [&](int t4, int j) {
-    return __builtin_amdgcn_raw_buffer_load_b128(s_rsrc, column16, sbase[j] + (uint32_t)(t4 < NT4 ? t4 : NT4 - 1) * 1024u, 0);
+    return __builtin_amdgcn_raw_buffer_load_b128(s_rsrc, column16, sbase[j] + (uint32_t)(t4 < NT4 ? t4 : NT4 - 1) * 256u, 0);
   };
   auto loadA1 = [&](int stage, int t, int it) {   // k past K re-reads the row's end, where the packed weights are zero
     const int k = (t < NT ? t : NT - 1) * SBK + a_kc;
@@ -303,7 +313,8 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
 }
 
 // field by field, so that the descriptors stay in scalar registers
-__device__ __forceinline__ QuantProblem select_problem(const QuantArgs& a, bool shared) {
+template <typename ARGS>
+__device__ __forceinline__ QuantProblem select_problem(const ARGS& a, bool shared) {
   QuantProblem Q;
 #define FMOE_SEL(f) Q.f = shared ? a.p1.f : a.p0.f
   FMOE_SEL(s.A); FMOE_SEL(s.lda); FMOE_SEL(s.map1); FMOE_SEL(s.map2); FMOE_SEL(s.map1_limit); FMOE_SEL(s.Bp);
@@ -314,26 +325,69 @@ __device__ __forceinline__ QuantProblem select_problem(const QuantArgs& a, bool 
   return Q;
 }
 
-// Item -> (tile entry, column block), a.cols = column blocks per entry in the launch.
+struct QuantThinArgs {
+  QuantProblem p0, p1;
+  const int32_t* expert_offsets;   // null without room for rows
+  const int32_t* n_dev;            // or null
+  int E, n_cap, row_cap;
+  int cols;                        // column blocks of an expert in this launch
+  int shared_items, shared_cols;   // items of the shared group(s), the first ones, shared_cols of them a group
+};
+
+// Items: the shared groups' column blocks, then those of the routed experts that have rows, in ascending order.  Which
+// expert the j-th of them is every wavefront finds from the offsets: no launch to build lists for a few rows.  Experts
+// whose offsets are malformed are skipped as in fmoe_build_tiles.
 template <bool SWIGLU>
-__global__ __launch_bounds__(64, 2) void ffn_quant_thin_kernel(QuantArgs a) {
-  const int ti = (int)blockIdx.x / a.cols;
-  if (ti >= *a.n_tiles) return;
-  fmoe_tile tile = load_entry(a.tiles, ti);
-  take_row_tile(tile, tile.rt, SBM);
-  const bool shared = tile.group >= a.E;
+__global__ __launch_bounds__(64, 2) void ffn_quant_thin_kernel(QuantThinArgs a) {
+  const int lane = threadIdx.x, item = (int)blockIdx.x;
+  const bool shared = item < a.shared_items;
+  int group, cb, row0, rows;
+  if (shared) {
+    group = item / a.shared_cols;
+    cb = item - group * a.shared_cols;
+    row0 = 0;
+    rows = resolve_count(a.n_cap, a.n_dev);
+  } else {
+    const int routed = item - a.shared_items;
+    int left = routed / a.cols;    // experts with rows ahead of this item's
+    cb = routed - left * a.cols;
+    int r0[4], r1[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int e = 64 * q + lane;
+      r0[q] = r1[q] = 0;
+      if (e < a.E) {
+        r0[q] = a.expert_offsets[e];
+        r1[q] = a.expert_offsets[e + 1];
+      }
+    }
+    group = -1;
+    row0 = rows = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const bool some = r0[q] >= 0 && r1[q] > r0[q] && r1[q] <= a.row_cap;
+      const unsigned long long mask = __ballot(some);
+      const int here = __popcll(mask);
+      if (group < 0 && left < here) {   // uniform
+        const int rank = __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
+        const int at = __ffsll((long long)__ballot(some && rank == left)) - 1;
+        group = 64 * q + at;
+        row0 = __builtin_amdgcn_readlane(r0[q], at);
+        rows = __builtin_amdgcn_readlane(r1[q], at) - row0;
+      }
+      left -= here;
+    }
+    if (group < 0) return;
+  }
   QuantProblem Q = select_problem(a, shared);
-  const int cb = tile.col0 * 4 + ((int)blockIdx.x - ti * a.cols);
   if (cb >= Q.s.nbw) return;
-  const int group = shared ? tile.group - a.E : tile.group;
   if (shared) {   // per-shared-expert slices of the hidden buffer / output (down GEMM)
     Q.s.A += (size_t)group * Q.s.a_group_off;
     Q.s.C += (size_t)group * Q.s.c_group_off;
   }
-  for (int left = tile.rows; left > 0; left -= THIN_ROWS, tile.row0 += THIN_ROWS) {
-    tile.rows = left < THIN_ROWS ? left : THIN_ROWS;
-    thin_quant_tile<SWIGLU>(Q, tile, group, cb);
-  }
+  // one turn unless a caller's own row lists name a token several times for one expert
+  for (; rows > 0; rows -= THIN_ROWS, row0 += THIN_ROWS)
+    thin_quant_tile<SWIGLU>(Q, row0, rows < THIN_ROWS ? rows : THIN_ROWS, group, cb);
 }
 
 // The work item of a workgroup, dealt out as deal.h says; column tiles are taken NCB at a time (a.cols = such groups per tile
@@ -395,11 +449,10 @@ __global__ __launch_bounds__(256) void pack_quant_kernel(const uint32_t* __restr
     const bool scales = u >= total;
     size_t q = scales ? u - total : u;
     const int lane = scales ? (int)(q & 15) : (int)(q & 63);
-    const int w = (int)(scales ? q >> 4 : q >> 6) & 3;
-    q >>= scales ? 6 : 8;
+    q >>= scales ? 4 : 6;
     const int kt = (int)(q % (scales ? NT4 : NT));
     q /= scales ? NT4 : NT;
-    const int b = (int)(q % nbt) * 4 + w, g = (int)(q / nbt);
+    const int b = (int)(q % (nbt * 4)), g = (int)(q / (nbt * 4));
     u32x4_t v = {0u, 0u, 0u, 0u};
     if (!scales) {
 #pragma unroll
@@ -477,8 +530,11 @@ int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStrea
   return FMOE_OK;
 }
 
-int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* perm_src, void* y,
-                  void* y_shared, char* base, const fmoe_ws_layout& L, const fmoe_ffn_geom& geo, hipStream_t stream) {
+// At most THIN_ROWS tokens: no expert has more rows, and the weight stream wants the finest work items.
+bool quant_ffn_is_thin(const fmoe_ctx* ctx, int n_cap) { return n_cap <= THIN_ROWS && ctx->ffn_shape == 0; }
+
+int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,
+                  const int32_t* expert_offsets, const int32_t* perm_src, void* y, void* y_shared, char* base, const fmoe_ws_layout& L, const fmoe_ffn_geom& geo, hipStream_t stream) {
   const fmoe_config& c = ctx->cfg;
   const int d = c.d_model, E = c.n_experts, F = c.d_ffn;
   const int Ft = c.n_shared * c.d_ffn_shared;
@@ -523,18 +579,19 @@ int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, i
   }
   g1.cols = g1.cols_entry = geo.cols1;
   g2.cols = g2.cols_entry = geo.cols2;
-  // at most THIN_ROWS tokens: no tile has more rows, and the weight stream wants the finest work items
-  const bool thin = n_cap <= THIN_ROWS && ctx->ffn_shape == 0;
+  const bool thin = quant_ffn_is_thin(ctx, n_cap);
   const bool dense = !thin && geo.dense;
-  // tile entries the lists of a thin call can have (geo.tile_cap allows for one of every expert)
   const int row_cap = n_cap * ctx->kmax;
-  const int all = geo.tile_cap - (row_cap < E ? E - row_cap : 0);
-  const unsigned entries = (unsigned)(all > 0 ? all : 0);
   auto launch = [&](auto swiglu, QuantArgs g) {
     constexpr bool S = decltype(swiglu)::value;
     if (thin) {
-      g.cols *= 4;
-      hipLaunchKernelGGL(ffn_quant_thin_kernel<S>, dim3(entries * g.cols), dim3(64), 0, stream, g);
+      QuantThinArgs h{g.p0, g.p1, expert_offsets, n_dev, E, n_cap, row_cap, g.p0.s.nbw, 0, 1};
+      if (Ft > 0) {
+        h.shared_cols = g.p1.s.nbw;
+        h.shared_items = (S ? 1 : c.n_shared) * g.p1.s.nbw;
+      }
+      const unsigned items = (unsigned)(h.shared_items + (row_cap < E ? row_cap : E) * h.cols);
+      if (items > 0) hipLaunchKernelGGL(ffn_quant_thin_kernel<S>, dim3(items), dim3(64), 0, stream, h);
     } else if (dense) {
       g.cols = (g.cols + 1) / 2;
       hipLaunchKernelGGL(ffn_quant_dense_kernel<S>, dim3(dense_blocks(geo.tile_cap, g.cols)), dim3(256), 0, stream, g);
