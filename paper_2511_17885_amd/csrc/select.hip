@@ -6,8 +6,12 @@
 // log(s) is z (softmax: the row's normaliser cancels) or -log(1 + exp(-z)); as a softmax over the list the renormalised
 // gates need no division by a sum of scores that may have underflowed.
 //
-// Keys that come from a score are compared in 64 bits: two scores in 32 bits can be equal or change places where the
-// logits differ, and with thousands of tokens some pair of neighbours does.
+// Keys that come from a score are defined in 64 bits: two scores in 32 bits can be equal or change places where the
+// logits differ, and with thousands of tokens some pair of neighbours does.  They are compared in 32 bits first, with the
+// exponential and reciprocal of the hardware.  A key is then off by at most 2^-21 of the largest score a token can have and
+// half a rounding of its own; where two keys that are next to each other in the list, or on either side of its end, or
+// two groups on either side of theirs, are not further apart than twice that (taken twice), the wavefront does it again in
+// 64 bits.  One wavefront in a hundred does for 256 experts with a bias of deviation 0.1.
 //
 // Sixteen lanes have a token (four tokens a wavefront), lane j of them the experts 64 q + 4 j + i: a row is read in
 // pieces of 16 bytes, and a reduction over the row is one over a lane's registers and four steps inside the vector unit.
@@ -41,15 +45,48 @@ __device__ __forceinline__ float clean(float z) { return z > -INFINITY ? fminf(z
 
 __device__ __forceinline__ float log_sigmoid(float z) { return fminf(z, 0.0f) - log1pf(expf(-fabsf(z))); }
 
+// A lane's elements of a row of E, four at a time where rows are whole fours (their starts then are aligned); past the end
+// the first ones again.
+template <typename T, int NQ>
+__device__ __forceinline__ void read_row(const T* __restrict__ row, int E, int j, T (&v)[4 * NQ]) {
+  typedef T four_t __attribute__((ext_vector_type(4)));
+  if ((E & 3) == 0) {   // uniform
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int e = 64 * q + 4 * j;
+      const four_t w = *reinterpret_cast<const four_t*>(row + (e < E ? e : 0));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * q + i] = w[i];
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4 * NQ; ++r) {
+      const int e = 64 * (r >> 2) + 4 * j + (r & 3);
+      v[r] = row[e < E ? e : 0];
+    }
+  }
+}
+template <typename T, int NQ>
+__device__ __forceinline__ void write_row(T* __restrict__ row, int E, int j, const T (&v)[4 * NQ]) {
+  typedef T four_t __attribute__((ext_vector_type(4)));
+  if ((E & 3) == 0) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+      if (64 * q + 4 * j < E)
+        *reinterpret_cast<four_t*>(row + 64 * q + 4 * j) = four_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4 * NQ; ++r)
+      if (64 * (r >> 2) + 4 * j + (r & 3) < E) row[64 * (r >> 2) + 4 * j + (r & 3)] = v[r];
+  }
+}
 // A lane's logits of row t; experts past E are masked.
 template <typename ZT, int NQ>
 __device__ __forceinline__ void load_row(const ZT* __restrict__ z, int t, int E, int j, float (&v)[4 * NQ]) {
-  const ZT* row = z + (size_t)t * E;
+  ZT raw[4 * NQ];
+  read_row<ZT, NQ>(z + (size_t)t * E, E, j, raw);
 #pragma unroll
-  for (int r = 0; r < 4 * NQ; ++r) {
-    const int e = 64 * (r >> 2) + 4 * j + (r & 3);
-    v[r] = e < E ? clean(to_f32(row[e])) : -INFINITY;
-  }
+  for (int r = 0; r < 4 * NQ; ++r) v[r] = 64 * (r >> 2) + 4 * j + (r & 3) < E ? clean(to_f32(raw[r])) : -INFINITY;
 }
 
 // Of a row's logits: the largest (0 if all are masked) and the sum of exp(z - largest).
@@ -69,18 +106,90 @@ __device__ __forceinline__ float row_exp_sum(const float (&z)[N], float m) {
   return row_sum_butterfly(s);
 }
 
+// Expert of register r of a lane.
+__device__ __forceinline__ int expert_of(int r, int j) { return 64 * (r >> 2) + 4 * j + (r & 3); }
+
+// LDS written by lanes of this wavefront is read by others of it.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Masks the experts of a token's groups that do not stay.  key: what a group's score is made of; order: what ranks the
+// experts; ks: the token's row in LDS.  Returns whether the scores on either side of the line are further apart than `slack`
+// plus `relative` times their size (32 bits; not asked for in 64).
+template <typename T, int N>
+__device__ __forceinline__ bool keep_groups(const SelectArgs& a, int j, const T (&key)[N], T (&order)[N], T* ks, T slack,
+                                            T relative) {
+#pragma unroll
+  for (int r = 0; r < N; ++r) ks[expert_of(r, j)] = key[r];
+  wave_sync();
+  // lane g has group g: its largest key, or the sum of its two largest
+  T one = -INFINITY, two = -INFINITY;
+  if (j < a.groups) {
+    const T* const own = ks + j * a.group_size;
+    for (int i = 0; i < a.group_size; ++i) {
+      const T v = own[i];
+      two = v > one ? one : larger(two, v);
+      one = larger(one, v);
+    }
+  }
+  const T score = (a.sum_two && two > -INFINITY) ? one + two : one;
+  // rank among the groups: larger scores, or equal ones of lower groups, are ahead
+  int ahead = 0;
+  for (int g = 0; g < a.groups; ++g) {
+    const T o = __shfl(score, (threadIdx.x & 48) + g, 64);
+    ahead += (o > score || (o == score && g < j)) ? 1 : 0;
+  }
+  const bool in = j < a.groups && ahead < a.topk_groups;
+  const unsigned mask = (unsigned)(__ballot(in) >> (threadIdx.x & 48)) & 0xffffu;
+#pragma unroll
+  for (int r = 0; r < N; ++r)
+    if (!((mask >> ((expert_of(r, j) * a.group_mul >> 16) & 15)) & 1u)) order[r] = -INFINITY;   // (past E masked already)
+  if (a.topk_groups == a.groups) return true;
+  const T last = -row_max(in ? -score : (T)-INFINITY), next = row_max(j < a.groups && !in ? score : (T)-INFINITY);
+  return next == -INFINITY || last - next > slack + relative * (fabs(last) + fabs(next));
+}
+
+// k rounds of the largest that is left (ties: lowest expert); lane j keeps entry j: its expert (-1: none) and key.
+template <typename T, int N>
+__device__ __forceinline__ int list_largest(int k, int rounds, int j, T (&order)[N], T& my_key) {
+  int mine = -1;
+  my_key = -INFINITY;
+  for (int round = 0; round < rounds; ++round) {
+    T v = order[0];
+#pragma unroll
+    for (int r = 1; r < N; ++r) v = larger(v, order[r]);
+    const T top = row_max(v);
+    int e = 0x7fff;
+#pragma unroll
+    for (int r = N - 1; r >= 0; --r) e = order[r] == top ? expert_of(r, j) : e;
+    e = row_min(e);
+    if (j == round && round < k && top > -INFINITY) {
+      mine = e;
+      my_key = top;
+    }
+    if (round < k) {
+#pragma unroll
+      for (int r = 0; r < N; ++r) order[r] = expert_of(r, j) == e ? (T)-INFINITY : order[r];
+    }
+  }
+  return mine;
+}
+
 // KEYED: the keys are scores with a bias, or sums of scores rank the groups; else the logits are the keys.
 template <typename ZT, int NQ, bool KEYED>
 __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
   constexpr int N = 4 * NQ, STRIDE = 64 * NQ + 4;
-  typedef std::conditional_t<KEYED, double, float> key_t;
-  __shared__ float zs[ROWS][STRIDE];
-  __shared__ key_t ks[ROWS][STRIDE];   // keys, for groups
+  typedef std::conditional_t<KEYED, double, float> wide_t;
+  __shared__ wide_t ks[ROWS][STRIDE];   // keys, for groups
   const int j = threadIdx.x & 15, tok = threadIdx.x >> 4;
   const bool tv = (int)blockIdx.x * ROWS + tok < a.T;
   const int t = tv ? (int)blockIdx.x * ROWS + tok : a.T - 1;
+  const ZT* const logits = static_cast<const ZT*>(a.z);
   float z[N];
-  load_row<ZT, NQ>(static_cast<const ZT*>(a.z), t, a.E, j, z);
+  load_row<ZT, NQ>(logits, t, a.E, j, z);
   const bool visual = a.is_visual != nullptr && a.is_visual[t] != 0;
   const int k = visual ? a.k_visual : a.k_text;
 
@@ -91,88 +200,75 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
     inv = sum > 0.0f ? 1.0f / sum : 0.0f;
   }
   if (a.scores != nullptr && tv) {
+    float s[N];
 #pragma unroll
-    for (int r = 0; r < N; ++r) {
-      const int e = 64 * (r >> 2) + 4 * j + (r & 3);
-      const float s = a.sigmoid ? 1.0f / (1.0f + expf(-z[r])) : expf(z[r] - m) * inv;
-      if (e < a.E) a.scores[(size_t)t * a.E + e] = s;
-    }
+    for (int r = 0; r < N; ++r) s[r] = a.sigmoid ? 1.0f / (1.0f + expf(-z[r])) : expf(z[r] - m) * inv;
+    write_row<float, NQ>(a.scores + (size_t)t * a.E, a.E, j, s);
   }
 
-  key_t key[N], order[N];   // order: what ranks the experts; key: what a group's score is made of
-#pragma unroll
-  for (int r = 0; r < N; ++r) zs[tok][64 * (r >> 2) + 4 * j + (r & 3)] = z[r];
+  int mine;
   if constexpr (KEYED) {
-    double sum = 0.0;
-    if (!a.sigmoid) {
+    float bias[N];
+    if (a.bias != nullptr) {   // uniform
+      read_row<float, NQ>(a.bias, a.E, j, bias);
+    } else {
 #pragma unroll
-      for (int r = 0; r < N; ++r) sum += exp((double)z[r] - (double)m);
-      sum = row_sum_butterfly(sum);
+      for (int r = 0; r < N; ++r) bias[r] = 0.0f;
     }
+    bool sure = true;
+    {
+      const float largest = a.sigmoid ? 1.0f : inv;
+      const float slack = largest * 0x1p-19f;
+      constexpr float RELATIVE = 0x1p-22f;
+      float key[N], order[N];
 #pragma unroll
-    for (int r = 0; r < N; ++r) {
-      const int e = 64 * (r >> 2) + 4 * j + (r & 3);
-      const double s = a.sigmoid ? 1.0 / (1.0 + exp(-(double)z[r])) : exp((double)z[r] - (double)m) / sum;
-      const float b = a.bias != nullptr && e < a.E ? a.bias[e] : 0.0f;
-      const bool in = z[r] > -INFINITY && b > -INFINITY;
-      key[r] = in ? s + (double)b : -INFINITY;
-      order[r] = a.bias != nullptr ? key[r] : (double)z[r];
-    }
-  } else {
+      for (int r = 0; r < N; ++r) {
+        const float s = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + __expf(-z[r])) : __expf(z[r] - m) * inv;
+        key[r] = z[r] > -INFINITY && bias[r] > -INFINITY ? s + bias[r] : -INFINITY;
+        order[r] = a.bias != nullptr ? key[r] : z[r];
+      }
+      if (a.groups > 1)
+        sure = keep_groups<float, N>(a, j, key, order, reinterpret_cast<float*>(ks[tok]), 2.0f * slack, 2.0f * RELATIVE);
+      float my_key;
+      mine = list_largest<float, N>(k, a.Kmax, j, order, my_key);
+      if (a.bias != nullptr) {
+        // the largest that is not listed; then every entry against the one behind it
+        float rest = order[0];
 #pragma unroll
-    for (int r = 0; r < N; ++r) order[r] = key[r] = z[r];
-  }
-
-  if (a.groups > 1) {
-#pragma unroll
-    for (int r = 0; r < N; ++r) ks[tok][64 * (r >> 2) + 4 * j + (r & 3)] = key[r];
-  }
-  __syncthreads();
-  if (a.groups > 1) {
-    // lane g has group g: its largest key, or the sum of its two largest
-    key_t one = -INFINITY, two = -INFINITY;
-    if (j < a.groups) {
-      const int e0 = j * a.group_size;
-      for (int i = 0; i < a.group_size; ++i) {
-        const key_t v = ks[tok][e0 + i];
-        two = v > one ? one : larger(two, v);
-        one = larger(one, v);
+        for (int r = 1; r < N; ++r) rest = larger(rest, order[r]);
+        rest = row_max(rest);
+        const int listed = __popc((unsigned)(__ballot(mine >= 0) >> (threadIdx.x & 48)) & 0xffffu);
+        const float behind = __shfl(my_key, (threadIdx.x & 48) + ((j + 1) & 15), 64);
+        const float next = j + 1 < listed ? behind : rest;
+        sure = sure && (mine < 0 || next == -INFINITY || my_key - next > slack + RELATIVE * (fabsf(my_key) + fabsf(next)));
       }
     }
-    const key_t score = (a.sum_two && two > -INFINITY) ? one + two : one;
-    // rank among the groups: larger scores, or equal ones of lower groups, are ahead
-    int ahead = 0;
-    for (int g = 0; g < a.groups; ++g) {
-      const key_t o = __shfl(score, (threadIdx.x & 48) + g, 64);
-      ahead += (o > score || (o == score && g < j)) ? 1 : 0;
-    }
-    const unsigned long long stay = __ballot(j < a.groups && ahead < a.topk_groups);
-    const unsigned mask = (unsigned)(stay >> (threadIdx.x & 48)) & 0xffffu;
+    if (__any(!sure)) {
+      double key[N], order[N], sum = 0.0, my_key;
+      if (!a.sigmoid) {
 #pragma unroll
-    for (int r = 0; r < N; ++r) {
-      const int e = 64 * (r >> 2) + 4 * j + (r & 3);
-      if (!((mask >> ((e * a.group_mul >> 16) & 15)) & 1u)) order[r] = -INFINITY;   // (past E masked already)
+        for (int r = 0; r < N; ++r) sum += exp((double)z[r] - (double)m);
+        sum = row_sum_butterfly(sum);
+      }
+#pragma unroll
+      for (int r = 0; r < N; ++r) {
+        const double s = a.sigmoid ? 1.0 / (1.0 + exp(-(double)z[r])) : exp((double)z[r] - (double)m) / sum;
+        key[r] = z[r] > -INFINITY && bias[r] > -INFINITY ? s + (double)bias[r] : -INFINITY;
+        order[r] = a.bias != nullptr ? key[r] : (double)z[r];
+      }
+      wave_sync();
+      if (a.groups > 1) (void)keep_groups<double, N>(a, j, key, order, ks[tok], 0.0, 0.0);
+      mine = list_largest<double, N>(k, a.Kmax, j, order, my_key);
     }
+  } else {
+    float key[N], my_key;
+#pragma unroll
+    for (int r = 0; r < N; ++r) key[r] = z[r];
+    if (a.groups > 1) (void)keep_groups<float, N>(a, j, key, z, ks[tok], 0.0f, 0.0f);
+    mine = list_largest<float, N>(k, a.Kmax, j, z, my_key);
   }
 
-  // k rounds of the largest that is left (ties: lowest expert); lane j keeps entry j
-  int mine = -1;
-  for (int round = 0; round < a.Kmax; ++round) {
-    key_t v = order[0];
-#pragma unroll
-    for (int r = 1; r < N; ++r) v = larger(v, order[r]);
-    const key_t top = row_max(v);
-    int e = 0x7fff;
-#pragma unroll
-    for (int r = N - 1; r >= 0; --r) e = order[r] == top ? 64 * (r >> 2) + 4 * j + (r & 3) : e;
-    e = row_min(e);
-    if (j == round && round < k && top > -INFINITY) mine = e;
-#pragma unroll
-    for (int r = 0; r < N; ++r)
-      if (64 * (r >> 2) + 4 * j + (r & 3) == e) order[r] = -INFINITY;
-  }
-
-  const float zl = mine >= 0 ? zs[tok][mine] : -INFINITY;
+  const float zl = mine >= 0 ? clean(to_f32(logits[(size_t)t * a.E + mine])) : -INFINITY;
   float g;
   if (a.renorm) {
     const float l = mine >= 0 ? (a.sigmoid ? log_sigmoid(zl) : zl) : -INFINITY;
@@ -252,11 +348,18 @@ __global__ __launch_bounds__(256) void select_backward_kernel(SelectBackwardArgs
     float z[N];
     load_row<ZT, NQ>(static_cast<const ZT*>(a.z), t, a.E, j, z);
     float ds[N];
+    if (a.d_scores != nullptr) {   // uniform
+      read_row<float, NQ>(a.d_scores + (size_t)t * a.E, a.E, j, ds);
+    } else {
 #pragma unroll
-    for (int r = 0; r < N; ++r) {
-      const int x = 64 * (r >> 2) + 4 * j + (r & 3);
-      ds[r] = (a.d_scores != nullptr && x < a.E ? a.d_scores[(size_t)t * a.E + x] : 0.0f) + (a.renorm ? 0.0f : d[r]);
-      if (!a.renorm) d[r] = 0.0f;
+      for (int r = 0; r < N; ++r) ds[r] = 0.0f;
+    }
+    if (!a.renorm) {
+#pragma unroll
+      for (int r = 0; r < N; ++r) {
+        ds[r] += d[r];
+        d[r] = 0.0f;
+      }
     }
     if (a.sigmoid) {
 #pragma unroll
@@ -278,12 +381,10 @@ __global__ __launch_bounds__(256) void select_backward_kernel(SelectBackwardArgs
     }
   }
   if (tv) {
-    ZT* const out = static_cast<ZT*>(a.d_z) + (size_t)t * a.E;
+    ZT out[N];
 #pragma unroll
-    for (int r = 0; r < N; ++r) {
-      const int x = 64 * (r >> 2) + 4 * j + (r & 3);
-      if (x < a.E) out[x] = gradient<ZT>(d[r]);
-    }
+    for (int r = 0; r < N; ++r) out[r] = gradient<ZT>(d[r]);
+    write_row<ZT, NQ>(static_cast<ZT*>(a.d_z) + (size_t)t * a.E, a.E, j, out);
   }
 }
 
