@@ -34,6 +34,14 @@ __device__ __forceinline__ int row_min(int v) {
   v = min(v, row_rotate<2>(v));
   return min(v, row_rotate<1>(v));
 }
+// Largest over the row, in one instruction a step (all lanes of the wavefront are on).
+__device__ __forceinline__ int row_max(int v) {
+  v = max(v, __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true));
+  v = max(v, __builtin_amdgcn_mov_dpp(v, 0x124, 0xf, 0xf, true));
+  v = max(v, __builtin_amdgcn_mov_dpp(v, 0x122, 0xf, 0xf, true));
+  return max(v, __builtin_amdgcn_mov_dpp(v, 0x121, 0xf, 0xf, true));
+}
+
 // The same in 64 bits.
 template <int ROT>
 __device__ __forceinline__ double row_rotate(double v) {

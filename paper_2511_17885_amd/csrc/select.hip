@@ -17,6 +17,7 @@
 // pieces of 16 bytes, and a reduction over the row is one over a lane's registers and four steps inside the vector unit.
 
 #include <float.h>
+#include <limits.h>
 
 #include <type_traits>
 
@@ -116,40 +117,160 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// v of the lane whose number differs in bit LOG2 (0 or 1), or, among lanes that agree within their fours, of the other four
+// of the same eight (2).
+template <int LOG2>
+__device__ __forceinline__ float lane_partner(float v) {
+  constexpr int CTRL = LOG2 == 0 ? 0xb1 : LOG2 == 1 ? 0x4e : 0x141;   // quad permutations, half-row mirror
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int LOG2>
+__device__ __forceinline__ double lane_partner(double v) {
+  constexpr int CTRL = LOG2 == 0 ? 0xb1 : LOG2 == 1 ? 0x4e : 0x141;
+  return __hiloint2double(__builtin_amdgcn_mov_dpp(__double2hiint(v), CTRL, 0xf, 0xf, true),
+                          __builtin_amdgcn_mov_dpp(__double2loint(v), CTRL, 0xf, 0xf, true));
+}
+template <typename T>
+__device__ __forceinline__ T smaller(T v, T o) { return (o < v) ? o : v; }
+
+// The two largest so far, and two more.
+template <typename T>
+__device__ __forceinline__ void two_largest(T& one, T& two, T o1, T o2) {
+  two = larger(smaller(one, o1), larger(two, o2));
+  one = larger(one, o1);
+}
+
 // Masks the experts of a token's groups that do not stay.  key: what a group's score is made of; order: what ranks the
 // experts; ks: the token's row in LDS.  Returns whether the scores on either side of the line are further apart than `slack`
-// plus `relative` times their size (32 bits; not asked for in 64).
+// plus `relative` times their size (32 bits; not asked for in 64).  2^log2p lanes have a group.
 template <typename T, int N>
 __device__ __forceinline__ bool keep_groups(const SelectArgs& a, int j, const T (&key)[N], T (&order)[N], T* ks, T slack,
                                             T relative) {
+  typedef T four_t __attribute__((ext_vector_type(4)));
 #pragma unroll
-  for (int r = 0; r < N; ++r) ks[expert_of(r, j)] = key[r];
+  for (int q = 0; q < N / 4; ++q)
+    *reinterpret_cast<four_t*>(ks + 64 * q + 4 * j) = four_t{key[4 * q], key[4 * q + 1], key[4 * q + 2], key[4 * q + 3]};
   wave_sync();
-  // lane g has group g: its largest key, or the sum of its two largest
+  const int log2p = a.groups <= 2 ? 3 : a.groups <= 4 ? 2 : a.groups <= 8 ? 1 : 0;   // uniform
+  const int g = j >> log2p, part = j & ((1 << log2p) - 1);
+  const bool fours = (a.group_size & 3) == 0;
   T one = -INFINITY, two = -INFINITY;
-  if (j < a.groups) {
-    const T* const own = ks + j * a.group_size;
-    for (int i = 0; i < a.group_size; ++i) {
-      const T v = own[i];
-      two = v > one ? one : larger(two, v);
-      one = larger(one, v);
+  if (g < a.groups) {
+    const T* const own = ks + g * a.group_size;
+    if (fours) {
+      for (int i = 4 * part; i < a.group_size; i += 4 << log2p) {
+        const four_t v = *reinterpret_cast<const four_t*>(own + i);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          two = larger(two, smaller(one, v[x]));
+          one = larger(one, v[x]);
+        }
+      }
+    } else {
+      for (int i = part; i < a.group_size; i += 1 << log2p) {
+        const T v = own[i];
+        two = larger(two, smaller(one, v));
+        one = larger(one, v);
+      }
     }
   }
+  if (log2p > 0) two_largest(one, two, lane_partner<0>(one), lane_partner<0>(two));
+  if (log2p > 1) two_largest(one, two, lane_partner<1>(one), lane_partner<1>(two));
+  if (log2p > 2) two_largest(one, two, lane_partner<2>(one), lane_partner<2>(two));
   const T score = (a.sum_two && two > -INFINITY) ? one + two : one;
   // rank among the groups: larger scores, or equal ones of lower groups, are ahead
+  wave_sync();   // the keys have been read
+  if (part == 0) ks[g] = score;
+  wave_sync();
   int ahead = 0;
-  for (int g = 0; g < a.groups; ++g) {
-    const T o = __shfl(score, (threadIdx.x & 48) + g, 64);
-    ahead += (o > score || (o == score && g < j)) ? 1 : 0;
+  for (int h = 0; h < a.groups; ++h) {
+    const T o = ks[h];
+    ahead += (o > score || (o == score && h < g)) ? 1 : 0;
   }
-  const bool in = j < a.groups && ahead < a.topk_groups;
+  const bool in = g < a.groups && ahead < a.topk_groups;
   const unsigned mask = (unsigned)(__ballot(in) >> (threadIdx.x & 48)) & 0xffffu;
+  const auto stays = [&](int e) { return (mask >> (((e * a.group_mul >> 16) << log2p) & 15)) & 1u; };   // (past E masked already)
+  if (fours) {
 #pragma unroll
-  for (int r = 0; r < N; ++r)
-    if (!((mask >> ((expert_of(r, j) * a.group_mul >> 16) & 15)) & 1u)) order[r] = -INFINITY;   // (past E masked already)
+    for (int q = 0; q < N / 4; ++q) {
+      const bool on = stays(64 * q + 4 * j);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) order[4 * q + i] = on ? order[4 * q + i] : (T)-INFINITY;
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < N; ++r) order[r] = stays(expert_of(r, j)) ? order[r] : (T)-INFINITY;
+  }
+  wave_sync();   // the scores have been read
   if (a.topk_groups == a.groups) return true;
-  const T last = -row_max(in ? -score : (T)-INFINITY), next = row_max(j < a.groups && !in ? score : (T)-INFINITY);
+  const T last = -row_max(in ? -score : (T)-INFINITY), next = row_max(g < a.groups && !in ? score : (T)-INFINITY);
   return next == -INFINITY || last - next > slack + relative * (fabs(last) + fabs(next));
+}
+
+// The list by integers that hold key and expert, all different: a lane's are sorted once, then every round takes the largest
+// head and its lane moves up.  Lane j keeps entry j; `rest`: the largest that is not listed.  Below 0: masked.
+constexpr int NONE = INT_MIN;
+template <int N, int DEPTH>
+__device__ __forceinline__ void pop_rounds(int rounds, int j, int (&s)[N], int& mine) {
+  for (int round = 0; round < rounds; ++round) {
+    const int top = row_max(s[0]);
+    mine = j == round ? top : mine;
+    const bool won = s[0] == top;
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) {
+      const int here = s[i], next = i + 1 < N ? s[i + 1 < N ? i + 1 : 0] : NONE;   // (values: not a choice of places)
+      s[i] = won ? next : here;
+    }
+  }
+}
+template <int N>
+__device__ __forceinline__ int list_packed(int rounds, int j, int (&s)[N], int& rest) {
+  // Batcher's merge exchange, largest first
+#pragma unroll
+  for (int p = 1; p < N; p *= 2) {
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2) {
+#pragma unroll
+      for (int x = k % p; x + k < N; x += 2 * k) {
+#pragma unroll
+        for (int i = 0; i < k; ++i) {
+          const int lo = x + i, hi = x + i + k;
+          if (hi < N && lo / (2 * p) == hi / (2 * p)) {
+            const int big = max(s[lo], s[hi]), small = min(s[lo], s[hi]);
+            s[lo] = big;
+            s[hi] = small;
+          }
+        }
+      }
+    }
+  }
+  int mine = NONE;
+  // a lane is asked for at most `rounds` heads, and one more for `rest`
+  if (N > 8 && rounds <= 8) pop_rounds<N, N < 9 ? N : 9>(rounds, j, s, mine);
+  else pop_rounds<N, N>(rounds, j, s, mine);
+  rest = row_max(s[0]);
+  return mine;
+}
+__device__ __forceinline__ int unpack_expert(int packed) { return packed < 0 ? -1 : 255 - (packed & 255); }
+__device__ __forceinline__ int masked_below_zero(int packed, float order) { return packed | (order > -INFINITY ? 0 : NONE); }
+
+// Key and expert in one integer: the distance to the row's largest key `top` in 2^23 steps over RANGE, then the expert, lower
+// ones larger.  Keys further below than RANGE are all 0.
+constexpr float KEY_RANGE = 4.0f;      // of scores (0 .. 1) with a bias
+constexpr float LOGIT_RANGE = 64.0f;
+template <int N>
+__device__ __forceinline__ void pack_below(const float (&order)[N], float top, float range, int j, int (&s)[N]) {
+#pragma unroll
+  for (int r = 0; r < N; ++r) {
+    const int q = min((int)fmaxf(((order[r] - top) + range) * (0x1p23f / range), 0.0f), 0x7fffff);
+    s[r] = masked_below_zero((q << 8) | (255 - expert_of(r, j)), order[r]);
+  }
+}
+// Whether entries j < k of the list differ from the ones behind them by more than `steps` and none is past the range.
+__device__ __forceinline__ bool apart(int mine, int rest, int k, int rounds, int j, int steps) {
+  const int behind = row_rotate<15>(mine);   // of lane j + 1
+  const int next = j + 1 < rounds ? behind : rest;
+  return (j >= k) | (mine < 0) | (((mine >> 8) > 0) & ((next < 0) | ((mine >> 8) - (next >> 8) > steps)));
 }
 
 // k rounds of the largest that is left (ties: lowest expert); lane j keeps entry j: its expert (-1: none) and key.
@@ -179,11 +300,11 @@ __device__ __forceinline__ int list_largest(int k, int rounds, int j, T (&order)
 }
 
 // KEYED: the keys are scores with a bias, or sums of scores rank the groups; else the logits are the keys.
-template <typename ZT, int NQ, bool KEYED>
+template <typename ZT, int NQ, bool KEYED, bool SIGMOID>
 __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
   constexpr int N = 4 * NQ, STRIDE = 64 * NQ + 4;
   typedef std::conditional_t<KEYED, double, float> wide_t;
-  __shared__ wide_t ks[ROWS][STRIDE];   // keys, for groups
+  __shared__ __align__(32) wide_t ks[ROWS][STRIDE];   // keys, for groups
   const int j = threadIdx.x & 15, tok = threadIdx.x >> 4;
   const bool tv = (int)blockIdx.x * ROWS + tok < a.T;
   const int t = tv ? (int)blockIdx.x * ROWS + tok : a.T - 1;
@@ -194,7 +315,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
   const int k = visual ? a.k_visual : a.k_text;
 
   float m = 0.0f, inv = 1.0f;   // softmax scores are exp(z - m) * inv
-  if (!a.sigmoid && (KEYED || a.scores != nullptr || !a.renorm)) {
+  if (!SIGMOID && (KEYED || a.scores != nullptr || !a.renorm)) {
     m = row_largest(z);
     const float sum = row_exp_sum(z, m);
     inv = sum > 0.0f ? 1.0f / sum : 0.0f;
@@ -202,7 +323,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
   if (a.scores != nullptr && tv) {
     float s[N];
 #pragma unroll
-    for (int r = 0; r < N; ++r) s[r] = a.sigmoid ? 1.0f / (1.0f + expf(-z[r])) : expf(z[r] - m) * inv;
+    for (int r = 0; r < N; ++r) s[r] = SIGMOID ? 1.0f / (1.0f + expf(-z[r])) : expf(z[r] - m) * inv;
     write_row<float, NQ>(a.scores + (size_t)t * a.E, a.E, j, s);
   }
 
@@ -215,69 +336,84 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
 #pragma unroll
       for (int r = 0; r < N; ++r) bias[r] = 0.0f;
     }
+    // masked experts have bias -inf, whose sum with a score is -inf: no branches around the scores
+#pragma unroll
+    for (int r = 0; r < N; ++r) bias[r] = (z[r] > -INFINITY) & (bias[r] > -INFINITY) ? bias[r] : -INFINITY;
     bool sure = true;
     {
-      const float largest = a.sigmoid ? 1.0f : inv;
-      const float slack = largest * 0x1p-19f;
-      constexpr float RELATIVE = 0x1p-22f;
+      const float slack = (SIGMOID ? 1.0f : inv) * 0x1p-19f;
       float key[N], order[N];
 #pragma unroll
       for (int r = 0; r < N; ++r) {
-        const float s = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + __expf(-z[r])) : __expf(z[r] - m) * inv;
-        key[r] = z[r] > -INFINITY && bias[r] > -INFINITY ? s + bias[r] : -INFINITY;
+        const float s = SIGMOID ? __builtin_amdgcn_rcpf(1.0f + __expf(-z[r])) : __expf(z[r] - m) * inv;
+        key[r] = s + bias[r];
         order[r] = a.bias != nullptr ? key[r] : z[r];
       }
       if (a.groups > 1)
-        sure = keep_groups<float, N>(a, j, key, order, reinterpret_cast<float*>(ks[tok]), 2.0f * slack, 2.0f * RELATIVE);
-      float my_key;
-      mine = list_largest<float, N>(k, a.Kmax, j, order, my_key);
-      if (a.bias != nullptr) {
-        // the largest that is not listed; then every entry against the one behind it
-        float rest = order[0];
-#pragma unroll
-        for (int r = 1; r < N; ++r) rest = larger(rest, order[r]);
-        rest = row_max(rest);
-        const int listed = __popc((unsigned)(__ballot(mine >= 0) >> (threadIdx.x & 48)) & 0xffffu);
-        const float behind = __shfl(my_key, (threadIdx.x & 48) + ((j + 1) & 15), 64);
-        const float next = j + 1 < listed ? behind : rest;
-        sure = sure && (mine < 0 || next == -INFINITY || my_key - next > slack + RELATIVE * (fabsf(my_key) + fabsf(next)));
-      }
+        sure = keep_groups<float, N>(a, j, key, order, reinterpret_cast<float*>(ks[tok]), 2.0f * slack, 0x1p-21f);
+      const float top = row_largest(order);
+      const float range = a.bias != nullptr ? KEY_RANGE : LOGIT_RANGE;
+      int packed[N], rest;
+      pack_below(order, top, range, j, packed);
+      const int entry = list_packed(a.Kmax, j, packed, rest);
+      // besides the scores' errors: half a rounding of the key, of its distance and of the two steps to the integer, twice;
+      // and the two integers' own
+      const float off = (a.bias != nullptr ? slack + 0x1p-23f * fabsf(top) : 0.0f) + 0x1p-21f * range;
+      const int steps = (int)fminf(off * (0x1p23f / range), 1e6f) + 3;
+      sure = sure && fabsf(top) < 1e30f && apart(entry, rest, k, a.Kmax, j, steps);
+      mine = j < k ? unpack_expert(entry) : -1;
     }
     if (__any(!sure)) {
       double key[N], order[N], sum = 0.0, my_key;
-      if (!a.sigmoid) {
+      if (!SIGMOID) {
 #pragma unroll
         for (int r = 0; r < N; ++r) sum += exp((double)z[r] - (double)m);
         sum = row_sum_butterfly(sum);
       }
 #pragma unroll
       for (int r = 0; r < N; ++r) {
-        const double s = a.sigmoid ? 1.0 / (1.0 + exp(-(double)z[r])) : exp((double)z[r] - (double)m) / sum;
-        key[r] = z[r] > -INFINITY && bias[r] > -INFINITY ? s + (double)bias[r] : -INFINITY;
+        const double s = SIGMOID ? 1.0 / (1.0 + exp(-(double)z[r])) : exp((double)z[r] - (double)m) / sum;
+        key[r] = s + (double)bias[r];
         order[r] = a.bias != nullptr ? key[r] : (double)z[r];
       }
-      wave_sync();
       if (a.groups > 1) (void)keep_groups<double, N>(a, j, key, order, ks[tok], 0.0, 0.0);
       mine = list_largest<double, N>(k, a.Kmax, j, order, my_key);
     }
   } else {
-    float key[N], my_key;
+    float order[N], my_key;
 #pragma unroll
-    for (int r = 0; r < N; ++r) key[r] = z[r];
-    if (a.groups > 1) (void)keep_groups<float, N>(a, j, key, z, ks[tok], 0.0f, 0.0f);
-    mine = list_largest<float, N>(k, a.Kmax, j, z, my_key);
+    for (int r = 0; r < N; ++r) order[r] = z[r];
+    if (a.groups > 1) (void)keep_groups<float, N>(a, j, z, order, ks[tok], 0.0f, 0.0f);
+    int packed[N], rest;
+    if constexpr (sizeof(ZT) == 2) {
+      // a bf16 logit's sixteen bits and the expert are one integer: exact, equal ones in order of the expert
+#pragma unroll
+      for (int r = 0; r < N; ++r) {
+        int o = __float_as_int(order[r] == FLT_MAX ? INFINITY : order[r] + 0.0f);   // as it came; -0 is +0
+        o ^= (o >> 31) & 0x7fffffff;                                                  // in order as a signed integer
+        packed[r] = masked_below_zero((((o >> 16) + 0x8000) << 8) | (255 - expert_of(r, j)), order[r]);
+      }
+      const int entry = list_packed(a.Kmax, j, packed, rest);
+      mine = j < k ? unpack_expert(entry) : -1;
+    } else {
+      const float top = row_largest(order);
+      pack_below(order, top, LOGIT_RANGE, j, packed);
+      const int entry = list_packed(a.Kmax, j, packed, rest);
+      mine = j < k ? unpack_expert(entry) : -1;
+      if (__any(!(fabsf(top) < 1e30f && apart(entry, rest, k, a.Kmax, j, 7)))) mine = list_largest<float, N>(k, a.Kmax, j, order, my_key);
+    }
   }
 
   const float zl = mine >= 0 ? clean(to_f32(logits[(size_t)t * a.E + mine])) : -INFINITY;
   float g;
   if (a.renorm) {
-    const float l = mine >= 0 ? (a.sigmoid ? log_sigmoid(zl) : zl) : -INFINITY;
+    const float l = mine >= 0 ? (SIGMOID ? log_sigmoid(zl) : zl) : -INFINITY;
     const float lm = row_max(l);
     const float p = mine >= 0 ? expf(l - lm) : 0.0f;
     const float sum = row_sum_butterfly(p);   // (every lane takes part)
     g = mine >= 0 ? p / sum : 0.0f;
   } else {
-    g = mine < 0 ? 0.0f : a.sigmoid ? 1.0f / (1.0f + expf(-zl)) : expf(zl - m) * inv;
+    g = mine < 0 ? 0.0f : SIGMOID ? 1.0f / (1.0f + expf(-zl)) : expf(zl - m) * inv;
   }
   if (tv && j < a.Kmax) {
     a.idx[(size_t)t * a.Kmax + j] = mine;
@@ -391,8 +527,13 @@ __global__ __launch_bounds__(256) void select_backward_kernel(SelectBackwardArgs
 template <typename ZT, int NQ>
 void run_select(const SelectArgs& a, bool keyed, hipStream_t stream) {
   const dim3 grid((a.T + ROWS - 1) / ROWS), block(256);
-  if (keyed) hipLaunchKernelGGL((select_kernel<ZT, NQ, true>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((select_kernel<ZT, NQ, false>), grid, block, 0, stream, a);
+#define FMOE_SELECT(KEYED, SIGMOID) \
+  hipLaunchKernelGGL((select_kernel<ZT, NQ, KEYED, SIGMOID>), grid, block, 0, stream, a)
+  if (keyed && a.sigmoid) FMOE_SELECT(true, true);
+  else if (keyed) FMOE_SELECT(true, false);
+  else if (a.sigmoid) FMOE_SELECT(false, true);
+  else FMOE_SELECT(false, false);
+#undef FMOE_SELECT
 }
 template <typename ZT>
 void run_select_by_size(const SelectArgs& a, bool keyed, hipStream_t stream) {
