@@ -124,29 +124,19 @@ __device__ __forceinline__ float lane_partner(float v) {
   constexpr int CTRL = LOG2 == 0 ? 0xb1 : LOG2 == 1 ? 0x4e : 0x141;   // quad permutations, half-row mirror
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
 }
-template <int LOG2>
-__device__ __forceinline__ double lane_partner(double v) {
-  constexpr int CTRL = LOG2 == 0 ? 0xb1 : LOG2 == 1 ? 0x4e : 0x141;
-  return __hiloint2double(__builtin_amdgcn_mov_dpp(__double2hiint(v), CTRL, 0xf, 0xf, true),
-                          __builtin_amdgcn_mov_dpp(__double2loint(v), CTRL, 0xf, 0xf, true));
-}
-template <typename T>
-__device__ __forceinline__ T smaller(T v, T o) { return (o < v) ? o : v; }
-
 // The two largest so far, and two more.
-template <typename T>
-__device__ __forceinline__ void two_largest(T& one, T& two, T o1, T o2) {
-  two = larger(smaller(one, o1), larger(two, o2));
-  one = larger(one, o1);
+__device__ __forceinline__ void two_largest(float& one, float& two, float o1, float o2) {
+  two = fmaxf(fminf(one, o1), fmaxf(two, o2));
+  one = fmaxf(one, o1);
 }
 
 // Masks the experts of a token's groups that do not stay.  key: what a group's score is made of; order: what ranks the
 // experts; ks: the token's row in LDS.  Returns whether the scores on either side of the line are further apart than `slack`
-// plus `relative` times their size (32 bits; not asked for in 64).  2^log2p lanes have a group.
-template <typename T, int N>
-__device__ __forceinline__ bool keep_groups(const SelectArgs& a, int j, const T (&key)[N], T (&order)[N], T* ks, T slack,
-                                            T relative) {
-  typedef T four_t __attribute__((ext_vector_type(4)));
+// plus `relative` times their size.  2^log2p lanes have a group.
+template <int N>
+__device__ __forceinline__ bool keep_groups(const SelectArgs& a, int j, const float (&key)[N], float (&order)[N], float* ks,
+                                            float slack, float relative) {
+  typedef float four_t __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int q = 0; q < N / 4; ++q)
     *reinterpret_cast<four_t*>(ks + 64 * q + 4 * j) = four_t{key[4 * q], key[4 * q + 1], key[4 * q + 2], key[4 * q + 3]};
@@ -154,37 +144,37 @@ __device__ __forceinline__ bool keep_groups(const SelectArgs& a, int j, const T 
   const int log2p = a.groups <= 2 ? 3 : a.groups <= 4 ? 2 : a.groups <= 8 ? 1 : 0;   // uniform
   const int g = j >> log2p, part = j & ((1 << log2p) - 1);
   const bool fours = (a.group_size & 3) == 0;
-  T one = -INFINITY, two = -INFINITY;
+  float one = -INFINITY, two = -INFINITY;
   if (g < a.groups) {
-    const T* const own = ks + g * a.group_size;
+    const float* const own = ks + g * a.group_size;
     if (fours) {
       for (int i = 4 * part; i < a.group_size; i += 4 << log2p) {
         const four_t v = *reinterpret_cast<const four_t*>(own + i);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          two = larger(two, smaller(one, v[x]));
-          one = larger(one, v[x]);
+          two = fmaxf(two, fminf(one, v[x]));
+          one = fmaxf(one, v[x]);
         }
       }
     } else {
       for (int i = part; i < a.group_size; i += 1 << log2p) {
-        const T v = own[i];
-        two = larger(two, smaller(one, v));
-        one = larger(one, v);
+        const float v = own[i];
+        two = fmaxf(two, fminf(one, v));
+        one = fmaxf(one, v);
       }
     }
   }
   if (log2p > 0) two_largest(one, two, lane_partner<0>(one), lane_partner<0>(two));
   if (log2p > 1) two_largest(one, two, lane_partner<1>(one), lane_partner<1>(two));
   if (log2p > 2) two_largest(one, two, lane_partner<2>(one), lane_partner<2>(two));
-  const T score = (a.sum_two && two > -INFINITY) ? one + two : one;
+  const float score = (a.sum_two && two > -INFINITY) ? one + two : one;
   // rank among the groups: larger scores, or equal ones of lower groups, are ahead
   wave_sync();   // the keys have been read
   if (part == 0) ks[g] = score;
   wave_sync();
   int ahead = 0;
   for (int h = 0; h < a.groups; ++h) {
-    const T o = ks[h];
+    const float o = ks[h];
     ahead += (o > score || (o == score && h < g)) ? 1 : 0;
   }
   const bool in = g < a.groups && ahead < a.topk_groups;
@@ -195,16 +185,16 @@ __device__ __forceinline__ bool keep_groups(const SelectArgs& a, int j, const T 
     for (int q = 0; q < N / 4; ++q) {
       const bool on = stays(64 * q + 4 * j);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) order[4 * q + i] = on ? order[4 * q + i] : (T)-INFINITY;
+      for (int i = 0; i < 4; ++i) order[4 * q + i] = on ? order[4 * q + i] : -INFINITY;
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < N; ++r) order[r] = stays(expert_of(r, j)) ? order[r] : (T)-INFINITY;
+    for (int r = 0; r < N; ++r) order[r] = stays(expert_of(r, j)) ? order[r] : -INFINITY;
   }
   wave_sync();   // the scores have been read
   if (a.topk_groups == a.groups) return true;
-  const T last = -row_max(in ? -score : (T)-INFINITY), next = row_max(g < a.groups && !in ? score : (T)-INFINITY);
-  return next == -INFINITY || last - next > slack + relative * (fabs(last) + fabs(next));
+  const float last = -row_max(in ? -score : -INFINITY), next = row_max(g < a.groups && !in ? score : -INFINITY);
+  return next == -INFINITY || last - next > slack + relative * (fabsf(last) + fabsf(next));
 }
 
 // The list by integers that hold key and expert, all different: a lane's are sorted once, then every round takes the largest
@@ -273,28 +263,75 @@ __device__ __forceinline__ bool apart(int mine, int rest, int k, int rounds, int
   return (j >= k) | (mine < 0) | (((mine >> 8) > 0) & ((next < 0) | ((mine >> 8) - (next >> 8) > steps)));
 }
 
-// k rounds of the largest that is left (ties: lowest expert); lane j keeps entry j: its expert (-1: none) and key.
-template <typename T, int N>
-__device__ __forceinline__ int list_largest(int k, int rounds, int j, T (&order)[N], T& my_key) {
-  int mine = -1;
-  my_key = -INFINITY;
-  for (int round = 0; round < rounds; ++round) {
-    T v = order[0];
+// ---- one token by a whole wavefront, in 64 bits: what the definition says, for the few that are close.
+__device__ __forceinline__ double wave_max(double v) {
 #pragma unroll
-    for (int r = 1; r < N; ++r) v = larger(v, order[r]);
-    const T top = row_max(v);
+  for (int s = 32; s >= 1; s >>= 1) v = larger(v, __shfl_xor(v, s, 64));
+  return v;
+}
+// Lane i of the result: entry i of the token's list.  Lane l has experts 4 l .. 4 l + 3; ks: room for E doubles.
+template <typename ZT, bool KEYED, bool SIGMOID>
+__device__ int list_wide(const SelectArgs& a, int t, int k, double* ks) {
+  const int lane = threadIdx.x & 63;
+  const ZT* const row = static_cast<const ZT*>(a.z) + (size_t)t * a.E;
+  double z[4], key[4], order[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) z[i] = 4 * lane + i < a.E ? clean(to_f32(row[4 * lane + i])) : -INFINITY;
+  double m = 0.0, sum = 1.0;
+  if (KEYED && !SIGMOID) {
+    m = wave_max(larger(larger(z[0], z[1]), larger(z[2], z[3])));
+    if (!(m > -INFINITY)) m = 0.0;
+    sum = exp(z[0] - m) + exp(z[1] - m) + exp(z[2] - m) + exp(z[3] - m);
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) sum += __shfl_xor(sum, s, 64);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int e = 4 * lane + i;
+    order[i] = key[i] = z[i];
+    if (KEYED) {
+      const float b = a.bias != nullptr && e < a.E ? a.bias[e] : 0.0f;
+      const double s = SIGMOID ? 1.0 / (1.0 + exp(-z[i])) : exp(z[i] - m) / sum;
+      key[i] = z[i] > -INFINITY && b > -INFINITY ? s + (double)b : -INFINITY;
+      if (a.bias != nullptr) order[i] = key[i];
+    }
+  }
+  if (a.groups > 1) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (4 * lane + i < a.E) ks[4 * lane + i] = key[i];
+    wave_sync();
+    double one = -INFINITY, two = -INFINITY;   // lane g: group g
+    for (int i = 0; i < a.group_size && lane < a.groups; ++i) {
+      const double v = ks[lane * a.group_size + i];
+      two = v > one ? one : larger(two, v);
+      one = larger(one, v);
+    }
+    wave_sync();
+    const double score = (a.sum_two && two > -INFINITY) ? one + two : one;
+    int ahead = 0;
+    for (int g = 0; g < a.groups; ++g) {
+      const double o = __shfl(score, g, 64);
+      ahead += (o > score || (o == score && g < lane)) ? 1 : 0;
+    }
+    const unsigned mask = (unsigned)__ballot(lane < a.groups && ahead < a.topk_groups);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (!((mask >> (((4 * lane + i) * a.group_mul >> 16) & 15)) & 1u)) order[i] = -INFINITY;
+  }
+  int mine = -1;
+  for (int round = 0; round < k; ++round) {
+    const double top = wave_max(larger(larger(order[0], order[1]), larger(order[2], order[3])));
+    if (!(top > -INFINITY)) break;
     int e = 0x7fff;
 #pragma unroll
-    for (int r = N - 1; r >= 0; --r) e = order[r] == top ? expert_of(r, j) : e;
-    e = row_min(e);
-    if (j == round && round < k && top > -INFINITY) {
-      mine = e;
-      my_key = top;
-    }
-    if (round < k) {
+    for (int i = 3; i >= 0; --i) e = order[i] == top ? 4 * lane + i : e;
 #pragma unroll
-      for (int r = 0; r < N; ++r) order[r] = expert_of(r, j) == e ? (T)-INFINITY : order[r];
-    }
+    for (int s = 32; s >= 1; s >>= 1) e = min(e, __shfl_xor(e, s, 64));   // ties: lowest expert
+    if (lane == round) mine = e;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (4 * lane + i == e) order[i] = -INFINITY;
   }
   return mine;
 }
@@ -303,8 +340,7 @@ __device__ __forceinline__ int list_largest(int k, int rounds, int j, T (&order)
 template <typename ZT, int NQ, bool KEYED, bool SIGMOID>
 __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
   constexpr int N = 4 * NQ, STRIDE = 64 * NQ + 4;
-  typedef std::conditional_t<KEYED, double, float> wide_t;
-  __shared__ __align__(32) wide_t ks[ROWS][STRIDE];   // keys, for groups
+  __shared__ __align__(16) float ks[ROWS][STRIDE];   // keys, for groups
   const int j = threadIdx.x & 15, tok = threadIdx.x >> 4;
   const bool tv = (int)blockIdx.x * ROWS + tok < a.T;
   const int t = tv ? (int)blockIdx.x * ROWS + tok : a.T - 1;
@@ -327,64 +363,40 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
     write_row<float, NQ>(a.scores + (size_t)t * a.E, a.E, j, s);
   }
 
-  int mine;
+  // the list in 32 bits, and whether it is sure
+  float order[N];
+  bool sure = true;
+  int packed[N], rest, steps = 7;   // of two logits: half a rounding of the distance and of the step to the integer each, the integers' own
+  float range = LOGIT_RANGE;
   if constexpr (KEYED) {
-    float bias[N];
+    float bias[N], key[N];
     if (a.bias != nullptr) {   // uniform
       read_row<float, NQ>(a.bias, a.E, j, bias);
     } else {
 #pragma unroll
       for (int r = 0; r < N; ++r) bias[r] = 0.0f;
     }
+    const float slack = (SIGMOID ? 1.0f : inv) * 0x1p-19f;
     // masked experts have bias -inf, whose sum with a score is -inf: no branches around the scores
 #pragma unroll
-    for (int r = 0; r < N; ++r) bias[r] = (z[r] > -INFINITY) & (bias[r] > -INFINITY) ? bias[r] : -INFINITY;
-    bool sure = true;
-    {
-      const float slack = (SIGMOID ? 1.0f : inv) * 0x1p-19f;
-      float key[N], order[N];
-#pragma unroll
-      for (int r = 0; r < N; ++r) {
-        const float s = SIGMOID ? __builtin_amdgcn_rcpf(1.0f + __expf(-z[r])) : __expf(z[r] - m) * inv;
-        key[r] = s + bias[r];
-        order[r] = a.bias != nullptr ? key[r] : z[r];
-      }
-      if (a.groups > 1)
-        sure = keep_groups<float, N>(a, j, key, order, reinterpret_cast<float*>(ks[tok]), 2.0f * slack, 0x1p-21f);
-      const float top = row_largest(order);
-      const float range = a.bias != nullptr ? KEY_RANGE : LOGIT_RANGE;
-      int packed[N], rest;
-      pack_below(order, top, range, j, packed);
-      const int entry = list_packed(a.Kmax, j, packed, rest);
-      // besides the scores' errors: half a rounding of the key, of its distance and of the two steps to the integer, twice;
-      // and the two integers' own
-      const float off = (a.bias != nullptr ? slack + 0x1p-23f * fabsf(top) : 0.0f) + 0x1p-21f * range;
-      const int steps = (int)fminf(off * (0x1p23f / range), 1e6f) + 3;
-      sure = sure && fabsf(top) < 1e30f && apart(entry, rest, k, a.Kmax, j, steps);
-      mine = j < k ? unpack_expert(entry) : -1;
+    for (int r = 0; r < N; ++r) {
+      bias[r] = (z[r] > -INFINITY) & (bias[r] > -INFINITY) ? bias[r] : -INFINITY;
+      const float s = SIGMOID ? __builtin_amdgcn_rcpf(1.0f + __expf(-z[r])) : __expf(z[r] - m) * inv;
+      key[r] = s + bias[r];
+      order[r] = a.bias != nullptr ? key[r] : z[r];
     }
-    if (__any(!sure)) {
-      double key[N], order[N], sum = 0.0, my_key;
-      if (!SIGMOID) {
-#pragma unroll
-        for (int r = 0; r < N; ++r) sum += exp((double)z[r] - (double)m);
-        sum = row_sum_butterfly(sum);
-      }
-#pragma unroll
-      for (int r = 0; r < N; ++r) {
-        const double s = SIGMOID ? 1.0 / (1.0 + exp(-(double)z[r])) : exp((double)z[r] - (double)m) / sum;
-        key[r] = s + (double)bias[r];
-        order[r] = a.bias != nullptr ? key[r] : (double)z[r];
-      }
-      if (a.groups > 1) (void)keep_groups<double, N>(a, j, key, order, ks[tok], 0.0, 0.0);
-      mine = list_largest<double, N>(k, a.Kmax, j, order, my_key);
+    if (a.groups > 1) sure = keep_groups<N>(a, j, key, order, ks[tok], 2.0f * slack, 0x1p-21f);
+    const float top = row_largest(order);
+    if (a.bias != nullptr) {
+      range = KEY_RANGE;
+      steps = (int)fminf((slack + 0x1p-23f * fabsf(top) + 0x1p-21f * KEY_RANGE) * (0x1p23f / KEY_RANGE), 1e6f) + 3;
     }
+    pack_below(order, top, range, j, packed);
+    sure = sure & (fabsf(top) < 1e30f);
   } else {
-    float order[N], my_key;
 #pragma unroll
     for (int r = 0; r < N; ++r) order[r] = z[r];
-    if (a.groups > 1) (void)keep_groups<float, N>(a, j, z, order, ks[tok], 0.0f, 0.0f);
-    int packed[N], rest;
+    if (a.groups > 1) (void)keep_groups<N>(a, j, z, order, ks[tok], 0.0f, 0.0f);
     if constexpr (sizeof(ZT) == 2) {
       // a bf16 logit's sixteen bits and the expert are one integer: exact, equal ones in order of the expert
 #pragma unroll
@@ -393,14 +405,24 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
         o ^= (o >> 31) & 0x7fffffff;                                                  // in order as a signed integer
         packed[r] = masked_below_zero((((o >> 16) + 0x8000) << 8) | (255 - expert_of(r, j)), order[r]);
       }
-      const int entry = list_packed(a.Kmax, j, packed, rest);
-      mine = j < k ? unpack_expert(entry) : -1;
     } else {
       const float top = row_largest(order);
       pack_below(order, top, LOGIT_RANGE, j, packed);
-      const int entry = list_packed(a.Kmax, j, packed, rest);
-      mine = j < k ? unpack_expert(entry) : -1;
-      if (__any(!(fabsf(top) < 1e30f && apart(entry, rest, k, a.Kmax, j, 7)))) mine = list_largest<float, N>(k, a.Kmax, j, order, my_key);
+      sure = fabsf(top) < 1e30f;
+    }
+  }
+  const int entry = list_packed(a.Kmax, j, packed, rest);
+  int mine = j < k ? unpack_expert(entry) : -1;
+  if constexpr (KEYED || sizeof(ZT) == 4) {
+    sure = sure & apart(entry, rest, k, a.Kmax, j, steps);
+    unsigned long long again = __ballot(!sure);
+    while (again != 0) {   // uniform
+      const int first = (__ffsll((long long)again) - 1) & 48;   // the token's first lane
+      again &= ~(0xffffull << first);
+      const int list = list_wide<ZT, KEYED, SIGMOID>(a, __shfl(t, first, 64), __shfl(k, first, 64),
+                                                     reinterpret_cast<double*>(ks[tok & 12]));
+      const int mine_again = __shfl(list, j, 64);
+      mine = (threadIdx.x & 48) == (unsigned)first ? mine_again : mine;
     }
   }
 
