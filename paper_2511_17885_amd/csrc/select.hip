@@ -42,7 +42,7 @@ struct SelectArgs {
 };
 
 // A logit as the definitions take it: NaN is masked like -inf, +inf is the largest finite number.
-__device__ __forceinline__ float clean(float z) { return z > -INFINITY ? fminf(z, FLT_MAX) : -INFINITY; }
+__device__ __forceinline__ float clean(float z) { return fminf(fmaxf(z, -INFINITY), FLT_MAX); }
 
 __device__ __forceinline__ float log_sigmoid(float z) { return fminf(z, 0.0f) - log1pf(expf(-fabsf(z))); }
 
@@ -90,13 +90,17 @@ __device__ __forceinline__ void load_row(const ZT* __restrict__ z, int t, int E,
   for (int r = 0; r < 4 * NQ; ++r) v[r] = 64 * (r >> 2) + 4 * j + (r & 3) < E ? clean(to_f32(raw[r])) : -INFINITY;
 }
 
-// Of a row's logits: the largest (0 if all are masked) and the sum of exp(z - largest).
+// Of a row: the largest, of its logits also 0 if all are masked, and the sum of exp(z - largest).
 template <int N>
-__device__ __forceinline__ float row_largest(const float (&z)[N]) {
+__device__ __forceinline__ float row_peak(const float (&z)[N]) {
   float m = z[0];
 #pragma unroll
-  for (int r = 1; r < N; ++r) m = larger(m, z[r]);
-  m = row_max(m);
+  for (int r = 1; r < N; ++r) m = fmaxf(m, z[r]);
+  return row_max(m);
+}
+template <int N>
+__device__ __forceinline__ float row_largest(const float (&z)[N]) {
+  const float m = row_peak(z);
   return m > -INFINITY ? m : 0.0f;
 }
 template <int N>
@@ -245,22 +249,24 @@ __device__ __forceinline__ int unpack_expert(int packed) { return packed < 0 ? -
 __device__ __forceinline__ int masked_below_zero(int packed, float order) { return packed | (order > -INFINITY ? 0 : NONE); }
 
 // Key and expert in one integer: the distance to the row's largest key `top` in 2^23 steps over RANGE, then the expert, lower
-// ones larger.  Keys further below than RANGE are all 0.
+// ones larger.  Keys further below than RANGE, and masked ones, have no steps.
 constexpr float KEY_RANGE = 4.0f;      // of scores (0 .. 1) with a bias
 constexpr float LOGIT_RANGE = 64.0f;
 template <int N>
 __device__ __forceinline__ void pack_below(const float (&order)[N], float top, float range, int j, int (&s)[N]) {
+  const float scale = 8388600.0f / range, offset = (range - top) * scale;   // (the largest stays below 2^23)
+  const int lane_part = (15 - j) * 4;
 #pragma unroll
   for (int r = 0; r < N; ++r) {
-    const int q = min((int)fmaxf(((order[r] - top) + range) * (0x1p23f / range), 0.0f), 0x7fffff);
-    s[r] = masked_below_zero((q << 8) | (255 - expert_of(r, j)), order[r]);
+    const unsigned q = (unsigned)fmaf(order[r], scale, offset);   // saturates at 0, also for -inf
+    s[r] = (int)((q << 8) | lane_part) | (192 - 64 * (r >> 2) + 3 - (r & 3));   // .. 255 - expert
   }
 }
-// Whether entries j < k of the list differ from the ones behind them by more than `steps` and none is past the range.
+// Whether entries j < k of the list differ from the ones behind them by more than `steps` and all are in range.
 __device__ __forceinline__ bool apart(int mine, int rest, int k, int rounds, int j, int steps) {
   const int behind = row_rotate<15>(mine);   // of lane j + 1
   const int next = j + 1 < rounds ? behind : rest;
-  return (j >= k) | (mine < 0) | (((mine >> 8) > 0) & ((next < 0) | ((mine >> 8) - (next >> 8) > steps)));
+  return (j >= k) | (((mine >> 8) > 0) & ((mine >> 8) - (next >> 8) > steps));
 }
 
 // ---- one token by a whole wavefront, in 64 bits: what the definition says, for the few that are close.
@@ -366,8 +372,6 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
   // the list in 32 bits, and whether it is sure
   float order[N];
   bool sure = true;
-  int packed[N], rest, steps = 7;   // of two logits: half a rounding of the distance and of the step to the integer each, the integers' own
-  float range = LOGIT_RANGE;
   if constexpr (KEYED) {
     float bias[N], key[N];
     if (a.bias != nullptr) {   // uniform
@@ -377,44 +381,55 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
       for (int r = 0; r < N; ++r) bias[r] = 0.0f;
     }
     const float slack = (SIGMOID ? 1.0f : inv) * 0x1p-19f;
-    // masked experts have bias -inf, whose sum with a score is -inf: no branches around the scores
 #pragma unroll
     for (int r = 0; r < N; ++r) {
-      bias[r] = (z[r] > -INFINITY) & (bias[r] > -INFINITY) ? bias[r] : -INFINITY;
       const float s = SIGMOID ? __builtin_amdgcn_rcpf(1.0f + __expf(-z[r])) : __expf(z[r] - m) * inv;
-      key[r] = s + bias[r];
-      order[r] = a.bias != nullptr ? key[r] : z[r];
+      const float u = fmaxf(s + bias[r], -INFINITY);   // bias NaN or -inf: masked
+      key[r] = z[r] > -INFINITY ? u : -INFINITY;
+    }
+    if (a.bias != nullptr) {
+#pragma unroll
+      for (int r = 0; r < N; ++r) order[r] = key[r];
+    } else {
+#pragma unroll
+      for (int r = 0; r < N; ++r) order[r] = z[r];
     }
     if (a.groups > 1) sure = keep_groups<N>(a, j, key, order, ks[tok], 2.0f * slack, 0x1p-21f);
-    const float top = row_largest(order);
-    if (a.bias != nullptr) {
-      range = KEY_RANGE;
-      steps = (int)fminf((slack + 0x1p-23f * fabsf(top) + 0x1p-21f * KEY_RANGE) * (0x1p23f / KEY_RANGE), 1e6f) + 3;
-    }
-    pack_below(order, top, range, j, packed);
-    sure = sure & (fabsf(top) < 1e30f);
   } else {
 #pragma unroll
     for (int r = 0; r < N; ++r) order[r] = z[r];
     if (a.groups > 1) (void)keep_groups<N>(a, j, z, order, ks[tok], 0.0f, 0.0f);
-    if constexpr (sizeof(ZT) == 2) {
-      // a bf16 logit's sixteen bits and the expert are one integer: exact, equal ones in order of the expert
-#pragma unroll
-      for (int r = 0; r < N; ++r) {
-        int o = __float_as_int(order[r] == FLT_MAX ? INFINITY : order[r] + 0.0f);   // as it came; -0 is +0
-        o ^= (o >> 31) & 0x7fffffff;                                                  // in order as a signed integer
-        packed[r] = masked_below_zero((((o >> 16) + 0x8000) << 8) | (255 - expert_of(r, j)), order[r]);
-      }
-    } else {
-      const float top = row_largest(order);
-      pack_below(order, top, LOGIT_RANGE, j, packed);
-      sure = fabsf(top) < 1e30f;
-    }
   }
-  const int entry = list_packed(a.Kmax, j, packed, rest);
-  int mine = j < k ? unpack_expert(entry) : -1;
-  if constexpr (KEYED || sizeof(ZT) == 4) {
-    sure = sure & apart(entry, rest, k, a.Kmax, j, steps);
+  int packed[N], rest, mine;
+  if constexpr (!KEYED && sizeof(ZT) == 2) {
+    // a bf16 logit's sixteen bits and the expert are one integer: exact, equal ones in order of the expert
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      int o = __float_as_int(order[r] == FLT_MAX ? INFINITY : order[r] + 0.0f);   // as it came; -0 is +0
+      o ^= (o >> 31) & 0x7fffffff;                                                  // in order as a signed integer
+      packed[r] = masked_below_zero((((o >> 16) + 0x8000) << 8) | (255 - expert_of(r, j)), order[r]);
+    }
+    const int entry = list_packed(a.Kmax, j, packed, rest);
+    mine = j < k ? unpack_expert(entry) : -1;
+  } else {
+    const float peak = row_peak(order);
+    const bool scored = KEYED && a.bias != nullptr;   // uniform
+    const float range = scored ? KEY_RANGE : LOGIT_RANGE;
+    pack_below(order, peak, range, j, packed);
+    const int entry = list_packed(a.Kmax, j, packed, rest);
+    mine = j < k ? unpack_expert(entry) : -1;
+    // Two integers are off by a rounding of the step to them and their own each, two scored keys by `slack` and half a
+    // rounding each.  (The offset's rounding is the same for all; while the peak is below 8 ranges it is within what is left
+    // between the largest integer and 2^23.)
+    float off = 0.0f;
+    if constexpr (KEYED)
+      if (scored) off = ((SIGMOID ? 1.0f : inv) * 0x1p-19f + 0x1p-23f * (fabsf(peak) + KEY_RANGE)) * (0x1p23f / KEY_RANGE);
+    const int steps = (int)fminf(off, 1e6f) + 3;
+    sure = sure & (fabsf(peak) < 8.0f * range) & apart(entry, rest, k, a.Kmax, j, steps);
+    if (peak == -INFINITY) {   // nothing to choose from
+      sure = true;
+      mine = -1;
+    }
     unsigned long long again = __ballot(!sure);
     while (again != 0) {   // uniform
       const int first = (__ffsll((long long)again) - 1) & 48;   // the token's first lane
@@ -429,9 +444,14 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
   const float zl = mine >= 0 ? clean(to_f32(logits[(size_t)t * a.E + mine])) : -INFINITY;
   float g;
   if (a.renorm) {
-    const float l = mine >= 0 ? (SIGMOID ? log_sigmoid(zl) : zl) : -INFINITY;
-    const float lm = row_max(l);
-    const float p = mine >= 0 ? expf(l - lm) : 0.0f;
+    float p;
+    if (SIGMOID && !__any(mine >= 0 && zl < -60.0f)) {   // no score underflows: shares of the scores themselves
+      p = mine >= 0 ? 1.0f / (1.0f + expf(-zl)) : 0.0f;
+    } else {
+      const float l = mine >= 0 ? (SIGMOID ? log_sigmoid(zl) : zl) : -INFINITY;
+      const float lm = row_max(l);
+      p = mine >= 0 ? expf(l - lm) : 0.0f;
+    }
     const float sum = row_sum_butterfly(p);   // (every lane takes part)
     g = mine >= 0 ? p / sum : 0.0f;
   } else {
