@@ -269,11 +269,24 @@ __device__ __forceinline__ bool apart(int mine, int rest, int k, int rounds, int
   return (j >= k) | (((mine >> 8) > 0) & ((mine >> 8) - (next >> 8) > steps));
 }
 
-// ---- one token by a whole wavefront, in 64 bits: what the definition says, for the few that are close.
+// ---- one token by a whole wavefront, in 64 bits: what the definition says, for the few that are close.  A wavefront that
+// comes here is one the launch waits for, so what counts is latency: reductions go through the rows of 16 and four lane
+// reads, not through LDS.
+__device__ __forceinline__ double read_lane(double v, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
 __device__ __forceinline__ double wave_max(double v) {
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) v = larger(v, __shfl_xor(v, s, 64));
-  return v;
+  v = row_max(v);
+  return larger(larger(read_lane(v, 0), read_lane(v, 16)), larger(read_lane(v, 32), read_lane(v, 48)));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+  v = row_sum_butterfly(v);
+  return (read_lane(v, 0) + read_lane(v, 16)) + (read_lane(v, 32) + read_lane(v, 48));
+}
+__device__ __forceinline__ int wave_min(int v) {
+  v = row_min(v);
+  return min(min(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+             min(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
 }
 // Lane i of the result: entry i of the token's list.  Lane l has experts 4 l .. 4 l + 3; ks: room for E doubles.
 template <typename ZT, bool KEYED, bool SIGMOID>
@@ -287,9 +300,7 @@ __device__ int list_wide(const SelectArgs& a, int t, int k, double* ks) {
   if (KEYED && !SIGMOID) {
     m = wave_max(larger(larger(z[0], z[1]), larger(z[2], z[3])));
     if (!(m > -INFINITY)) m = 0.0;
-    sum = exp(z[0] - m) + exp(z[1] - m) + exp(z[2] - m) + exp(z[3] - m);
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) sum += __shfl_xor(sum, s, 64);
+    sum = wave_sum((exp(z[0] - m) + exp(z[1] - m)) + (exp(z[2] - m) + exp(z[3] - m)));
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -307,23 +318,30 @@ __device__ int list_wide(const SelectArgs& a, int t, int k, double* ks) {
     for (int i = 0; i < 4; ++i)
       if (4 * lane + i < a.E) ks[4 * lane + i] = key[i];
     wave_sync();
-    double one = -INFINITY, two = -INFINITY;   // lane g: group g
-    for (int i = 0; i < a.group_size && lane < a.groups; ++i) {
-      const double v = ks[lane * a.group_size + i];
+    double one = -INFINITY, two = -INFINITY;   // lane 4 g + q: of group g the elements q, q + 4, ..
+    const int g0 = lane >> 2;
+    for (int i = lane & 3; i < a.group_size && g0 < a.groups; i += 4) {
+      const double v = ks[g0 * a.group_size + i];
       two = v > one ? one : larger(two, v);
       one = larger(one, v);
+    }
+#pragma unroll
+    for (int s = 1; s <= 2; s <<= 1) {   // (of equal ones both count)
+      const double o1 = __shfl_xor(one, s, 64), o2 = __shfl_xor(two, s, 64);
+      two = larger(o1 > one ? one : o1, larger(two, o2));
+      one = larger(one, o1);
     }
     wave_sync();
     const double score = (a.sum_two && two > -INFINITY) ? one + two : one;
     int ahead = 0;
     for (int g = 0; g < a.groups; ++g) {
-      const double o = __shfl(score, g, 64);
-      ahead += (o > score || (o == score && g < lane)) ? 1 : 0;
+      const double o = read_lane(score, 4 * g);
+      ahead += (o > score || (o == score && g < g0)) ? 1 : 0;
     }
-    const unsigned mask = (unsigned)__ballot(lane < a.groups && ahead < a.topk_groups);
+    const unsigned long long stay = __ballot(g0 < a.groups && ahead < a.topk_groups);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (!((mask >> (((4 * lane + i) * a.group_mul >> 16) & 15)) & 1u)) order[i] = -INFINITY;
+      if (!((stay >> (((4 * lane + i) * a.group_mul >> 16) * 4 & 60)) & 1u)) order[i] = -INFINITY;
   }
   int mine = -1;
   for (int round = 0; round < k; ++round) {
@@ -332,8 +350,7 @@ __device__ int list_wide(const SelectArgs& a, int t, int k, double* ks) {
     int e = 0x7fff;
 #pragma unroll
     for (int i = 3; i >= 0; --i) e = order[i] == top ? 4 * lane + i : e;
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) e = min(e, __shfl_xor(e, s, 64));   // ties: lowest expert
+    e = wave_min(e);   // ties: lowest expert
     if (lane == round) mine = e;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
