@@ -1356,10 +1356,12 @@ fmoe_ffn_geom fmoe_geom(const fmoe_ctx* ctx, int n_cap) {
   if (c.d_model >= FMOE_DENSE_MIN_K && c.d_ffn >= FMOE_DENSE_MIN_K && work >= FMOE_DENSE_ITEMS_SOME)
     min_rows = work >= FMOE_DENSE_ITEMS ? FMOE_DENSE_MIN_ROWS : FMOE_DENSE_MIN_ROWS_SOME;
   g.dense = c.dtype == FMOE_BF16 && (long long)n_cap * ctx->kmax >= min_rows * c.n_experts;
+  if (ctx->quant) g.dense = quant_ffn_is_dense(ctx, n_cap);
   if (ctx->ffn_shape == 1) g.dense = false;
   if (ctx->ffn_shape == 2) g.dense = c.dtype == FMOE_BF16;
-  for (int w = 0; w < 4; ++w)
-    if (fmoe_packed_bytes(ctx, w) > 0xffffffffull) g.dense = false;
+  if (!ctx->quant)   // (a group of 4-bit weights is addressed on its own)
+    for (int w = 0; w < 4; ++w)
+      if (fmoe_packed_bytes(ctx, w) > 0xffffffffull) g.dense = false;
   g.run = g.dense ? FMOE_DENSE_TILE_RUN : FMOE_TILE_RUN;
   const int Ft = c.n_shared * c.d_ffn_shared;
   g.cols1 = (c.d_ffn + 63) / 64;           // 64 hidden columns per block

@@ -533,6 +533,22 @@ int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStrea
 // At most THIN_ROWS tokens: no expert has more rows, and the weight stream wants the finest work items.
 bool quant_ffn_is_thin(const fmoe_ctx* ctx, int n_cap) { return n_cap <= THIN_ROWS && ctx->ffn_shape == 0; }
 
+// Two column tiles an item from so many items on that the chip is busy with them: row tiles the call can have (one of every
+// expert with rows, and the further ones) times pairs of column tiles of the narrower GEMM.  One / two column tiles, us,
+// gate/up and down, weights from memory: d 1280, 64 experts of 896, two shared (320 items and more) 17 tokens 32 / 29, 100
+// tokens 46 / 48, 416 tokens 66 / 54; d 2048, 64 of 1408, two shared (512) 17 tokens 58 / 55, 200 tokens 100 / 78; 128 of
+// 768 (768) 17 tokens 53 / 45, 416 tokens 114 / 89; d 512, 256 of 512 (512) 20 tokens 24 / 23, 500 tokens 54 / 50; against
+// it d 512, 64 of 512 (128) 20 tokens 16 / 18, 500 tokens 24 / 32; d 1288, 16 of 904, one shared (96) 17 tokens 20 / 24, 600
+// tokens 36 / 44; d 4096, 8 of 1536 17 tokens (96) 38 / 40, 300 tokens (144) 60 / 77, 1200 tokens (312) 123 / 117.
+constexpr long long QUANT_DENSE_ITEMS = 300;
+bool quant_ffn_is_dense(const fmoe_ctx* ctx, int n_cap) {
+  const fmoe_config& c = ctx->cfg;
+  const int pairs1 = (c.d_ffn + 127) / 128, pairs2 = (c.d_model + 255) / 256;
+  const long long rows = (long long)n_cap * ctx->kmax;
+  const long long tiles = (rows < c.n_experts ? rows : c.n_experts) + rows / SBM;
+  return tiles * (pairs1 < pairs2 ? pairs1 : pairs2) >= QUANT_DENSE_ITEMS;
+}
+
 int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,
                   const int32_t* expert_offsets, const int32_t* perm_src, void* y, void* y_shared, char* base, const fmoe_ws_layout& L, const fmoe_ffn_geom& geo, hipStream_t stream) {
   const fmoe_config& c = ctx->cfg;
