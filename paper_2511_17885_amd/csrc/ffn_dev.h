@@ -140,9 +140,11 @@ __device__ __forceinline__ void lds_read_frags(uint32_t addr, u32x4_t (&f)[NRB])
 // operands of the wait).
 template <int NRB, int OFF>
 __device__ __forceinline__ void lds_issue_frags_at(uint32_t addr, u32x4_t (&f)[NRB]) {
-  static_assert(NRB == 2 || NRB == 3 || NRB == 4, "supported fragment counts");
+  static_assert(NRB >= 1 && NRB <= 4, "supported fragment counts");
   static_assert(OFF >= 0 && OFF + (NRB - 1) * 2048 < 65536, "offset field of an LDS instruction");
-  if constexpr (NRB == 2) {
+  if constexpr (NRB == 1) {
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=&v"(f[0]) : "v"(addr), "n"(OFF) : "memory");
+  } else if constexpr (NRB == 2) {
     asm volatile("ds_read_b128 %0, %2 offset:%3\n\tds_read_b128 %1, %2 offset:%4"
                  : "=&v"(f[0]), "=&v"(f[1]) : "v"(addr), "n"(OFF), "n"(OFF + 2048) : "memory");
   } else if constexpr (NRB == 3) {
@@ -158,8 +160,10 @@ __device__ __forceinline__ void lds_issue_frags_at(uint32_t addr, u32x4_t (&f)[N
 }
 template <int NRB>
 __device__ __forceinline__ void lds_settle_frags(u32x4_t (&f)[NRB]) {
-  static_assert(NRB == 2 || NRB == 3 || NRB == 4, "supported fragment counts");
-  if constexpr (NRB == 2) {
+  static_assert(NRB >= 1 && NRB <= 4, "supported fragment counts");
+  if constexpr (NRB == 1) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f[0]) : : "memory");
+  } else if constexpr (NRB == 2) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f[0]), "+v"(f[1]) : : "memory");
   } else if constexpr (NRB == 3) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]) : : "memory");

@@ -35,11 +35,11 @@ struct QuantArgs {
 __host__ __device__ inline int quant_tiles(int K) { return (K + SBK - 1) / SBK; }
 __host__ __device__ inline int quant_scale_tiles(int K) { return (quant_tiles(K) + 3) / 4; }
 
-// Eight codes times the scale in byte I of `scales`.
+// Eight codes times the scale in byte I of `scales`.  The instruction takes the exponent of its scale operand and nothing else
+// (checked on the card for every exponent with thousands of other bits): the byte is only shifted there.
 template <int I>
 __device__ __forceinline__ u32x4_t dequantize(uint32_t codes, uint32_t scales) {
-  const uint32_t e = (I == 0 ? scales << 23 : I == 1 ? scales << 15 : I == 2 ? scales << 7 : scales >> 1) & 0x7f800000u;
-  const float s = __uint_as_float(e);
+  const float s = __uint_as_float(I == 0 ? scales << 23 : I == 1 ? scales << 15 : I == 2 ? scales << 7 : scales >> 1);
   return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2)),
@@ -49,7 +49,6 @@ __device__ __forceinline__ u32x4_t dequantize(uint32_t codes, uint32_t scales) {
 // One wavefront, one column block, sixteen rows: codes, scales and rows straight into registers in matrix order, no LDS and
 // no barrier, for calls of at most THIN_ROWS tokens, where the weights are all there is to move.  Rows past the tile reuse
 // its last one, row indices are clamped as in gather_offsets.
-constexpr int THIN_HINT = 0;
 constexpr int THIN_ROWS = 16;
 constexpr int THIN_SLOTS = 8;    // k tiles (64 wide) of codes in flight
 constexpr int THIN_A_SLOTS = 8;   // and of rows, which come from L2
@@ -62,7 +61,8 @@ __device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, int row0,
   const int lane = threadIdx.x;
   const int K = P.K, N = P.N;
   const int NT = quant_tiles(K), NT4 = quant_scale_tiles(K);
-  // The streams' descriptors end with the column block: loads past the last k tile return zeros and fetch nothing
+  // The streams' descriptors end with the column block: loads past the last k tile return zeros and fetch nothing (the
+  // whole offset is the lanes': a scalar one would be taken off the size first)
   const __amdgpu_buffer_rsrc_t b_rsrc = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<u32x4_t*>(P.Bp) + (size_t)group * P.group_stride + (size_t)cb * NT * 64, 0, NT * 1024, 0x00020000);
   const __amdgpu_buffer_rsrc_t s_rsrc = __builtin_amdgcn_make_buffer_rsrc(
@@ -72,17 +72,17 @@ __device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, int row0,
   const uint32_t lane16 = (uint32_t)lane * 16u, column16 = (uint32_t)(lane & 15) * 16u;
   const int kq = (lane >> 4) * 8;
   u32x4_t breg[S], sreg[S / 4], areg[SA][2];
-  auto load_b = [&](int slot, int t) { breg[slot] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane16 + (uint32_t)t * 1024u, 0, THIN_HINT); };
+  auto load_b = [&](int slot, int t) { breg[slot] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane16 + (uint32_t)t * 1024u, 0, 0); };
   auto load_s = [&](int slot, int t4) {
     sreg[slot] = __builtin_amdgcn_raw_buffer_load_b128(s_rsrc, column16 + (uint32_t)t4 * 256u, 0, 0);
   };
-  uint32_t a_row;   // byte offset of the lane's row
-  auto load_a = [&](int slot, int t) {   // k past K re-reads the row's end, where the packed weights are zero
+  // byte offsets of the lane's pieces in k tile 0, and in the last one less its start; past the end the last tile again
+  uint32_t a_src[2], a_last[2];
+  auto load_a = [&](int slot, int t) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int k = t * SBK + s * 32 + kq;
-      areg[slot][s] = __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, a_row + (uint32_t)(k < K ? k : K - 8) * 2u, 0, 0);
-    }
+    for (int s = 0; s < 2; ++s)
+      areg[slot][s] = __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, t < NT - 1 ? a_src[s] : a_last[s],
+                                                            (t < NT ? t : NT - 1) * (SBK * 2), 0);
   };
   // the weights do not need the row indices (two dependent loads)
   const uint32_t a_max_row = 0xffffffffu / ((uint32_t)P.lda * 2u) - 1u;
@@ -97,7 +97,13 @@ __device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, int row0,
   __builtin_amdgcn_sched_barrier(0);
   if (P.map1 && P.map1_limit > 0) src = src < 0 ? 0 : (src >= P.map1_limit ? P.map1_limit - 1 : src);
   if (P.map2) src = P.map2[src];
-  a_row = ((uint32_t)src < a_max_row ? (uint32_t)src : a_max_row) * (uint32_t)P.lda * 2u;
+  const uint32_t a_row = ((uint32_t)src < a_max_row ? (uint32_t)src : a_max_row) * (uint32_t)P.lda * 2u;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {   // k past K re-reads the row's end, where the packed weights are zero
+    const int k_last = (NT - 1) * SBK, piece = s * 32 + kq;
+    a_src[s] = a_row + (uint32_t)piece * 2u;
+    a_last[s] = a_row + (uint32_t)(k_last + piece < K ? piece : K - 8 - k_last) * 2u;
+  }
 #pragma unroll
   for (int t = 0; t < SA; ++t) load_a(t, t);
   __builtin_amdgcn_sched_barrier(0);
@@ -147,16 +153,31 @@ __device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, int row0,
   }
 }
 
-// One work item of a workgroup: a tile of up to 128 rows (NAB live bands of 32) times NCB column tiles, column block w of
-// each for wavefront w.  Rows go through a ring of four LDS stages as in ffn.hip; codes and scales into registers, three k
-// tiles ahead; a k tile is one barrier.  Every load is unconditional (past the end the last tile again), so the number of
-// loads in flight at a wait is a compile-time constant.  Row blocks are taken two at a time, the next pair's operands
-// requested from LDS before the present pair's products.
-template <bool SWIGLU, int NAB, int NCB>
+template <int I, int N, typename C, typename F>
+__device__ __forceinline__ void while_for(C&& c, F&& f) {   // static_for that ends at the first i for which c(i) is not true
+  if constexpr (I < N) {
+    if (c(std::integral_constant<int, I>{})) {
+      f(std::integral_constant<int, I>{});
+      while_for<I + 1, N>(c, f);
+    }
+  }
+}
+
+// One work item of a workgroup: a tile of rows (NAB live bands of 32, LDS stages of ROWS) times NCB column tiles, column block
+// w of each for wavefront w.  Rows go through a ring of LDS stages as in ffn.hip; codes and scales into registers, all as
+// many k tiles ahead; a k tile is one barrier.  Every load is unconditional (past the end the last tile again), so the number
+// of loads in flight at a wait is a compile-time constant.  Row blocks are taken two at a time, the next pair's operands
+// requested from LDS before the present pair's products.  HALF: of the only band the first 16 rows.
+template <bool SWIGLU, int NAB, int NCB, int STAGES, int ROWS, bool HALF = false>
 __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_tile& tile, int group, int ct0, int ct_limit,
                                            bf16_t* As) {
-  constexpr int NRB = 2 * NAB;
-  constexpr int STAGES = 4, AHEAD = 3;
+  static_assert(STAGES == 4 || STAGES == 8, "a unit of scales serves four k tiles");
+  static_assert(32 * NAB <= ROWS, "the rows fit in a stage");
+  static_assert(!HALF || NAB == 1, "half a band is half of the only one");
+  constexpr int NRB = HALF ? 1 : 2 * NAB;
+  constexpr int PB = HALF ? 1 : 2;   // row blocks taken together
+  constexpr int AHEAD = STAGES - 1, UNITS = STAGES / 4;
+  constexpr int PER_TILE = NAB + NCB;
   const StreamProblem& P = Q.s;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -180,20 +201,18 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
   const uint32_t lane16 = (uint32_t)lane * 16u, column16 = (uint32_t)(lane & 15) * 16u;
   const int a_kc = ((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) * 8;
 
-  u32x4_t breg[STAGES][NCB], scales[NCB], next_scales[NCB];
-  uint32_t a_src[NAB];
+  u32x4_t breg[STAGES][NCB], scales[UNITS][NCB], next_scales[NCB];
+  uint32_t a_src[NAB], a_last[NAB];   // byte offsets of the lane's pieces in k tile 0, and in the last one less its start
   auto loadB1 = [&](int slot, int t, int j) {
     breg[slot][j] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane16, bbase[j] + (uint32_t)(t < NT ? t : NT - 1) * 1024u, 0);
   };
   auto loadS1 = [&](int t4, int j) {
     return __builtin_amdgcn_raw_buffer_load_b128(s_rsrc, column16, sbase[j] + (uint32_t)(t4 < NT4 ? t4 : NT4 - 1) * 256u, 0);
   };
-  auto loadA1 = [&](int stage, int t, int it) {   // k past K re-reads the row's end, where the packed weights are zero
-    const int k = (t < NT ? t : NT - 1) * SBK + a_kc;
-    const int kk = k < K ? k : K - 8;
+  auto loadA1 = [&](int stage, int t, int it) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        a_rsrc, FMOE_LPTR(As + stage * (SBM * SBK) + (32 * it + 8 * wave) * SBK), 16,
-        a_src[it] + (uint32_t)kk * 2u, 0, 0, 0);
+        a_rsrc, FMOE_LPTR(As + stage * (ROWS * SBK) + (32 * it + 8 * wave) * SBK), 16,
+        t < NT - 1 ? a_src[it] : a_last[it], (uint32_t)(t < NT ? t : NT - 1) * (SBK * 2u), 0, 0);
   };
   const uint32_t lds0 = (uint32_t)(uintptr_t)FMOE_LPTR(As);
   const uint32_t frag_row = lds0 + (uint32_t)(lane & 15) * (SBK * 2);
@@ -205,20 +224,28 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
   gather_first<NAB>(P, tile, src);
   order_loads();
 #pragma unroll
-  for (int j = 0; j < NCB; ++j) scales[j] = loadS1(0, j);
+  for (int q = 0; q < UNITS; ++q)
+#pragma unroll
+    for (int j = 0; j < NCB; ++j) scales[q][j] = loadS1(q, j);
 #pragma unroll
   for (int t = 0; t < AHEAD; ++t)
 #pragma unroll
     for (int j = 0; j < NCB; ++j) loadB1(t, t, j);
   order_loads();
   gather_offsets<NAB>(P, src, a_src);
+  // k past K re-reads the row's end, where the packed weights are zero
+  const int k_last = (NT - 1) * SBK, piece_last = k_last + a_kc < K ? a_kc : K - 8 - k_last;
+#pragma unroll
+  for (int it = 0; it < NAB; ++it) {
+    a_last[it] = a_src[it] + (uint32_t)piece_last * 2u;
+    a_src[it] += (uint32_t)a_kc * 2u;
+  }
 #pragma unroll
   for (int t = 0; t < AHEAD; ++t) {
 #pragma unroll
     for (int it = 0; it < NAB; ++it) loadA1(t, t, it);
     order_loads();
   }
-  FMOE_WAIT_VM((AHEAD - 1) * NAB);   // the first tile's rows; later ones have as many newer loads as in the steady state
 
   // Accumulators: the compiler's with one column tile, hand-placed ones with two (number (j*NRB + rb)*2 + f), which it would
   // put in part into scratch memory
@@ -231,18 +258,23 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
     for (int rb = 0; rb < NRB; ++rb) acc[rb][0] = acc[rb][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  u32x4_t fa[2][2];
+  u32x4_t fa[2][PB];
   u32x4_t fb[NCB][2];
-  // k tile t = base + U: products, and the loads of tile t + AHEAD (with U == 0 the next four tiles' scales)
+  // k tile t, U = t % STAGES: products, and the loads of tile t + AHEAD.  Scales: with one unit in registers the next one is
+  // requested with the unit's first tile; with two a unit's successor but one takes its place behind its last tile.
   auto ktile = [&](auto uc, int t) {
     constexpr int U = decltype(uc)::value;
-    constexpr int PER_TILE = NAB + NCB;
-    constexpr int NL = PER_TILE + (U == 0 ? NCB : 0);   // loads this tile issues
-    // loads newer than this tile's rows: those of the two tiles before (the scales count where they are sure to be among them)
-    FMOE_WAIT_VM((AHEAD - 1) * PER_TILE + (U == 2 ? NCB : 0));
+    constexpr bool SCALES = UNITS == 1 ? U == 0 : U % 4 == 3;
+    constexpr int NL = PER_TILE + (SCALES ? NCB : 0);   // loads this tile issues
+    constexpr int unit = (U / 4) % UNITS;
+    // Loads newer than this tile's rows: behind the prologue, whose rows come after all its weights, the later rows of it
+    // and what the tiles so far have issued; then what the AHEAD - 1 tiles before have issued.  (Loads of scales are counted
+    // only where they are sure to be among them.)
+    if (t < AHEAD) FMOE_WAIT_VM((U < AHEAD ? AHEAD - 1 - U : 0) * NAB + U * PER_TILE);   // uniform
+    else FMOE_WAIT_VM((AHEAD - 1) * PER_TILE);
     block_barrier();   // every wavefront's share of the tile is in LDS; all are done with the tile before
-    constexpr int off = U * (SBM * SBK * 2);
-    lds_issue_frags_at<2, off>(frag_a0, fa[0]);
+    constexpr int off = U * (ROWS * SBK * 2);
+    lds_issue_frags_at<PB, off>(frag_a0, fa[0]);
     static_for<0, 2 * NAB>([&](auto pc) {
       constexpr int p = decltype(pc)::value, s = p / NAB, h = p % NAB, cur = p & 1, nxt = cur ^ 1;
       if constexpr (h == 0) {
@@ -250,28 +282,29 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
         for (int j = 0; j < NCB; ++j) {
           uint32_t c0 = breg[U][j][2 * s], c1 = breg[U][j][2 * s + 1];
           if constexpr (NAMED) asm volatile("" : "+v"(c0), "+v"(c1));   // not converted earlier: there are no registers for it
-          fb[j][0] = dequantize<2 * s>(c0, scales[j][U]);
-          fb[j][1] = dequantize<2 * s + 1>(c1, scales[j][U]);
+          fb[j][0] = dequantize<2 * s>(c0, scales[unit][j][U % 4]);
+          fb[j][1] = dequantize<2 * s + 1>(c1, scales[unit][j][U % 4]);
           // a conversion's result must not be read by the very next instruction, and the compiler does not see that the
           // hand-placed matrix instructions do
           if constexpr (NAMED) asm volatile("s_nop 0" : "+v"(fb[j][0]), "+v"(fb[j][1]));
         }
       }
-      lds_settle_frags<2>(fa[cur]);
-      if constexpr (h + 1 < NAB) lds_issue_frags_at<2, off + (h + 1) * 4096>(s ? frag_a1 : frag_a0, fa[nxt]);
-      else if constexpr (s == 0) lds_issue_frags_at<2, off>(frag_a1, fa[nxt]);
+      lds_settle_frags<PB>(fa[cur]);
+      if constexpr (h + 1 < NAB) lds_issue_frags_at<PB, off + (h + 1) * 4096>(s ? frag_a1 : frag_a0, fa[nxt]);
+      else if constexpr (s == 0) lds_issue_frags_at<PB, off>(frag_a1, fa[nxt]);
 #pragma unroll
       for (int i = 0; i < NL; ++i) {   // load i of the tile goes out with pair i * (2 NAB) / NL
         if ((i * 2 * NAB) / NL != p) continue;
         if (i < NAB) loadA1((U + AHEAD) % STAGES, t + AHEAD, i);
         else if (i < PER_TILE) loadB1((U + AHEAD) % STAGES, t + AHEAD, i - NAB);
-        else next_scales[i - PER_TILE] = loadS1(t / 4 + 1, i - PER_TILE);
+        else if constexpr (UNITS == 1) next_scales[i - PER_TILE] = loadS1(t / 4 + 1, i - PER_TILE);
+        else scales[unit][i - PER_TILE] = loadS1(t / 4 + UNITS, i - PER_TILE);   // (behind the tile's conversions)
       }
       static_for<0, NCB>([&](auto jc) {
         constexpr int j = decltype(jc)::value;
         const bf16x8_t b0 = __builtin_bit_cast(bf16x8_t, fb[j][0]), b1 = __builtin_bit_cast(bf16x8_t, fb[j][1]);
-        static_for<0, 2>([&](auto rc) {
-          constexpr int rb = 2 * h + decltype(rc)::value;
+        static_for<0, PB>([&](auto rc) {
+          constexpr int rb = PB * h + decltype(rc)::value;
           const bf16x8_t a8 = __builtin_bit_cast(bf16x8_t, fa[cur][decltype(rc)::value]);
           if constexpr (NAMED) {
             mfma_at<(j * NRB + rb) * 2>(a8, b0);
@@ -283,21 +316,16 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
         });
       });
     });
-    if constexpr (U == 3) {
+    if constexpr (UNITS == 1 && U == 3) {
 #pragma unroll
-      for (int j = 0; j < NCB; ++j) scales[j] = next_scales[j];
+      for (int j = 0; j < NCB; ++j) scales[0][j] = next_scales[j];
     }
   };
   int t0 = 0;
-  for (; t0 + 4 <= NT; t0 += 4) static_for<0, 4>([&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
-  const int left = NT - t0;   // uniform
-  if (left == 1) {
-    static_for<0, 1>([&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
-  } else if (left == 2) {
-    static_for<0, 2>([&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
-  } else if (left == 3) {
-    static_for<0, 3>([&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
-  }
+  for (; t0 + STAGES <= NT; t0 += STAGES)
+    static_for<0, STAGES>([&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
+  while_for<0, STAGES - 1>([&](auto uc) { return t0 + decltype(uc)::value < NT; },   // uniform
+                           [&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
   FMOE_WAIT_VM(0);   // the loads issued past the end have landed before the ring is reused
   // the last matrix instructions have retired before hand-placed accumulators are read, see ffn.hip
   if constexpr (NAMED) asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
@@ -306,7 +334,8 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
     if (ct0 + j < ct_limit)   // uniform
       store_tile<SWIGLU, NAB, STAGES>(P, tile, ct0 + j, [&](auto rbc, auto fc) {
         constexpr int rb = decltype(rbc)::value, f = decltype(fc)::value;
-        if constexpr (NAMED) return read_acc<(j * NRB + rb) * 2 + f>();
+        if constexpr (rb >= NRB) return f32x4_t{0.f, 0.f, 0.f, 0.f};   // rows that are not stored
+        else if constexpr (NAMED) return read_acc<(j * NRB + rb) * 2 + f>();
         else return acc[rb][f];
       }, As);
   });
@@ -391,8 +420,8 @@ __global__ __launch_bounds__(64, 2) void ffn_quant_thin_kernel(QuantThinArgs a) 
 }
 
 // The work item of a workgroup, dealt out as deal.h says; column tiles are taken NCB at a time (a.cols = such groups per tile
-// entry).
-template <bool SWIGLU, int NCB>
+// entry), row tiles are BM rows.
+template <bool SWIGLU, int NCB, int BM, int STAGES>
 __device__ __forceinline__ void quant_item(const QuantArgs& a, bf16_t* As) {
   int nt_launch, strip_cols;
   bool single;
@@ -407,7 +436,7 @@ __device__ __forceinline__ void quant_item(const QuantArgs& a, bf16_t* As) {
   if (nt_launch >= c_eff) return;
   int row_tile = tile.rt;
   if (tile.nrt > 1) dense_run_order(tile.rt, tile.nrt, c_eff, strip_cols, row_tile, nt_launch);
-  take_row_tile(tile, row_tile, SBM);
+  take_row_tile(tile, row_tile, BM);
   const int ct0 = tile.col0 + nt_launch * NCB;
   const int ct_limit = tile.col0 + ct_here;
   const int group = shared ? tile.group - a.E : tile.group;
@@ -415,24 +444,37 @@ __device__ __forceinline__ void quant_item(const QuantArgs& a, bf16_t* As) {
     Q.s.A += (size_t)group * Q.s.a_group_off;
     Q.s.C += (size_t)group * Q.s.c_group_off;
   }
-  switch ((tile.rows + 31) >> 5) {   // live 32-row bands of the tile, uniform per block
-    case 1: quant_tile<SWIGLU, 1, NCB>(Q, tile, group, ct0, ct_limit, As); break;
-    case 2: quant_tile<SWIGLU, 2, NCB>(Q, tile, group, ct0, ct_limit, As); break;
-    case 3: quant_tile<SWIGLU, 3, NCB>(Q, tile, group, ct0, ct_limit, As); break;
-    default: quant_tile<SWIGLU, 4, NCB>(Q, tile, group, ct0, ct_limit, As); break;
+  if constexpr (BM == 32) {
+    if (tile.rows <= 16) quant_tile<SWIGLU, 1, NCB, STAGES, BM, true>(Q, tile, group, ct0, ct_limit, As);   // uniform
+    else quant_tile<SWIGLU, 1, NCB, STAGES, BM>(Q, tile, group, ct0, ct_limit, As);
+  } else {
+    switch ((tile.rows + 31) >> 5) {   // live 32-row bands of the tile, uniform per block
+      case 1: quant_tile<SWIGLU, 1, NCB, STAGES, BM>(Q, tile, group, ct0, ct_limit, As); break;
+      case 2: quant_tile<SWIGLU, 2, NCB, STAGES, BM>(Q, tile, group, ct0, ct_limit, As); break;
+      case 3: quant_tile<SWIGLU, 3, NCB, STAGES, BM>(Q, tile, group, ct0, ct_limit, As); break;
+      default: quant_tile<SWIGLU, 4, NCB, STAGES, BM>(Q, tile, group, ct0, ct_limit, As); break;
+    }
   }
 }
 
-// One column tile an item (few rows an expert), two (many); by name, since the build looks at the second one's registers.
+// Three forms: row tiles of 32 and one column tile, seven k tiles ahead, four workgroups a CU, for a few rows an expert, where
+// the weights have to be on their way in great numbers; 128 rows and one column tile; 128 rows and two.  By name, since the
+// build looks at the last one's registers.
+constexpr int NARROW_ROWS = 32, NARROW_STAGES = 8;
+template <bool SWIGLU>
+__global__ __launch_bounds__(256, 4) void ffn_quant_narrow_kernel(QuantArgs a) {
+  __shared__ __align__(16) bf16_t As[NARROW_STAGES * NARROW_ROWS * SBK];
+  quant_item<SWIGLU, 1, NARROW_ROWS, NARROW_STAGES>(a, As);
+}
 template <bool SWIGLU>
 __global__ __launch_bounds__(256, 2) void ffn_quant_stream_kernel(QuantArgs a) {
   __shared__ __align__(16) bf16_t As[4 * SBM * SBK];
-  quant_item<SWIGLU, 1>(a, As);
+  quant_item<SWIGLU, 1, SBM, 4>(a, As);
 }
 template <bool SWIGLU>
 __global__ __launch_bounds__(256, 2) void ffn_quant_dense_kernel(QuantArgs a) {
   __shared__ __align__(16) bf16_t As[4 * SBM * SBK];
-  quant_item<SWIGLU, 2>(a, As);
+  quant_item<SWIGLU, 2, SBM, 4>(a, As);
 }
 
 // Source rows [group][n][k]: codes two to a byte, scales one byte per 32 k.  PAIR: gate and up (fragments 0 and 1), else
@@ -530,24 +572,22 @@ int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStrea
   return FMOE_OK;
 }
 
-// At most THIN_ROWS tokens: no expert has more rows, and the weight stream wants the finest work items.
-bool quant_ffn_is_thin(const fmoe_ctx* ctx, int n_cap) { return n_cap <= THIN_ROWS && ctx->ffn_shape == 0; }
-
-// Two column tiles an item from so many items on that the chip is busy with them: row tiles the call can have (one of every
-// expert with rows, and the further ones) times pairs of column tiles of the narrower GEMM.  One / two column tiles, us,
-// gate/up and down, weights from memory: d 1280, 64 experts of 896, two shared (320 items and more) 17 tokens 32 / 29, 100
-// tokens 46 / 48, 416 tokens 66 / 54; d 2048, 64 of 1408, two shared (512) 17 tokens 58 / 55, 200 tokens 100 / 78; 128 of
-// 768 (768) 17 tokens 53 / 45, 416 tokens 114 / 89; d 512, 256 of 512 (512) 20 tokens 24 / 23, 500 tokens 54 / 50; against
-// it d 512, 64 of 512 (128) 20 tokens 16 / 18, 500 tokens 24 / 32; d 1288, 16 of 904, one shared (96) 17 tokens 20 / 24, 600
-// tokens 36 / 44; d 4096, 8 of 1536 17 tokens (96) 38 / 40, 300 tokens (144) 60 / 77, 1200 tokens (312) 123 / 117.
+// Which form a call takes.  Thin: at most THIN_ROWS tokens, no expert has more rows and the weight stream wants the finest
+// work items.
+constexpr long long QUANT_NARROW_ROWS = 1000000;
 constexpr long long QUANT_DENSE_ITEMS = 300;
-bool quant_ffn_is_dense(const fmoe_ctx* ctx, int n_cap) {
+quant_form quant_ffn_form(const fmoe_ctx* ctx, int n_cap) {
   const fmoe_config& c = ctx->cfg;
-  const int pairs1 = (c.d_ffn + 127) / 128, pairs2 = (c.d_model + 255) / 256;
+  if (ctx->ffn_shape == 1) return QUANT_STREAM;
+  if (ctx->ffn_shape == 2) return QUANT_DENSE;
+  if (n_cap <= THIN_ROWS) return QUANT_THIN;
   const long long rows = (long long)n_cap * ctx->kmax;
+  if (rows < QUANT_NARROW_ROWS * c.n_experts) return QUANT_NARROW;
+  const int pairs1 = (c.d_ffn + 127) / 128, pairs2 = (c.d_model + 255) / 256;
   const long long tiles = (rows < c.n_experts ? rows : c.n_experts) + rows / SBM;
-  return tiles * (pairs1 < pairs2 ? pairs1 : pairs2) >= QUANT_DENSE_ITEMS;
+  return tiles * (pairs1 < pairs2 ? pairs1 : pairs2) >= QUANT_DENSE_ITEMS ? QUANT_DENSE : QUANT_STREAM;
 }
+int quant_row_tile(quant_form form) { return form == QUANT_NARROW ? NARROW_ROWS : SBM; }
 
 int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,
                   const int32_t* expert_offsets, const int32_t* perm_src, void* y, void* y_shared, char* base, const fmoe_ws_layout& L, const fmoe_ffn_geom& geo, hipStream_t stream) {
@@ -595,12 +635,12 @@ int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, i
   }
   g1.cols = g1.cols_entry = geo.cols1;
   g2.cols = g2.cols_entry = geo.cols2;
-  const bool thin = quant_ffn_is_thin(ctx, n_cap);
-  const bool dense = !thin && geo.dense;
+  const quant_form form = quant_ffn_form(ctx, n_cap);
+  const bool dense = form == QUANT_DENSE;
   const int row_cap = n_cap * ctx->kmax;
   auto launch = [&](auto swiglu, QuantArgs g) {
     constexpr bool S = decltype(swiglu)::value;
-    if (thin) {
+    if (form == QUANT_THIN) {
       QuantThinArgs h{g.p0, g.p1, expert_offsets, n_dev, E, n_cap, row_cap, g.p0.s.nbw, 0, 1};
       if (Ft > 0) {
         h.shared_cols = g.p1.s.nbw;
@@ -611,6 +651,8 @@ int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, i
     } else if (dense) {
       g.cols = (g.cols + 1) / 2;
       hipLaunchKernelGGL(ffn_quant_dense_kernel<S>, dim3(dense_blocks(geo.tile_cap, g.cols)), dim3(256), 0, stream, g);
+    } else if (form == QUANT_NARROW) {
+      hipLaunchKernelGGL(ffn_quant_narrow_kernel<S>, dim3(dense_blocks(geo.tile_cap, g.cols)), dim3(256), 0, stream, g);
     } else {
       hipLaunchKernelGGL(ffn_quant_stream_kernel<S>, dim3(dense_blocks(geo.tile_cap, g.cols)), dim3(256), 0, stream, g);
     }
