@@ -1360,11 +1360,7 @@ fmoe_ffn_geom fmoe_geom(const fmoe_ctx* ctx, int n_cap) {
   if (ctx->ffn_shape == 2) g.dense = c.dtype == FMOE_BF16;
   for (int w = 0; w < 4; ++w)
     if (fmoe_packed_bytes(ctx, w) > 0xffffffffull) g.dense = false;
-  if (ctx->quant) {   // (a group of 4-bit weights is addressed on its own)
-    const quant_form form = quant_ffn_form(ctx, n_cap);
-    g.bm = quant_row_tile(form);
-    g.dense = form != QUANT_THIN;
-  }
+  if (ctx->quant) g.dense = quant_ffn_form(ctx, n_cap) == QUANT_DENSE;   // (a group of 4-bit weights is addressed on its own)
   g.run = g.dense ? FMOE_DENSE_TILE_RUN : FMOE_TILE_RUN;
   const int Ft = c.n_shared * c.d_ffn_shared;
   g.cols1 = (c.d_ffn + 63) / 64;           // 64 hidden columns per block
@@ -1568,7 +1564,7 @@ int launch_expert_ffn(const fmoe_ctx* ctx, const void* x, const int32_t* kept_id
   if (n_cap == 0 || (row_cap == 0 && !has_shared)) return FMOE_OK;
   char* base = static_cast<char*>(ws);
   const fmoe_ffn_geom geo = fmoe_geom(ctx, n_cap);
-  if (!tiles_ready && !(ctx->quant && quant_ffn_form(ctx, n_cap) == QUANT_THIN)) {
+  if (!tiles_ready && !(ctx->quant && quant_ffn_form(ctx, n_cap) != QUANT_DENSE)) {
     fmoe_prof_scope prof(ctx, SLOT_TILES, stream);
     hipLaunchKernelGGL(build_tiles_kernel, dim3(1), dim3(256), 0, stream, expert_offsets, c.n_experts,
                        row_cap, n_cap, n_dev, c.n_shared, geo,

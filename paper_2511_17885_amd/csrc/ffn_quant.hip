@@ -354,127 +354,190 @@ __device__ __forceinline__ QuantProblem select_problem(const ARGS& a, bool share
   return Q;
 }
 
-struct QuantThinArgs {
-  QuantProblem p0, p1;
+// The forms for few rows find their work item from the experts' offsets: no launch to build lists, which would take as long as
+// a GEMM of a token or two.  Items: the shared groups', then those of the routed experts in ascending order, an expert's row
+// tiles next to each other for every column unit, since they share its weights.  With row tiles the sequence is cut into eight
+// contiguous shares, one per XCD (consecutive workgroups go round the XCDs).
+struct QuantListArgs {
+  QuantProblem p0, p1;             // routed experts; shared group
   const int32_t* expert_offsets;   // null without room for rows
   const int32_t* n_dev;            // or null
   int E, n_cap, row_cap;
-  int cols;                        // column blocks of an expert in this launch
-  int shared_items, shared_cols;   // items of the shared group(s), the first ones, shared_cols of them a group
+  int cols;                        // column units of an expert
+  int shared_groups, shared_cols;  // shared groups in this launch, column units of one
 };
+struct QuantItem {
+  int group, unit, row0, rows;     // group < 0: none
+  bool shared;
+};
+// Row tiles of BM rows.  Experts whose offsets are malformed are skipped as in fmoe_build_tiles.  Uniform.
+template <int BM>
+__device__ __forceinline__ QuantItem find_tile(const QuantListArgs& a, int block) {
+  constexpr int Q = FMOE_MAX_EXPERTS / 64;
+  const int lane = threadIdx.x & 63;
+  int r0[Q], cnt[Q], first[Q];   // of expert 64 q + lane: first row, rows, first tile
+  int tiles = 0;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const int e = 64 * q + lane;
+    r0[q] = cnt[q] = 0;
+    if (64 * q < a.E && a.row_cap > 0) {   // uniform
+      const int at = e < a.E ? e : a.E - 1;
+      r0[q] = a.expert_offsets[at];
+      cnt[q] = a.expert_offsets[at + 1];
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const bool good = 64 * q + lane < a.E && r0[q] >= 0 && cnt[q] > r0[q] && cnt[q] <= a.row_cap;
+    cnt[q] = good ? cnt[q] - r0[q] : 0;
+    const int nt = cnt[q] / BM + (cnt[q] % BM != 0);
+    const int scan = wave_scan(nt);
+    first[q] = tiles + scan - nt;
+    tiles += __builtin_amdgcn_readlane(scan, 63);
+  }
+  const int n = resolve_count(a.n_cap, a.n_dev);
+  const int shared_tiles = n / BM + (n % BM != 0), per_group = shared_tiles * a.shared_cols;
+  const int shared_items = per_group * a.shared_groups;
+  const int items = shared_items + tiles * a.cols, share = (items + 7) >> 3;
+  QuantItem it{-1, 0, 0, 0, false};
+  const int place = block >> 3;
+  int g = (block & 7) * share + place;
+  if (place >= share || g >= items) return it;
+  if (g < shared_items) {
+    it.shared = true;
+    it.group = g / per_group;
+    g -= it.group * per_group;
+    it.unit = g / shared_tiles;
+    it.row0 = (g - it.unit * shared_tiles) * BM;
+    it.rows = n - it.row0 < BM ? n - it.row0 : BM;
+    return it;
+  }
+  g -= shared_items;
+  const int tile = g / a.cols;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const int nt = cnt[q] / BM + (cnt[q] % BM != 0);
+    const unsigned long long mine = __ballot(first[q] <= tile && tile < first[q] + nt);
+    if (mine != 0) {   // in one q only
+      const int at = __ffsll((long long)mine) - 1;
+      const int e_first = __builtin_amdgcn_readlane(first[q], at), e_tiles = __builtin_amdgcn_readlane(nt, at);
+      const int e_rows = __builtin_amdgcn_readlane(cnt[q], at);
+      g -= e_first * a.cols;
+      it.group = 64 * q + at;
+      it.unit = g / e_tiles;
+      const int row = (g - it.unit * e_tiles) * BM;
+      it.row0 = __builtin_amdgcn_readlane(r0[q], at) + row;
+      it.rows = e_rows - row < BM ? e_rows - row : BM;
+    }
+  }
+  return it;
+}
+// One row tile an expert, whatever its rows; workgroup = place in the sequence.  Without the sums over all experts and the
+// shares: a token or two are all latency (one token, d 2048, 64 experts of 1408 and two shared 15.1 -> 13.6 us).
+__device__ __forceinline__ QuantItem find_expert(const QuantListArgs& a, int item) {
+  constexpr int Q = FMOE_MAX_EXPERTS / 64;
+  const int lane = threadIdx.x & 63;
+  QuantItem it{-1, 0, 0, 0, false};
+  const int shared_items = a.shared_groups * a.shared_cols;
+  if (item < shared_items) {
+    it.shared = true;
+    it.group = item / a.shared_cols;
+    it.unit = item - it.group * a.shared_cols;
+    it.rows = resolve_count(a.n_cap, a.n_dev);
+    return it;
+  }
+  int ahead = (item - shared_items) / a.cols;   // experts with rows ahead of this item's
+  it.unit = item - shared_items - ahead * a.cols;
+  int r0[Q], r1[Q];
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    r0[q] = r1[q] = 0;
+    if (64 * q + lane < a.E) {
+      r0[q] = a.expert_offsets[64 * q + lane];
+      r1[q] = a.expert_offsets[64 * q + lane + 1];
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const bool some = r0[q] >= 0 && r1[q] > r0[q] && r1[q] <= a.row_cap;
+    const unsigned long long mask = __ballot(some);
+    const int here = __popcll(mask);
+    if (it.group < 0 && ahead < here) {   // uniform
+      const int rank = __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
+      const int at = __ffsll((long long)__ballot(some && rank == ahead)) - 1;
+      it.group = 64 * q + at;
+      it.row0 = __builtin_amdgcn_readlane(r0[q], at);
+      it.rows = __builtin_amdgcn_readlane(r1[q], at) - it.row0;
+    }
+    ahead -= here;
+  }
+  return it;
+}
+// The item's problem, with the slices of a shared expert of the hidden buffer and the output (down GEMM).
+template <typename ARGS>
+__device__ __forceinline__ QuantProblem item_problem(const ARGS& a, bool shared, int group) {
+  QuantProblem Q = select_problem(a, shared);
+  if (shared) {
+    Q.s.A += (size_t)group * Q.s.a_group_off;
+    Q.s.C += (size_t)group * Q.s.c_group_off;
+  }
+  return Q;
+}
 
-// Items: the shared groups' column blocks, then those of the routed experts that have rows, in ascending order.  Which
-// expert the j-th of them is every wavefront finds from the offsets: no launch to build lists for a few rows.  Experts
-// whose offsets are malformed are skipped as in fmoe_build_tiles.
 template <bool SWIGLU>
-__global__ __launch_bounds__(64, 2) void ffn_quant_thin_kernel(QuantThinArgs a) {
-  const int lane = threadIdx.x, item = (int)blockIdx.x;
-  const bool shared = item < a.shared_items;
-  int group, cb, row0, rows;
-  if (shared) {
-    group = item / a.shared_cols;
-    cb = item - group * a.shared_cols;
-    row0 = 0;
-    rows = resolve_count(a.n_cap, a.n_dev);
-  } else {
-    const int routed = item - a.shared_items;
-    int left = routed / a.cols;    // experts with rows ahead of this item's
-    cb = routed - left * a.cols;
-    int r0[4], r1[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int e = 64 * q + lane;
-      r0[q] = r1[q] = 0;
-      if (e < a.E) {
-        r0[q] = a.expert_offsets[e];
-        r1[q] = a.expert_offsets[e + 1];
-      }
-    }
-    group = -1;
-    row0 = rows = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const bool some = r0[q] >= 0 && r1[q] > r0[q] && r1[q] <= a.row_cap;
-      const unsigned long long mask = __ballot(some);
-      const int here = __popcll(mask);
-      if (group < 0 && left < here) {   // uniform
-        const int rank = __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
-        const int at = __ffsll((long long)__ballot(some && rank == left)) - 1;
-        group = 64 * q + at;
-        row0 = __builtin_amdgcn_readlane(r0[q], at);
-        rows = __builtin_amdgcn_readlane(r1[q], at) - row0;
-      }
-      left -= here;
-    }
-    if (group < 0) return;
-  }
-  QuantProblem Q = select_problem(a, shared);
-  if (cb >= Q.s.nbw) return;
-  if (shared) {   // per-shared-expert slices of the hidden buffer / output (down GEMM)
-    Q.s.A += (size_t)group * Q.s.a_group_off;
-    Q.s.C += (size_t)group * Q.s.c_group_off;
-  }
+__global__ __launch_bounds__(64, 2) void ffn_quant_thin_kernel(QuantListArgs a) {
+  const QuantItem it = find_expert(a, (int)blockIdx.x);
+  if (it.group < 0) return;
+  const QuantProblem Q = item_problem(a, it.shared, it.group);
   // one turn unless a caller's own row lists name a token several times for one expert
-  for (; rows > 0; rows -= THIN_ROWS, row0 += THIN_ROWS)
-    thin_quant_tile<SWIGLU>(Q, row0, rows < THIN_ROWS ? rows : THIN_ROWS, group, cb);
+  for (int done = 0; done < it.rows; done += THIN_ROWS)
+    thin_quant_tile<SWIGLU>(Q, it.row0 + done, it.rows - done < THIN_ROWS ? it.rows - done : THIN_ROWS, it.group, it.unit);
 }
 
-// The work item of a workgroup, dealt out as deal.h says; column tiles are taken NCB at a time (a.cols = such groups per tile
-// entry), row tiles are BM rows.
-template <bool SWIGLU, int NCB, int BM, int STAGES>
-__device__ __forceinline__ void quant_item(const QuantArgs& a, bf16_t* As) {
-  int nt_launch, strip_cols;
-  bool single;
-  const int ti = dense_entry((int)blockIdx.x, a.n_tiles[0], a.n_tiles[2], a.cols, nt_launch, single, strip_cols);
-  if (ti < 0) return;
-  fmoe_tile tile = load_entry(a.tiles, ti);
-  const bool shared = tile.group >= a.E;
-  QuantProblem Q = select_problem(a, shared);
-  // column tiles this entry really has, and groups of NCB of them
-  const int ct_here = (Q.s.n_col_tiles - tile.col0 < a.cols_entry) ? (Q.s.n_col_tiles - tile.col0) : a.cols_entry;
-  const int c_eff = (ct_here + NCB - 1) / NCB;
-  if (nt_launch >= c_eff) return;
-  int row_tile = tile.rt;
-  if (tile.nrt > 1) dense_run_order(tile.rt, tile.nrt, c_eff, strip_cols, row_tile, nt_launch);
-  take_row_tile(tile, row_tile, BM);
-  const int ct0 = tile.col0 + nt_launch * NCB;
-  const int ct_limit = tile.col0 + ct_here;
-  const int group = shared ? tile.group - a.E : tile.group;
-  if (shared) {
-    Q.s.A += (size_t)group * Q.s.a_group_off;
-    Q.s.C += (size_t)group * Q.s.c_group_off;
-  }
-  if constexpr (BM == 32) {
-    if (tile.rows <= 16) quant_tile<SWIGLU, 1, NCB, STAGES, BM, true>(Q, tile, group, ct0, ct_limit, As);   // uniform
-    else quant_tile<SWIGLU, 1, NCB, STAGES, BM>(Q, tile, group, ct0, ct_limit, As);
-  } else {
-    switch ((tile.rows + 31) >> 5) {   // live 32-row bands of the tile, uniform per block
-      case 1: quant_tile<SWIGLU, 1, NCB, STAGES, BM>(Q, tile, group, ct0, ct_limit, As); break;
-      case 2: quant_tile<SWIGLU, 2, NCB, STAGES, BM>(Q, tile, group, ct0, ct_limit, As); break;
-      case 3: quant_tile<SWIGLU, 3, NCB, STAGES, BM>(Q, tile, group, ct0, ct_limit, As); break;
-      default: quant_tile<SWIGLU, 4, NCB, STAGES, BM>(Q, tile, group, ct0, ct_limit, As); break;
-    }
-  }
-}
-
-// Three forms: row tiles of 32 and one column tile, seven k tiles ahead, four workgroups a CU, for a few rows an expert, where
-// the weights have to be on their way in great numbers; 128 rows and one column tile; 128 rows and two.  By name, since the
-// build looks at the last one's registers.
+// Row tiles of 32 and one column tile, seven k tiles ahead, four workgroups a CU, for a few rows an expert, where the weights
+// have to be on their way in great numbers.
 constexpr int NARROW_ROWS = 32, NARROW_STAGES = 8;
 template <bool SWIGLU>
-__global__ __launch_bounds__(256, 4) void ffn_quant_narrow_kernel(QuantArgs a) {
+__global__ __launch_bounds__(256, 4) void ffn_quant_narrow_kernel(QuantListArgs a) {
   __shared__ __align__(16) bf16_t As[NARROW_STAGES * NARROW_ROWS * SBK];
-  quant_item<SWIGLU, 1, NARROW_ROWS, NARROW_STAGES>(a, As);
+  const QuantItem it = find_tile<NARROW_ROWS>(a, (int)blockIdx.x);
+  if (it.group < 0) return;
+  const QuantProblem Q = item_problem(a, it.shared, it.group);
+  fmoe_tile tile{};
+  tile.row0 = it.row0;
+  tile.rows = it.rows;
+  if (it.rows <= 16) quant_tile<SWIGLU, 1, 1, NARROW_STAGES, NARROW_ROWS, true>(Q, tile, it.group, it.unit, it.unit + 1, As);   // uniform
+  else quant_tile<SWIGLU, 1, 1, NARROW_STAGES, NARROW_ROWS>(Q, tile, it.group, it.unit, it.unit + 1, As);
 }
-template <bool SWIGLU>
-__global__ __launch_bounds__(256, 2) void ffn_quant_stream_kernel(QuantArgs a) {
-  __shared__ __align__(16) bf16_t As[4 * SBM * SBK];
-  quant_item<SWIGLU, 1, SBM, 4>(a, As);
-}
+
+// Tiles of 128 rows and two column tiles, dealt out as deal.h says; column tiles are taken two at a time (a.cols = such pairs
+// per tile entry).  (The build looks at the registers of a kernel of this name.)
 template <bool SWIGLU>
 __global__ __launch_bounds__(256, 2) void ffn_quant_dense_kernel(QuantArgs a) {
   __shared__ __align__(16) bf16_t As[4 * SBM * SBK];
-  quant_item<SWIGLU, 2, SBM, 4>(a, As);
+  int pair, strip_cols;
+  bool single;
+  const int ti = dense_entry((int)blockIdx.x, a.n_tiles[0], a.n_tiles[2], a.cols, pair, single, strip_cols);
+  if (ti < 0) return;
+  fmoe_tile tile = load_entry(a.tiles, ti);
+  const bool shared = tile.group >= a.E;
+  const int group = shared ? tile.group - a.E : tile.group;
+  const QuantProblem Q = item_problem(a, shared, group);
+  // column tiles this entry really has, and pairs of them
+  const int ct_here = (Q.s.n_col_tiles - tile.col0 < a.cols_entry) ? (Q.s.n_col_tiles - tile.col0) : a.cols_entry;
+  const int pairs = (ct_here + 1) / 2;
+  if (pair >= pairs) return;
+  int row_tile = tile.rt;
+  if (tile.nrt > 1) dense_run_order(tile.rt, tile.nrt, pairs, strip_cols, row_tile, pair);
+  take_row_tile(tile, row_tile, SBM);
+  const int ct0 = tile.col0 + pair * 2, ct_limit = tile.col0 + ct_here;
+  switch ((tile.rows + 31) >> 5) {   // live 32-row bands of the tile, uniform per block
+    case 1: quant_tile<SWIGLU, 1, 2, 4, SBM>(Q, tile, group, ct0, ct_limit, As); break;
+    case 2: quant_tile<SWIGLU, 2, 2, 4, SBM>(Q, tile, group, ct0, ct_limit, As); break;
+    case 3: quant_tile<SWIGLU, 3, 2, 4, SBM>(Q, tile, group, ct0, ct_limit, As); break;
+    default: quant_tile<SWIGLU, 4, 2, 4, SBM>(Q, tile, group, ct0, ct_limit, As); break;
+  }
 }
 
 // Source rows [group][n][k]: codes two to a byte, scales one byte per 32 k.  PAIR: gate and up (fragments 0 and 1), else
@@ -572,22 +635,37 @@ int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStrea
   return FMOE_OK;
 }
 
-// Which form a call takes.  Thin: at most THIN_ROWS tokens, no expert has more rows and the weight stream wants the finest
-// work items.
-constexpr long long QUANT_NARROW_ROWS = 1000000;
+// Which form a call takes, by what it can route (capacities).  All times: us, gate/up and down, weights from memory.
+//  * Thin for at most THIN_ROWS tokens (no expert has more rows) that touch up to so many bytes of weights: a wavefront an
+//    item and no LDS, the shortest way from launch to result; with more to stream, the narrow form has more on its way.
+//    Thin / narrow: d 2048, 64 experts of 1408 and two shared (5 MB an expert) one token 14 / 18, 3 tokens 25 / 26, 4 tokens
+//    28 / 28, 8 tokens 38 / 36; 128 of 768 one token 12 / 16, 4 tokens 21 / 22, 6 tokens 28 / 27; d 1280, 64 of 896, two
+//    shared one token 11 / 14, 8 tokens 17 / 19; d 4096, 8 of 1536 one token 16 / 21, 16 tokens 22 / 24.
+//  * Dense from so many rows an expert on, if there also are so many items that the chip is busy with them: row tiles the
+//    call can have (one of every expert with rows, and the further ones) times pairs of column tiles of the narrower GEMM.
+//    Narrow / dense: d 2048, 64 experts of 1408 and two shared, 19 rows an expert 77 / 80, 56 rows 131 / 134, 100 rows 193 /
+//    184, 150 rows 266 / 230; d 1280, 64 of 896, two shared 39 rows 54 / 55, 75 rows 78 / 74, 150 rows 129 / 111; 128 of 768
+//    50 rows 117 / 141, 100 rows 182 / 180, 200 rows 309 / 256; d 512, 256 of 512 50 rows 63 / 68, 100 rows 94 / 85; with
+//    few items d 4096, 8 of 1536 150 rows (204 items) 67 / 78, 300 rows (312) 117 / 119, 600 rows (540) 207 / 194; d 1288,
+//    16 of 904, one shared 150 rows (204) 47 / 51, 300 rows (318) 81 / 74.
+constexpr size_t QUANT_THIN_BYTES = 112u << 20;
+constexpr long long QUANT_DENSE_ROWS = 64;
 constexpr long long QUANT_DENSE_ITEMS = 300;
 quant_form quant_ffn_form(const fmoe_ctx* ctx, int n_cap) {
   const fmoe_config& c = ctx->cfg;
-  if (ctx->ffn_shape == 1) return QUANT_STREAM;
+  if (ctx->ffn_shape == 1) return QUANT_NARROW;
   if (ctx->ffn_shape == 2) return QUANT_DENSE;
-  if (n_cap <= THIN_ROWS) return QUANT_THIN;
-  const long long rows = (long long)n_cap * ctx->kmax;
-  if (rows < QUANT_NARROW_ROWS * c.n_experts) return QUANT_NARROW;
+  const long long rows = (long long)n_cap * ctx->kmax, experts = rows < c.n_experts ? rows : c.n_experts;
+  if (n_cap <= THIN_ROWS) {
+    const size_t expert = (fmoe_quant_bytes(ctx, 0, nullptr) + fmoe_quant_bytes(ctx, 1, nullptr)) / c.n_experts;
+    const size_t shared = fmoe_quant_bytes(ctx, 2, nullptr) + fmoe_quant_bytes(ctx, 3, nullptr);
+    return (size_t)experts * expert + shared <= QUANT_THIN_BYTES ? QUANT_THIN : QUANT_NARROW;
+  }
+  if (rows < QUANT_DENSE_ROWS * c.n_experts) return QUANT_NARROW;
   const int pairs1 = (c.d_ffn + 127) / 128, pairs2 = (c.d_model + 255) / 256;
-  const long long tiles = (rows < c.n_experts ? rows : c.n_experts) + rows / SBM;
-  return tiles * (pairs1 < pairs2 ? pairs1 : pairs2) >= QUANT_DENSE_ITEMS ? QUANT_DENSE : QUANT_STREAM;
+  const long long items = (experts + rows / SBM) * (pairs1 < pairs2 ? pairs1 : pairs2);
+  return items >= QUANT_DENSE_ITEMS ? QUANT_DENSE : QUANT_NARROW;
 }
-int quant_row_tile(quant_form form) { return form == QUANT_NARROW ? NARROW_ROWS : SBM; }
 
 int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,
                   const int32_t* expert_offsets, const int32_t* perm_src, void* y, void* y_shared, char* base, const fmoe_ws_layout& L, const fmoe_ffn_geom& geo, hipStream_t stream) {
@@ -633,37 +711,40 @@ int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, i
     q.A = reinterpret_cast<const bf16_t*>(base + L.h_shared); q.lda = Ft; q.a_group_off = c.d_ffn_shared;
     q.C = static_cast<bf16_t*>(y_shared); q.ldc = d; q.c_group_off = (long long)n_cap * d; q.n_col_tiles = geo.scols2;
   }
-  g1.cols = g1.cols_entry = geo.cols1;
-  g2.cols = g2.cols_entry = geo.cols2;
   const quant_form form = quant_ffn_form(ctx, n_cap);
   const bool dense = form == QUANT_DENSE;
   const int row_cap = n_cap * ctx->kmax;
-  auto launch = [&](auto swiglu, QuantArgs g) {
+  auto launch = [&](auto swiglu, QuantArgs g, int cols) {
     constexpr bool S = decltype(swiglu)::value;
-    if (form == QUANT_THIN) {
-      QuantThinArgs h{g.p0, g.p1, expert_offsets, n_dev, E, n_cap, row_cap, g.p0.s.nbw, 0, 1};
-      if (Ft > 0) {
-        h.shared_cols = g.p1.s.nbw;
-        h.shared_items = (S ? 1 : c.n_shared) * g.p1.s.nbw;
-      }
-      const unsigned items = (unsigned)(h.shared_items + (row_cap < E ? row_cap : E) * h.cols);
-      if (items > 0) hipLaunchKernelGGL(ffn_quant_thin_kernel<S>, dim3(items), dim3(64), 0, stream, h);
-    } else if (dense) {
-      g.cols = (g.cols + 1) / 2;
+    if (dense) {
+      g.cols_entry = cols;
+      g.cols = (cols + 1) / 2;
       hipLaunchKernelGGL(ffn_quant_dense_kernel<S>, dim3(dense_blocks(geo.tile_cap, g.cols)), dim3(256), 0, stream, g);
-    } else if (form == QUANT_NARROW) {
-      hipLaunchKernelGGL(ffn_quant_narrow_kernel<S>, dim3(dense_blocks(geo.tile_cap, g.cols)), dim3(256), 0, stream, g);
-    } else {
-      hipLaunchKernelGGL(ffn_quant_stream_kernel<S>, dim3(dense_blocks(geo.tile_cap, g.cols)), dim3(256), 0, stream, g);
+      return;
     }
+    // column units: column blocks in the thin form, tiles of four in the narrow one
+    const bool thin = form == QUANT_THIN;
+    const int bm = thin ? FMOE_MAX_EXPERTS * THIN_ROWS : NARROW_ROWS;   // (more rows than a thin call has)
+    QuantListArgs h{g.p0, g.p1, expert_offsets, n_dev, E, n_cap, row_cap, 0, 0, 0};
+    h.cols = thin ? g.p0.s.nbw : (g.p0.s.nbw + 3) / 4;
+    if (Ft > 0) {
+      h.shared_groups = S ? 1 : c.n_shared;
+      h.shared_cols = thin ? g.p1.s.nbw : (g.p1.s.nbw + 3) / 4;
+    }
+    const long long tiles = (row_cap < E ? row_cap : E) + row_cap / bm;   // that the routed experts can have
+    const long long items = tiles * h.cols + (long long)((n_cap + bm - 1) / bm) * h.shared_cols * h.shared_groups;
+    if (items == 0) return;
+    const unsigned blocks = (unsigned)((items + 7) / 8 * 8);
+    if (thin) hipLaunchKernelGGL(ffn_quant_thin_kernel<S>, dim3(blocks), dim3(64), 0, stream, h);
+    else hipLaunchKernelGGL(ffn_quant_narrow_kernel<S>, dim3(blocks), dim3(256), 0, stream, h);
   };
   {
     fmoe_prof_scope prof(ctx, dense ? SLOT_GEMM1_DENSE : SLOT_GEMM1, stream);
-    launch(std::true_type{}, g1);
+    launch(std::true_type{}, g1, geo.cols1);
   }
   {
     fmoe_prof_scope prof(ctx, dense ? SLOT_GEMM2_DENSE : SLOT_GEMM2, stream);
-    launch(std::false_type{}, g2);
+    launch(std::false_type{}, g2, geo.cols2);
   }
   return FMOE_OK;
 }
