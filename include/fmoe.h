@@ -153,7 +153,9 @@ int fmoe_set_selection(fmoe_ctx* ctx, int32_t strategy, int32_t k_base, uint64_t
  * and 256 where d_model or S_m is below 736.  Calls of at most 16 tokens take a third, thin shape (a wavefront per
  * column block).  All add the products of a dot product in ascending k, so their
  * outputs are bit-identical.  shape 0 = choose by size (default), 1 = always weight-stream,
- * 2 = always dense; anything else is FMOE_ERR_INVALID_ARG.  No effect on fp32 contexts. */
+ * 2 = always dense; anything else is FMOE_ERR_INVALID_ARG.  No effect on fp32 contexts.  With 4-bit weights
+ * (fmoe_set_weights_quant) 1 is the form for few rows an expert, 2 the one for many, 0 chooses, also a third one for a
+ * few tokens; the outputs again are the same bits. */
 int fmoe_set_ffn_shape(fmoe_ctx* ctx, int32_t shape);
 
 /* Register the layer's weights (Eq.1, Eq.4).  Pointers are borrowed until the next call or
@@ -185,7 +187,8 @@ int fmoe_set_weights(fmoe_ctx* ctx, const void* router_w, const float* router_bi
  * dequantized matrices, bit for bit.  (Elements that fp32 cannot hold, 2^128 and more, count as infinite.)
  * The library keeps private copies in matrix-core operand order (4.25 bits a weight, padded as those of
  * fmoe_set_weights; allocated by the first call, freed by fmoe_destroy): the caller's expert tensors may be freed or
- * changed once the stream has drained. */
+ * changed once the stream has drained.  A context that has been given both forms keeps the copies of both.
+ * A matrix of 2^32 weights (d_model times S_m, or times N_s S_s) and more is refused with FMOE_ERR_UNSUPPORTED. */
 int fmoe_set_weights_quant(fmoe_ctx* ctx, const void* router_w, const float* router_bias,
                            const fmoe_quant_tensor* w_gate, const fmoe_quant_tensor* w_up,
                            const fmoe_quant_tensor* w_down, const fmoe_quant_tensor* ws_gate,
@@ -230,7 +233,8 @@ int fmoe_route(fmoe_ctx* ctx, const void* x, const uint8_t* is_visual, int32_t T
  * topk_gate [T,Kmax]: gate_scale * s / (sum of the listed s) with the context's renormalize, else gate_scale * s; 0 in
  * padding.  The quotient is taken in logarithms: it is right also where the scores themselves underflow.
  * scores [T,E] fp32 or NULL: s, 0 where the logit is masked (fmoe_prune takes them as probs).
- * The outputs feed fmoe_permute and fmoe_combine as those of fmoe_route do.  fmoe_set_selection has no effect here. */
+ * The outputs feed fmoe_permute and fmoe_combine as those of fmoe_route do; they share no memory with the inputs.
+ * fmoe_set_selection has no effect here.  n_groups above 16 is FMOE_ERR_UNSUPPORTED. */
 int fmoe_select_experts(fmoe_ctx* ctx, const fmoe_select_params* params, const void* logits, int32_t logits_dtype,
                         const uint8_t* is_visual, const float* select_bias, int32_t T, float* scores,
                         int32_t* topk_idx, float* topk_gate, void* stream);
@@ -239,7 +243,7 @@ int fmoe_select_experts(fmoe_ctx* ctx, const fmoe_select_params* params, const v
  * logits, logits_dtype, params and the context's renormalize as in the forward call; topk_idx [T,Kmax] its output (distinct
  * experts in a row; entries outside 0 .. E-1 are empty).  d_gate [T,Kmax] fp32: gradient of topk_gate (not
  * looked at in empty places).  d_scores [T,E] fp32 or NULL: gradient of scores.
- * d_logits [T,E] of logits_dtype, every element written; 0 for masked experts. */
+ * d_logits [T,E] of logits_dtype, every element written; 0 for masked experts.  It shares no memory with the inputs. */
 int fmoe_select_experts_backward(fmoe_ctx* ctx, const fmoe_select_params* params, const void* logits,
                                  int32_t logits_dtype, const int32_t* topk_idx, const float* d_gate,
                                  const float* d_scores, int32_t T, void* d_logits, void* stream);

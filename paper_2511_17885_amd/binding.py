@@ -274,9 +274,11 @@ class FMoE:
             torch.cuda.current_stream().synchronize()
             self._weights = (router_bias,)
 
-    def set_weights_quant(self, router_w, router_bias, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None):
-        """fmoe_set_weights_quant: every expert matrix as (codes, scales) (quantize_weights).  The context copies them; the
-        pairs may be dropped at any time (the binding holds on to the router alone)."""
+    def set_weights_quant(self, router_w, router_bias, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None,
+                          release_packed=False):
+        """fmoe_set_weights_quant: every expert matrix as (codes, scales) (quantize_weights).  The context makes copies on
+        the current stream; the binding holds on to the tensors unless release_packed asks it to wait for the stream and
+        keep the router bias alone."""
         c = self.cfg
         E, H, S, N, Ss = c.n_experts, c.d_model, c.d_ffn, c.n_shared, c.d_ffn_shared
         _expect(router_w, "router_w", self.torch_dtype, (E, H))
@@ -292,8 +294,11 @@ class FMoE:
             _expect(pair[0], f"codes of {name}", torch.uint8, (g, n, K // 2))
             _expect(pair[1], f"scales of {name}", torch.uint8, (g, n, (K + QUANT_GROUP - 1) // QUANT_GROUP))
             tensors.append(C.byref(FmoeQuantTensor(pair[0].data_ptr(), pair[1].data_ptr())))
-        self._weights = (router_w, router_bias)
+        self._weights = (router_w, router_bias, *pairs)
         _check(self.lib.fmoe_set_weights_quant(self._ctx, _ptr(router_w), _ptr(router_bias), *tensors, _stream()))
+        if release_packed:
+            torch.cuda.current_stream().synchronize()
+            self._weights = (router_bias,)
 
     def workspace_bytes(self, max_tokens, max_seqs=1):
         return int(self.lib.fmoe_workspace_bytes(self._ctx, max_tokens, max_seqs))

@@ -320,6 +320,10 @@ int fmoe_set_weights_quant(fmoe_ctx* ctx, const void* router_w, const float* rou
     if (!aligned16(w[i]->codes))
       return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_set_weights_quant: codes %p not 16-byte aligned", w[i]->codes);
   }
+  const fmoe_config& c = ctx->cfg;
+  const size_t widest = (size_t)c.n_shared * c.d_ffn_shared > (size_t)c.d_ffn ? (size_t)c.n_shared * c.d_ffn_shared : (size_t)c.d_ffn;
+  if (((size_t)c.d_model + 64) * (widest + 64) > 0xffffffffull)   // 32-bit offsets inside a packed matrix
+    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "fmoe_set_weights_quant: a matrix of %d x %zu weights", c.d_model, widest);
   if (!router_w) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_set_weights_quant: router_w is NULL");
   if (!aligned16(router_w) || !aligned16(router_bias))
     return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_set_weights_quant: router_w / router_bias not 16-byte aligned");
@@ -327,7 +331,9 @@ int fmoe_set_weights_quant(fmoe_ctx* ctx, const void* router_w, const float* rou
   if ((rc = set_router(ctx, router_w, router_bias, s)) != FMOE_OK) return rc;
   for (int i = 0; i < 4; ++i) {
     const size_t bytes = fmoe_quant_bytes(ctx, i, nullptr);
-    if (bytes && !ctx->pq[i]) FMOE_HIP_CHECK(hipMalloc(&ctx->pq[i], bytes));
+    if (bytes == 0 || ctx->pq[i]) continue;
+    FMOE_HIP_CHECK(hipSetDevice(ctx->device));
+    FMOE_HIP_CHECK(hipMalloc(&ctx->pq[i], bytes));
   }
   if ((rc = launch_pack_quant(ctx, w, s)) != FMOE_OK) return rc;
   ctx->quant = true;
@@ -727,7 +733,8 @@ int fmoe_profile_slots(void) { return SLOT_COUNT; }
 
 const char* fmoe_profile_name(int slot) {
   // kernel symbols (the two expert GEMMs: bf16 symbol; fp32 contexts run grouped_gemm_kernel, calls of at most 16
-  // tokens ffn_thin_kernel; scan and scatter in one launch are timed as the scatter)
+  // tokens ffn_thin_kernel, contexts with 4-bit weights the ffn_quant kernels, the dense one in the dense slots; scan and
+  // scatter in one launch are timed as the scatter)
   static const char* names[SLOT_COUNT] = {
       "route_kernel", "seq_ordinals_kernel", "window_score_kernel", "compact_kernel",
       "prune_dispatch_small_kernel", "permute_count_kernel", "permute_scan_kernel",

@@ -8,10 +8,11 @@
 //
 // Keys that come from a score are defined in 64 bits: two scores in 32 bits can be equal or change places where the
 // logits differ, and with thousands of tokens some pair of neighbours does.  They are compared in 32 bits first, with the
-// exponential and reciprocal of the hardware.  A key is then off by at most 2^-21 of the largest score a token can have and
-// half a rounding of its own; where two keys that are next to each other in the list, or on either side of its end, or
-// two groups on either side of theirs, are not further apart than twice that (taken twice), the wavefront does it again in
-// 64 bits.  One wavefront in a hundred does for 256 experts with a bias of deviation 0.1.
+// exponential and reciprocal of the hardware.  Two sigmoid scores are then off by less than 2^-21 together; two softmax scores
+// that go with close keys by less than 27 * 2^-24 of the largest score the row can have (22 for the normaliser, whose error
+// they share); 2^-19 of it is allowed for, and half a rounding of each key.  A token whose list, the place behind its end, or
+// the line between its groups has keys closer than that is done again in 64 bits, by its whole wavefront.  Of 22016 tokens
+// with 256 experts in eight groups and a bias of deviation 0.1 some twenty are.
 //
 // Sixteen lanes have a token (four tokens a wavefront), lane j of them the experts 64 q + 4 j + i: a row is read in
 // pieces of 16 bytes, and a reduction over the row is one over a lane's registers and four steps inside the vector unit.
@@ -136,7 +137,7 @@ __device__ __forceinline__ void two_largest(float& one, float& two, float o1, fl
 
 // Masks the experts of a token's groups that do not stay.  key: what a group's score is made of; order: what ranks the
 // experts; ks: the token's row in LDS.  Returns whether the scores on either side of the line are further apart than `slack`
-// plus `relative` times their size.  2^log2p lanes have a group.
+// plus `relative` times the largest keys that went into any.  2^log2p lanes have a group.
 template <int N>
 __device__ __forceinline__ bool keep_groups(const SelectArgs& a, int j, const float (&key)[N], float (&order)[N], float* ks,
                                             float slack, float relative) {
@@ -198,7 +199,8 @@ __device__ __forceinline__ bool keep_groups(const SelectArgs& a, int j, const fl
   wave_sync();   // the scores have been read
   if (a.topk_groups == a.groups) return true;
   const float last = -row_max(in ? -score : -INFINITY), next = row_max(g < a.groups && !in ? score : -INFINITY);
-  return next == -INFINITY || last - next > slack + relative * (fabsf(last) + fabsf(next));
+  const float size = row_max(fabsf(one > -INFINITY ? one : 0.0f) + fabsf(two > -INFINITY ? two : 0.0f));
+  return next == -INFINITY || last - next > slack + relative * size;
 }
 
 // The list by integers that hold key and expert, all different: a lane's are sorted once, then every round takes the largest
@@ -435,13 +437,15 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
     pack_below(order, peak, range, j, packed);
     const int entry = list_packed(a.Kmax, j, packed, rest);
     mine = j < k ? unpack_expert(entry) : -1;
-    // Two integers are off by a rounding of the step to them and their own each, two scored keys by `slack` and half a
-    // rounding each.  (The offset's rounding is the same for all; while the peak is below 8 ranges it is within what is left
-    // between the largest integer and 2^23.)
-    float off = 0.0f;
+    // The way from key to integer is monotonic, so logits whose integers differ are in order.  Two scored keys can be off by
+    // `slack` and half a rounding each, and their integers lose less than two steps more.  (The offset's rounding is the same
+    // for all; while the peak is below 8 ranges it is within what is left between the largest integer and 2^23.)
+    int steps = 0;
     if constexpr (KEYED)
-      if (scored) off = ((SIGMOID ? 1.0f : inv) * 0x1p-19f + 0x1p-23f * (fabsf(peak) + KEY_RANGE)) * (0x1p23f / KEY_RANGE);
-    const int steps = (int)fminf(off, 1e6f) + 3;
+      if (scored) {
+        const float off = (SIGMOID ? 1.0f : inv) * 0x1p-19f + 0x1p-23f * (fabsf(peak) + KEY_RANGE);
+        steps = (int)fminf(off * (0x1p23f / KEY_RANGE), 1e6f) + 3;
+      }
     sure = sure & (fabsf(peak) < 8.0f * range) & apart(entry, rest, k, a.Kmax, j, steps);
     if (peak == -INFINITY) {   // nothing to choose from
       sure = true;

@@ -521,6 +521,13 @@ def test_set_weights_quant_refuses_bad_arguments():
     ctx = _ctx(dtype=binding.FMOE_F32)
     assert call(q(), q(), q(), *none) == -5 and b"bf16" in lib.fmoe_last_error()
     lib.fmoe_destroy(ctx)
+    # offsets inside a packed matrix are 32 bits wide
+    for d_model, d_ffn, shared, d_shared in ((65536, 65536, 0, 0), (65536, 64, 2, 32768)):
+        ctx = C.c_void_p()
+        cfg = binding.FmoeConfig(d_model, 4, d_ffn, shared, d_shared, 2, 1, 1, binding.FMOE_BF16)
+        assert lib.fmoe_create(C.byref(ctx), C.byref(cfg), 0) == 0
+        assert call(*([q()] * (6 if shared else 3)), *(none if not shared else ())) == -5
+        lib.fmoe_destroy(ctx)
 
 
 def test_quantize_refuses_bad_arguments():

@@ -280,6 +280,33 @@ def test_select_decides_by_keys_that_are_equal_in_32_bits():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_select_biases_of_any_size(sigmoid):
+    """Keys whose size hides the scores in 32 bits (they differ by a score's last bits at 1000), groups whose two largest keys
+    cancel, and keys further apart than a list's integers span."""
+    rng = np.random.default_rng(77)
+    E = 64
+    z = rng.standard_normal((40, E)).astype(np.float32)
+    for k, groups, bias in ((6, 1, np.full(E, 1000.0)), (8, 8, np.where(np.arange(E) % 2 == 0, 300.0, -300.0)),
+                            (8, 32 // 2, np.where(np.arange(E) % 4 == 0, 1e4, np.where(np.arange(E) % 4 == 1, -1e4, -3e4))),
+                            (16, 1, rng.choice([-9.0, 0.0, 9.0], size=E)), (5, 1, np.zeros(E)), (3, 4, np.full(E, -1e6))):
+        cfg = _cfg(E, k, k, sigmoid=sigmoid, groups=groups, topk_groups=max(1, groups // 2), group_score=1)
+        b = bias.astype(np.float32)
+        idx = _context(cfg).select_experts(_params(cfg), _gpu(z), None, _gpu(b))[1].cpu().numpy()
+        assert np.array_equal(idx, _reference(z, None, b, cfg)[1]), (k, groups)
+
+
+@pytest.mark.gpu
+def test_select_large_logits():
+    rng = np.random.default_rng(78)
+    for scale, offset in ((1.0, 1e4), (100.0, 0.0), (1e5, -1e6), (1e-3, 0.0), (1e-3, 5e3)):
+        z = (scale * rng.standard_normal((50, 96)) + offset).astype(np.float32)
+        for cfg in (_cfg(96, 8, 8), _cfg(96, 8, 8, sigmoid=True, groups=6, topk_groups=2)):
+            idx = _context(cfg).select_experts(_params(cfg), _gpu(z))[1].cpu().numpy()
+            assert np.array_equal(idx, _reference(z, None, None, cfg)[1]), (scale, offset)
+
+
+@pytest.mark.gpu
 def test_select_many_rows_and_replay():
     """More rows than blocks run at once; the same from a captured graph, three times, with other work between."""
     T, cfg = 40000, _cfg(256, 8, 4, sigmoid=True, groups=8, topk_groups=4, group_score=1, scale=2.5)
