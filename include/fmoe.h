@@ -163,7 +163,7 @@ int fmoe_set_ffn_shape(fmoe_ctx* ctx, int32_t shape);
  * before the softmax); w_gate, w_up [E,S_m,H]; w_down [E,H,S_m]; ws_gate, ws_up
  * [N_s,S_s,H]; ws_down [N_s,H,S_s] (NULL iff N_s == 0).  An expert is the three-matrix gated
  * FFN  y = W_down (silu(W_gate x) * (W_up x))  without biases (flop model of App. E).
- * Device allocations (the only ones the library makes; made on the first call, reused by later calls
+ * Device allocations (with those of fmoe_set_weights_quant the only ones of the library; made on the first call, reused by later calls
  * on the same context, freed by fmoe_destroy):
  *  - a private fp32 copy of the router matrix in the router kernel's operand order (E*H*4 bytes
  *    rounded up to 16x16 blocks and whole 128-wide k chunks);

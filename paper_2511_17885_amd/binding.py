@@ -170,12 +170,14 @@ def _float_type(t, what):
     return FMOE_BF16 if t.dtype == torch.bfloat16 else FMOE_F32
 
 
-def _expect(t, what, dtype, shape):
-    """The library takes plain pointers: a tensor of another type or shape would be read past its end."""
+def _expect(t, what, dtype, shape, device):
+    """The library takes plain pointers: a tensor of another type or shape would be read past its end, one of another device
+    not at all."""
     if t is None:
         return
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, not {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
 
 
 def _on(device):
@@ -203,8 +205,8 @@ def quantize_weights(w, saturate=True):
 def dequantize_weights(codes, scales, dtype=torch.bfloat16):
     """The weights [..., K] that codes [..., K/2] and scales [..., ceil(K/32)] stand for (fmoe_dequantize_weights)."""
     K = codes.shape[-1] * 2
-    _expect(codes, "codes", torch.uint8, codes.shape)
-    _expect(scales, "scales", torch.uint8, (*codes.shape[:-1], (K + QUANT_GROUP - 1) // QUANT_GROUP))
+    _expect(codes, "codes", torch.uint8, codes.shape, codes.device)
+    _expect(scales, "scales", torch.uint8, (*codes.shape[:-1], (K + QUANT_GROUP - 1) // QUANT_GROUP), codes.device)
     w = torch.empty((*codes.shape[:-1], K), dtype=dtype, device=codes.device)
     with _on(w.device):
         _check(load().fmoe_dequantize_weights(_ptr(codes), _ptr(scales), w.numel() // max(K, 1), K,
@@ -281,8 +283,8 @@ class FMoE:
         keep the router bias alone."""
         c = self.cfg
         E, H, S, N, Ss = c.n_experts, c.d_model, c.d_ffn, c.n_shared, c.d_ffn_shared
-        _expect(router_w, "router_w", self.torch_dtype, (E, H))
-        _expect(router_bias, "router_bias", torch.float32, (E,))
+        _expect(router_w, "router_w", self.torch_dtype, (E, H), self.device)
+        _expect(router_bias, "router_bias", torch.float32, (E,), self.device)
         names = ("w_gate", "w_up", "w_down", "ws_gate", "ws_up", "ws_down")
         shapes = ((E, S, H), (E, S, H), (E, H, S), (N, Ss, H), (N, Ss, H), (N, H, Ss))
         pairs = (w_gate, w_up, w_down, ws_gate, ws_up, ws_down)
@@ -291,8 +293,8 @@ class FMoE:
             if pair is None:
                 tensors.append(None)
                 continue
-            _expect(pair[0], f"codes of {name}", torch.uint8, (g, n, K // 2))
-            _expect(pair[1], f"scales of {name}", torch.uint8, (g, n, (K + QUANT_GROUP - 1) // QUANT_GROUP))
+            _expect(pair[0], f"codes of {name}", torch.uint8, (g, n, K // 2), self.device)
+            _expect(pair[1], f"scales of {name}", torch.uint8, (g, n, (K + QUANT_GROUP - 1) // QUANT_GROUP), self.device)
             tensors.append(C.byref(FmoeQuantTensor(pair[0].data_ptr(), pair[1].data_ptr())))
         self._weights = (router_w, router_bias, *pairs)
         _check(self.lib.fmoe_set_weights_quant(self._ctx, _ptr(router_w), _ptr(router_bias), *tensors, _stream()))
@@ -341,9 +343,9 @@ class FMoE:
         T = logits.shape[0]
         K = max(self.kmax, 1)
         dtype = _float_type(logits, "logits")
-        _expect(logits, "logits", logits.dtype, (T, self.E))
-        _expect(is_visual, "is_visual", torch.uint8, (T,))
-        _expect(select_bias, "select_bias", torch.float32, (self.E,))
+        _expect(logits, "logits", logits.dtype, (T, self.E), self.device)
+        _expect(is_visual, "is_visual", torch.uint8, (T,), self.device)
+        _expect(select_bias, "select_bias", torch.float32, (self.E,), self.device)
         scores = self._f32(T, self.E) if want_scores else None
         idx, gate = self._i32(T, K), self._f32(T, K)
         _check(self.lib.fmoe_select_experts(self._ctx, C.byref(params), _ptr(logits), dtype, _ptr(is_visual),
@@ -357,10 +359,10 @@ class FMoE:
         scores [T, E]."""
         T = logits.shape[0]
         dtype = _float_type(logits, "logits")
-        _expect(logits, "logits", logits.dtype, (T, self.E))
-        _expect(topk_idx, "topk_idx", torch.int32, (T, self.kmax))
-        _expect(d_gate, "d_gate", torch.float32, (T, self.kmax))
-        _expect(d_scores, "d_scores", torch.float32, (T, self.E))
+        _expect(logits, "logits", logits.dtype, (T, self.E), self.device)
+        _expect(topk_idx, "topk_idx", torch.int32, (T, self.kmax), self.device)
+        _expect(d_gate, "d_gate", torch.float32, (T, self.kmax), self.device)
+        _expect(d_scores, "d_scores", torch.float32, (T, self.E), self.device)
         d_logits = torch.empty_like(logits)
         _check(self.lib.fmoe_select_experts_backward(self._ctx, C.byref(params), _ptr(logits), dtype, _ptr(topk_idx),
                                                      _ptr(d_gate), _ptr(d_scores), T, _ptr(d_logits), _stream()))

@@ -21,8 +21,6 @@
 #include <float.h>
 #include <limits.h>
 
-#include <type_traits>
-
 #include "common.h"
 #include "rows.h"
 
@@ -263,7 +261,8 @@ __device__ __forceinline__ void pack_below(const float (&order)[N], float top, f
   const int lane_part = (15 - j) * 4;
 #pragma unroll
   for (int r = 0; r < N; ++r) {
-    const unsigned q = (unsigned)fmaf(order[r], scale, offset);   // saturates at 0, also for -inf
+    unsigned q;   // the instruction saturates at 0, also for -inf and NaN; a cast would leave that undefined
+    asm("v_cvt_u32_f32 %0, %1" : "=v"(q) : "v"(fmaf(order[r], scale, offset)));
     s[r] = (int)((q << 8) | lane_part) | (192 - 64 * (r >> 2) + 3 - (r & 3));   // .. 255 - expert
   }
 }

@@ -397,6 +397,109 @@ def test_weights_can_be_registered_again_in_either_form():
     assert torch.equal(layer.m.expert_ffn(x, None, 20, offsets, src)[0], quant)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("E,T", [(130, 3), (130, 200), (256, 16), (256, 500)])
+def test_experts_of_more_than_one_wavefront_of_groups(E, T):
+    rng = np.random.default_rng(E + T)
+    _check_experts(_Layer(rng, 40, E, 24, 1, 16, 4, 4), rng, T, E, 4, 1, skew=1.5)
+
+
+@pytest.mark.gpu
+def test_experts_of_row_lists_with_the_same_token_many_times():
+    """Sixteen tokens, 32 rows of one expert: the form for a few tokens takes several turns; the row lists are the caller's."""
+    rng = np.random.default_rng(55)
+    layer = _Layer(rng, 72, 3, 40, 1, 24, 2, 2)
+    x, _ = _bf16(rng, 16, 72)
+    src = torch.from_numpy(rng.integers(0, 16, size=32).astype(np.int32)).cuda()
+    src[:20] = 7
+    for bounds in ([0, 0, 32, 32], [0, 17, 17, 32], [3, 3, 3, 32]):
+        offsets = torch.tensor(bounds, dtype=torch.int32, device="cuda")
+        want = layer.bf16.expert_ffn(x, None, 16, offsets, src)
+        for shape in (0, 1, 2):
+            layer.m.set_ffn_shape(shape)
+            got = layer.m.expert_ffn(x, None, 16, offsets, src)
+            assert torch.equal(got[0][bounds[0]:], want[0][bounds[0]:]) and torch.equal(got[1], want[1]), (bounds, shape)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [8, 120])
+def test_experts_with_malformed_offsets_are_left_out(T):
+    """Offsets below 0, past the room for rows or descending: the expert has no rows, the others are what they are."""
+    rng = np.random.default_rng(56)
+    layer = _Layer(rng, 64, 4, 32, 0, 0, 2, 2)
+    x, _ = _bf16(rng, T, 64)
+    src = torch.arange(2 * T, dtype=torch.int32, device="cuda") % T
+    good = torch.tensor([0, 3, 6, 9, 12], dtype=torch.int32, device="cuda")
+    for shape in (0, 1, 2):
+        layer.m.set_ffn_shape(shape)
+        want = layer.m.expert_ffn(x, None, T, good, src)[0][:12].clone()
+        for bad, rows in (([0, 3, 6, 9, 2 * T + 1], slice(0, 9)), ([-5, 3, 6, 9, 12], slice(3, 12)), ([0, 3, 6, 1, 1], slice(0, 6))):
+            got = layer.m.expert_ffn(x, None, T, torch.tensor(bad, dtype=torch.int32, device="cuda"), src)[0]
+            assert torch.equal(got[rows], want[rows]), (shape, bad)
+
+
+@pytest.mark.gpu
+def test_scales_at_any_address_and_weights_inside_a_larger_tensor():
+    rng = np.random.default_rng(57)
+    layer = _Layer(rng, 64, 2, 32, 0, 0, 1, 1)
+    x, _ = _bf16(rng, 9, 64)
+    offsets, src = (torch.from_numpy(v).cuda() for v in _rows(rng, 9, 2, 1))
+    want = layer.m.expert_ffn(x, None, 9, offsets, src)[0]
+    moved = []
+    for c, s in layer.pairs:
+        room = torch.zeros(s.numel() + 3, dtype=torch.uint8, device="cuda")
+        room[3:] = s.flatten()
+        moved.append((c, room[3:].view(s.shape)))
+        w = binding.dequantize_weights(c, moved[-1][1])
+        assert torch.equal(w, binding.dequantize_weights(c, s))
+    other = binding.FMoE(d_model=64, n_experts=2, d_ffn=32, k_text=1, k_visual=1, dtype="bf16")
+    other.set_weights_quant(layer.router, None, *moved)
+    assert torch.equal(other.expert_ffn(x, None, 9, offsets, src)[0], want)
+
+
+@pytest.mark.gpu
+def test_quantize_offsets_past_32_bits():
+    """2.2 billion weights: the last rows come out as they do alone."""
+    rows, K = 2_200_000, 1000
+    w = torch.zeros(rows, K, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda"); gen.manual_seed(3)
+    w[-50:] = torch.randn(50, K, generator=gen, device="cuda").to(torch.bfloat16)
+    codes, scales = binding.quantize_weights(w)
+    c, s = binding.quantize_weights(w[-50:].clone())
+    assert torch.equal(codes[-50:], c) and torch.equal(scales[-50:], s)
+    assert (scales[:-50] == 127).all()
+    back = binding.dequantize_weights(codes, scales)
+    assert torch.equal(back[-50:], binding.dequantize_weights(c, s)) and not back[:-50].any()
+
+
+@pytest.mark.gpu
+def test_experts_on_two_streams_at_once():
+    """Two contexts; one context with two workspaces of the caller."""
+    rng = np.random.default_rng(58)
+    layers = [_Layer(rng, 136, 8, 72, 1, 40, 2, 2, plain=False) for _ in range(2)]
+    lib = binding.load()
+    p = lambda t: C.c_void_p(t.data_ptr())  # noqa: E731
+    streams, jobs = [torch.cuda.Stream() for _ in range(4)], []
+    for i, T in enumerate((5, 90, 300, 16)):
+        m = layers[i % 2].m
+        x, _ = _bf16(rng, T, 136)
+        offsets, src = (torch.from_numpy(v).cuda() for v in _rows(rng, T, 8, 2))
+        ws = torch.empty(m.workspace_bytes(T, 1), dtype=torch.uint8, device="cuda")
+        out = [(torch.zeros(2 * T, 136, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, 136, dtype=torch.bfloat16, device="cuda"))
+               for _ in range(6)]
+        jobs.append((m, T, x, offsets, src, ws, out, m.expert_ffn(x, None, T, offsets, src)))
+    torch.cuda.synchronize()
+    for turn in range(6):
+        for stream, (m, T, x, offsets, src, ws, out, _) in zip(streams, jobs):
+            y, ysh = out[turn]
+            assert lib.fmoe_expert_ffn(m._ctx, p(x), None, T, None, p(offsets), p(src), p(y), p(ysh), p(ws), ws.numel(),
+                                       C.c_void_p(stream.cuda_stream)) == 0
+    torch.cuda.synchronize()
+    for *_, out, want in jobs:
+        for y, ysh in out:
+            assert torch.equal(y, want[0]) and torch.equal(ysh, want[1].view_as(ysh))
+
+
 # --------------------------------------------------------------------------------------------------------- whole layers
 
 
@@ -572,6 +675,27 @@ def test_binding_refuses_tensors_that_do_not_fit():
         m.set_weights_quant(router.float(), None, *good)
     with pytest.raises(ValueError):
         m.set_weights_quant(router, torch.zeros(3), *good)
+
+
+@pytest.mark.gpu
+def test_binding_refuses_tensors_that_do_not_fit_or_are_on_the_host():
+    m = binding.FMoE(d_model=64, n_experts=4, d_ffn=32, k_text=2, k_visual=1, dtype="bf16")
+    router = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    pair = lambda *s: (torch.zeros(*s[:-1], s[-1] // 2, dtype=torch.uint8, device="cuda"), torch.zeros(*s[:-1], s[-1] // 32, dtype=torch.uint8, device="cuda"))  # noqa: E731
+    good = [pair(4, 32, 64), pair(4, 32, 64), pair(4, 64, 32)]
+    m.set_weights_quant(router, None, *good)
+    for i in range(3):
+        c, s = good[i]
+        for bad in ((c[:3].contiguous(), s), (c, s[:, :-1].contiguous()), (c.cpu(), s), (c, s.cpu()), (c.int(), s)):
+            with pytest.raises(ValueError):
+                m.set_weights_quant(router, None, *good[:i], bad, *good[i + 1:])
+    for args in ((router.float(), None), (router.cpu(), None), (router, torch.zeros(3, device="cuda")), (router, torch.zeros(4))):
+        with pytest.raises(ValueError):
+            m.set_weights_quant(*args, *good)
+    with pytest.raises(ValueError):
+        binding.dequantize_weights(good[0][0], good[0][1].cpu())
+    with pytest.raises(ValueError):
+        binding.quantize_weights(torch.zeros(4, 64))
 
 
 def test_build_check_catches_registers_used_before_an_lds_read_has_landed(tmp_path):

@@ -444,6 +444,73 @@ def test_select_empty_batch():
     assert m.select_experts_backward(_params(cfg), z, idx, gate).shape == (0, 8)
 
 
+@pytest.mark.gpu
+def test_select_on_two_streams_at_once_and_on_rows_inside_a_larger_tensor():
+    cfgs = (_cfg(256, 8, 4, sigmoid=True, groups=8, topk_groups=4, group_score=1), _cfg(64, 6, 3, renorm=False))
+    jobs, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    gen = torch.Generator(device="cuda"); gen.manual_seed(9)
+    for cfg in cfgs:
+        z = torch.randn(3010, cfg["E"], generator=gen, device="cuda")[10:]     # contiguous, not at the start
+        bias = 0.1 * torch.randn(cfg["E"], generator=gen, device="cuda")
+        m, p = _context(cfg), _params(cfg)
+        want = m.select_experts(p, z, None, bias, want_scores=True)
+        d_gate = torch.randn(3000, cfg["kmax"], generator=gen, device="cuda")
+        jobs.append((m, p, z, bias, d_gate, want, m.select_experts_backward(p, z, want[1], d_gate, want[0])))
+        head = _reference(z[:20].cpu().numpy(), None, bias.cpu().numpy(), cfg)[1]
+        assert np.array_equal(want[1][:20].cpu().numpy(), head)
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, (m, p, z, bias, d_gate, want, want_d) in enumerate(jobs):
+            with torch.cuda.stream(streams[i]):
+                out = m.select_experts(p, z, None, bias, want_scores=True)
+                got[i].append((*out, m.select_experts_backward(p, z, out[1], d_gate, out[0])))
+    torch.cuda.synchronize()
+    for i, job in enumerate(jobs):
+        for out in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(out, (*job[5], job[6])))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_select_offsets_past_32_bits(dtype):
+    """4.4 and 2.2 GB of logits: rows far behind come out as they do alone."""
+    E, T = 256, 4_300_000 * (1 if dtype == torch.float32 else 2)
+    cfg = _cfg(E, 4, 4, sigmoid=True)
+    m, p = _context(cfg), _params(cfg)
+    z = torch.zeros(T, E, dtype=dtype, device="cuda")
+    gen = torch.Generator(device="cuda"); gen.manual_seed(1)
+    z[-100:] = torch.randn(100, E, generator=gen, device="cuda").to(dtype)
+    _, idx, gate = m.select_experts(p, z)
+    d_gate = torch.ones(T, 4, device="cuda")
+    d_gate[:, 1] = -2.0
+    d = m.select_experts_backward(p, z, idx, d_gate)
+    tail = z[-100:].clone()
+    _, i, g = m.select_experts(p, tail)
+    assert torch.equal(idx[-100:], i) and torch.equal(gate[-100:], g)
+    assert torch.equal(d[-100:], m.select_experts_backward(p, tail, i, d_gate[-100:].contiguous()))
+    assert (idx[:-100] == torch.arange(4, dtype=torch.int32, device="cuda")).all()
+
+
+@pytest.mark.gpu
+def test_select_backward_of_lists_that_were_not_chosen_here():
+    """Any distinct experts may be listed, in any order and with gaps; places outside 0 .. E-1 are empty."""
+    rng = np.random.default_rng(31)
+    for sigmoid in (False, True):
+        for renorm in (False, True):
+            cfg = _cfg(20, 5, 5, sigmoid=sigmoid, renorm=renorm, scale=0.7)
+            z = rng.standard_normal((30, 20)).astype(np.float32)
+            idx = np.stack([rng.choice(20, size=5, replace=False) for _ in range(30)]).astype(np.int32)
+            idx[rng.random(idx.shape) < 0.3] = -1
+            idx[0, 2], idx[1, 0], idx[2] = 20, 2 ** 31 - 1, -7
+            d_gate = rng.standard_normal(idx.shape).astype(np.float32)
+            got = _context(cfg).select_experts_backward(_params(cfg), _gpu(z), _gpu(idx), _gpu(d_gate)).double().cpu().numpy()
+            for t in range(30):
+                on = (idx[t] >= 0) & (idx[t] < 20)
+                want = _gradient(z[t], np.concatenate([idx[t][on], np.full(5 - on.sum(), -1)]), d_gate[t][on], None, cfg)
+                assert (np.abs(got[t] - want) <= _backward_bound(_clean(z[t]), d_gate[t], None, cfg)).all(), t
+
+
 # --------------------------------------------------------------------------------------------------------- refusals
 
 
@@ -492,3 +559,15 @@ def test_select_binding_refuses_tensors_of_other_shapes():
             call()
     with pytest.raises(TypeError):
         m.select_experts(p, z.double())
+
+
+@pytest.mark.gpu
+def test_select_binding_refuses_tensors_on_the_host():
+    cfg = _cfg(8, 2, 1)
+    m, p = _context(cfg), _params(cfg)
+    z, idx, dg = torch.zeros(4, 8, device="cuda"), torch.zeros(4, 2, dtype=torch.int32, device="cuda"), torch.zeros(4, 2, device="cuda")
+    for call in (lambda: m.select_experts(p, z.cpu()), lambda: m.select_experts(p, z, torch.zeros(4, dtype=torch.uint8)),
+                 lambda: m.select_experts(p, z, None, torch.zeros(8)), lambda: m.select_experts_backward(p, z, idx.cpu(), dg),
+                 lambda: m.select_experts_backward(p, z, idx, dg.cpu()), lambda: m.select_experts_backward(p, z, idx, dg, z.cpu())):
+        with pytest.raises(ValueError, match="on cuda:0"):
+            call()
