@@ -11,12 +11,21 @@
 // exponential and reciprocal of the hardware.  Two sigmoid scores are then off by less than 2^-21 together; two softmax scores
 // that go with close keys by less than 27 * 2^-24 of the largest score the row can have (22 for the normaliser, whose error
 // they share); 2^-19 of it is allowed for, and half a rounding of each key.  Where keys in a token's list or behind its end are
-// closer than that, its entries and the next one are put in order in 64 bits, a lane an entry; where that is not enough (the
-// line between groups, more than one key close behind the list) the token is done again by its whole wavefront.  Of 22016
-// tokens with 256 experts in eight groups and a bias of deviation 0.1 some twenty are of the first kind.
+// closer than that, its entries and the next one are put in order in 64 bits, a lane an entry; where that is not enough (more
+// than one key close behind the list) its whole wavefront lists the token again.  Where the scores of groups on either side of
+// the line are that close, the wavefront chooses the token's groups.  Of 22016 tokens with 256 experts in eight groups and a
+// bias of deviation 0.1 some twenty are of the first kind and a few of the last.
 //
 // Sixteen lanes have a token (four tokens a wavefront), lane j of them the experts 64 q + 4 j + i: a row is read in
 // pieces of 16 bytes, and a reduction over the row is one over a lane's registers and four steps inside the vector unit.
+//
+// Bound: vector instructions (some thousand a wavefront, 256 experts) behind one wait for the logits, and for few tokens the
+// launch.  22016 tokens, 256 experts, sigmoid, bias, eight groups: 16.6 us, 1.4 TB/s.  Step by step: everything in 64 bits
+// 41.4; keys in 32 bits and only what is close in 64, rows four at a time 34.6; lists by integers sorted in a lane, so that
+// a round is one reduction 24.1; fewer instructions for keys, integers and gates 21.5; reductions of the whole wavefront without
+// LDS 19.0; close entries put in order instead of listed again 18.6; only the groups chosen again 16.6.  The few tokens in 64
+// bits still are 1.8 of it, at the end of the launch.  A wavefront that takes several rows in turn, the next ones' logits on
+// their way, took 25 where this took 21.5.
 
 #include <float.h>
 #include <limits.h>
@@ -136,18 +145,128 @@ __device__ __forceinline__ void two_largest(float& one, float& two, float o1, fl
   one = fmaxf(one, o1);
 }
 
+// ---- one token by a whole wavefront, in 64 bits: what the definition says, for the few that are close.  A wavefront that
+// comes here is one the launch waits for, so what counts is latency: reductions go through the rows of 16 and four lane
+// reads, not through LDS.
+__device__ __forceinline__ double read_lane(double v, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+__device__ __forceinline__ double wave_max(double v) {
+  v = row_max(v);
+  return larger(larger(read_lane(v, 0), read_lane(v, 16)), larger(read_lane(v, 32), read_lane(v, 48)));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+  v = row_sum_butterfly(v);
+  return (read_lane(v, 0) + read_lane(v, 16)) + (read_lane(v, 32) + read_lane(v, 48));
+}
+__device__ __forceinline__ int wave_min(int v) {
+  v = row_min(v);
+  return min(min(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+             min(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+// Keys of experts 4 l .. 4 l + 3 of token t in lane l.
+template <typename ZT, bool KEYED, bool SIGMOID>
+__device__ __forceinline__ void keys_wide(const SelectArgs& a, int t, double (&z)[4], double (&key)[4]) {
+  const int lane = threadIdx.x & 63;
+  const ZT* const row = static_cast<const ZT*>(a.z) + (size_t)t * a.E;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) z[i] = 4 * lane + i < a.E ? clean(to_f32(row[4 * lane + i])) : -INFINITY;
+  double m = 0.0, sum = 1.0;
+  if (KEYED && !SIGMOID) {
+    m = wave_max(larger(larger(z[0], z[1]), larger(z[2], z[3])));
+    if (!(m > -INFINITY)) m = 0.0;
+    sum = wave_sum((exp(z[0] - m) + exp(z[1] - m)) + (exp(z[2] - m) + exp(z[3] - m)));
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int e = 4 * lane + i;
+    key[i] = z[i];
+    if (KEYED) {
+      const float b = a.bias != nullptr && e < a.E ? a.bias[e] : 0.0f;
+      const double s = SIGMOID ? 1.0 / (1.0 + exp(-z[i])) : exp(z[i] - m) / sum;
+      key[i] = z[i] > -INFINITY && b > -INFINITY ? s + (double)b : -INFINITY;
+    }
+  }
+}
+// Bits 4 g: the groups g of token t that stay.  ks: room for E doubles.
+template <typename ZT, bool SIGMOID>
+__device__ unsigned long long groups_wide(const SelectArgs& a, int t, double* ks) {
+  const int lane = threadIdx.x & 63;
+  double z[4], key[4];
+  keys_wide<ZT, true, SIGMOID>(a, t, z, key);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (4 * lane + i < a.E) ks[4 * lane + i] = key[i];
+  wave_sync();
+  double one = -INFINITY, two = -INFINITY;   // lane 4 g + q: of group g the elements q, q + 4, ..
+  const int g0 = lane >> 2;
+  for (int i = lane & 3; i < a.group_size && g0 < a.groups; i += 4) {
+    const double v = ks[g0 * a.group_size + i];
+    two = v > one ? one : larger(two, v);
+    one = larger(one, v);
+  }
+#pragma unroll
+  for (int s = 1; s <= 2; s <<= 1) {   // (of equal ones both count)
+    const double o1 = __shfl_xor(one, s, 64), o2 = __shfl_xor(two, s, 64);
+    two = larger(o1 > one ? one : o1, larger(two, o2));
+    one = larger(one, o1);
+  }
+  wave_sync();
+  const double score = (a.sum_two && two > -INFINITY) ? one + two : one;
+  int ahead = 0;
+  for (int g = 0; g < a.groups; ++g) {
+    const double o = read_lane(score, 4 * g);
+    ahead += (o > score || (o == score && g < g0)) ? 1 : 0;
+  }
+  return __ballot(g0 < a.groups && ahead < a.topk_groups);
+}
+// Lane i of the result: entry i of the token's list.  stays(e): whether the group of expert e stays.
+template <typename ZT, bool KEYED, bool SIGMOID, typename F>
+__device__ int list_wide(const SelectArgs& a, int t, int k, F&& stays) {
+  const int lane = threadIdx.x & 63;
+  double z[4], order[4];
+  keys_wide<ZT, KEYED, SIGMOID>(a, t, z, order);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (a.bias == nullptr) order[i] = z[i];
+    if (!stays(4 * lane + i)) order[i] = -INFINITY;
+  }
+  int mine = -1;
+  for (int round = 0; round < k; ++round) {
+    const double top = wave_max(larger(larger(order[0], order[1]), larger(order[2], order[3])));
+    if (!(top > -INFINITY)) break;
+    int e = 0x7fff;
+#pragma unroll
+    for (int i = 3; i >= 0; --i) e = order[i] == top ? 4 * lane + i : e;
+    e = wave_min(e);   // ties: lowest expert
+    if (lane == round) mine = e;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (4 * lane + i == e) order[i] = -INFINITY;
+  }
+  return mine;
+}
+
 // Masks the experts of a token's groups that do not stay.  key: what a group's score is made of; order: what ranks the
-// experts; ks: the token's row in LDS.  Returns whether the scores on either side of the line are further apart than `slack`
-// plus `relative` times the largest keys that went into any.  2^log2p lanes have a group.
-template <int N>
-__device__ __forceinline__ bool keep_groups(const SelectArgs& a, int j, const float (&key)[N], float (&order)[N], float* ks,
-                                            float slack, float relative) {
+// experts; rows: the tokens' rows in LDS.  Where keys are SCORED and the scores on either side of the line are not further
+// apart than `slack` plus `relative` times the largest keys that went into any, the token's groups are chosen in 64 bits.
+// 2^log2p lanes have a group; bits g << log2p of the result: the groups that stay.
+__device__ __forceinline__ int lanes_of_group(const SelectArgs& a) {
+  return a.groups <= 2 ? 3 : a.groups <= 4 ? 2 : a.groups <= 8 ? 1 : 0;   // uniform; logarithm
+}
+__device__ __forceinline__ bool stays(const SelectArgs& a, unsigned mask, int log2p, int e) {   // (past E masked already)
+  return (mask >> (((e * a.group_mul >> 16) << log2p) & 15)) & 1u;
+}
+template <typename ZT, bool SCORED, bool SIGMOID, int N, int STRIDE>
+__device__ __forceinline__ unsigned keep_groups(const SelectArgs& a, int t, int tok, int j, const float (&key)[N],
+                                                float (&order)[N], float (&rows)[ROWS][STRIDE], float slack, float relative) {
+  float* const ks = rows[tok];
   typedef float four_t __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int q = 0; q < N / 4; ++q)
     *reinterpret_cast<four_t*>(ks + 64 * q + 4 * j) = four_t{key[4 * q], key[4 * q + 1], key[4 * q + 2], key[4 * q + 3]};
   wave_sync();
-  const int log2p = a.groups <= 2 ? 3 : a.groups <= 4 ? 2 : a.groups <= 8 ? 1 : 0;   // uniform
+  const int log2p = lanes_of_group(a);
   const int g = j >> log2p, part = j & ((1 << log2p) - 1);
   const bool fours = (a.group_size & 3) == 0;
   float one = -INFINITY, two = -INFINITY;
@@ -183,25 +302,34 @@ __device__ __forceinline__ bool keep_groups(const SelectArgs& a, int j, const fl
     const float o = ks[h];
     ahead += (o > score || (o == score && h < g)) ? 1 : 0;
   }
-  const bool in = g < a.groups && ahead < a.topk_groups;
+  wave_sync();   // the scores have been read
+  bool in = g < a.groups && ahead < a.topk_groups;
+  if constexpr (SCORED) {
+    const float last = -row_max(in ? -score : -INFINITY), next = row_max(g < a.groups && !in ? score : -INFINITY);
+    const float size = row_max(fabsf(one > -INFINITY ? one : 0.0f) + fabsf(two > -INFINITY ? two : 0.0f));
+    const bool sure = a.topk_groups == a.groups || next == -INFINITY || last - next > slack + relative * size;
+    unsigned long long again = __ballot(!sure);
+    while (again != 0) {   // uniform
+      const int first = (__ffsll((long long)again) - 1) & 48;   // the token's first lane
+      again &= ~(0xffffull << first);
+      const unsigned long long stay =
+          groups_wide<ZT, SIGMOID>(a, __shfl(t, first, 64), reinterpret_cast<double*>(rows[tok & 12]));
+      if ((threadIdx.x & 48) == (unsigned)first) in = (stay >> (4 * g)) & 1u;
+    }
+  }
   const unsigned mask = (unsigned)(__ballot(in) >> (threadIdx.x & 48)) & 0xffffu;
-  const auto stays = [&](int e) { return (mask >> (((e * a.group_mul >> 16) << log2p) & 15)) & 1u; };   // (past E masked already)
   if (fours) {
 #pragma unroll
     for (int q = 0; q < N / 4; ++q) {
-      const bool on = stays(64 * q + 4 * j);
+      const bool on = stays(a, mask, log2p, 64 * q + 4 * j);
 #pragma unroll
       for (int i = 0; i < 4; ++i) order[4 * q + i] = on ? order[4 * q + i] : -INFINITY;
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < N; ++r) order[r] = stays(expert_of(r, j)) ? order[r] : -INFINITY;
+    for (int r = 0; r < N; ++r) order[r] = stays(a, mask, log2p, expert_of(r, j)) ? order[r] : -INFINITY;
   }
-  wave_sync();   // the scores have been read
-  if (a.topk_groups == a.groups) return true;
-  const float last = -row_max(in ? -score : -INFINITY), next = row_max(g < a.groups && !in ? score : -INFINITY);
-  const float size = row_max(fabsf(one > -INFINITY ? one : 0.0f) + fabsf(two > -INFINITY ? two : 0.0f));
-  return next == -INFINITY || last - next > slack + relative * size;
+  return mask;
 }
 
 // The list by integers that hold key and expert, all different: a lane's are sorted once, then every round takes the largest
@@ -273,96 +401,6 @@ __device__ __forceinline__ bool apart(int mine, int rest, int k, int rounds, int
   return (j >= k) | (((mine >> 8) > 0) & ((mine >> 8) - (next >> 8) > steps));
 }
 
-// ---- one token by a whole wavefront, in 64 bits: what the definition says, for the few that are close.  A wavefront that
-// comes here is one the launch waits for, so what counts is latency: reductions go through the rows of 16 and four lane
-// reads, not through LDS.
-__device__ __forceinline__ double read_lane(double v, int lane) {
-  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
-}
-__device__ __forceinline__ double wave_max(double v) {
-  v = row_max(v);
-  return larger(larger(read_lane(v, 0), read_lane(v, 16)), larger(read_lane(v, 32), read_lane(v, 48)));
-}
-__device__ __forceinline__ double wave_sum(double v) {
-  v = row_sum_butterfly(v);
-  return (read_lane(v, 0) + read_lane(v, 16)) + (read_lane(v, 32) + read_lane(v, 48));
-}
-__device__ __forceinline__ int wave_min(int v) {
-  v = row_min(v);
-  return min(min(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
-             min(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
-}
-// Lane i of the result: entry i of the token's list.  Lane l has experts 4 l .. 4 l + 3; ks: room for E doubles.
-template <typename ZT, bool KEYED, bool SIGMOID>
-__device__ int list_wide(const SelectArgs& a, int t, int k, double* ks) {
-  const int lane = threadIdx.x & 63;
-  const ZT* const row = static_cast<const ZT*>(a.z) + (size_t)t * a.E;
-  double z[4], key[4], order[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) z[i] = 4 * lane + i < a.E ? clean(to_f32(row[4 * lane + i])) : -INFINITY;
-  double m = 0.0, sum = 1.0;
-  if (KEYED && !SIGMOID) {
-    m = wave_max(larger(larger(z[0], z[1]), larger(z[2], z[3])));
-    if (!(m > -INFINITY)) m = 0.0;
-    sum = wave_sum((exp(z[0] - m) + exp(z[1] - m)) + (exp(z[2] - m) + exp(z[3] - m)));
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int e = 4 * lane + i;
-    order[i] = key[i] = z[i];
-    if (KEYED) {
-      const float b = a.bias != nullptr && e < a.E ? a.bias[e] : 0.0f;
-      const double s = SIGMOID ? 1.0 / (1.0 + exp(-z[i])) : exp(z[i] - m) / sum;
-      key[i] = z[i] > -INFINITY && b > -INFINITY ? s + (double)b : -INFINITY;
-      if (a.bias != nullptr) order[i] = key[i];
-    }
-  }
-  if (a.groups > 1) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (4 * lane + i < a.E) ks[4 * lane + i] = key[i];
-    wave_sync();
-    double one = -INFINITY, two = -INFINITY;   // lane 4 g + q: of group g the elements q, q + 4, ..
-    const int g0 = lane >> 2;
-    for (int i = lane & 3; i < a.group_size && g0 < a.groups; i += 4) {
-      const double v = ks[g0 * a.group_size + i];
-      two = v > one ? one : larger(two, v);
-      one = larger(one, v);
-    }
-#pragma unroll
-    for (int s = 1; s <= 2; s <<= 1) {   // (of equal ones both count)
-      const double o1 = __shfl_xor(one, s, 64), o2 = __shfl_xor(two, s, 64);
-      two = larger(o1 > one ? one : o1, larger(two, o2));
-      one = larger(one, o1);
-    }
-    wave_sync();
-    const double score = (a.sum_two && two > -INFINITY) ? one + two : one;
-    int ahead = 0;
-    for (int g = 0; g < a.groups; ++g) {
-      const double o = read_lane(score, 4 * g);
-      ahead += (o > score || (o == score && g < g0)) ? 1 : 0;
-    }
-    const unsigned long long stay = __ballot(g0 < a.groups && ahead < a.topk_groups);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (!((stay >> (((4 * lane + i) * a.group_mul >> 16) * 4 & 60)) & 1u)) order[i] = -INFINITY;
-  }
-  int mine = -1;
-  for (int round = 0; round < k; ++round) {
-    const double top = wave_max(larger(larger(order[0], order[1]), larger(order[2], order[3])));
-    if (!(top > -INFINITY)) break;
-    int e = 0x7fff;
-#pragma unroll
-    for (int i = 3; i >= 0; --i) e = order[i] == top ? 4 * lane + i : e;
-    e = wave_min(e);   // ties: lowest expert
-    if (lane == round) mine = e;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (4 * lane + i == e) order[i] = -INFINITY;
-  }
-  return mine;
-}
-
 // f(v, i) of the fifteen other lanes of the row
 template <int ROT = 1, typename F>
 __device__ __forceinline__ void static_for_rotations(double v, int i, F&& f) {
@@ -431,9 +469,9 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
     write_row<float, NQ>(a.scores + (size_t)t * a.E, a.E, j, s);
   }
 
-  // the list in 32 bits, and whether it is sure
+  // the list in 32 bits
   float order[N];
-  bool sure = true;
+  unsigned groups = 0xffffu;   // that stay
   if constexpr (KEYED) {
     float bias[N], key[N];
     if (a.bias != nullptr) {   // uniform
@@ -456,11 +494,11 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
 #pragma unroll
       for (int r = 0; r < N; ++r) order[r] = z[r];
     }
-    if (a.groups > 1) sure = keep_groups<N>(a, j, key, order, ks[tok], 2.0f * slack, 0x1p-21f);
+    if (a.groups > 1) groups = keep_groups<ZT, true, SIGMOID>(a, t, tok, j, key, order, ks, 2.0f * slack, 0x1p-21f);
   } else {
 #pragma unroll
     for (int r = 0; r < N; ++r) order[r] = z[r];
-    if (a.groups > 1) (void)keep_groups<N>(a, j, z, order, ks[tok], 0.0f, 0.0f);
+    if (a.groups > 1) groups = keep_groups<ZT, false, SIGMOID>(a, t, tok, j, z, order, ks, 0.0f, 0.0f);
   }
   int packed[N], rest, mine;
   if constexpr (!KEYED && sizeof(ZT) == 2) {
@@ -494,7 +532,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
     const bool sorted = apart(entry, rest, k, rounds, j, steps) | none;
     // do the entries hold the list for certain?  Their integers then are in range, and the k-th is apart from the rest
     const bool held = (j != k - 1) | (((entry >> 8) > 0) & ((entry >> 8) - (rest >> 8) > steps));
-    sure = (sure & held & (fabsf(peak) < 8.0f * range)) | none;
+    const bool sure = (held & (fabsf(peak) < 8.0f * range)) | none;
     if (none) mine = -1;
     if (__any(!sorted & sure)) {   // uniform
       bool by_score = false;
@@ -507,8 +545,10 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
     while (again != 0) {   // uniform
       const int first = (__ffsll((long long)again) - 1) & 48;   // the token's first lane
       again &= ~(0xffffull << first);
+      const unsigned on = (unsigned)__shfl((int)groups, first, 64);
+      const int log2p = lanes_of_group(a);
       const int list = list_wide<ZT, KEYED, SIGMOID>(a, __shfl(t, first, 64), __shfl(k, first, 64),
-                                                     reinterpret_cast<double*>(ks[tok & 12]));
+                                                     [&](int e) { return a.groups <= 1 || stays(a, on, log2p, e); });
       const int mine_again = __shfl(list, j, 64);
       mine = (threadIdx.x & 48) == (unsigned)first ? mine_again : mine;
     }
