@@ -20,10 +20,10 @@
 // pieces of 16 bytes, and a reduction over the row is one over a lane's registers and four steps inside the vector unit.
 //
 // Bound: vector instructions (some thousand a wavefront, 256 experts) behind one wait for the logits, and for few tokens the
-// launch.  22016 tokens, 256 experts, sigmoid, bias, eight groups: 16.6 us, 1.4 TB/s.  Step by step: everything in 64 bits
+// launch.  22016 tokens, 256 experts, sigmoid, bias, eight groups: 16.5 us, 1.4 TB/s.  Step by step: everything in 64 bits
 // 41.4; keys in 32 bits and only what is close in 64, rows four at a time 34.6; lists by integers sorted in a lane, so that
 // a round is one reduction 24.1; fewer instructions for keys, integers and gates 21.5; reductions of the whole wavefront without
-// LDS 19.0; close entries put in order instead of listed again 18.6; only the groups chosen again 16.6.  The few tokens in 64
+// LDS 19.0; close entries put in order instead of listed again 18.6; only the groups chosen again 16.6; row maxima as integers 16.5.  The few tokens in 64
 // bits still are 1.8 of it, at the end of the launch.  A wavefront that takes several rows in turn, the next ones' logits on
 // their way, took 25 where this took 21.5.
 
@@ -101,13 +101,20 @@ __device__ __forceinline__ void load_row(const ZT* __restrict__ z, int t, int E,
   for (int r = 0; r < 4 * NQ; ++r) v[r] = 64 * (r >> 2) + 4 * j + (r & 3) < E ? clean(to_f32(raw[r])) : -INFINITY;
 }
 
+// Largest over the row of a number that is not NaN, as integers of the same order: an instruction a step.
+__device__ __forceinline__ float row_top(float v) {
+  int o = __float_as_int(v);
+  o = row_max(o ^ ((o >> 31) & 0x7fffffff));
+  return __int_as_float(o ^ ((o >> 31) & 0x7fffffff));
+}
+
 // Of a row: the largest, of its logits also 0 if all are masked, and the sum of exp(z - largest).
 template <int N>
 __device__ __forceinline__ float row_peak(const float (&z)[N]) {
   float m = z[0];
 #pragma unroll
   for (int r = 1; r < N; ++r) m = fmaxf(m, z[r]);
-  return row_max(m);
+  return row_top(m);
 }
 template <int N>
 __device__ __forceinline__ float row_largest(const float (&z)[N]) {
@@ -305,8 +312,8 @@ __device__ __forceinline__ unsigned keep_groups(const SelectArgs& a, int t, int 
   wave_sync();   // the scores have been read
   bool in = g < a.groups && ahead < a.topk_groups;
   if constexpr (SCORED) {
-    const float last = -row_max(in ? -score : -INFINITY), next = row_max(g < a.groups && !in ? score : -INFINITY);
-    const float size = row_max(fabsf(one > -INFINITY ? one : 0.0f) + fabsf(two > -INFINITY ? two : 0.0f));
+    const float last = -row_top(in ? -score : -INFINITY), next = row_top(g < a.groups && !in ? score : -INFINITY);
+    const float size = row_top(fabsf(one > -INFINITY ? one : 0.0f) + fabsf(two > -INFINITY ? two : 0.0f));
     const bool sure = a.topk_groups == a.groups || next == -INFINITY || last - next > slack + relative * size;
     unsigned long long again = __ballot(!sure);
     while (again != 0) {   // uniform
@@ -562,7 +569,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
       p = mine >= 0 ? 1.0f / (1.0f + expf(-zl)) : 0.0f;
     } else {
       const float l = mine >= 0 ? (SIGMOID ? log_sigmoid(zl) : zl) : -INFINITY;
-      const float lm = row_max(l);
+      const float lm = row_top(l);
       p = mine >= 0 ? expf(l - lm) : 0.0f;
     }
     const float sum = row_sum_butterfly(p);   // (every lane takes part)
@@ -619,7 +626,7 @@ __global__ __launch_bounds__(256) void select_backward_kernel(SelectBackwardArgs
   if (a.renorm || (a.sigmoid && !DENSE)) {
     if (a.renorm) {
       const float l = a.sigmoid ? log_sigmoid(zl) : zl;
-      const float lm = row_max(in ? l : -INFINITY);
+      const float lm = row_top(in ? l : -INFINITY);
       float p = in && l > -INFINITY ? expf(l - lm) : 0.0f;
       const float sum = row_sum_butterfly(p);
       p = sum > 0.0f ? p / sum : 0.0f;
