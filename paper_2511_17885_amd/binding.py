@@ -6,7 +6,6 @@ been built, loading raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -175,16 +174,18 @@ def _expect(t, what, dtype, shape, device):
     not at all."""
     if t is None:
         return
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, not {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")
 
 
-def _on(device):
-    """Makes the device of a call without a context the current one, where it is not (1.3 us)."""
+def _call(device, entry, *args):
+    """A call without a context, on the device of its tensors, which mostly is the current one."""
     if device.type == "cuda" and device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
+        _check(entry(*args, torch._C._cuda_getCurrentRawStream(device.index)))
+    else:
+        with torch.cuda.device(device):
+            _check(entry(*args, _stream()))
 
 
 def quantize_weights(w, saturate=True):
@@ -193,12 +194,11 @@ def quantize_weights(w, saturate=True):
     dtype = _float_type(w, "w")
     if not w.is_contiguous():
         raise ValueError("w must be contiguous")
-    K = w.shape[-1]
-    codes = torch.empty((*w.shape[:-1], K // 2), dtype=torch.uint8, device=w.device)
-    scales = torch.empty((*w.shape[:-1], (K + QUANT_GROUP - 1) // QUANT_GROUP), dtype=torch.uint8, device=w.device)
-    with _on(w.device):
-        _check(load().fmoe_quantize_weights(_ptr(w), dtype, w.numel() // max(K, 1), K, int(bool(saturate)), _ptr(codes),
-                                            _ptr(scales), _stream()))
+    *lead, K = w.shape
+    codes = torch.empty(*lead, K // 2, dtype=torch.uint8, device=w.device)
+    scales = torch.empty(*lead, (K + QUANT_GROUP - 1) // QUANT_GROUP, dtype=torch.uint8, device=w.device)
+    _call(w.device, load().fmoe_quantize_weights, _ptr(w), dtype, w.numel() // max(K, 1), K, int(bool(saturate)), _ptr(codes),
+          _ptr(scales))
     return codes, scales
 
 
@@ -207,10 +207,9 @@ def dequantize_weights(codes, scales, dtype=torch.bfloat16):
     K = codes.shape[-1] * 2
     _expect(codes, "codes", torch.uint8, codes.shape, codes.device)
     _expect(scales, "scales", torch.uint8, (*codes.shape[:-1], (K + QUANT_GROUP - 1) // QUANT_GROUP), codes.device)
-    w = torch.empty((*codes.shape[:-1], K), dtype=dtype, device=codes.device)
-    with _on(w.device):
-        _check(load().fmoe_dequantize_weights(_ptr(codes), _ptr(scales), w.numel() // max(K, 1), K,
-                                              _float_type(w, "w"), _ptr(w), _stream()))
+    w = torch.empty(*codes.shape[:-1], K, dtype=dtype, device=codes.device)
+    _call(w.device, load().fmoe_dequantize_weights, _ptr(codes), _ptr(scales), w.numel() // max(K, 1), K,
+          _float_type(w, "w"), _ptr(w))
     return w
 
 
@@ -312,10 +311,10 @@ class FMoE:
         return self._ws
 
     def _i32(self, *shape):
-        return torch.empty(shape, dtype=torch.int32, device=self.device)
+        return torch.empty(*shape, dtype=torch.int32, device=self.device)
 
     def _f32(self, *shape):
-        return torch.empty(shape, dtype=torch.float32, device=self.device)
+        return torch.empty(*shape, dtype=torch.float32, device=self.device)
 
     # ---- instrumentation
     def profile_enable(self, on=True):
