@@ -165,8 +165,8 @@ __device__ __forceinline__ void while_for(C&& c, F&& f) {   // static_for that e
 
 // One work item of a workgroup: a tile of rows (NAB live bands of 32, LDS stages of ROWS) times NCB column tiles, column block
 // w of each for wavefront w.  Rows go through a ring of LDS stages as in ffn.hip; codes and scales into registers, all as
-// many k tiles ahead; a k tile is one barrier.  Every load is unconditional (past the end the last tile again), so the number
-// of loads in flight at a wait is a compile-time constant.  Row blocks are taken two at a time, the next pair's operands
+// many k tiles ahead; a k tile is one barrier.  Every load of the loop is unconditional (past the end the last tile
+// again), so the number of loads in flight at a wait is a compile-time constant.  Row blocks are taken two at a time, the next pair's operands
 // requested from LDS before the present pair's products.  HALF: of the only band the first 16 rows.
 template <bool SWIGLU, int NAB, int NCB, int STAGES, int ROWS, bool HALF = false>
 __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_tile& tile, int group, int ct0, int ct_limit,
@@ -260,18 +260,27 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
 
   u32x4_t fa[2][PB];
   u32x4_t fb[NCB][2];
-  // k tile t, U = t % STAGES: products, and the loads of tile t + AHEAD.  Scales: with one unit in registers the next one is
+  // k tile t, U = t % STAGES: products, and the loads of tile t + AHEAD; of the LAST tiles, fewer than STAGES, products only,
+  // since all of theirs are on the way.  (Loads of theirs would be past the end, and the compiler drops those into registers that
+  // nothing reads: the counts below would be too large.)  Scales: with one unit in registers the next one is
   // requested with the unit's first tile; with two a unit's successor but one takes its place behind its last tile.
-  auto ktile = [&](auto uc, int t) {
+  auto ktile = [&](auto uc, auto last, int t) {
     constexpr int U = decltype(uc)::value;
+    constexpr bool LAST = decltype(last)::value;
     constexpr bool SCALES = UNITS == 1 ? U == 0 : U % 4 == 3;
-    constexpr int NL = PER_TILE + (SCALES ? NCB : 0);   // loads this tile issues
+    constexpr int NL = LAST ? 0 : PER_TILE + (SCALES ? NCB : 0);   // loads this tile issues
     constexpr int unit = (U / 4) % UNITS;
     // Loads newer than this tile's rows: behind the prologue, whose rows come after all its weights, the later rows of it
     // and what the tiles so far have issued; then what the AHEAD - 1 tiles before have issued.  (Loads of scales are counted
     // only where they are sure to be among them.)
-    if (t < AHEAD) FMOE_WAIT_VM((U < AHEAD ? AHEAD - 1 - U : 0) * NAB + U * PER_TILE);   // uniform
-    else FMOE_WAIT_VM((AHEAD - 1) * PER_TILE);
+    constexpr int LATER = U < AHEAD ? AHEAD - 1 - U : 0;   // tiles requested behind this one, ahead of tile t - U
+    if constexpr (LAST) {
+      if (t < AHEAD) FMOE_WAIT_VM(LATER * NAB);   // uniform
+      else FMOE_WAIT_VM(LATER * PER_TILE);
+    } else {
+      if (t < AHEAD) FMOE_WAIT_VM(LATER * NAB + U * PER_TILE);
+      else FMOE_WAIT_VM((AHEAD - 1) * PER_TILE);
+    }
     block_barrier();   // every wavefront's share of the tile is in LDS; all are done with the tile before
     constexpr int off = U * (ROWS * SBK * 2);
     lds_issue_frags_at<PB, off>(frag_a0, fa[0]);
@@ -316,16 +325,16 @@ __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_til
         });
       });
     });
-    if constexpr (UNITS == 1 && U == 3) {
+    if constexpr (UNITS == 1 && U == 3 && !LAST) {
 #pragma unroll
       for (int j = 0; j < NCB; ++j) scales[0][j] = next_scales[j];
     }
   };
   int t0 = 0;
   for (; t0 + STAGES <= NT; t0 += STAGES)
-    static_for<0, STAGES>([&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
+    static_for<0, STAGES>([&](auto uc) { ktile(uc, std::false_type{}, t0 + decltype(uc)::value); });
   while_for<0, STAGES - 1>([&](auto uc) { return t0 + decltype(uc)::value < NT; },   // uniform
-                           [&](auto uc) { ktile(uc, t0 + decltype(uc)::value); });
+                           [&](auto uc) { ktile(uc, std::true_type{}, t0 + decltype(uc)::value); });
   FMOE_WAIT_VM(0);   // the loads issued past the end have landed before the ring is reused
   // the last matrix instructions have retired before hand-placed accumulators are read, see ffn.hip
   if constexpr (NAMED) asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");

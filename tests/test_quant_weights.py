@@ -405,6 +405,24 @@ def test_experts_of_more_than_one_wavefront_of_groups(E, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("K", [8, 24, 64, 72, 128, 192, 256, 264, 320, 384, 448, 520])
+def test_experts_of_many_tiles_with_short_reductions(K):
+    """Many experts of some tens of rows: either product with reductions of one to nine k tiles, against the bf16 kernels."""
+    rng = np.random.default_rng(K)
+    E, T, k = 256, 1300, 8
+    for d, F in ((K, 48), (56, K)):
+        layer = _Layer(rng, d, E, F, 1, F, k, k)
+        x, _ = _bf16(rng, T, d)
+        offsets, src = (torch.from_numpy(v).cuda() for v in _rows(rng, T, E, k, skew=0.8))
+        want, want_sh = layer.bf16.expert_ffn(x, None, T, offsets, src)
+        for shape in (0, 1, 2):
+            layer.m.set_ffn_shape(shape)
+            for _ in range(10):   # (a wait that is too short shows now and then)
+                y, ysh = layer.m.expert_ffn(x, None, T, offsets, src)
+                assert torch.equal(y, want) and torch.equal(ysh, want_sh), (d, F, shape)
+
+
+@pytest.mark.gpu
 def test_experts_of_row_lists_with_the_same_token_many_times():
     """Sixteen tokens, 32 rows of one expert: the form for a few tokens takes several turns; the row lists are the caller's."""
     rng = np.random.default_rng(55)
