@@ -134,7 +134,7 @@ int launch_pack_experts(fmoe_ctx* ctx, hipStream_t stream);
 // bytes of the packed 4-bit weights of matrix `which` (as above) and, if asked for, how many of them are codes
 size_t fmoe_quant_bytes(const fmoe_ctx* ctx, int which, size_t* codes);
 int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStream_t stream);
-enum quant_form { QUANT_THIN, QUANT_NARROW, QUANT_DENSE };   // (only the last one needs tile lists)
+enum quant_form { QUANT_THIN, QUANT_NARROW, QUANT_MIDDLE, QUANT_DENSE };   // (only the last one needs tile lists)
 quant_form quant_ffn_form(const fmoe_ctx* ctx, int n_cap);
 int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,
                   const int32_t* expert_offsets, const int32_t* perm_src, void* y, void* y_shared, char* base,

@@ -374,16 +374,16 @@ struct QuantListArgs {
   int E, n_cap, row_cap;
   int cols;                        // column units of an expert
   int shared_groups, shared_cols;  // shared groups in this launch, column units of one
+  int log2_bm;                     // rows of a row tile (narrow kernel)
 };
 struct QuantItem {
   int group, unit, row0, rows;     // group < 0: none
   bool shared;
 };
-// Row tiles of BM rows.  Experts whose offsets are malformed are skipped as in fmoe_build_tiles.  Uniform.
-template <int BM>
+// Row tiles of 1 << a.log2_bm rows.  Experts whose offsets are malformed are skipped as in fmoe_build_tiles.  Uniform.
 __device__ __forceinline__ QuantItem find_tile(const QuantListArgs& a, int block) {
   constexpr int Q = FMOE_MAX_EXPERTS / 64;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, bm = 1 << a.log2_bm;
   int r0[Q], cnt[Q], first[Q];   // of expert 64 q + lane: first row, rows, first tile
   int tiles = 0;
 #pragma unroll
@@ -400,13 +400,13 @@ __device__ __forceinline__ QuantItem find_tile(const QuantListArgs& a, int block
   for (int q = 0; q < Q; ++q) {
     const bool good = 64 * q + lane < a.E && r0[q] >= 0 && cnt[q] > r0[q] && cnt[q] <= a.row_cap;
     cnt[q] = good ? cnt[q] - r0[q] : 0;
-    const int nt = cnt[q] / BM + (cnt[q] % BM != 0);
+    const int nt = (cnt[q] + bm - 1) >> a.log2_bm;
     const int scan = wave_scan(nt);
     first[q] = tiles + scan - nt;
     tiles += __builtin_amdgcn_readlane(scan, 63);
   }
   const int n = resolve_count(a.n_cap, a.n_dev);
-  const int shared_tiles = n / BM + (n % BM != 0), per_group = shared_tiles * a.shared_cols;
+  const int shared_tiles = (n + bm - 1) >> a.log2_bm, per_group = shared_tiles * a.shared_cols;
   const int shared_items = per_group * a.shared_groups;
   const int items = shared_items + tiles * a.cols, share = (items + 7) >> 3;
   QuantItem it{-1, 0, 0, 0, false};
@@ -418,15 +418,15 @@ __device__ __forceinline__ QuantItem find_tile(const QuantListArgs& a, int block
     it.group = g / per_group;
     g -= it.group * per_group;
     it.unit = g / shared_tiles;
-    it.row0 = (g - it.unit * shared_tiles) * BM;
-    it.rows = n - it.row0 < BM ? n - it.row0 : BM;
+    it.row0 = (g - it.unit * shared_tiles) * bm;
+    it.rows = n - it.row0 < bm ? n - it.row0 : bm;
     return it;
   }
   g -= shared_items;
   const int tile = g / a.cols;
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
-    const int nt = cnt[q] / BM + (cnt[q] % BM != 0);
+    const int nt = (cnt[q] + bm - 1) >> a.log2_bm;
     const unsigned long long mine = __ballot(first[q] <= tile && tile < first[q] + nt);
     if (mine != 0) {   // in one q only
       const int at = __ffsll((long long)mine) - 1;
@@ -435,9 +435,9 @@ __device__ __forceinline__ QuantItem find_tile(const QuantListArgs& a, int block
       g -= e_first * a.cols;
       it.group = 64 * q + at;
       it.unit = g / e_tiles;
-      const int row = (g - it.unit * e_tiles) * BM;
+      const int row = (g - it.unit * e_tiles) * bm;
       it.row0 = __builtin_amdgcn_readlane(r0[q], at) + row;
-      it.rows = e_rows - row < BM ? e_rows - row : BM;
+      it.rows = e_rows - row < bm ? e_rows - row : bm;
     }
   }
   return it;
@@ -504,20 +504,25 @@ __global__ __launch_bounds__(64, 2) void ffn_quant_thin_kernel(QuantListArgs a) 
     thin_quant_tile<SWIGLU>(Q, it.row0 + done, it.rows - done < THIN_ROWS ? it.rows - done : THIN_ROWS, it.group, it.unit);
 }
 
-// Row tiles of 32 and one column tile, seven k tiles ahead, four workgroups a CU, for a few rows an expert, where the weights
-// have to be on their way in great numbers.
-constexpr int NARROW_ROWS = 32, NARROW_STAGES = 8;
+// One column tile and four workgroups a CU, for a few rows an expert, where the weights have to be on their way in great
+// numbers.  Row tiles of 32, seven k tiles ahead; or of 64: those of more than 32 rows in the same ring as stages twice as
+// large, three ahead, so that an expert's weights are read and converted once and not twice.
+constexpr int NARROW_ROWS = 32, MIDDLE_ROWS = 64, NARROW_STAGES = 8;
 template <bool SWIGLU>
 __global__ __launch_bounds__(256, 4) void ffn_quant_narrow_kernel(QuantListArgs a) {
   __shared__ __align__(16) bf16_t As[NARROW_STAGES * NARROW_ROWS * SBK];
-  const QuantItem it = find_tile<NARROW_ROWS>(a, (int)blockIdx.x);
+  const QuantItem it = find_tile(a, (int)blockIdx.x);
   if (it.group < 0) return;
   const QuantProblem Q = item_problem(a, it.shared, it.group);
   fmoe_tile tile{};
   tile.row0 = it.row0;
   tile.rows = it.rows;
-  if (it.rows <= 16) quant_tile<SWIGLU, 1, 1, NARROW_STAGES, NARROW_ROWS, true>(Q, tile, it.group, it.unit, it.unit + 1, As);   // uniform
-  else quant_tile<SWIGLU, 1, 1, NARROW_STAGES, NARROW_ROWS>(Q, tile, it.group, it.unit, it.unit + 1, As);
+  if (it.rows <= 16)   // uniform
+    quant_tile<SWIGLU, 1, 1, NARROW_STAGES, NARROW_ROWS, true>(Q, tile, it.group, it.unit, it.unit + 1, As);
+  else if (it.rows <= NARROW_ROWS)
+    quant_tile<SWIGLU, 1, 1, NARROW_STAGES, NARROW_ROWS>(Q, tile, it.group, it.unit, it.unit + 1, As);
+  else
+    quant_tile<SWIGLU, 2, 1, NARROW_STAGES / 2, MIDDLE_ROWS>(Q, tile, it.group, it.unit, it.unit + 1, As);
 }
 
 // Tiles of 128 rows and two column tiles, dealt out as deal.h says; column tiles are taken two at a time (a.cols = such pairs
@@ -644,7 +649,8 @@ int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStrea
   return FMOE_OK;
 }
 
-// Which form a call takes, by what it can route (capacities).  All times: us, gate/up and down, weights from memory.
+// Which form a call takes, by what it can route (capacities).  All times: us, gate/up and down, weights from memory;
+// "2048, 64 of 1408": d_model, experts, their hidden size.
 //  * Thin for at most THIN_ROWS tokens (no expert has more rows) that touch up to so many bytes of weights: a wavefront an
 //    item and no LDS, the shortest way from launch to result; with more to stream, the narrow form has more on its way.
 //    Thin / narrow: d 2048, 64 experts of 1408 and two shared (5 MB an expert) one token 14 / 18, 3 tokens 25 / 26, 4 tokens
@@ -657,23 +663,34 @@ int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStrea
 //    50 rows 117 / 141, 100 rows 182 / 180, 200 rows 309 / 256; d 512, 256 of 512 50 rows 63 / 68, 100 rows 94 / 85; with
 //    few items d 4096, 8 of 1536 150 rows (204 items) 67 / 78, 300 rows (312) 117 / 119, 600 rows (540) 207 / 194; d 1288,
 //    16 of 904, one shared 150 rows (204) 47 / 51, 300 rows (318) 81 / 74.
+//  * Of the forms with one column tile, tiles of 64 rows from so many rows an expert on, if those also are items enough (rows
+//    that the call can have, in tiles of 64, times column tiles of the narrower GEMM).  32 / 64: 2048, 64 of 1408, two shared 9
+//    rows 66 / 66, 28 rows 94 / 91, 47 rows 121 / 113; 1280, 64 of 896, two shared 19 rows 42 / 42, 39 rows 55 / 54, 56 rows
+//    66 / 64; 512, 256 of 512 16 rows 40 / 38, 47 rows 60 / 54; 128 of 768 50 rows 119 / 113; with few items 4096, 8 of 1536 37
+//    rows (288) 42 / 47, 50 rows (336) 51 / 50, 62 rows (360) 54 / 51, 100 rows (480) 71 / 67; 1288, 16 of 904, one shared 50
+//    rows (308) 24 / 26, 62 rows (341) 26 / 27.
 constexpr size_t QUANT_THIN_BYTES = 112u << 20;
 constexpr long long QUANT_DENSE_ROWS = 64;
 constexpr long long QUANT_DENSE_ITEMS = 300;
+constexpr long long QUANT_MIDDLE_ROWS = 16;
+constexpr long long QUANT_MIDDLE_ITEMS = 350;
 quant_form quant_ffn_form(const fmoe_ctx* ctx, int n_cap) {
   const fmoe_config& c = ctx->cfg;
-  if (ctx->ffn_shape == 1) return QUANT_NARROW;
   if (ctx->ffn_shape == 2) return QUANT_DENSE;
+  const bool few = ctx->ffn_shape == 1;
   const long long rows = (long long)n_cap * ctx->kmax, experts = rows < c.n_experts ? rows : c.n_experts;
-  if (n_cap <= THIN_ROWS) {
+  if (!few && n_cap <= THIN_ROWS) {
     const size_t expert = (fmoe_quant_bytes(ctx, 0, nullptr) + fmoe_quant_bytes(ctx, 1, nullptr)) / c.n_experts;
     const size_t shared = fmoe_quant_bytes(ctx, 2, nullptr) + fmoe_quant_bytes(ctx, 3, nullptr);
     return (size_t)experts * expert + shared <= QUANT_THIN_BYTES ? QUANT_THIN : QUANT_NARROW;
   }
-  if (rows < QUANT_DENSE_ROWS * c.n_experts) return QUANT_NARROW;
-  const int pairs1 = (c.d_ffn + 127) / 128, pairs2 = (c.d_model + 255) / 256;
-  const long long items = (experts + rows / SBM) * (pairs1 < pairs2 ? pairs1 : pairs2);
-  return items >= QUANT_DENSE_ITEMS ? QUANT_DENSE : QUANT_NARROW;
+  const int tiles1 = (c.d_ffn + 63) / 64, tiles2 = (c.d_model + 127) / 128, pairs1 = (tiles1 + 1) / 2, pairs2 = (tiles2 + 1) / 2;
+  if (!few && rows >= QUANT_DENSE_ROWS * c.n_experts &&
+      (experts + rows / SBM) * (pairs1 < pairs2 ? pairs1 : pairs2) >= QUANT_DENSE_ITEMS)
+    return QUANT_DENSE;
+  return rows >= QUANT_MIDDLE_ROWS * c.n_experts &&
+                 (experts + rows / MIDDLE_ROWS) * (tiles1 < tiles2 ? tiles1 : tiles2) >= QUANT_MIDDLE_ITEMS
+             ? QUANT_MIDDLE : QUANT_NARROW;
 }
 
 int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,
@@ -733,15 +750,17 @@ int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, i
     }
     // column units: column blocks in the thin form, tiles of four in the narrow one
     const bool thin = form == QUANT_THIN;
-    const int bm = thin ? FMOE_MAX_EXPERTS * THIN_ROWS : NARROW_ROWS;   // (more rows than a thin call has)
-    QuantListArgs h{g.p0, g.p1, expert_offsets, n_dev, E, n_cap, row_cap, 0, 0, 0};
+    const int log2_bm = form == QUANT_MIDDLE ? 6 : 5;
+    static_assert(MIDDLE_ROWS == 1 << 6 && NARROW_ROWS == 1 << 5, "rows of a tile");
+    QuantListArgs h{g.p0, g.p1, expert_offsets, n_dev, E, n_cap, row_cap, 0, 0, 0, log2_bm};
     h.cols = thin ? g.p0.s.nbw : (g.p0.s.nbw + 3) / 4;
     if (Ft > 0) {
       h.shared_groups = S ? 1 : c.n_shared;
       h.shared_cols = thin ? g.p1.s.nbw : (g.p1.s.nbw + 3) / 4;
     }
-    const long long tiles = (row_cap < E ? row_cap : E) + row_cap / bm;   // that the routed experts can have
-    const long long items = tiles * h.cols + (long long)((n_cap + bm - 1) / bm) * h.shared_cols * h.shared_groups;
+    const long long tiles = (row_cap < E ? row_cap : E) + (thin ? 0 : row_cap >> log2_bm);   // that the routed experts can have
+    const long long shared_tiles = thin ? n_cap > 0 : ((long long)n_cap + (1 << log2_bm) - 1) >> log2_bm;
+    const long long items = tiles * h.cols + shared_tiles * h.shared_cols * h.shared_groups;
     if (items == 0) return;
     const unsigned blocks = (unsigned)((items + 7) / 8 * 8);
     if (thin) hipLaunchKernelGGL(ffn_quant_thin_kernel<S>, dim3(blocks), dim3(64), 0, stream, h);
