@@ -4,7 +4,9 @@
 // A weight is a bf16 number exactly, so the products are those of the bf16 kernels: a wavefront turns eight codes into an
 // operand of v_mfma_f32_16x16x32_bf16 by four conversion instructions that apply the scale as well, and the matrix
 // instruction does the rest, in the same order of k.  A context with 4-bit weights gives the same bits as a bf16 context
-// that is given the dequantized ones.
+// that is given the dequantized ones.  So h = silu(gate) * up is rounded to bf16 on its way to the down product, as there: the
+// outputs are 0.0024 of their size from the 64-bit ones where their own rounding makes 0.0017.  Two bf16 parts of h would keep
+// it, for twice the matrix instructions of the down product and other bits than a bf16 context.
 //
 // Packing (fmoe_set_weights_quant, matrix-core operand order as in ffn.hip): of a column block (16 features, gate and up;
 // or 32 output features) and a k tile of 64, lane l has one 16-byte unit: word 2s + f = the eight codes of k step s and
@@ -48,7 +50,9 @@ __device__ __forceinline__ u32x4_t dequantize(uint32_t codes, uint32_t scales) {
 
 // One wavefront, one column block, sixteen rows: codes, scales and rows straight into registers in matrix order, no LDS and
 // no barrier, for calls of at most THIN_ROWS tokens, where the weights are all there is to move.  Rows past the tile reuse
-// its last one, row indices are clamped as in gather_offsets.
+// its last one, row indices are clamped as in gather_offsets.  Bound: in each of the two launches a chain of latencies (offsets,
+// row indices, rows and the first weights), then the weights.  d 2048, 64 experts of 1408 and two shared, one token: 8.0 + 5.6
+// us for 36 MB.
 constexpr int THIN_ROWS = 16;
 constexpr int THIN_SLOTS = 8;    // k tiles (64 wide) of codes in flight
 constexpr int THIN_A_SLOTS = 8;   // and of rows, which come from L2
@@ -166,8 +170,8 @@ __device__ __forceinline__ void while_for(C&& c, F&& f) {   // static_for that e
 // One work item of a workgroup: a tile of rows (NAB live bands of 32, LDS stages of ROWS) times NCB column tiles, column block
 // w of each for wavefront w.  Rows go through a ring of LDS stages as in ffn.hip; codes and scales into registers, all as
 // many k tiles ahead; a k tile is one barrier.  Every load of the loop is unconditional (past the end the last tile
-// again), so the number of loads in flight at a wait is a compile-time constant.  Row blocks are taken two at a time, the next pair's operands
-// requested from LDS before the present pair's products.  HALF: of the only band the first 16 rows.
+// again), so the number of loads in flight at a wait is a compile-time constant.  Row blocks are taken two at a time, the next
+// pair's operands requested from LDS before the present pair's products.  HALF: of the only band the first 16 rows.
 template <bool SWIGLU, int NAB, int NCB, int STAGES, int ROWS, bool HALF = false>
 __device__ __forceinline__ void quant_tile(const QuantProblem& Q, const fmoe_tile& tile, int group, int ct0, int ct_limit,
                                            bf16_t* As) {
@@ -506,7 +510,9 @@ __global__ __launch_bounds__(64, 2) void ffn_quant_thin_kernel(QuantListArgs a) 
 
 // One column tile and four workgroups a CU, for a few rows an expert, where the weights have to be on their way in great
 // numbers.  Row tiles of 32, seven k tiles ahead; or of 64: those of more than 32 rows in the same ring as stages twice as
-// large, three ahead, so that an expert's weights are read and converted once and not twice.
+// large, three ahead, so that an expert's weights are read and converted once and not twice.  Bound: the weights for a row or
+// two an expert (d 2048, 64 experts of 1408 and two shared, 8 tokens: 15.7 + 10.8 us for 111 MB, 4.2 TB/s), from some ten on the
+// issue of conversions and matrix instructions (d 1280, 64 of 896, two shared, 416 tokens: 27.7 + 17.0 us; the weights: 25).
 constexpr int NARROW_ROWS = 32, MIDDLE_ROWS = 64, NARROW_STAGES = 8;
 template <bool SWIGLU>
 __global__ __launch_bounds__(256, 4) void ffn_quant_narrow_kernel(QuantListArgs a) {
@@ -526,7 +532,9 @@ __global__ __launch_bounds__(256, 4) void ffn_quant_narrow_kernel(QuantListArgs 
 }
 
 // Tiles of 128 rows and two column tiles, dealt out as deal.h says; column tiles are taken two at a time (a.cols = such pairs
-// per tile entry).  (The build looks at the registers of a kernel of this name.)
+// per tile entry).  Bound: the matrix instructions, at the rate of a large library product (4096 tokens, d 2048, 64 experts of
+// 1408 and two shared: 208 + 119 us, 1146 TFLOP/s over both and the lists; a product of 8192^3 1158).  (The build looks at the
+// registers of a kernel of this name.)
 template <bool SWIGLU>
 __global__ __launch_bounds__(256, 2) void ffn_quant_dense_kernel(QuantArgs a) {
   __shared__ __align__(16) bf16_t As[4 * SBM * SBK];
@@ -694,7 +702,8 @@ quant_form quant_ffn_form(const fmoe_ctx* ctx, int n_cap) {
 }
 
 int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,
-                  const int32_t* expert_offsets, const int32_t* perm_src, void* y, void* y_shared, char* base, const fmoe_ws_layout& L, const fmoe_ffn_geom& geo, hipStream_t stream) {
+                  const int32_t* expert_offsets, const int32_t* perm_src, void* y, void* y_shared, char* base,
+                  const fmoe_ws_layout& L, const fmoe_ffn_geom& geo, hipStream_t stream) {
   const fmoe_config& c = ctx->cfg;
   const int d = c.d_model, E = c.n_experts, F = c.d_ffn;
   const int Ft = c.n_shared * c.d_ffn_shared;
