@@ -661,24 +661,28 @@ int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStrea
 // "2048, 64 of 1408": d_model, experts, their hidden size.
 //  * Thin for at most THIN_ROWS tokens (no expert has more rows) that touch up to so many bytes of weights: a wavefront an
 //    item and no LDS, the shortest way from launch to result; with more to stream, the narrow form has more on its way.
-//    Thin / narrow: d 2048, 64 experts of 1408 and two shared (5 MB an expert) one token 14 / 18, 3 tokens 25 / 26, 4 tokens
-//    28 / 28, 8 tokens 38 / 36; 128 of 768 one token 12 / 16, 4 tokens 21 / 22, 6 tokens 28 / 27; d 1280, 64 of 896, two
-//    shared one token 11 / 14, 8 tokens 17 / 19; d 4096, 8 of 1536 one token 16 / 21, 16 tokens 22 / 24.
-//  * Dense from so many rows an expert on, if there also are so many items that the chip is busy with them: row tiles the
-//    call can have (one of every expert with rows, and the further ones) times pairs of column tiles of the narrower GEMM.
-//    Narrow / dense: d 2048, 64 experts of 1408 and two shared, 19 rows an expert 77 / 80, 56 rows 131 / 134, 100 rows 193 /
-//    184, 150 rows 266 / 230; d 1280, 64 of 896, two shared 39 rows 54 / 55, 75 rows 78 / 74, 150 rows 129 / 111; 128 of 768
-//    50 rows 117 / 141, 100 rows 182 / 180, 200 rows 309 / 256; d 512, 256 of 512 50 rows 63 / 68, 100 rows 94 / 85; with
-//    few items d 4096, 8 of 1536 150 rows (204 items) 67 / 78, 300 rows (312) 117 / 119, 600 rows (540) 207 / 194; d 1288,
-//    16 of 904, one shared 150 rows (204) 47 / 51, 300 rows (318) 81 / 74.
+//    Thin / narrow (MB: what the rule counts): 2048, 64 of 1408 and two shared one token 13.4 / 16.9 (37), 2 tokens 19.4 / 21.0
+//    (64), 3 tokens 24.6 / 24.9 (92), 4 tokens 28 / 28 (119); 128 of 768 one token 12.5 / 15.2 (20), 4
+//    tokens 21.1 / 21.4 (80), 5 tokens 25.3 / 24.3 (100); 1280, 64 of 896, two shared 4 tokens 13.9 / 15.8 (48), 8 tokens 16.8 / 18.3
+//    (92); 4096, 8 of 1536, one shared one token 15.5 / 20.6 (30), 8 tokens 24.2 / 25.1 and 16 tokens 27.6 / 25.8 (90).
+//  * Dense from so many rows an expert, so much work (rows times weights of a matrix: what it gains has to make up for its
+//    launch that builds lists and for two workgroups a CU instead of four) and so many items on, row tiles the call can have
+//    (one of every expert with rows, and the further ones) times pairs of column tiles of the narrower GEMM.  Tiles of 64 /
+//    dense (10^9 rows times weights): 2048, 64 of 1408 and two shared 100 rows an expert 165 / 180 (18), 150 rows 226 / 228 (28),
+//    200 rows 285 / 272 (37); 128 of 768 150 rows 205 / 215 (30), 200 rows 256 / 251 (40); 2560, 72 of 1536 125 rows 297 / 296
+//    (35), 158 rows 363 / 340 (45); with less work 1280, 64 of 896, two shared 169 rows 117 / 124 (12), 200 rows 130 / 132 (15),
+//    244 rows 154 / 147 (18); 512, 256 of 512 200 rows 119 / 130 (13), 300 rows 166 / 165 (20); 768, 64 of 768 250 rows 76 / 78 (9),
+//    500 rows 130 / 127 (19); 4096, 8 of 1536 225 rows 109 / 122 (11), 375 rows 162 / 155 (19); 1288, 16 of 904 400 rows 71 / 82
+//    (7), 800 rows 139 / 135 (15), 1200 rows 209 / 182 (22).
 //  * Of the forms with one column tile, tiles of 64 rows from so many rows an expert on, if those also are items enough (rows
 //    that the call can have, in tiles of 64, times column tiles of the narrower GEMM).  32 / 64: 2048, 64 of 1408, two shared 9
 //    rows 66 / 66, 28 rows 94 / 91, 47 rows 121 / 113; 1280, 64 of 896, two shared 19 rows 42 / 42, 39 rows 55 / 54, 56 rows
 //    66 / 64; 512, 256 of 512 16 rows 40 / 38, 47 rows 60 / 54; 128 of 768 50 rows 119 / 113; with few items 4096, 8 of 1536 37
 //    rows (288) 42 / 47, 50 rows (336) 51 / 50, 62 rows (360) 54 / 51, 100 rows (480) 71 / 67; 1288, 16 of 904, one shared 50
 //    rows (308) 24 / 26, 62 rows (341) 26 / 27.
-constexpr size_t QUANT_THIN_BYTES = 112u << 20;
-constexpr long long QUANT_DENSE_ROWS = 64;
+constexpr size_t QUANT_THIN_BYTES = 92u << 20;
+constexpr long long QUANT_DENSE_ROWS = 150;
+constexpr long long QUANT_DENSE_WORK = 16000000000;
 constexpr long long QUANT_DENSE_ITEMS = 300;
 constexpr long long QUANT_MIDDLE_ROWS = 16;
 constexpr long long QUANT_MIDDLE_ITEMS = 350;
@@ -693,7 +697,7 @@ quant_form quant_ffn_form(const fmoe_ctx* ctx, int n_cap) {
     return (size_t)experts * expert + shared <= QUANT_THIN_BYTES ? QUANT_THIN : QUANT_NARROW;
   }
   const int tiles1 = (c.d_ffn + 63) / 64, tiles2 = (c.d_model + 127) / 128, pairs1 = (tiles1 + 1) / 2, pairs2 = (tiles2 + 1) / 2;
-  if (!few && rows >= QUANT_DENSE_ROWS * c.n_experts &&
+  if (!few && rows >= QUANT_DENSE_ROWS * c.n_experts && (double)rows * c.d_model * c.d_ffn >= QUANT_DENSE_WORK &&
       (experts + rows / SBM) * (pairs1 < pairs2 ? pairs1 : pairs2) >= QUANT_DENSE_ITEMS)
     return QUANT_DENSE;
   return rows >= QUANT_MIDDLE_ROWS * c.n_experts &&
