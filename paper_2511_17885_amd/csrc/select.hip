@@ -537,9 +537,18 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
         steps = (int)fminf(off * (0x1p23f / KEY_RANGE), 1e6f) + 3;
       }
     const bool none = peak == -INFINITY;   // nothing to choose from
-    const bool sorted = apart(entry, rest, k, rounds, j, steps) | none;
+    bool sorted = apart(entry, rest, k, rounds, j, steps) | none;
     // do the entries hold the list for certain?  Their integers then are in range, and the k-th is apart from the rest
-    const bool held = (j != k - 1) | (((entry >> 8) > 0) & ((entry >> 8) - (rest >> 8) > steps));
+    bool held = (j != k - 1) | (((entry >> 8) > 0) & ((entry >> 8) - (rest >> 8) > steps));
+    if (__any(!held & ((entry >> 8) == 0) & !none)) {   // uniform
+      // no k-th entry in range: the list is complete if what is not in range is masked
+      bool lost = false;
+#pragma unroll
+      for (int r = 0; r < N; ++r) lost |= (order[r] > -INFINITY) & (peak - order[r] > 0.99f * range);
+      const bool complete = ((__ballot(lost) >> (threadIdx.x & 48)) & 0xffffu) == 0;
+      held |= complete & ((entry >> 8) == 0);
+      sorted |= complete & ((entry >> 8) == 0);
+    }
     const bool sure = (held & (fabsf(peak) < 8.0f * range)) | none;
     if (none) mine = -1;
     if (__any(!sorted & sure)) {   // uniform

@@ -307,6 +307,29 @@ def test_select_large_logits():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("E", [40, 100, 256])
+def test_select_fewer_usable_experts_than_are_asked_for(E, with_bias):
+    """Rows with none to ten usable experts of which eight are asked for, near, equal and further apart than integers span."""
+    rng = np.random.default_rng(E)
+    z = np.full((66, E), -np.inf, np.float32)
+    for t in range(66):
+        n = t % 11
+        where = rng.choice(E, size=n, replace=False)
+        kind = t // 11
+        values = rng.standard_normal(n) * (1.0, 1e-6, 0.0, 40.0, 400.0, 1e5)[kind]
+        z[t, where] = values.astype(np.float32)
+    bias = rng.choice([-9.0, -3.9, -4.1, 0.0, 0.1], size=E).astype(np.float32) if with_bias else None
+    for sigmoid in (False, True):
+        for groups, topk in ((1, 1), (4, 2)):
+            cfg = _cfg(E, 8, 8, sigmoid=sigmoid, groups=groups, topk_groups=topk)
+            idx, gate = _context(cfg).select_experts(_params(cfg), _gpu(z), None, _gpu(bias))[1:]
+            want = _reference(z, None, bias, cfg)[1]
+            assert np.array_equal(idx.cpu().numpy(), want), (sigmoid, groups)
+            assert (gate.cpu().numpy()[want < 0] == 0).all()
+
+
+@pytest.mark.gpu
 def test_select_many_rows_and_replay():
     """More rows than blocks run at once; the same from a captured graph, three times, with other work between."""
     T, cfg = 40000, _cfg(256, 8, 4, sigmoid=True, groups=8, topk_groups=4, group_score=1, scale=2.5)
