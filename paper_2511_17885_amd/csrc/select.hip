@@ -387,13 +387,17 @@ __device__ __forceinline__ int list_packed(int rounds, int j, int (&s)[N], int& 
 __device__ __forceinline__ int unpack_expert(int packed) { return packed < 0 ? -1 : 255 - (packed & 255); }
 __device__ __forceinline__ int masked_below_zero(int packed, float order) { return packed | (order > -INFINITY ? 0 : NONE); }
 
-// Key and expert in one integer: the distance to the row's largest key `top` in 2^23 steps over RANGE, then the expert, lower
-// ones larger.  Keys further below than RANGE, and masked ones, have no steps.
+// Key and expert in one integer: the distance to the row's largest key `top` in steps, KEY_STEPS over RANGE, then the expert,
+// lower ones larger.  Keys further below than RANGE, and masked ones, have no steps.
+// The largest key has to stay below 2^23 steps, or its integer is negative.  For |top| below 8 ranges, range - top is below 9
+// ranges and off by at most 2^-24 of itself, 4.5 steps; the product with the scale (which is exact in either range) by as much;
+// the fused sum by half a step: at most KEY_STEPS + 9.5 (8 at every such number), and the key has 32 to spare.
 constexpr float KEY_RANGE = 4.0f;      // of scores (0 .. 1) with a bias
 constexpr float LOGIT_RANGE = 64.0f;
+constexpr float KEY_STEPS = 0x1p23f - 32.0f;
 template <int N>
 __device__ __forceinline__ void pack_below(const float (&order)[N], float top, float range, int j, int (&s)[N]) {
-  const float scale = 8388600.0f / range, offset = (range - top) * scale;   // (the largest stays below 2^23)
+  const float scale = KEY_STEPS / range, offset = (range - top) * scale;
   const int lane_part = (15 - j) * 4;
 #pragma unroll
   for (int r = 0; r < N; ++r) {
@@ -529,7 +533,7 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
     mine = (entry >> 8) > 0 ? unpack_expert(entry) : -1;   // (without steps: masked, or further below than all in range)
     // The way from key to integer is monotonic, so logits whose integers differ are in order.  Two scored keys can be off by
     // `slack` and half a rounding each, and their integers lose less than two steps more.  (The offset's rounding is the same
-    // for all; while the peak is below 8 ranges it is within what is left between the largest integer and 2^23.)
+    // for all, and while the peak is below 8 ranges the largest integer stays below 2^23: KEY_STEPS.)
     int steps = 0;
     if constexpr (KEYED)
       if (scored) {

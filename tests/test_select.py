@@ -534,6 +534,80 @@ def test_select_backward_of_lists_that_were_not_chosen_here():
                 assert (np.abs(got[t] - want) <= _backward_bound(_clean(z[t]), d_gate[t], None, cfg)).all(), t
 
 
+# ------------------------------------------------------------------------- row maxima of any size, rows beside each other
+
+
+def _lists(z, bias, cfg):
+    """Lists [T, kmax] of rows without masked logits, all of them at once: the definition by stable sorts in 64 bits."""
+    z = z.astype(np.float64)
+    T, E = z.shape
+    if cfg["sigmoid"]:
+        s = 1.0 / (1.0 + np.exp(-z))
+    else:
+        s = np.exp(z - z.max(1, keepdims=True))
+        s = s / s.sum(1, keepdims=True)
+    key = z if bias is None else s + bias.astype(np.float64)
+    if cfg["groups"] > 1:
+        members = (s if bias is None and cfg["group_score"] else key).reshape(T, cfg["groups"], -1)
+        score = np.sort(members, axis=2)[:, :, -2:].sum(2) if cfg["group_score"] else members.max(2)
+        best = np.argsort(-score, axis=1, kind="stable")[:, :cfg["topk_groups"]]
+        stays = np.zeros(score.shape, bool)
+        np.put_along_axis(stays, best, True, 1)
+        key = np.where(np.repeat(stays, E // cfg["groups"], axis=1), key, -np.inf)
+    return np.argsort(-key, axis=1, kind="stable")[:, :cfg["kmax"]].astype(np.int32)
+
+
+def _maxima(reach):
+    """fp32 numbers between -reach and reach: evenly spread, 300 neighbours at either side of every place where reach / 8
+    less the number comes to another binade, and neighbours all through the last sixteenth below."""
+    half = np.float32(reach)
+    parts = [np.linspace(-reach, reach, 6000).astype(np.float32),
+             np.linspace(-reach, -reach * 15 / 16, 2000).astype(np.float32)]
+    for n in range(-3, 4):
+        edge = np.float32(reach / 8 * (1 - 2.0 ** n))
+        bits = np.arange(-300, 300) * np.spacing(np.abs(edge) + np.float32(1e-3))
+        parts.append((edge + bits).astype(np.float32))
+    for at in (-reach * 239.5 / 256, -reach * 239.004 / 256):
+        parts.append((np.float32(at) + np.arange(64) * np.spacing(half / 2)).astype(np.float32))
+    return np.concatenate(parts)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group_score", [0, 1])
+@pytest.mark.parametrize("groups", [1, 8])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_select_row_maxima_of_any_size(dtype, groups, group_score):
+    """The list compares keys by their distance to the row's largest: rows whose largest logit is any number from -512 to 512
+    and beyond, on and beside the places where that distance is rounded to another step."""
+    rng = np.random.default_rng(groups)
+    top = np.concatenate([_maxima(512.0), np.linspace(-700, 700, 500).astype(np.float32)])
+    z = (top[:, None] - 3.0 * rng.random((len(top), 64))).astype(np.float32)
+    z[np.arange(len(top)), rng.integers(0, 64, size=len(top))] = top
+    if dtype == "bf16":
+        z = torch.from_numpy(z).to(torch.bfloat16).float().numpy()
+    for sigmoid in (False, True):
+        cfg = _cfg(64, 6, 6, sigmoid=sigmoid, groups=groups, topk_groups=max(1, groups // 2), group_score=group_score)
+        idx = _context(cfg).select_experts(_params(cfg), _gpu(z, torch.bfloat16 if dtype == "bf16" else None))[1].cpu().numpy()
+        wrong = (idx != _lists(z, None, cfg)).any(1)
+        assert not wrong.any(), (sigmoid, int(wrong.sum()), top[wrong][:5])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups", [1, 8])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_select_biased_maxima_of_any_size(sigmoid, groups):
+    """The same for keys with a bias, whose size is the bias's: from -32 to 32 and beyond, closely from -31 to -29."""
+    rng = np.random.default_rng(5 + groups)
+    z = rng.standard_normal((400, 64)).astype(np.float32)
+    cfg = _cfg(64, 6, 6, sigmoid=sigmoid, groups=groups, topk_groups=max(1, groups // 2), group_score=1)
+    m, p, zg = _context(cfg), _params(cfg), _gpu(z)
+    for size in np.concatenate([np.linspace(-40.0, 40.0, 81), np.linspace(-31.0, -29.0, 81), [4 - 2.0 ** n for n in range(-2, 6)]]):
+        bias = (size + 0.01 * rng.standard_normal(64)).astype(np.float32)
+        idx = m.select_experts(p, zg, None, _gpu(bias))[1].cpu().numpy()
+        wrong = (idx != _lists(z, bias, cfg)).any(1)
+        assert not wrong.any(), (size, int(wrong.sum()))
+
+
 # --------------------------------------------------------------------------------------------------------- refusals
 
 
