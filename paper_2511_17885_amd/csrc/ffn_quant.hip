@@ -460,6 +460,7 @@ __device__ __forceinline__ QuantItem find_expert(const QuantListArgs& a, int ite
     it.rows = resolve_count(a.n_cap, a.n_dev);
     return it;
   }
+  if (a.row_cap == 0) return it;                // a launch is whole eights of workgroups, the offsets may be null
   int ahead = (item - shared_items) / a.cols;   // experts with rows ahead of this item's
   it.unit = item - shared_items - ahead * a.cols;
   int r0[Q], r1[Q];

@@ -440,6 +440,31 @@ def test_experts_of_row_lists_with_the_same_token_many_times():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 5, 16, 17, 200])
+@pytest.mark.parametrize("d,shared,F_shared", [(72, 1, 40), (136, 2, 40), (264, 3, 136), (8, 1, 8)])
+def test_shared_experts_alone_need_no_offsets(T, d, shared, F_shared):
+    """No expert is listed (k 0): offsets, rows and y may be null.  The shared experts' column units (3 and 3, 5 and 10, 26 and
+    27, 1 and 1 in the two products) are not whole eights, as a launch's workgroups are."""
+    rng = np.random.default_rng(T + d)
+    layer = _Layer(rng, d, 4, 32, shared, F_shared, 0, 0)
+    x, x64 = _bf16(rng, T, d)
+    _, want = layer.bf16.expert_ffn(x, None, T, None, None)
+    lib, m = binding.load(), layer.m
+    p = lambda t: C.c_void_p(t.data_ptr())  # noqa: E731
+    for shape in (0, 1, 2):
+        m.set_ffn_shape(shape)
+        assert torch.equal(m.expert_ffn(x, None, T, None, None)[1], want), shape
+        out = torch.full((shared, T, d), 9.0, dtype=torch.bfloat16, device="cuda")
+        ws = m.workspace(T, 1)
+        assert lib.fmoe_expert_ffn(m._ctx, p(x), None, T, None, None, None, None, p(out), p(ws), ws.numel(),
+                                   C.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+        assert torch.equal(out, want), shape
+    for i in range(shared):
+        want64, bound = _ffn(x64, *[w[i] for w in layer.w[3:]])
+        assert (np.abs(want[i].double().cpu().numpy() - want64) <= bound).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [8, 120])
 def test_experts_with_malformed_offsets_are_left_out(T):
     """Offsets below 0, past the room for rows or descending: the expert has no rows, the others are what they are."""
