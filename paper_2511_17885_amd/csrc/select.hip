@@ -578,13 +578,16 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
   const float zl = mine >= 0 ? clean(to_f32(logits[(size_t)t * a.E + mine])) : -INFINITY;
   float g;
   if (a.renorm) {
-    float p;
-    if (SIGMOID && !__any(mine >= 0 && zl < -60.0f)) {   // no score underflows: shares of the scores themselves
-      p = mine >= 0 ? 1.0f / (1.0f + expf(-zl)) : 0.0f;
-    } else {
+    // Sigmoid: shares of the scores themselves where none of the token's own underflows.  (By its own logits, so that its
+    // gates are the same whatever tokens are beside it.)
+    const unsigned long long low = SIGMOID ? __ballot(mine >= 0 && zl < -60.0f) : ~0ull;
+    float p = 0.0f;
+    if (SIGMOID) p = mine >= 0 ? 1.0f / (1.0f + expf(-zl)) : 0.0f;
+    if (low != 0) {   // uniform
       const float l = mine >= 0 ? (SIGMOID ? log_sigmoid(zl) : zl) : -INFINITY;
       const float lm = row_top(l);
-      p = mine >= 0 ? expf(l - lm) : 0.0f;
+      const float shifted = mine >= 0 ? expf(l - lm) : 0.0f;
+      p = ((low >> (threadIdx.x & 48)) & 0xffffu) != 0 ? shifted : p;
     }
     const float sum = row_sum_butterfly(p);   // (every lane takes part)
     g = mine >= 0 ? p / sum : 0.0f;

@@ -608,6 +608,35 @@ def test_select_biased_maxima_of_any_size(sigmoid, groups):
         assert not wrong.any(), (size, int(wrong.sum()))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_select_of_a_row_does_not_depend_on_the_rows_beside_it(sigmoid, renorm):
+    """Rows alone, and each beside rows whose scores underflow, whose logits are all masked, or whose keys are equal: the same
+    bits; so is the gradient."""
+    rng = np.random.default_rng(6)
+    E, T = 64, 45
+    z = (3.0 * rng.standard_normal((T, E))).astype(np.float32)
+    low = (rng.standard_normal((T, E)) - 70.0).astype(np.float32)
+    bias = (0.1 * rng.standard_normal(E)).astype(np.float32)
+    others = [low, np.full((T, E), -np.inf, np.float32), np.zeros((T, E), np.float32)]
+    mixed = np.stack([z] + others, 1).reshape(4 * T, E)
+    for groups in (1, 8):
+        for b in (None, bias):
+            cfg = _cfg(E, 6, 6, sigmoid=sigmoid, renorm=renorm, groups=groups, topk_groups=max(1, groups // 2), group_score=1, scale=2.5)
+            m, p = _context(cfg), _params(cfg)
+            together = m.select_experts(p, _gpu(mixed), None, _gpu(b), want_scores=True)
+            d_gate = torch.randn(4 * T, 6, device="cuda")
+            d_z = m.select_experts_backward(p, _gpu(mixed), together[1], d_gate, together[0])
+            for i, rows in enumerate([z] + others):
+                alone = m.select_experts(p, _gpu(rows), None, _gpu(b), want_scores=True)
+                assert all(torch.equal(x, y[i::4]) for x, y in zip(alone, together)), (groups, i)
+                d = m.select_experts_backward(p, _gpu(rows), alone[1], d_gate[i::4].contiguous(), alone[0])
+                assert torch.equal(d, d_z[i::4]), (groups, i)
+                one = m.select_experts(p, _gpu(rows[7:8]), None, _gpu(b), want_scores=True)
+                assert all(torch.equal(x, y[7:8]) for x, y in zip(one, alone)), (groups, i)
+
+
 # --------------------------------------------------------------------------------------------------------- refusals
 
 
