@@ -54,13 +54,12 @@ __device__ __forceinline__ u32x4_t dequantize(uint32_t codes, uint32_t scales) {
 // row indices, rows and the first weights), then the weights.  d 2048, 64 experts of 1408 and two shared, one token: 8.0 + 5.6
 // us for 36 MB.
 constexpr int THIN_ROWS = 16;
-constexpr int THIN_SLOTS = 8;    // k tiles (64 wide) of codes in flight
-constexpr int THIN_A_SLOTS = 8;   // and of rows, which come from L2
+constexpr int THIN_SLOTS = 8;    // k tiles (64 wide) of codes, and of rows, in flight
 
 template <bool SWIGLU>
 __device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, int row0, int rows, int group, int cb) {
-  constexpr int S = THIN_SLOTS, SA = THIN_A_SLOTS;
-  static_assert(S % 4 == 0 && S % SA == 0, "a unit of scales serves four k tiles");
+  constexpr int S = THIN_SLOTS;
+  static_assert(S % 4 == 0, "a unit of scales serves four k tiles");
   const StreamProblem& P = Q.s;
   const int lane = threadIdx.x;
   const int K = P.K, N = P.N;
@@ -75,7 +74,7 @@ __device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, int row0,
       __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(P.A), 0, 0xffffffff, 0x00020000);
   const uint32_t lane16 = (uint32_t)lane * 16u, column16 = (uint32_t)(lane & 15) * 16u;
   const int kq = (lane >> 4) * 8;
-  u32x4_t breg[S], sreg[S / 4], areg[SA][2];
+  u32x4_t breg[S], sreg[S / 4], areg[S][2];
   auto load_b = [&](int slot, int t) { breg[slot] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, lane16 + (uint32_t)t * 1024u, 0, 0); };
   auto load_s = [&](int slot, int t4) {
     sreg[slot] = __builtin_amdgcn_raw_buffer_load_b128(s_rsrc, column16 + (uint32_t)t4 * 256u, 0, 0);
@@ -109,13 +108,13 @@ __device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, int row0,
     a_last[s] = a_row + (uint32_t)(k_last + piece < K ? piece : K - 8 - k_last) * 2u;
   }
 #pragma unroll
-  for (int t = 0; t < SA; ++t) load_a(t, t);
+  for (int t = 0; t < S; ++t) load_a(t, t);
   __builtin_amdgcn_sched_barrier(0);
 
   f32x4_t acc[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
   auto multiply = [&](int slot) {
     const uint32_t sc = sreg[slot / 4][slot % 4];
-    const bf16x8_t a0 = __builtin_bit_cast(bf16x8_t, areg[slot % SA][0]), a1 = __builtin_bit_cast(bf16x8_t, areg[slot % SA][1]);
+    const bf16x8_t a0 = __builtin_bit_cast(bf16x8_t, areg[slot][0]), a1 = __builtin_bit_cast(bf16x8_t, areg[slot][1]);
     acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, __builtin_bit_cast(bf16x8_t, dequantize<0>(breg[slot][0], sc)), acc[0], 0, 0, 0);
     acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, __builtin_bit_cast(bf16x8_t, dequantize<1>(breg[slot][1], sc)), acc[1], 0, 0, 0);
     acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, __builtin_bit_cast(bf16x8_t, dequantize<2>(breg[slot][2], sc)), acc[0], 0, 0, 0);
@@ -128,17 +127,16 @@ __device__ __forceinline__ void thin_quant_tile(const QuantProblem& Q, int row0,
       multiply(u);
       __builtin_amdgcn_sched_barrier(0);
       load_b(u, t0 + u + S);
-      load_a(u % SA, t0 + u + SA);
+      load_a(u, t0 + u + S);
       if (u % 4 == 3) load_s(u / 4, (t0 + S) / 4 + u / 4);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // fewer than S tiles are left, all of their codes on the way
+  // fewer than S tiles are left, all of their codes and rows on the way
 #pragma unroll
   for (int u = 0; u < S - 1; ++u) {
     if (t0 + u >= NT) break;   // uniform
     multiply(u);
-    if (u + SA < S - 1) load_a(u % SA, t0 + u + SA);
   }
   // accumulator register v of lane l: row 4*(l/16) + v, column l%16
 #pragma unroll
