@@ -269,8 +269,9 @@ class FMoE:
         """release_packed: a bf16 context reads its expert weights from the library's packed copies only,
         so once the packing kernels have run the caller's expert tensors need not be kept alive; with
         this flag the binding waits for the stream and holds on to the router bias alone."""
-        self._weights = (router_w, router_bias, w_gate, w_up, w_down, ws_gate, ws_up, ws_down)
-        _check(self.lib.fmoe_set_weights(self._ctx, *[_ptr(t) for t in self._weights], _stream()))
+        weights = (router_w, router_bias, w_gate, w_up, w_down, ws_gate, ws_up, ws_down)
+        _check(self.lib.fmoe_set_weights(self._ctx, *[_ptr(t) for t in weights], _stream()))
+        self._weights = weights   # not before: a refused call leaves the context with those of the last one
         if release_packed and self.cfg.dtype == FMOE_BF16:
             torch.cuda.current_stream().synchronize()
             self._weights = (router_bias,)
@@ -295,8 +296,8 @@ class FMoE:
             _expect(pair[0], f"codes of {name}", torch.uint8, (g, n, K // 2), self.device)
             _expect(pair[1], f"scales of {name}", torch.uint8, (g, n, (K + QUANT_GROUP - 1) // QUANT_GROUP), self.device)
             tensors.append(C.byref(FmoeQuantTensor(pair[0].data_ptr(), pair[1].data_ptr())))
-        self._weights = (router_w, router_bias, *pairs)
         _check(self.lib.fmoe_set_weights_quant(self._ctx, _ptr(router_w), _ptr(router_bias), *tensors, _stream()))
+        self._weights = (router_w, router_bias, *pairs)
         if release_packed:
             torch.cuda.current_stream().synchronize()
             self._weights = (router_bias,)

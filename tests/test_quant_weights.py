@@ -741,6 +741,22 @@ def test_binding_refuses_tensors_that_do_not_fit_or_are_on_the_host():
         binding.quantize_weights(torch.zeros(4, 64))
 
 
+def test_a_refused_registration_keeps_the_tensors_of_the_one_in_force(monkeypatch):
+    """The context goes on borrowing the tensors that it was given before, so the binding has to hold on to them."""
+    monkeypatch.setattr(binding, "_stream", lambda: 0)
+    m = binding.FMoE(d_model=64, n_experts=4, d_ffn=32, k_text=2, k_visual=1, dtype="f32")
+    m.device = torch.device("cpu")
+    pair = lambda *s: (torch.zeros(*s[:-1], s[-1] // 2, dtype=torch.uint8), torch.zeros(*s[:-1], s[-1] // 32, dtype=torch.uint8))  # noqa: E731
+    held = m._weights = (torch.zeros(4, 64), None)
+    with pytest.raises(binding.FmoeError, match="bf16 context"):
+        m.set_weights_quant(torch.zeros(4, 64), None, pair(4, 32, 64), pair(4, 32, 64), pair(4, 64, 32))
+    assert m._weights is held
+    odd = torch.zeros(4 * 64 + 1)[1:].view(4, 64)
+    with pytest.raises(binding.FmoeError, match="16-byte aligned"):
+        m.set_weights(odd, None, torch.zeros(4, 32, 64), torch.zeros(4, 32, 64), torch.zeros(4, 64, 32))
+    assert m._weights is held
+
+
 def test_build_check_catches_registers_used_before_an_lds_read_has_landed(tmp_path):
     from paper_2511_17885_amd import build
     issue = "\t;;#ASMSTART\n\tds_read_b128 v[4:7], v1 offset:64\n\t;;#ASMEND\n"
