@@ -188,7 +188,8 @@ int fmoe_set_weights(fmoe_ctx* ctx, const void* router_w, const float* router_bi
  * The library keeps private copies in matrix-core operand order (4.25 bits a weight, padded as those of
  * fmoe_set_weights; allocated by the first call, freed by fmoe_destroy): the caller's expert tensors may be freed or
  * changed once the stream has drained.  A context that has been given both forms keeps the copies of both.
- * A matrix of 2^32 weights (d_model times S_m, or times N_s S_s) and more is refused with FMOE_ERR_UNSUPPORTED. */
+ * A layer whose (d_model + 64) times (S_m + 64), or times (N_s S_s + 64), comes to 2^32 or more is refused with
+ * FMOE_ERR_UNSUPPORTED. */
 int fmoe_set_weights_quant(fmoe_ctx* ctx, const void* router_w, const float* router_bias,
                            const fmoe_quant_tensor* w_gate, const fmoe_quant_tensor* w_up,
                            const fmoe_quant_tensor* w_down, const fmoe_quant_tensor* ws_gate,
@@ -233,7 +234,8 @@ int fmoe_route(fmoe_ctx* ctx, const void* x, const uint8_t* is_visual, int32_t T
  * topk_gate [T,Kmax]: gate_scale * s / (sum of the listed s) with the context's renormalize, else gate_scale * s; 0 in
  * padding.  The quotient is taken in logarithms: it is right also where the scores themselves underflow.
  * scores [T,E] fp32 or NULL: s, 0 where the logit is masked (fmoe_prune takes them as probs).
- * The outputs feed fmoe_permute and fmoe_combine as those of fmoe_route do; they share no memory with the inputs.
+ * The outputs feed fmoe_permute and fmoe_combine as those of fmoe_route do; they share no memory with the inputs.  A
+ * token's outputs are the same bits whatever tokens are beside it.
  * fmoe_set_selection has no effect here.  n_groups above 16 is FMOE_ERR_UNSUPPORTED. */
 int fmoe_select_experts(fmoe_ctx* ctx, const fmoe_select_params* params, const void* logits, int32_t logits_dtype,
                         const uint8_t* is_visual, const float* select_bias, int32_t T, float* scores,
@@ -307,7 +309,8 @@ int fmoe_permute_noalloc(fmoe_ctx* ctx, const int32_t* topk_idx, const int32_t* 
 /* The expert FFNs of Eq.4 as a grouped GEMM: for every row r of expert e,
  * y[r] = FFN_e(x[token(perm_src[r])]); the activation silu(.)*(.) is rounded to dtype between
  * the two products.  y [n_kept*Kmax capacity, H] dtype.  y_shared [N_s, n_kept, H] dtype or NULL
- * iff N_s == 0: the output of shared expert i for kept position p at (i*n_kept + p)*H.
+ * iff N_s == 0: the output of shared expert i for kept position p at (i*n_kept + p)*H.  With Kmax 0 (no expert is
+ * listed, the shared ones run alone) expert_offsets, perm_src and y may be NULL.
  * bf16: rows of x are addressed with 32-bit byte offsets, so every token index in kept_idx must
  * lie within the first 4 GiB of x (2^32 / (2*H) tokens); hidden buffers beyond 4 GiB are
  * refused with FMOE_ERR_UNSUPPORTED. */

@@ -339,7 +339,9 @@ class FMoE:
         return probs, idx[:, :self.kmax], gate[:, :self.kmax]
 
     def select_experts(self, params, logits, is_visual=None, select_bias=None, want_scores=False):
-        """fmoe_select_experts on logits [T, E] (float32 or bfloat16).  Returns (scores or None, topk_idx, topk_gate)."""
+        """fmoe_select_experts on logits [T, E] (float32 or bfloat16).  Returns (scores or None, topk_idx, topk_gate), which
+        carry no autograd graph even if the logits require a gradient: that one is select_experts_backward's, from the
+        gradients of topk_gate and scores that the caller's own backward pass has."""
         T = logits.shape[0]
         K = max(self.kmax, 1)
         dtype = _float_type(logits, "logits")
