@@ -300,7 +300,8 @@ __device__ __forceinline__ unsigned keep_groups(const SelectArgs& a, int t, int 
   if (log2p > 0) two_largest(one, two, lane_partner<0>(one), lane_partner<0>(two));
   if (log2p > 1) two_largest(one, two, lane_partner<1>(one), lane_partner<1>(two));
   if (log2p > 2) two_largest(one, two, lane_partner<2>(one), lane_partner<2>(two));
-  const float score = (a.sum_two && two > -INFINITY) ? one + two : one;
+  // (keys of the type's lowest value: a sum past it is not the score of a group that has none)
+  const float score = (a.sum_two && two > -INFINITY) ? fmaxf(one + two, -FLT_MAX) : one;
   // rank among the groups: larger scores, or equal ones of lower groups, are ahead
   wave_sync();   // the keys have been read
   if (part == 0) ks[g] = score;

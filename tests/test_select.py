@@ -637,6 +637,28 @@ def test_select_of_a_row_does_not_depend_on_the_rows_beside_it(sigmoid, renorm):
                 assert all(torch.equal(x, y[7:8]) for x, y in zip(one, alone)), (groups, i)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("lowest", [-FLT_MAX, -3e38, -1.8e38, 3e38, FLT_MAX])
+def test_select_groups_whose_two_largest_keys_overflow_in_32_bits(lowest, sigmoid):
+    """Biases of the type's lowest or largest value: the sum of a group's two largest keys does not fit in fp32, and still is
+    the score of a group that has usable experts, not of one that has none."""
+    rng = np.random.default_rng(8)
+    for E, groups, topk_groups in ((16, 2, 1), (48, 8, 3), (64, 16, 5), (200, 4, 2)):
+        z = rng.standard_normal((60, E)).astype(np.float32)
+        z[rng.random(z.shape) < 0.6] = -np.inf
+        size = E // groups
+        for t in range(60):      # one or more groups without any usable expert, the others with few
+            g = rng.choice(groups, size=rng.integers(1, groups), replace=False)
+            z[t, (g[:, None] * size + np.arange(size)).ravel()] = -np.inf
+        bias = (0.1 * rng.standard_normal(E)).astype(np.float32)
+        bias[rng.random(E) < 0.8] = lowest
+        for b in (bias, np.full(E, lowest, np.float32)):
+            cfg = _cfg(E, 6, 6, sigmoid=sigmoid, groups=groups, topk_groups=topk_groups, group_score=1)
+            idx = _context(cfg).select_experts(_params(cfg), _gpu(z), None, _gpu(b))[1].cpu().numpy()
+            assert np.array_equal(idx, _reference(z, None, b, cfg)[1]), (E, groups)
+
+
 # --------------------------------------------------------------------------------------------------------- refusals
 
 
