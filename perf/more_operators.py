@@ -193,7 +193,7 @@ def prepare(case, seed):
         s.moe = binding.FMoE(d_model=d, n_experts=E, d_ffn=F, n_shared=shared, d_ffn_shared=F if shared else 0, k_text=k,
                              k_visual=c["k_visual"], dtype="bf16")
         if c["op"] == "experts8":
-            s.moe.set_weights_rows8(*s.weights)
+            s.moe.set_weights_quant_rows(*s.weights)
         elif c["weights"] == "4bit":
             s.moe.set_weights_quant(s.router, None, *s.weights)
         else:
@@ -336,14 +336,14 @@ def _own(s):
     if c["op"] == "norm":
         return list(binding.rms_norm(s.x, s.weight, EPS, delta=s.delta))
     if c["op"] == "rows8":
-        h, codes, scales = binding.rms_norm_rows8(s.x, s.weight, EPS, delta=s.delta)
+        h, codes, scales = binding.rms_norm_quant(s.x, s.weight, EPS, delta=s.delta)
         return [h, codes, scales]
     if c["op"] == "backward":
         return list(binding.rms_norm_backward(s.x, s.weight, EPS, s.d_n, d_h=s.d_h))
     if c["op"] == "layer":
         norm = None if s.weight is None else (s.weight, EPS)
         return list(s.moe.layer_decode(s.x, s.is_visual, norm=norm, delta=s.delta, params=s.params, select_bias=s.bias))
-    y, y_shared = s.moe.expert_ffn_rows8(s.codes, s.scales, None, c["T"], s.offsets, s.perm_src)
+    y, y_shared = s.moe.expert_ffn_quant_rows(s.codes, s.scales, None, c["T"], s.offsets, s.perm_src)
     return [y[:s.rows]] if y_shared is None else [y[:s.rows], y_shared]
 
 
