@@ -15,7 +15,7 @@
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All work is
  *    enqueued asynchronously on it; no call synchronises with the host and no hot call
  *    (route / select_experts and its backward / prune / permute / expert_ffn / combine / layer_forward / quantize_weights
- *    / dequantize_weights) allocates memory.
+ *    / dequantize_weights / rms_norm, its form with 8-bit rows and its backward) allocates memory.
  *    Scratch comes from a caller-provided workspace sized by fmoe_workspace_bytes().  A hot call
  *    is a sequence of kernel launches and nothing else (no memset, no copy), so it can be
  *    captured into a HIP graph on `stream` and replayed.
@@ -206,6 +206,34 @@ int fmoe_quantize_weights(const void* w, int32_t dtype, int64_t rows, int32_t K,
                           uint8_t* scales, void* stream);
 int fmoe_dequantize_weights(const void* codes, const uint8_t* scales, int64_t rows, int32_t K, int32_t dtype, void* w,
                             void* stream);
+
+/* Root-mean-square norm of rows with the addition in front of it (no context: the current device):
+ *   h = x + delta, rounded to the type;   n = h * weight / sqrt(mean over the row of h^2 + eps).
+ * x, delta, h, n [T, d] of `dtype`; weight [d] of `weight_dtype` (fmoe_dtype); delta NULL: h = x; h NULL: not written.
+ * n is rounded once from its exact value (the sum of squares and the root are taken in 64 bits).  A row with an infinity or
+ * NaN, or of zeros with eps 0, gives what IEEE arithmetic makes of the formula.  h and n may each be x or delta, not the same
+ * tensor.  d % 8 == 0, d <= 16384; eps >= 0; all pointers 16-byte aligned. */
+int fmoe_rms_norm(const void* x, const void* delta, const void* weight, int32_t dtype, int32_t weight_dtype, int32_t T,
+                  int32_t d, float eps, void* h, void* n, void* stream);
+
+/* fmoe_rms_norm with n in 8 bits ("rows in 8 bits", for fmoe_expert_ffn_quant_rows): codes [T, d] bytes, e4m3 numbers (sign, four
+ * exponent bits of bias 7, three mantissa bits, no infinities); scales [T, 4 * ceil(d / 128)] bytes: byte g of a row, 2^(byte - 127),
+ * belongs to the codes 32g .. 32g+31 of it (the last group may be shorter), the bytes behind the groups are 127.
+ * A group's scale is the least power of two with which its largest magnitude is at most 448 scales, at least 2^-126, and 1
+ * for zeros; a code is the nearest, ties to the even one.  A group that holds an infinity or NaN gets codes 0 and scale byte 255.
+ * The rounding is the only one from the exact value.  codes and scales share no memory with the inputs. */
+int fmoe_rms_norm_quant(const void* x, const void* delta, const void* weight, int32_t dtype, int32_t weight_dtype, int32_t T,
+                        int32_t d, float eps, void* h, uint8_t* codes, uint8_t* scales, void* stream);
+
+/* Gradient of fmoe_rms_norm.  h [T, d] as the forward call left it (x without delta), weight and eps as there; d_n [T, d]
+ * gradient of n, d_h [T, d] that of h from elsewhere (the residual stream) or NULL; both of `dtype`.
+ * d_x [T, d] of `dtype`: the gradient of x, which is that of delta too; it may be d_n or d_h.  d_weight [d] fp32 or NULL; the
+ * order of its sum is fixed.  ws: fmoe_rms_norm_workspace_bytes(T, d) bytes, 256-byte aligned, not needed without d_weight.
+ * With T == 0 d_weight becomes 0.  Limits as in fmoe_rms_norm. */
+size_t fmoe_rms_norm_workspace_bytes(int32_t T, int32_t d);   /* [host] */
+int fmoe_rms_norm_backward(const void* h, const void* weight, const void* d_n, const void* d_h, int32_t dtype,
+                           int32_t weight_dtype, int32_t T, int32_t d, float eps, void* d_x, float* d_weight, void* ws,
+                           size_t ws_bytes, void* stream);
 
 /* Bytes of workspace that any hot call needs for up to max_tokens tokens in up to max_seqs
  * sequences with this context (for the Kmax current at the time of the call). [host] */

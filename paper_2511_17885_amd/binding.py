@@ -27,7 +27,8 @@ EXPORTS = ["fmoe_version", "fmoe_last_error", "fmoe_create", "fmoe_destroy", "fm
            "fmoe_magnitude_stability", "fmoe_row_cosine", "fmoe_gate_cosine", "fmoe_flops_ratios",
            "fmoe_kept_counts", "fmoe_stage_retention", "fmoe_stack_plan", "fmoe_stack_workspace_bytes",
            "fmoe_stack_forward", "fmoe_permute_noalloc", "fmoe_set_ffn_shape", "fmoe_set_weights_quant",
-           "fmoe_quantize_weights", "fmoe_dequantize_weights", "fmoe_select_experts", "fmoe_select_experts_backward"]
+           "fmoe_quantize_weights", "fmoe_dequantize_weights", "fmoe_select_experts", "fmoe_select_experts_backward",
+           "fmoe_rms_norm", "fmoe_rms_norm_quant", "fmoe_rms_norm_workspace_bytes", "fmoe_rms_norm_backward"]
 
 
 class FmoeConfig(C.Structure):
@@ -94,6 +95,12 @@ def load():
     lib.fmoe_set_weights_quant.argtypes = [vp, vp, vp, qt, qt, qt, qt, qt, qt, vp]
     lib.fmoe_quantize_weights.argtypes = [vp, i32, C.c_int64, i32, i32, vp, vp, vp]
     lib.fmoe_dequantize_weights.argtypes = [vp, vp, C.c_int64, i32, i32, vp, vp]
+    f32 = C.c_float
+    lib.fmoe_rms_norm.argtypes = [vp, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp]
+    lib.fmoe_rms_norm_quant.argtypes = [vp, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, vp]
+    lib.fmoe_rms_norm_workspace_bytes.argtypes = [i32, i32]
+    lib.fmoe_rms_norm_workspace_bytes.restype = sz
+    lib.fmoe_rms_norm_backward.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, sz, vp]
     sp = C.POINTER(FmoeSelectParams)
     lib.fmoe_select_experts.argtypes = [vp, sp, vp, i32, vp, vp, i32, vp, vp, vp, vp]
     lib.fmoe_select_experts_backward.argtypes = [vp, sp, vp, i32, vp, vp, vp, i32, vp, vp]
@@ -129,7 +136,7 @@ def load():
     lib.fmoe_profile_read.argtypes = [vp, C.POINTER(C.c_float)]
     for name in EXPORTS:
         if name not in ("fmoe_version", "fmoe_last_error", "fmoe_destroy", "fmoe_workspace_bytes",
-                        "fmoe_profile_name", "fmoe_stack_workspace_bytes"):
+                        "fmoe_profile_name", "fmoe_stack_workspace_bytes", "fmoe_rms_norm_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -211,6 +218,58 @@ def dequantize_weights(codes, scales, dtype=torch.bfloat16):
     _call(w.device, load().fmoe_dequantize_weights, _ptr(codes), _ptr(scales), w.numel() // max(K, 1), K,
           _float_type(w, "w"), _ptr(w))
     return w
+
+
+def _norm_args(x, weight, delta):
+    d = x.shape[-1]
+    dtype = _float_type(x, "x")
+    _expect(x, "x", x.dtype, x.shape, x.device)
+    _expect(delta, "delta", x.dtype, x.shape, x.device)
+    weight_dtype = _float_type(weight, "weight")
+    _expect(weight, "weight", weight.dtype, (d,), x.device)
+    return dtype, weight_dtype, x.numel() // max(d, 1), d
+
+
+def rms_norm(x, weight, eps=1e-6, delta=None):
+    """fmoe_rms_norm of rows x [..., d] (float32 or bfloat16), after the addition of delta if given.  weight [d] of either type.
+    Returns (h, n): h = x + delta, x itself without delta.  They carry no autograd graph (rms_norm_backward)."""
+    dtype, weight_dtype, T, d = _norm_args(x, weight, delta)
+    h, n = (None if delta is None else torch.empty_like(x)), torch.empty_like(x)
+    _call(x.device, load().fmoe_rms_norm, _ptr(x), _ptr(delta), _ptr(weight), dtype, weight_dtype, T, d, eps, _ptr(h), _ptr(n))
+    return (x if h is None else h), n
+
+
+def rms_norm_quant(x, weight, eps=1e-6, delta=None):
+    """fmoe_rms_norm_quant: as rms_norm, with n in 8 bits.  Returns (h, codes [..., d] float8_e4m3fn, scales [..., 4 * ceil(d / 128)]
+    uint8): value k of a row is codes[k] * 2^(scales[k / 32] - 127)."""
+    dtype, weight_dtype, T, d = _norm_args(x, weight, delta)
+    h = None if delta is None else torch.empty_like(x)
+    codes = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    scales = torch.empty(*x.shape[:-1], row_scales(d), dtype=torch.uint8, device=x.device)
+    _call(x.device, load().fmoe_rms_norm_quant, _ptr(x), _ptr(delta), _ptr(weight), dtype, weight_dtype, T, d, eps, _ptr(h),
+          _ptr(codes), _ptr(scales))
+    return (x if h is None else h), codes, scales
+
+
+def row_scales(d):
+    """Scale bytes of a row of d values in 8 bits: one for 32, rounded up to words."""
+    return (d + 127) // 128 * 4
+
+
+def rms_norm_backward(h, weight, eps, d_n, d_h=None, want_weight=True):
+    """fmoe_rms_norm_backward: (gradient of x, which is delta's too; gradient of the weight [d] float32 or None) from those of n and,
+    if given, of h."""
+    dtype, weight_dtype, T, d = _norm_args(h, weight, None)
+    _expect(d_n, "d_n", h.dtype, h.shape, h.device)
+    _expect(d_h, "d_h", h.dtype, h.shape, h.device)
+    d_x, d_weight, ws, need = torch.empty_like(h), None, None, 0
+    if want_weight:
+        d_weight = torch.empty(d, dtype=torch.float32, device=h.device)
+        need = load().fmoe_rms_norm_workspace_bytes(T, d)
+        ws = torch.empty(need, dtype=torch.uint8, device=h.device)
+    _call(h.device, load().fmoe_rms_norm_backward, _ptr(h), _ptr(weight), _ptr(d_n), _ptr(d_h), dtype, weight_dtype, T, d, eps,
+          _ptr(d_x), _ptr(d_weight), _ptr(ws), need)
+    return d_x, d_weight
 
 
 class FMoE:

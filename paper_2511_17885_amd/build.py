@@ -27,6 +27,7 @@ SOURCES = {
     "ffn_quant.hip": [],
     "select.hip": [],
     "quant.hip": [],
+    "norm.hip": ["-ffp-contract=off"],
     "combine.hip": [],
     "diag.hip": [],
     "stack.hip": [],

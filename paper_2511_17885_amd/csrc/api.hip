@@ -104,6 +104,17 @@ int check_quant(const void* w, int32_t dtype, int64_t rows, int32_t K, const voi
   return FMOE_OK;
 }
 
+// Arguments that the norms share
+int check_norm(int32_t dtype, int32_t weight_dtype, int32_t T, int32_t d, float eps, const char* who) {
+  if ((dtype != FMOE_F32 && dtype != FMOE_BF16) || (weight_dtype != FMOE_F32 && weight_dtype != FMOE_BF16))
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: dtype %d or weight_dtype %d is neither FMOE_F32 nor FMOE_BF16", who, dtype, weight_dtype);
+  if (d <= 0) return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: d %d", who, d);
+  if (d % 8 || d > FMOE_NORM_MAX_D)
+    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "%s: d %d is not a multiple of 8 up to %d", who, d, FMOE_NORM_MAX_D);
+  if (!(eps >= 0.0f) || !std::isfinite(eps)) return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: eps %g", who, (double)eps);
+  return check_tokens(T);
+}
+
 // bf16 expert GEMMs address activation rows with 32-bit byte offsets into one buffer descriptor: the
 // layer input of n tokens and the hidden buffers of n tokens' rows must each stay below 4 GiB.
 int check_ffn_extent(const fmoe_ctx* ctx, int32_t n, const char* who) {
@@ -353,6 +364,52 @@ int fmoe_dequantize_weights(const void* codes, const uint8_t* scales, int64_t ro
   const int rc = check_quant(w, dtype, rows, K, codes, scales, "fmoe_dequantize_weights");
   if (rc != FMOE_OK || rows == 0) return rc;
   return launch_dequantize(codes, scales, rows, K, dtype, w, static_cast<hipStream_t>(stream));
+}
+
+int fmoe_rms_norm(const void* x, const void* delta, const void* weight, int32_t dtype, int32_t weight_dtype, int32_t T,
+                  int32_t d, float eps, void* h, void* n, void* stream) {
+  const int rc = check_norm(dtype, weight_dtype, T, d, eps, "fmoe_rms_norm");
+  if (rc != FMOE_OK || T == 0) return rc;
+  if (!x || !weight || !n) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_rms_norm: x / weight / n is NULL");
+  if (!aligned16(x) || !aligned16(delta) || !aligned16(weight) || !aligned16(h) || !aligned16(n))
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_rms_norm: tensor pointers must be 16-byte aligned");
+  if (h == n) return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_rms_norm: h and n are the same tensor");
+  return launch_rms_norm(x, delta, weight, dtype, weight_dtype, T, d, eps, h, n, nullptr, nullptr, static_cast<hipStream_t>(stream));
+}
+
+int fmoe_rms_norm_quant(const void* x, const void* delta, const void* weight, int32_t dtype, int32_t weight_dtype, int32_t T,
+                        int32_t d, float eps, void* h, uint8_t* codes, uint8_t* scales, void* stream) {
+  const int rc = check_norm(dtype, weight_dtype, T, d, eps, "fmoe_rms_norm_quant");
+  if (rc != FMOE_OK || T == 0) return rc;
+  if (!x || !weight || !codes || !scales)
+    return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_rms_norm_quant: x / weight / codes / scales is NULL");
+  if (!aligned16(x) || !aligned16(delta) || !aligned16(weight) || !aligned16(h) || !aligned16(codes) || !aligned16(scales))
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_rms_norm_quant: tensor pointers must be 16-byte aligned");
+  return launch_rms_norm(x, delta, weight, dtype, weight_dtype, T, d, eps, h, nullptr, codes, scales, static_cast<hipStream_t>(stream));
+}
+
+size_t fmoe_rms_norm_workspace_bytes(int32_t T, int32_t d) {
+  if (T < 0 || d <= 0) return 0;
+  return align_up((size_t)norm_backward_blocks(T > 0 ? T : 1, d) * d * 4);
+}
+
+int fmoe_rms_norm_backward(const void* h, const void* weight, const void* d_n, const void* d_h, int32_t dtype,
+                           int32_t weight_dtype, int32_t T, int32_t d, float eps, void* d_x, float* d_weight, void* ws,
+                           size_t ws_bytes, void* stream) {
+  const int rc = check_norm(dtype, weight_dtype, T, d, eps, "fmoe_rms_norm_backward");
+  if (rc != FMOE_OK || (T == 0 && !d_weight)) return rc;
+  if (T > 0 && (!h || !weight || !d_n || !d_x))
+    return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_rms_norm_backward: h / weight / d_n / d_x is NULL");
+  if (!aligned16(h) || !aligned16(weight) || !aligned16(d_n) || !aligned16(d_h) || !aligned16(d_x) || !aligned16(d_weight))
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_rms_norm_backward: tensor pointers must be 16-byte aligned");
+  if (d_weight && T > 0) {
+    if (!ws) return fmoe_fail(FMOE_ERR_WORKSPACE, "workspace is NULL");
+    if (reinterpret_cast<uintptr_t>(ws) & 255u) return fmoe_fail(FMOE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    const size_t need = fmoe_rms_norm_workspace_bytes(T, d);
+    if (ws_bytes < need) return fmoe_fail(FMOE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed for %d rows of %d", ws_bytes, need, T, d);
+  }
+  return launch_rms_norm_backward(h, weight, d_n, d_h, dtype, weight_dtype, T, d, eps, d_x, d_weight, static_cast<float*>(ws),
+                                  static_cast<hipStream_t>(stream));
 }
 
 size_t fmoe_workspace_bytes(const fmoe_ctx* ctx, int32_t max_tokens, int32_t max_seqs) {

@@ -11,6 +11,7 @@
 #define FMOE_MAX_TOPK 16
 #define FMOE_MAX_WINDOW 64
 #define FMOE_MAX_GROUPS 16       // expert groups in fmoe_select_experts
+#define FMOE_NORM_MAX_D 16384    // longest row of the norms
 #define FMOE_PERM_BLOCK 256   // kept positions per block in the permutation kernels
 #define FMOE_ROUTE_DISPATCH_TOKENS 16   // tokens up to which the router's one block does the dispatch too
 #define FMOE_TILE_M 64        // rows per grouped-GEMM tile (tile list granularity)
@@ -229,6 +230,13 @@ int launch_quantize(const void* w, int dtype, long long rows, int K, int saturat
                     hipStream_t stream);
 int launch_dequantize(const void* codes, const uint8_t* scales, long long rows, int K, int dtype, void* w,
                       hipStream_t stream);
+
+// ---- norms (norm.hip).  codes: rows in 8 bits instead of n
+int launch_rms_norm(const void* x, const void* delta, const void* weight, int dtype, int weight_dtype, int T, int d, float eps,
+                    void* h, void* n, void* codes, uint8_t* scales, hipStream_t stream);
+int norm_backward_blocks(int T, int d);   // partial sums [blocks, d] of the weight's gradient
+int launch_rms_norm_backward(const void* h, const void* weight, const void* d_n, const void* d_h, int dtype, int weight_dtype,
+                             int T, int d, float eps, void* d_x, float* d_weight, float* part, hipStream_t stream);
 
 // ---- diagnostics (diag.hip)
 int launch_adjacent_similarity(const float* probs, const uint8_t* is_visual, const int32_t* cu, int B, int T,

@@ -1,0 +1,345 @@
+// Root-mean-square norm of rows with the addition in front of it, its output in the storage type or in 8 bits, and its gradient.
+// Compiled with floating-point contraction off: the roundings that norm_dev.h relies on are written out.
+//
+// Bound: memory.  A wavefront has a row in registers (up to 4096 elements; a workgroup of four wavefronts has one of up to 16384,
+// or where there are few rows), reads it once and writes its outputs once.
+
+#include "norm_dev.h"
+
+namespace {
+
+using namespace rms;
+
+constexpr int MAX_D = FMOE_NORM_MAX_D;
+
+struct NormArgs {
+  const void *x, *delta, *w;
+  int T, d;
+  float eps;
+  void *h, *n;          // h may be null (nobody wants the sum), n with rows in 8 bits
+  uint32_t* codes;      // [T, d] bytes
+  uint8_t* scales;      // [T, scale_stride]
+  int scale_stride;     // groups of 32, rounded up to words
+};
+
+// Largest of the magnitudes' bits over four neighbouring lanes
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+  uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, false);   // lanes 1 0 3 2
+  v = v > o ? v : o;
+  o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false);            // lanes 2 3 0 1
+  return v > o ? v : o;
+}
+
+// A sum over the wavefronts of a workgroup that share a row (WPR of them); s_part: 4 doubles
+template <int WPR>
+__device__ __forceinline__ double row_total(double v, double* s_part) {
+  v = wave_sum(v);
+  if constexpr (WPR > 1) {
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();   // the last sum has been read
+    if ((threadIdx.x & 63) == 0) s_part[wave] = v;
+    __syncthreads();
+    v = (s_part[0] + s_part[1]) + (s_part[2] + s_part[3]);
+  }
+  return v;
+}
+
+// NU units of eight a lane; WPR wavefronts a row (1 or all 4).
+template <typename XT, typename WT, int NU, int WPR, bool ROWS8>
+__global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
+  __shared__ double s_part[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = WPR == 1 ? (int)blockIdx.x * 4 + wave : (int)blockIdx.x;
+  if (row >= a.T) return;   // uniform over those who share a row
+  const int first = WPR == 1 ? lane : (int)threadIdx.x;
+  constexpr int STEP = 64 * WPR;
+  const int units = a.d >> 3;
+  const size_t base = (size_t)row * a.d;
+  Unit<XT> h[NU], dl[NU];
+#pragma unroll
+  for (int i = 0; i < NU; ++i) {
+    const int u = first + STEP * i;
+    h[i].zero();
+    if (u < units) h[i].load(static_cast<const XT*>(a.x) + base + u * 8);
+  }
+  if (a.delta != nullptr) {
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int u = first + STEP * i;
+      dl[i].zero();
+      if (u < units) dl[i].load(static_cast<const XT*>(a.delta) + base + u * 8);
+    }
+#pragma unroll
+    for (int i = 0; i < NU; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; e += 2)
+        h[i].set2(e, add_rounded<XT>(h[i].get(e), dl[i].get(e)), add_rounded<XT>(h[i].get(e + 1), dl[i].get(e + 1)));
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < NU; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const double v = (double)h[i].get(e);
+      sum = fma(v, v, sum);
+    }
+  const Scale r = row_scale(row_total<WPR>(sum, s_part), a.d, a.eps);
+#pragma unroll
+  for (int i = 0; i < NU; ++i) {
+    const int u = first + STEP * i;
+    const bool in = u < units;
+    float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (in) {
+      load_weights<WT>(a.w, u * 8, w);
+      if (a.h != nullptr) h[i].store(static_cast<XT*>(a.h) + base + u * 8);
+    }
+    if constexpr (!ROWS8) {
+      Unit<XT> n;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2)
+        n.set2(e, value_rounded<XT>(h[i].get(e), w[e], r), value_rounded<XT>(h[i].get(e + 1), w[e + 1], r));
+      if (in) n.store(static_cast<XT*>(a.n) + base + u * 8);
+    } else {
+      // The group's scale: the least power of two with the largest magnitude at most 448 = 1.75 * 2^8 of it, at least 2^-126.
+      // Values rounded to odd keep what is needed to see that and to round to 4 significant bits.
+      float v[8];
+      uint32_t big = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float hi, lo;
+        value(h[i].get(e), w[e], r, hi, lo);
+        v[e] = in ? odd(hi, lo) : 0.0f;
+        const uint32_t m = __float_as_uint(v[e]) & 0x7fffffffu;
+        big = big > m ? big : m;
+      }
+      big = quad_max(big);
+      int e8 = (int)(big >> 23) - 8 + ((big & 0x7fffffu) > 0x600000u ? 1 : 0);
+      e8 = e8 < 1 ? 1 : e8;
+      if (big == 0u) e8 = 127;
+      const bool finite_group = big < 0x7f800000u;
+      const float scale = __uint_as_float((uint32_t)(finite_group ? e8 : 127) << 23);
+      typedef short s16x2_t __attribute__((ext_vector_type(2)));
+      s16x2_t c0 = {0, 0}, c1 = {0, 0};
+      c0 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c0, v[0], v[1], scale, false);
+      c0 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c0, v[2], v[3], scale, true);
+      c1 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c1, v[4], v[5], scale, false);
+      c1 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c1, v[6], v[7], scale, true);
+      if (in) {
+        uint2 c = {__builtin_bit_cast(uint32_t, c0), __builtin_bit_cast(uint32_t, c1)};
+        if (!finite_group) c = uint2{0u, 0u};
+        *reinterpret_cast<uint2*>(reinterpret_cast<char*>(a.codes) + base + u * 8) = c;
+      }
+      if ((u & 3) == 0 && (u >> 2) < a.scale_stride)
+        a.scales[(size_t)row * a.scale_stride + (u >> 2)] = (uint8_t)(finite_group ? e8 : 255);
+    }
+  }
+}
+
+struct NormBackwardArgs {
+  const void *h, *w, *dn, *dh;
+  int T, d;
+  float eps;
+  void* dx;
+  float* part;          // [blocks, d] or null: no gradient of the weight
+};
+
+// With c = h r and g = dn w: dx = dh + r (g - c mean(g c)); a workgroup's rows add dn c up for the weight, one partial sum each.
+template <typename XT, typename WT, int NU, int WPR>
+__global__ __launch_bounds__(256) void rms_norm_backward_kernel(NormBackwardArgs a) {
+  __shared__ double s_part[4];
+  __shared__ float s_dw[WPR == 1 ? 64 * NU * 8 : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int first = WPR == 1 ? lane : (int)threadIdx.x;
+  constexpr int STEP = 64 * WPR;
+  const int units = a.d >> 3;
+  float dw[NU][8];
+#pragma unroll
+  for (int i = 0; i < NU; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[i][e] = 0.0f;
+  Unit<WT> w[NU];
+#pragma unroll
+  for (int i = 0; i < NU; ++i) {
+    w[i].zero();
+    if (first + STEP * i < units) w[i].load(static_cast<const WT*>(a.w) + (first + STEP * i) * 8);
+  }
+  const int rows_a_step = WPR == 1 ? (int)gridDim.x * 4 : (int)gridDim.x;
+  for (int row = WPR == 1 ? (int)blockIdx.x * 4 + wave : (int)blockIdx.x; row < a.T; row += rows_a_step) {
+    const size_t base = (size_t)row * a.d;
+    Unit<XT> h[NU], g[NU], dh[NU];
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int u = first + STEP * i;
+      h[i].zero();
+      g[i].zero();
+      dh[i].zero();
+      if (u < units) {
+        h[i].load(static_cast<const XT*>(a.h) + base + u * 8);
+        g[i].load(static_cast<const XT*>(a.dn) + base + u * 8);
+        if (a.dh != nullptr) dh[i].load(static_cast<const XT*>(a.dh) + base + u * 8);
+      }
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < NU; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double v = (double)h[i].get(e);
+        sum = fma(v, v, sum);
+      }
+    const Scale r = row_scale(row_total<WPR>(sum, s_part), a.d, a.eps);
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NU; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float c = __builtin_amdgcn_ldexpf(h[i].get(e), r.q) * r.hi;
+        const float dn = g[i].get(e);
+        dot = fmaf(dn * w[i].get(e), c, dot);
+        dw[i][e] = fmaf(dn, c, dw[i][e]);
+      }
+    const float m = (float)(row_total<WPR>((double)dot, s_part) / (double)a.d);
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int u = first + STEP * i;
+      Unit<XT> out;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float c = __builtin_amdgcn_ldexpf(h[i].get(e), r.q) * r.hi;
+        const float t = __builtin_amdgcn_ldexpf(fmaf(-c, m, g[i].get(e) * w[i].get(e)) * r.hi, r.q);
+        v[e] = a.dh != nullptr ? t + dh[i].get(e) : t;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        if constexpr (sizeof(XT) == 2) out.set2(e, nearest_bf16(v[e]), nearest_bf16(v[e + 1]));
+        else out.set2(e, v[e], v[e + 1]);
+      }
+      if (u < units) out.store(static_cast<XT*>(a.dx) + base + u * 8);
+    }
+  }
+  if (a.part == nullptr) return;
+  float* const part = a.part + (size_t)blockIdx.x * a.d;
+  if constexpr (WPR == 1) {   // the wavefronts' sums one after the other
+    for (int turn = 0; turn < 4; ++turn) {
+      if (wave == turn) {
+#pragma unroll
+        for (int i = 0; i < NU; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int at = (i * 8 + e) * 64 + lane;   // no two lanes on a bank
+            dw[i][e] = turn == 0 ? dw[i][e] : s_dw[at] + dw[i][e];
+            if (turn < 3) s_dw[at] = dw[i][e];
+          }
+      }
+      __syncthreads();
+    }
+    if (wave != 3) return;
+  }
+#pragma unroll
+  for (int i = 0; i < NU; ++i) {
+    const int u = first + STEP * i;
+    if (u >= units) continue;
+    reinterpret_cast<f32x4_t*>(part + u * 8)[0] = f32x4_t{dw[i][0], dw[i][1], dw[i][2], dw[i][3]};
+    reinterpret_cast<f32x4_t*>(part + u * 8)[1] = f32x4_t{dw[i][4], dw[i][5], dw[i][6], dw[i][7]};
+  }
+}
+
+// The partial sums of every column, in a fixed order: four wavefronts a quarter of them each.
+__global__ __launch_bounds__(256) void rms_norm_weight_kernel(const float* __restrict__ part, int parts, int d,
+                                                              float* __restrict__ dw) {
+  __shared__ double s[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int k = (int)blockIdx.x * 64 + lane;
+  double sum = 0.0;
+  if (k < d) {
+#pragma unroll 8
+    for (int p = wave; p < parts; p += 4) sum += (double)part[(size_t)p * d + k];
+  }
+  s[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && k < d) dw[k] = (float)((s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]));
+}
+
+// Wavefronts a row: all four of a workgroup for rows that one cannot hold, and for few rows
+int waves_per_row(int T, int d) { return d > 4096 || T <= 1024 ? 4 : 1; }
+
+template <typename XT, typename WT, bool ROWS8>
+void run_norm(const NormArgs& a, hipStream_t stream) {
+  const int wpr = waves_per_row(a.T, a.d);
+  const int units = ROWS8 ? (a.d + 127) / 128 * 16 : a.d / 8, per_lane = (units + 64 * wpr - 1) / (64 * wpr);
+  const dim3 grid(wpr == 1 ? (a.T + 3) / 4 : a.T), block(256);
+#define FMOE_NORM(NU)                                                                                     \
+  do {                                                                                                    \
+    if (wpr == 1) hipLaunchKernelGGL((rms_norm_kernel<XT, WT, NU, 1, ROWS8>), grid, block, 0, stream, a); \
+    else hipLaunchKernelGGL((rms_norm_kernel<XT, WT, NU, 4, ROWS8>), grid, block, 0, stream, a);          \
+  } while (0)
+  if (per_lane <= 1) FMOE_NORM(1);
+  else if (per_lane <= 2) FMOE_NORM(2);
+  else if (per_lane <= 3) FMOE_NORM(3);
+  else if (per_lane <= 4) FMOE_NORM(4);
+  else FMOE_NORM(8);
+#undef FMOE_NORM
+}
+template <typename XT, typename WT>
+void run_backward(const NormBackwardArgs& a, int blocks, hipStream_t stream) {
+  const int wpr = waves_per_row(a.T, a.d);
+  const int per_lane = (a.d / 8 + 64 * wpr - 1) / (64 * wpr);
+  const dim3 grid(blocks), block(256);
+#define FMOE_NORM(NU)                                                                                       \
+  do {                                                                                                      \
+    if (wpr == 1) hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 1>), grid, block, 0, stream, a); \
+    else hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 4>), grid, block, 0, stream, a);          \
+  } while (0)
+  if (per_lane <= 1) FMOE_NORM(1);
+  else if (per_lane <= 2) FMOE_NORM(2);
+  else if (per_lane <= 3) FMOE_NORM(3);
+  else if (per_lane <= 4) FMOE_NORM(4);
+  else FMOE_NORM(8);
+#undef FMOE_NORM
+}
+
+}  // namespace
+
+// Workgroups of the backward kernel, and so partial sums of the weight's gradient
+int norm_backward_blocks(int T, int d) {
+  const int rows = waves_per_row(T, d) == 1 ? (T + 3) / 4 : T;
+  return rows < 512 ? rows : 512;
+}
+
+int launch_rms_norm(const void* x, const void* delta, const void* weight, int dtype, int weight_dtype, int T, int d, float eps,
+                    void* h, void* n, void* codes, uint8_t* scales, hipStream_t stream) {
+  static_assert(MAX_D == 256 * 8 * 8, "a workgroup holds a row");
+  const NormArgs a{x, delta, weight, T, d, eps, h, n, static_cast<uint32_t*>(codes), scales, (d + 127) / 128 * 4};
+  const bool b = dtype == FMOE_BF16, wb = weight_dtype == FMOE_BF16;
+  if (codes != nullptr) {
+    if (b && wb) run_norm<bf16_t, bf16_t, true>(a, stream);
+    else if (b) run_norm<bf16_t, float, true>(a, stream);
+    else if (wb) run_norm<float, bf16_t, true>(a, stream);
+    else run_norm<float, float, true>(a, stream);
+  } else {
+    if (b && wb) run_norm<bf16_t, bf16_t, false>(a, stream);
+    else if (b) run_norm<bf16_t, float, false>(a, stream);
+    else if (wb) run_norm<float, bf16_t, false>(a, stream);
+    else run_norm<float, float, false>(a, stream);
+  }
+  FMOE_HIP_CHECK(hipGetLastError());
+  return FMOE_OK;
+}
+
+int launch_rms_norm_backward(const void* h, const void* weight, const void* d_n, const void* d_h, int dtype, int weight_dtype,
+                             int T, int d, float eps, void* d_x, float* d_weight, float* part, hipStream_t stream) {
+  const int blocks = norm_backward_blocks(T, d);
+  const NormBackwardArgs a{h, weight, d_n, d_h, T, d, eps, d_x, d_weight != nullptr ? part : nullptr};
+  if (T > 0) {
+    const bool b = dtype == FMOE_BF16, wb = weight_dtype == FMOE_BF16;
+    if (b && wb) run_backward<bf16_t, bf16_t>(a, blocks, stream);
+    else if (b) run_backward<bf16_t, float>(a, blocks, stream);
+    else if (wb) run_backward<float, bf16_t>(a, blocks, stream);
+    else run_backward<float, float>(a, blocks, stream);
+  }
+  if (d_weight != nullptr)
+    hipLaunchKernelGGL(rms_norm_weight_kernel, dim3((d + 63) / 64), dim3(256), 0, stream, part, blocks, d, d_weight);
+  FMOE_HIP_CHECK(hipGetLastError());
+  return FMOE_OK;
+}
