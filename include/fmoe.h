@@ -14,7 +14,7 @@
  *    library only borrows them for the duration of the enqueued work.
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All work is
  *    enqueued asynchronously on it; no call synchronises with the host and no hot call
- *    (route / select_experts and its backward / prune / permute / expert_ffn / combine / layer_forward / quantize_weights
+ *    (route / select_experts and its backward / prune / permute / expert_ffn, also on 8-bit rows / combine / layer_forward / quantize_weights
  *    / dequantize_weights / rms_norm, its form with 8-bit rows and its backward) allocates memory.
  *    Scratch comes from a caller-provided workspace sized by fmoe_workspace_bytes().  A hot call
  *    is a sequence of kernel launches and nothing else (no memset, no copy), so it can be
@@ -163,7 +163,7 @@ int fmoe_set_ffn_shape(fmoe_ctx* ctx, int32_t shape);
  * before the softmax); w_gate, w_up [E,S_m,H]; w_down [E,H,S_m]; ws_gate, ws_up
  * [N_s,S_s,H]; ws_down [N_s,H,S_s] (NULL iff N_s == 0).  An expert is the three-matrix gated
  * FFN  y = W_down (silu(W_gate x) * (W_up x))  without biases (flop model of App. E).
- * Device allocations (with those of fmoe_set_weights_quant the only ones of the library; made on the first call, reused by later calls
+ * Device allocations (with those of fmoe_set_weights_quant and its form for 8-bit rows the only ones of the library; made on the first call, reused by later calls
  * on the same context, freed by fmoe_destroy):
  *  - a private fp32 copy of the router matrix in the router kernel's operand order (E*H*4 bytes
  *    rounded up to 16x16 blocks and whole 128-wide k chunks);
@@ -194,6 +194,14 @@ int fmoe_set_weights_quant(fmoe_ctx* ctx, const void* router_w, const float* rou
                            const fmoe_quant_tensor* w_gate, const fmoe_quant_tensor* w_up,
                            const fmoe_quant_tensor* w_down, const fmoe_quant_tensor* ws_gate,
                            const fmoe_quant_tensor* ws_up, const fmoe_quant_tensor* ws_down, void* stream);
+
+/* Registers 4-bit expert matrices for fmoe_expert_ffn_quant_rows, beside the weights in force for the other calls, which stay (none
+ * are needed).  Tensors, alignment, bf16 contexts and copies (4.25 bits a weight, the reduction padded to 128, the output columns to
+ * 64 / 128) as in fmoe_set_weights_quant.  d_model, d_ffn and d_ffn_shared must be multiples of 32, and (d_model + 128) times
+ * (S_m + 128), or times (N_s S_s + 128), below 2^32, else FMOE_ERR_UNSUPPORTED. */
+int fmoe_set_weights_quant_rows(fmoe_ctx* ctx, const fmoe_quant_tensor* w_gate, const fmoe_quant_tensor* w_up,
+                                const fmoe_quant_tensor* w_down, const fmoe_quant_tensor* ws_gate,
+                                const fmoe_quant_tensor* ws_up, const fmoe_quant_tensor* ws_down, void* stream);
 
 /* Weights to 4 bits and back (no context: the current device).  w [rows, K] of `dtype` (fmoe_dtype), K % 8 == 0; codes
  * and scales as in fmoe_quant_tensor; w and codes 16-byte aligned.
@@ -346,6 +354,16 @@ int fmoe_expert_ffn(fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int32
                     const int32_t* n_kept_dev, const int32_t* expert_offsets,
                     const int32_t* perm_src, void* y, void* y_shared, void* ws, size_t ws_bytes,
                     void* stream);
+
+/* fmoe_expert_ffn on rows in 8 bits and the weights of fmoe_set_weights_quant_rows: codes [T, d_model] and scales
+ * [T, 4 * ceil(d_model / 128)] as fmoe_rms_norm_quant writes them (16- and 4-byte aligned; the bytes behind a row's groups 127).
+ * The activation silu(.)*(.) is rounded to 8 bits in the same way (32 neighbouring columns a power of two) between the two
+ * products, which are added up in fp32; y and y_shared are bf16, rounded once.  fmoe_set_ffn_shape chooses between the forms for few
+ * and for many rows an expert here too; the outputs are the same bits.  A row whose input or activation holds an infinity or
+ * NaN gives NaN.  Every other argument as in fmoe_expert_ffn; the row limit of kept_idx is 2^32 / d_model tokens. */
+int fmoe_expert_ffn_quant_rows(fmoe_ctx* ctx, const uint8_t* codes, const uint8_t* scales, const int32_t* kept_idx,
+                               int32_t n_kept, const int32_t* n_kept_dev, const int32_t* expert_offsets,
+                               const int32_t* perm_src, void* y, void* y_shared, void* ws, size_t ws_bytes, void* stream);
 
 /* Eq.4: out[p] = (residual[t]) + sum_i y_shared[i][p] + sum_s topk_gate[t,s] * y[inv_perm[p,s]]
  * with t = kept_idx[p]; fp32 accumulation in that order, one rounding to dtype.  y, y_shared,

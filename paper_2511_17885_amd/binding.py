@@ -28,7 +28,8 @@ EXPORTS = ["fmoe_version", "fmoe_last_error", "fmoe_create", "fmoe_destroy", "fm
            "fmoe_kept_counts", "fmoe_stage_retention", "fmoe_stack_plan", "fmoe_stack_workspace_bytes",
            "fmoe_stack_forward", "fmoe_permute_noalloc", "fmoe_set_ffn_shape", "fmoe_set_weights_quant",
            "fmoe_quantize_weights", "fmoe_dequantize_weights", "fmoe_select_experts", "fmoe_select_experts_backward",
-           "fmoe_rms_norm", "fmoe_rms_norm_quant", "fmoe_rms_norm_workspace_bytes", "fmoe_rms_norm_backward"]
+           "fmoe_rms_norm", "fmoe_rms_norm_quant", "fmoe_rms_norm_workspace_bytes", "fmoe_rms_norm_backward",
+           "fmoe_set_weights_quant_rows", "fmoe_expert_ffn_quant_rows"]
 
 
 class FmoeConfig(C.Structure):
@@ -93,6 +94,8 @@ def load():
     lib.fmoe_set_weights.argtypes = [vp] + [vp] * 8 + [vp]
     qt = C.POINTER(FmoeQuantTensor)
     lib.fmoe_set_weights_quant.argtypes = [vp, vp, vp, qt, qt, qt, qt, qt, qt, vp]
+    lib.fmoe_set_weights_quant_rows.argtypes = [vp, qt, qt, qt, qt, qt, qt, vp]
+    lib.fmoe_expert_ffn_quant_rows.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.fmoe_quantize_weights.argtypes = [vp, i32, C.c_int64, i32, i32, vp, vp, vp]
     lib.fmoe_dequantize_weights.argtypes = [vp, vp, C.c_int64, i32, i32, vp, vp]
     f32 = C.c_float
@@ -341,12 +344,27 @@ class FMoE:
         the current stream; the binding holds on to the tensors unless release_packed asks it to wait for the stream and
         keep the router bias alone."""
         c = self.cfg
+        _expect(router_w, "router_w", self.torch_dtype, (c.n_experts, c.d_model), self.device)
+        _expect(router_bias, "router_bias", torch.float32, (c.n_experts,), self.device)
+        pairs = (w_gate, w_up, w_down, ws_gate, ws_up, ws_down)
+        tensors = self._quant_tensors(pairs)
+        _check(self.lib.fmoe_set_weights_quant(self._ctx, _ptr(router_w), _ptr(router_bias), *tensors, _stream()))
+        self._weights = (router_w, router_bias, *pairs)
+        if release_packed:
+            torch.cuda.current_stream().synchronize()
+            self._weights = (router_bias,)
+
+    def set_weights_quant_rows(self, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None):
+        """fmoe_set_weights_quant_rows: the matrices as in set_weights_quant, for expert_ffn_quant_rows; weights registered otherwise
+        stay in force for the other calls.  The context makes copies on the current stream, nothing is held on to."""
+        tensors = self._quant_tensors((w_gate, w_up, w_down, ws_gate, ws_up, ws_down))
+        _check(self.lib.fmoe_set_weights_quant_rows(self._ctx, *tensors, _stream()))
+
+    def _quant_tensors(self, pairs):
+        c = self.cfg
         E, H, S, N, Ss = c.n_experts, c.d_model, c.d_ffn, c.n_shared, c.d_ffn_shared
-        _expect(router_w, "router_w", self.torch_dtype, (E, H), self.device)
-        _expect(router_bias, "router_bias", torch.float32, (E,), self.device)
         names = ("w_gate", "w_up", "w_down", "ws_gate", "ws_up", "ws_down")
         shapes = ((E, S, H), (E, S, H), (E, H, S), (N, Ss, H), (N, Ss, H), (N, H, Ss))
-        pairs = (w_gate, w_up, w_down, ws_gate, ws_up, ws_down)
         tensors = []
         for pair, name, (g, n, K) in zip(pairs, names, shapes):
             if pair is None:
@@ -355,11 +373,7 @@ class FMoE:
             _expect(pair[0], f"codes of {name}", torch.uint8, (g, n, K // 2), self.device)
             _expect(pair[1], f"scales of {name}", torch.uint8, (g, n, (K + QUANT_GROUP - 1) // QUANT_GROUP), self.device)
             tensors.append(C.byref(FmoeQuantTensor(pair[0].data_ptr(), pair[1].data_ptr())))
-        _check(self.lib.fmoe_set_weights_quant(self._ctx, _ptr(router_w), _ptr(router_bias), *tensors, _stream()))
-        self._weights = (router_w, router_bias, *pairs)
-        if release_packed:
-            torch.cuda.current_stream().synchronize()
-            self._weights = (router_bias,)
+        return tensors
 
     def workspace_bytes(self, max_tokens, max_seqs=1):
         return int(self.lib.fmoe_workspace_bytes(self._ctx, max_tokens, max_seqs))
@@ -475,6 +489,27 @@ class FMoE:
         _check(self.lib.fmoe_expert_ffn(self._ctx, _ptr(x), _ptr(kept_idx), n_kept, _ptr(n_kept_dev),
                                         _ptr(expert_offsets), _ptr(perm_src), _ptr(y), _ptr(ysh),
                                         _ptr(ws), ws.numel(), _stream()))
+        return y, ysh
+
+    def expert_ffn_quant_rows(self, codes, scales, kept_idx, n_kept, expert_offsets, perm_src, n_kept_dev=None):
+        """fmoe_expert_ffn_quant_rows: expert_ffn on rows in 8 bits as rms_norm_quant gives them, codes [T, d] (float8_e4m3fn or
+        their bytes) and scales [T, row_scales(d)]."""
+        T = codes.shape[0]
+        if codes.dtype not in (torch.float8_e4m3fn, torch.uint8):
+            raise TypeError(f"codes must be float8_e4m3fn or uint8, not {codes.dtype}")
+        if kept_idx is None and n_kept > T:
+            raise ValueError(f"{n_kept} rows of {T}")
+        _expect(codes, "codes", codes.dtype, (T, self.d), self.device)
+        _expect(scales, "scales", torch.uint8, (T, row_scales(self.d)), self.device)
+        K = max(self.kmax, 1)
+        y = torch.empty((max(n_kept * K, 1), self.d), dtype=torch.bfloat16, device=self.device)
+        ysh = None
+        if self.cfg.n_shared > 0:
+            ysh = torch.empty((self.cfg.n_shared, max(n_kept, 1), self.d), dtype=torch.bfloat16, device=self.device)
+        ws = self.workspace(n_kept, 1)
+        _check(self.lib.fmoe_expert_ffn_quant_rows(self._ctx, _ptr(codes), _ptr(scales), _ptr(kept_idx), n_kept, _ptr(n_kept_dev),
+                                                   _ptr(expert_offsets), _ptr(perm_src), _ptr(y), _ptr(ysh), _ptr(ws), ws.numel(),
+                                                   _stream()))
         return y, ysh
 
     def combine(self, y, y_shared, inv_perm, topk_gate, kept_idx, n_kept, residual=None,

@@ -104,6 +104,24 @@ int check_quant(const void* w, int32_t dtype, int64_t rows, int32_t K, const voi
   return FMOE_OK;
 }
 
+// Matrices in 4 bits to be registered; `pad`: what either side of a packed matrix is padded to at most
+int check_quant_tensors(const fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, size_t pad, const char* who) {
+  const fmoe_config& c = ctx->cfg;
+  const bool has_shared = c.n_shared > 0;
+  if (!has_shared && (w[3] || w[4] || w[5]))
+    return fmoe_fail(FMOE_ERR_BAD_SHAPE, "%s: shared-expert weights given but n_shared = 0", who);
+  for (int i = 0; i < (has_shared ? 6 : 3); ++i) {
+    if (!w[i] || !w[i]->codes || !w[i]->scales)
+      return fmoe_fail(FMOE_ERR_NULL_PTR, "%s: a weight matrix, its codes or its scales are NULL", who);
+    if (!aligned16(w[i]->codes))
+      return fmoe_fail(FMOE_ERR_INVALID_ARG, "%s: codes %p not 16-byte aligned", who, w[i]->codes);
+  }
+  const size_t widest = (size_t)c.n_shared * c.d_ffn_shared > (size_t)c.d_ffn ? (size_t)c.n_shared * c.d_ffn_shared : (size_t)c.d_ffn;
+  if (((size_t)c.d_model + pad) * (widest + pad) > 0xffffffffull)   // 32-bit offsets inside a packed matrix
+    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "%s: a matrix of %d x %zu weights", who, c.d_model, widest);
+  return FMOE_OK;
+}
+
 // Arguments that the norms share
 int check_norm(int32_t dtype, int32_t weight_dtype, int32_t T, int32_t d, float eps, const char* who) {
   if ((dtype != FMOE_F32 && dtype != FMOE_BF16) || (weight_dtype != FMOE_F32 && weight_dtype != FMOE_BF16))
@@ -227,6 +245,8 @@ void fmoe_destroy(fmoe_ctx* ctx) {
     if (p) (void)hipFree(p);
   for (void* p : ctx->pq)
     if (p) (void)hipFree(p);
+  for (void* p : ctx->pr)
+    if (p) (void)hipFree(p);
   delete ctx;
 }
 
@@ -321,20 +341,8 @@ int fmoe_set_weights_quant(fmoe_ctx* ctx, const void* router_w, const float* rou
   if (rc != FMOE_OK) return rc;
   if (ctx->cfg.dtype != FMOE_BF16)
     return fmoe_fail(FMOE_ERR_UNSUPPORTED, "fmoe_set_weights_quant: 4-bit weights need a bf16 context");
-  const bool has_shared = ctx->cfg.n_shared > 0;
-  if (!has_shared && (ws_gate || ws_up || ws_down))
-    return fmoe_fail(FMOE_ERR_BAD_SHAPE, "fmoe_set_weights_quant: shared-expert weights given but n_shared = 0");
   const fmoe_quant_tensor* const w[6] = {w_gate, w_up, w_down, ws_gate, ws_up, ws_down};
-  for (int i = 0; i < (has_shared ? 6 : 3); ++i) {
-    if (!w[i] || !w[i]->codes || !w[i]->scales)
-      return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_set_weights_quant: a weight matrix, its codes or its scales are NULL");
-    if (!aligned16(w[i]->codes))
-      return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_set_weights_quant: codes %p not 16-byte aligned", w[i]->codes);
-  }
-  const fmoe_config& c = ctx->cfg;
-  const size_t widest = (size_t)c.n_shared * c.d_ffn_shared > (size_t)c.d_ffn ? (size_t)c.n_shared * c.d_ffn_shared : (size_t)c.d_ffn;
-  if (((size_t)c.d_model + 64) * (widest + 64) > 0xffffffffull)   // 32-bit offsets inside a packed matrix
-    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "fmoe_set_weights_quant: a matrix of %d x %zu weights", c.d_model, widest);
+  if ((rc = check_quant_tensors(ctx, w, 64, "fmoe_set_weights_quant")) != FMOE_OK) return rc;
   if (!router_w) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_set_weights_quant: router_w is NULL");
   if (!aligned16(router_w) || !aligned16(router_bias))
     return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_set_weights_quant: router_w / router_bias not 16-byte aligned");
@@ -349,6 +357,30 @@ int fmoe_set_weights_quant(fmoe_ctx* ctx, const void* router_w, const float* rou
   if ((rc = launch_pack_quant(ctx, w, s)) != FMOE_OK) return rc;
   ctx->quant = true;
   ctx->weights_set = true;
+  return FMOE_OK;
+}
+
+int fmoe_set_weights_quant_rows(fmoe_ctx* ctx, const fmoe_quant_tensor* w_gate, const fmoe_quant_tensor* w_up,
+                                const fmoe_quant_tensor* w_down, const fmoe_quant_tensor* ws_gate,
+                                const fmoe_quant_tensor* ws_up, const fmoe_quant_tensor* ws_down, void* stream) {
+  int rc = check_ctx(ctx, false);
+  if (rc != FMOE_OK) return rc;
+  const fmoe_config& c = ctx->cfg;
+  if (c.dtype != FMOE_BF16)
+    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "fmoe_set_weights_quant_rows: 4-bit weights need a bf16 context");
+  if (c.d_model % 32 || c.d_ffn % 32 || (c.n_shared > 0 && c.d_ffn_shared % 32))
+    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "fmoe_set_weights_quant_rows: d_model, d_ffn and d_ffn_shared must be multiples of 32");
+  const fmoe_quant_tensor* const w[6] = {w_gate, w_up, w_down, ws_gate, ws_up, ws_down};
+  if ((rc = check_quant_tensors(ctx, w, 128, "fmoe_set_weights_quant_rows")) != FMOE_OK) return rc;
+  ctx->rows8_set = false;
+  for (int i = 0; i < 4; ++i) {
+    const size_t bytes = fmoe_rows8_bytes(ctx, i);
+    if (bytes == 0 || ctx->pr[i]) continue;
+    FMOE_HIP_CHECK(hipSetDevice(ctx->device));
+    FMOE_HIP_CHECK(hipMalloc(&ctx->pr[i], bytes));
+  }
+  if ((rc = launch_pack_rows8(ctx, w, static_cast<hipStream_t>(stream))) != FMOE_OK) return rc;
+  ctx->rows8_set = true;
   return FMOE_OK;
 }
 
@@ -533,6 +565,29 @@ int fmoe_expert_ffn(fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int32
   return launch_expert_ffn(ctx, x, kept_idx, n_kept, n_kept_dev, expert_offsets, perm_src, y,
                            ctx->cfg.n_shared > 0 ? y_shared : nullptr, ws, L, false,
                            static_cast<hipStream_t>(stream));
+}
+
+int fmoe_expert_ffn_quant_rows(fmoe_ctx* ctx, const uint8_t* codes, const uint8_t* scales, const int32_t* kept_idx,
+                               int32_t n_kept, const int32_t* n_kept_dev, const int32_t* expert_offsets,
+                               const int32_t* perm_src, void* y, void* y_shared, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_ctx(ctx, false);
+  if (rc != FMOE_OK) return rc;
+  if ((rc = check_tokens(n_kept)) != FMOE_OK) return rc;
+  if ((rc = check_ffn_extent(ctx, n_kept, "fmoe_expert_ffn_quant_rows")) != FMOE_OK) return rc;
+  if (!ctx->rows8_set)
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_set_weights_quant_rows has not been called on this context");
+  if (n_kept == 0) return FMOE_OK;
+  if (!codes || !scales) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_expert_ffn_quant_rows: codes / scales is NULL");
+  if (ctx->kmax > 0 && (!expert_offsets || !perm_src || !y))
+    return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_expert_ffn_quant_rows: expert_offsets / perm_src / y is NULL");
+  if (ctx->cfg.n_shared > 0 && !y_shared)
+    return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_expert_ffn_quant_rows: y_shared is NULL but n_shared = %d", ctx->cfg.n_shared);
+  if (!aligned16(codes) || !aligned16(y) || !aligned16(y_shared) || (reinterpret_cast<uintptr_t>(scales) & 3u))
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_expert_ffn_quant_rows: codes / y / y_shared not 16-byte or scales not 4-byte aligned");
+  if ((rc = check_ws(ctx, ws, ws_bytes, n_kept, 1)) != FMOE_OK) return rc;
+  const fmoe_ws_layout L = fmoe_layout(ctx, n_kept, 1);
+  return launch_expert_ffn_rows8(ctx, codes, scales, kept_idx, n_kept, n_kept_dev, expert_offsets, perm_src, y,
+                                 ctx->cfg.n_shared > 0 ? y_shared : nullptr, ws, L, static_cast<hipStream_t>(stream));
 }
 
 int fmoe_combine(fmoe_ctx* ctx, const void* y, const void* y_shared, const int32_t* inv_perm,

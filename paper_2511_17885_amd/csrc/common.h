@@ -68,6 +68,8 @@ struct fmoe_ctx {
   // bf16 contexts: private copies of the expert weights in matrix-core operand order (ffn.hip)
   void *pk_gate_up, *pk_down, *pk_sgate_up, *pk_sdown;
   void* pq[4];               // the same of 4-bit weights (ffn_quant.hip): gate/up, down, shared gate/up, shared down
+  void* pr[4];               // 4-bit weights for rows in 8 bits (ffn_rows8.hip)
+  bool rows8_set;
   bool quant;                // the weights in force are the 4-bit ones
   bool weights_set;
   int sel_strategy, sel_k_base;   // selection-strategy ablation (fmoe_set_selection); 0 = off
@@ -135,6 +137,11 @@ int launch_pack_experts(fmoe_ctx* ctx, hipStream_t stream);
 // bytes of the packed 4-bit weights of matrix `which` (as above) and, if asked for, how many of them are codes
 size_t fmoe_quant_bytes(const fmoe_ctx* ctx, int which, size_t* codes);
 int launch_pack_quant(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStream_t stream);
+size_t fmoe_rows8_bytes(const fmoe_ctx* ctx, int which);
+int launch_pack_rows8(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStream_t stream);
+int launch_expert_ffn_rows8(const fmoe_ctx* ctx, const uint8_t* codes, const uint8_t* scales, const int32_t* kept_idx, int n_cap,
+                            const int32_t* n_dev, const int32_t* expert_offsets, const int32_t* perm_src, void* y, void* y_shared,
+                            void* ws, const fmoe_ws_layout& L, hipStream_t stream);
 enum quant_form { QUANT_THIN, QUANT_NARROW, QUANT_MIDDLE, QUANT_DENSE };   // (only the last one needs tile lists)
 quant_form quant_ffn_form(const fmoe_ctx* ctx, int n_cap);
 int run_ffn_quant(const fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,

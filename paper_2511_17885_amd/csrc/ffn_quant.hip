@@ -14,6 +14,7 @@
 // and four k tiles' words are one 16-byte unit per column: 17 bits per four weights in two linear streams.
 
 #include "ffn_dev.h"
+#include "quant_items.h"
 
 namespace {
 
@@ -378,72 +379,6 @@ struct QuantListArgs {
   int shared_groups, shared_cols;  // shared groups in this launch, column units of one
   int log2_bm;                     // rows of a row tile (narrow kernel)
 };
-struct QuantItem {
-  int group, unit, row0, rows;     // group < 0: none
-  bool shared;
-};
-// Row tiles of 1 << a.log2_bm rows.  Experts whose offsets are malformed are skipped as in fmoe_build_tiles.  Uniform.
-__device__ __forceinline__ QuantItem find_tile(const QuantListArgs& a, int block) {
-  constexpr int Q = FMOE_MAX_EXPERTS / 64;
-  const int lane = threadIdx.x & 63, bm = 1 << a.log2_bm;
-  int r0[Q], cnt[Q], first[Q];   // of expert 64 q + lane: first row, rows, first tile
-  int tiles = 0;
-#pragma unroll
-  for (int q = 0; q < Q; ++q) {
-    const int e = 64 * q + lane;
-    r0[q] = cnt[q] = 0;
-    if (64 * q < a.E && a.row_cap > 0) {   // uniform
-      const int at = e < a.E ? e : a.E - 1;
-      r0[q] = a.expert_offsets[at];
-      cnt[q] = a.expert_offsets[at + 1];
-    }
-  }
-#pragma unroll
-  for (int q = 0; q < Q; ++q) {
-    const bool good = 64 * q + lane < a.E && r0[q] >= 0 && cnt[q] > r0[q] && cnt[q] <= a.row_cap;
-    cnt[q] = good ? cnt[q] - r0[q] : 0;
-    const int nt = (cnt[q] + bm - 1) >> a.log2_bm;
-    const int scan = wave_scan(nt);
-    first[q] = tiles + scan - nt;
-    tiles += __builtin_amdgcn_readlane(scan, 63);
-  }
-  const int n = resolve_count(a.n_cap, a.n_dev);
-  const int shared_tiles = (n + bm - 1) >> a.log2_bm, per_group = shared_tiles * a.shared_cols;
-  const int shared_items = per_group * a.shared_groups;
-  const int items = shared_items + tiles * a.cols, share = (items + 7) >> 3;
-  QuantItem it{-1, 0, 0, 0, false};
-  const int place = block >> 3;
-  int g = (block & 7) * share + place;
-  if (place >= share || g >= items) return it;
-  if (g < shared_items) {
-    it.shared = true;
-    it.group = g / per_group;
-    g -= it.group * per_group;
-    it.unit = g / shared_tiles;
-    it.row0 = (g - it.unit * shared_tiles) * bm;
-    it.rows = n - it.row0 < bm ? n - it.row0 : bm;
-    return it;
-  }
-  g -= shared_items;
-  const int tile = g / a.cols;
-#pragma unroll
-  for (int q = 0; q < Q; ++q) {
-    const int nt = (cnt[q] + bm - 1) >> a.log2_bm;
-    const unsigned long long mine = __ballot(first[q] <= tile && tile < first[q] + nt);
-    if (mine != 0) {   // in one q only
-      const int at = __ffsll((long long)mine) - 1;
-      const int e_first = __builtin_amdgcn_readlane(first[q], at), e_tiles = __builtin_amdgcn_readlane(nt, at);
-      const int e_rows = __builtin_amdgcn_readlane(cnt[q], at);
-      g -= e_first * a.cols;
-      it.group = 64 * q + at;
-      it.unit = g / e_tiles;
-      const int row = (g - it.unit * e_tiles) * bm;
-      it.row0 = __builtin_amdgcn_readlane(r0[q], at) + row;
-      it.rows = e_rows - row < bm ? e_rows - row : bm;
-    }
-  }
-  return it;
-}
 // One row tile an expert, whatever its rows; workgroup = place in the sequence.  Without the sums over all experts and the
 // shares: a token or two are all latency (one token, d 2048, 64 experts of 1408 and two shared 15.1 -> 13.6 us).
 __device__ __forceinline__ QuantItem find_expert(const QuantListArgs& a, int item) {
@@ -610,20 +545,6 @@ __global__ __launch_bounds__(256) void pack_quant_kernel(const uint32_t* __restr
 // 16-byte units of one packed group: column tiles (of four column blocks) times k tiles
 inline size_t code_units(int nbw, int K) { return (size_t)((nbw + 3) / 4) * quant_tiles(K) * 256; }
 inline size_t scale_units(int nbw, int K) { return (size_t)((nbw + 3) / 4) * quant_scale_tiles(K) * 64; }
-
-struct PackedMatrix {
-  int groups, nbw, N, K;
-};
-// 0 gate/up, 1 down, 2 shared gate/up, 3 shared down
-PackedMatrix packed_matrix(const fmoe_config& c, int which) {
-  const int Ft = c.n_shared * c.d_ffn_shared;
-  switch (which) {
-    case 0: return {c.n_experts, (c.d_ffn + 15) / 16, c.d_ffn, c.d_model};
-    case 1: return {c.n_experts, (c.d_model + 31) / 32, c.d_model, c.d_ffn};
-    case 2: return {Ft > 0 ? 1 : 0, (Ft + 15) / 16, Ft, c.d_model};
-    default: return {Ft > 0 ? c.n_shared : 0, (c.d_model + 31) / 32, c.d_model, Ft > 0 ? c.d_ffn_shared : 8};
-  }
-}
 
 }  // namespace
 

@@ -5,6 +5,7 @@
 // or where there are few rows), reads it once and writes its outputs once.
 
 #include "norm_dev.h"
+#include "rows8_dev.h"
 
 namespace {
 
@@ -21,14 +22,6 @@ struct NormArgs {
   uint8_t* scales;      // [T, scale_stride]
   int scale_stride;     // groups of 32, rounded up to words
 };
-
-// Largest of the magnitudes' bits over four neighbouring lanes
-__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
-  uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, false);   // lanes 1 0 3 2
-  v = v > o ? v : o;
-  o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false);            // lanes 2 3 0 1
-  return v > o ? v : o;
-}
 
 // A sum over the wavefronts of a workgroup that share a row (WPR of them); s_part: 4 doubles
 template <int WPR>
@@ -100,37 +93,18 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
         n.set2(e, value_rounded<XT>(h[i].get(e), w[e], r), value_rounded<XT>(h[i].get(e + 1), w[e + 1], r));
       if (in) n.store(static_cast<XT*>(a.n) + base + u * 8);
     } else {
-      // The group's scale: the least power of two with the largest magnitude at most 448 = 1.75 * 2^8 of it, at least 2^-126.
-      // Values rounded to odd keep what is needed to see that and to round to 4 significant bits.
+      // values rounded to odd keep what the choice of the scale and the rounding to 4 significant bits need
       float v[8];
-      uint32_t big = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float hi, lo;
         value(h[i].get(e), w[e], r, hi, lo);
         v[e] = in ? odd(hi, lo) : 0.0f;
-        const uint32_t m = __float_as_uint(v[e]) & 0x7fffffffu;
-        big = big > m ? big : m;
       }
-      big = quad_max(big);
-      int e8 = (int)(big >> 23) - 8 + ((big & 0x7fffffu) > 0x600000u ? 1 : 0);
-      e8 = e8 < 1 ? 1 : e8;
-      if (big == 0u) e8 = 127;
-      const bool finite_group = big < 0x7f800000u;
-      const float scale = __uint_as_float((uint32_t)(finite_group ? e8 : 127) << 23);
-      typedef short s16x2_t __attribute__((ext_vector_type(2)));
-      s16x2_t c0 = {0, 0}, c1 = {0, 0};
-      c0 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c0, v[0], v[1], scale, false);
-      c0 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c0, v[2], v[3], scale, true);
-      c1 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c1, v[4], v[5], scale, false);
-      c1 = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c1, v[6], v[7], scale, true);
-      if (in) {
-        uint2 c = {__builtin_bit_cast(uint32_t, c0), __builtin_bit_cast(uint32_t, c1)};
-        if (!finite_group) c = uint2{0u, 0u};
-        *reinterpret_cast<uint2*>(reinterpret_cast<char*>(a.codes) + base + u * 8) = c;
-      }
-      if ((u & 3) == 0 && (u >> 2) < a.scale_stride)
-        a.scales[(size_t)row * a.scale_stride + (u >> 2)] = (uint8_t)(finite_group ? e8 : 255);
+      uint32_t scale;
+      const uint2 c = rows8::quantize(v, scale);
+      if (in) *reinterpret_cast<uint2*>(reinterpret_cast<char*>(a.codes) + base + u * 8) = c;
+      if ((u & 3) == 0 && (u >> 2) < a.scale_stride) a.scales[(size_t)row * a.scale_stride + (u >> 2)] = (uint8_t)scale;
     }
   }
 }
