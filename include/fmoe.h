@@ -14,7 +14,7 @@
  *    library only borrows them for the duration of the enqueued work.
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All work is
  *    enqueued asynchronously on it; no call synchronises with the host and no hot call
- *    (route / select_experts and its backward / prune / permute / expert_ffn, also on 8-bit rows / combine / layer_forward / quantize_weights
+ *    (route / select_experts and its backward / prune / permute / expert_ffn, also on 8-bit rows / combine / layer_forward / layer_decode / quantize_weights
  *    / dequantize_weights / rms_norm, its form with 8-bit rows and its backward) allocates memory.
  *    Scratch comes from a caller-provided workspace sized by fmoe_workspace_bytes().  A hot call
  *    is a sequence of kernel launches and nothing else (no memset, no copy), so it can be
@@ -107,6 +107,13 @@ typedef struct {
   int32_t group_score;  /* a group's score: 0 its largest key, 1 the sum of its two largest keys          */
   float gate_scale;     /* factor of every gate, finite                                                   */
 } fmoe_select_params;
+
+/* A root-mean-square norm (fmoe_rms_norm): weight [d_model] of weight_dtype, 16-byte aligned. */
+typedef struct {
+  const void* weight;
+  int32_t weight_dtype; /* fmoe_dtype */
+  float eps;
+} fmoe_norm_params;
 
 /* A matrix [rows, K] (K the length of the reduction) in 4 bits: codes [rows, K/2] bytes, element 2i in the low
  * half of byte i and element 2i+1 in the high half; scales [rows, ceil(K/32)] bytes, one for 32 neighbours of a row (the
@@ -395,6 +402,21 @@ int fmoe_layer_forward(fmoe_ctx* ctx, const fmoe_prune_params* params, const voi
                        const float* attn_importance, int add_residual, void* out,
                        int32_t* kept_idx, int32_t* new_cu_seqlens, uint8_t* is_visual_out,
                        void* ws, size_t ws_bytes, void* stream);
+
+/* The whole layer for a decoding step, at most 16 tokens, nothing pruned (bf16 contexts, weights of fmoe_set_weights or
+ * fmoe_set_weights_quant):  h = x + delta;  n = norm(h);  out = h + MoE(n)  (out = MoE(n) without add_residual).
+ * x, delta, out [T, d_model] bf16; delta NULL: h = x; norm NULL: n = h.  h and n are those of fmoe_rms_norm, n rounded to bf16.
+ * Logits: router_w n + router_bias, added up in 64 bits, rounded to fp32 once (so they may differ from fmoe_route's in the last
+ * bits); experts and gates from them as in fmoe_select_experts with params and select_bias, params NULL: softmax over the experts.
+ * is_visual [T] or NULL as there.  The activation silu(.)*(.) is rounded to bf16 between the two products; gates, experts,
+ * shared experts and residual are added up in fp32 in a fixed order, with one rounding.
+ * topk_idx [T,Kmax] and topk_gate [T,Kmax] as fmoe_select_experts writes them, or NULL.  out may be x or delta.
+ * ws: fmoe_layer_decode_workspace_bytes(ctx, T) bytes, 256-byte aligned.  fmoe_set_selection and fmoe_set_ffn_shape have no effect here.
+ * More than 16 tokens, fp32 contexts and d_model above 16384 are FMOE_ERR_UNSUPPORTED. */
+size_t fmoe_layer_decode_workspace_bytes(const fmoe_ctx* ctx, int32_t T);   /* [host] */
+int fmoe_layer_decode(fmoe_ctx* ctx, const fmoe_select_params* params, const fmoe_norm_params* norm, const void* x,
+                      const void* delta, const uint8_t* is_visual, const float* select_bias, int32_t T, int add_residual,
+                      void* out, int32_t* topk_idx, float* topk_gate, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- the layer stack: per-layer expert activation (Sec. 3.1) and pruning stages (Sec. 3.2, App. D) ----
  *

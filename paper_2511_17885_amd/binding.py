@@ -29,7 +29,8 @@ EXPORTS = ["fmoe_version", "fmoe_last_error", "fmoe_create", "fmoe_destroy", "fm
            "fmoe_stack_forward", "fmoe_permute_noalloc", "fmoe_set_ffn_shape", "fmoe_set_weights_quant",
            "fmoe_quantize_weights", "fmoe_dequantize_weights", "fmoe_select_experts", "fmoe_select_experts_backward",
            "fmoe_rms_norm", "fmoe_rms_norm_quant", "fmoe_rms_norm_workspace_bytes", "fmoe_rms_norm_backward",
-           "fmoe_set_weights_quant_rows", "fmoe_expert_ffn_quant_rows"]
+           "fmoe_set_weights_quant_rows", "fmoe_expert_ffn_quant_rows", "fmoe_layer_decode",
+           "fmoe_layer_decode_workspace_bytes"]
 
 
 class FmoeConfig(C.Structure):
@@ -62,6 +63,10 @@ class FmoeSelectParams(C.Structure):
 
 class FmoeQuantTensor(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class FmoeNormParams(C.Structure):
+    _fields_ = [("weight", C.c_void_p), ("weight_dtype", C.c_int32), ("eps", C.c_float)]
 
 
 class FmoeError(RuntimeError):
@@ -118,6 +123,9 @@ def load():
     lib.fmoe_combine.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
     lib.fmoe_layer_forward.argtypes = [vp, C.POINTER(FmoePruneParams), vp, vp, vp, i32, i32, vp,
                                        C.c_int, vp, vp, vp, vp, vp, sz, vp]
+    lib.fmoe_layer_decode_workspace_bytes.argtypes = [vp, i32]
+    lib.fmoe_layer_decode_workspace_bytes.restype = sz
+    lib.fmoe_layer_decode.argtypes = [vp, sp, C.POINTER(FmoeNormParams), vp, vp, vp, vp, i32, C.c_int, vp, vp, vp, vp, sz, vp]
     lib.fmoe_adjacent_similarity.argtypes = [vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
     lib.fmoe_magnitude_stability.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
     lib.fmoe_row_cosine.argtypes = [vp, vp, vp, i32, vp, vp, vp]
@@ -139,7 +147,8 @@ def load():
     lib.fmoe_profile_read.argtypes = [vp, C.POINTER(C.c_float)]
     for name in EXPORTS:
         if name not in ("fmoe_version", "fmoe_last_error", "fmoe_destroy", "fmoe_workspace_bytes",
-                        "fmoe_profile_name", "fmoe_stack_workspace_bytes", "fmoe_rms_norm_workspace_bytes"):
+                        "fmoe_profile_name", "fmoe_stack_workspace_bytes", "fmoe_rms_norm_workspace_bytes",
+                        "fmoe_layer_decode_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -541,6 +550,33 @@ class FMoE:
                                            _stream()))
         return out, kept_idx, new_cu, is_visual_out
 
+
+    def layer_decode(self, x, is_visual=None, norm=None, delta=None, params=None, select_bias=None, add_residual=True, out=None):
+        """fmoe_layer_decode: the layer for a decoding step, x [T, d] with at most 16 tokens.  norm: (weight [d], eps) or None;
+        delta [T, d]: added to x first; params: select_params(...), None for a softmax router.  Returns (out [T, d], topk_idx, topk_gate)."""
+        T, K = x.shape[0], max(self.kmax, 1)
+        _expect(x, "x", self.torch_dtype, (T, self.d), self.device)
+        _expect(delta, "delta", self.torch_dtype, (T, self.d), self.device)
+        _expect(is_visual, "is_visual", torch.uint8, (T,), self.device)
+        _expect(select_bias, "select_bias", torch.float32, (self.E,), self.device)
+        _expect(out, "out", self.torch_dtype, (T, self.d), self.device)
+        normed = None
+        if norm is not None:
+            weight, eps = norm
+            normed = C.byref(FmoeNormParams(weight.data_ptr(), _float_type(weight, "weight"), eps))
+            _expect(weight, "weight", weight.dtype, (self.d,), self.device)
+        if out is None:
+            out = torch.empty_like(x)
+        idx, gate = self._i32(T, K), self._f32(T, K)
+        need = int(self.lib.fmoe_layer_decode_workspace_bytes(self._ctx, T))
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        _check(self.lib.fmoe_layer_decode(self._ctx, C.byref(params) if params is not None else None, normed, _ptr(x), _ptr(delta),
+                                          _ptr(is_visual), _ptr(select_bias), T, int(bool(add_residual)), _ptr(out), _ptr(idx),
+                                          _ptr(gate), _ptr(self._ws), self._ws.numel(), _stream()))
+        if self.kmax == 0:
+            idx, gate = idx[:, :0], gate[:, :0]
+        return out, idx, gate
 
     # ---- diagnostics
     def adjacent_similarity(self, probs, is_visual, cu_seqlens):

@@ -30,6 +30,7 @@ SOURCES = {
     "quant.hip": [],
     "norm.hip": ["-ffp-contract=off"],
     "combine.hip": [],
+    "decode.hip": ["-ffp-contract=off"],
     "diag.hip": [],
     "stack.hip": [],
     "noalloc.hip": [],

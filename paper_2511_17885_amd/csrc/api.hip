@@ -749,6 +749,40 @@ int fmoe_layer_forward(fmoe_ctx* ctx, const fmoe_prune_params* params, const voi
                         out, s);
 }
 
+size_t fmoe_layer_decode_workspace_bytes(const fmoe_ctx* ctx, int32_t T) {
+  if (!ctx || T < 0 || T > FMOE_DECODE_TOKENS) return 0;
+  return fmoe_layout(ctx, T, 1).total + align_up(decode_part_bytes(ctx, T > 0 ? T : 1));
+}
+
+int fmoe_layer_decode(fmoe_ctx* ctx, const fmoe_select_params* params, const fmoe_norm_params* norm, const void* x,
+                      const void* delta, const uint8_t* is_visual, const float* select_bias, int32_t T, int add_residual,
+                      void* out, int32_t* topk_idx, float* topk_gate, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_ctx(ctx, false);
+  if (rc != FMOE_OK) return rc;
+  if (ctx->cfg.dtype != FMOE_BF16) return fmoe_fail(FMOE_ERR_UNSUPPORTED, "fmoe_layer_decode: a bf16 context is needed");
+  if ((rc = check_tokens(T)) != FMOE_OK) return rc;
+  if (T > FMOE_DECODE_TOKENS) return fmoe_fail(FMOE_ERR_UNSUPPORTED, "fmoe_layer_decode: %d tokens > %d", T, FMOE_DECODE_TOKENS);
+  if (params && (rc = check_select(ctx, params, FMOE_F32, "fmoe_layer_decode")) != FMOE_OK) return rc;
+  if (ctx->cfg.d_model > FMOE_NORM_MAX_D)
+    return fmoe_fail(FMOE_ERR_UNSUPPORTED, "fmoe_layer_decode: d_model %d > %d", ctx->cfg.d_model, FMOE_NORM_MAX_D);
+  if (norm) {
+    if ((rc = check_norm(FMOE_BF16, norm->weight_dtype, T, ctx->cfg.d_model, norm->eps, "fmoe_layer_decode")) != FMOE_OK) return rc;
+    if (!norm->weight) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_layer_decode: the norm's weight is NULL");
+    if (!aligned16(norm->weight)) return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_layer_decode: the norm's weight is not 16-byte aligned");
+  }
+  if ((rc = check_ctx(ctx, true)) != FMOE_OK) return rc;
+  if (T == 0) return FMOE_OK;
+  if (!x || !out) return fmoe_fail(FMOE_ERR_NULL_PTR, "fmoe_layer_decode: x / out is NULL");
+  if (!aligned16(x) || !aligned16(delta) || !aligned16(out) || !aligned16(select_bias))
+    return fmoe_fail(FMOE_ERR_INVALID_ARG, "fmoe_layer_decode: x / delta / out / select_bias not 16-byte aligned");
+  if (!ws) return fmoe_fail(FMOE_ERR_WORKSPACE, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(ws) & 255u) return fmoe_fail(FMOE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  const size_t need = fmoe_layer_decode_workspace_bytes(ctx, T);
+  if (ws_bytes < need) return fmoe_fail(FMOE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed for %d tokens", ws_bytes, need, T);
+  return launch_layer_decode(ctx, params, norm, x, delta, is_visual, select_bias, T, add_residual, out, topk_idx, topk_gate, ws,
+                             fmoe_layout(ctx, T, 1), static_cast<hipStream_t>(stream));
+}
+
 int fmoe_adjacent_similarity(fmoe_ctx* ctx, const float* probs, const uint8_t* is_visual,
                              const int32_t* cu_seqlens, int32_t B, int32_t T, float* pair_sim, float* mean,
                              int32_t* count, void* stream) {

@@ -14,6 +14,7 @@
 #define FMOE_NORM_MAX_D 16384    // longest row of the norms
 #define FMOE_PERM_BLOCK 256   // kept positions per block in the permutation kernels
 #define FMOE_ROUTE_DISPATCH_TOKENS 16   // tokens up to which the router's one block does the dispatch too
+#define FMOE_DECODE_TOKENS 16     // tokens up to which fmoe_layer_decode takes a call
 #define FMOE_TILE_M 64        // rows per grouped-GEMM tile (tile list granularity)
 #define FMOE_TILE_RUN 8       // row tiles per run of a group in the tile lists
 #define FMOE_DENSE_TILE_RUN 64   // the same for the dense shape
@@ -237,6 +238,12 @@ int launch_quantize(const void* w, int dtype, long long rows, int K, int saturat
                     hipStream_t stream);
 int launch_dequantize(const void* codes, const uint8_t* scales, long long rows, int K, int dtype, void* w,
                       hipStream_t stream);
+
+// ---- a layer for a few tokens (decode.hip)
+size_t decode_part_bytes(const fmoe_ctx* ctx, int T);
+int launch_layer_decode(const fmoe_ctx* ctx, const fmoe_select_params* params, const fmoe_norm_params* norm, const void* x,
+                        const void* delta, const uint8_t* is_visual, const float* select_bias, int T, int add_residual, void* out,
+                        int32_t* topk_idx, float* topk_gate, void* ws, const fmoe_ws_layout& L, hipStream_t stream);
 
 // ---- norms (norm.hip).  codes: rows in 8 bits instead of n
 int launch_rms_norm(const void* x, const void* delta, const void* weight, int dtype, int weight_dtype, int T, int d, float eps,

@@ -18,8 +18,6 @@
 
 namespace {
 
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-
 struct QuantProblem {
   StreamProblem s;            // Bp: codes, group_stride in 16-byte units
   const u32x4_t* Sp;          // scales
@@ -37,17 +35,6 @@ struct QuantArgs {
 
 __host__ __device__ inline int quant_tiles(int K) { return (K + SBK - 1) / SBK; }
 __host__ __device__ inline int quant_scale_tiles(int K) { return (quant_tiles(K) + 3) / 4; }
-
-// Eight codes times the scale in byte I of `scales`.  The instruction takes the exponent of its scale operand and nothing else
-// (checked on the card for every exponent with thousands of other bits): the byte is only shifted there.
-template <int I>
-__device__ __forceinline__ u32x4_t dequantize(uint32_t codes, uint32_t scales) {
-  const float s = __uint_as_float(I == 0 ? scales << 23 : I == 1 ? scales << 15 : I == 2 ? scales << 7 : scales >> 1);
-  return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3))};
-}
 
 // One wavefront, one column block, sixteen rows: codes, scales and rows straight into registers in matrix order, no LDS and
 // no barrier, for calls of at most THIN_ROWS tokens, where the weights are all there is to move.  Rows past the tile reuse

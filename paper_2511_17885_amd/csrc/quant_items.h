@@ -1,10 +1,21 @@
-// Work items of the expert products on 4-bit weights, found from the experts' offsets, and the shapes of the packed matrices.
+// Expert products on 4-bit weights: codes to bf16 operands, work items found from the experts' offsets, shapes of the packed matrices.
 #pragma once
 
-#include "common.h"
+#include "ffn_dev.h"
 
 #if defined(__HIPCC__)
 namespace {
+
+// Eight codes times the scale in byte I of `scales`.  The instruction takes the exponent of its scale operand and nothing else
+// (checked on the card for every exponent with thousands of other bits): the byte is only shifted there.
+template <int I>
+__device__ __forceinline__ u32x4_t dequantize(uint32_t codes, uint32_t scales) {
+  const float s = __uint_as_float(I == 0 ? scales << 23 : I == 1 ? scales << 15 : I == 2 ? scales << 7 : scales >> 1);
+  return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3))};
+}
 
 struct QuantItem {
   int group, unit, row0, rows;     // group < 0: none

@@ -1,0 +1,302 @@
+"""A whole layer for a few tokens in one call: norm, router, choice, experts, gates and residual, against the steps in 64 bits."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2511_17885_amd import binding
+from test_quant_weights import _ffn, _pack, _values
+
+U = 2.0 ** -24
+HALF_BF16 = 2.0 ** -8
+EPS = 1e-5
+
+
+class _Layer:
+    """A layer on the GPU with bf16 or 4-bit weights, and its matrices in 64 bits."""
+
+    def __init__(self, rng, d, E, F, shared=0, F_shared=0, k_text=2, k_visual=1, quant=False, bias=False, renormalize=True):
+        shapes = [(E, F, d), (E, F, d), (E, d, F)] + ([(shared, F_shared, d)] * 2 + [(shared, d, F_shared)] if shared else [])
+        self.router = (torch.from_numpy(rng.standard_normal((E, d)).astype(np.float32)) / math.sqrt(d)).to(torch.bfloat16)
+        self.bias = torch.from_numpy(rng.standard_normal(E).astype(np.float32)) if bias else None
+        self.m = binding.FMoE(d_model=d, n_experts=E, d_ffn=F, n_shared=shared, d_ffn_shared=F_shared, k_text=k_text,
+                              k_visual=k_visual, dtype="bf16", renormalize=renormalize)
+        self.bias_gpu = None if self.bias is None else self.bias.cuda()
+        if quant:
+            host = []
+            for g, n, K in shapes:
+                codes = rng.integers(0, 16, (g, n, K)).astype(np.uint8)
+                scale = 127 - int(round(math.log2(K) / 2)) - 1
+                host.append((codes, (scale + rng.integers(-1, 2, (g, n, -(-K // 32)))).astype(np.uint8)))
+            self.w = [_values(*h) for h in host]
+            pairs = [(torch.from_numpy(_pack(c)).cuda(), torch.from_numpy(s).cuda()) for c, s in host]
+            self.m.set_weights_quant(self.router.cuda(), self.bias_gpu, *pairs)
+        else:
+            host = [(torch.from_numpy(rng.standard_normal(s).astype(np.float32)) * 1.4 / math.sqrt(s[2])).to(torch.bfloat16) for s in shapes]
+            self.w = [h.double().numpy() for h in host]
+            self.m.set_weights(self.router.cuda(), self.bias_gpu, *[h.cuda() for h in host])
+        self.shared = shared
+
+
+def _bf16(rng, *shape):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(torch.bfloat16).cuda()
+
+
+def _expected(layer, h, n, idx, gate):
+    """out in 64 bits from n and the choice, and how far a correct kernel may be from it: the experts' own bounds (with a rounding
+    of their outputs that is not made here), a rounding of every addition in fp32 and the last one."""
+    n64, idx, gate = n.double().cpu().numpy(), idx.cpu().numpy(), gate.double().cpu().numpy()
+    want = np.zeros(n64.shape) if h is None else h.double().cpu().numpy()
+    slack, sizes, terms = np.zeros(n64.shape), np.abs(want), 1
+    for i in range(layer.shared):
+        y, e = _ffn(n64, *[w[i] for w in layer.w[3:]])
+        want, slack, sizes, terms = want + y, slack + e, sizes + np.abs(y), terms + 1
+    for e in np.unique(idx[idx >= 0]):
+        t = (idx == e).any(1)
+        g = (gate * (idx == e)).sum(1)[t, None]
+        y, s = _ffn(n64[t], *[w[e] for w in layer.w[:3]])
+        want[t] += g * y
+        slack[t] += np.abs(g) * s
+        sizes[t] += np.abs(g * y)
+    slack = slack + (terms + 2 * idx.shape[1] + 16) * U * sizes
+    return want, slack + HALF_BF16 * (np.abs(want) + slack) + 2.0 ** -133
+
+
+def _check(layer, x, delta=None, norm=None, is_visual=None, params=None, select_bias=None, add_residual=True):
+    m = layer.m
+    T = x.shape[0]
+    out, idx, gate = m.layer_decode(x, is_visual, norm, delta, params, select_bias, add_residual)
+    torch.cuda.synchronize()
+    h = x if delta is None else (x.double() + delta.double()).float().to(torch.bfloat16)   # exact in fp32: sizes are alike
+    n = h
+    if norm is not None:
+        h, n = binding.rms_norm(x, norm[0], norm[1], delta=delta)
+    z = n.double().cpu() @ layer.router.double().T
+    if layer.bias is not None:
+        z = z + layer.bias.double()
+    _, want_idx, want_gate = m.select_experts(params or binding.select_params(), z.float().cuda(), is_visual, select_bias)
+    assert torch.equal(idx, want_idx) and torch.equal(gate, want_gate)
+    want, bound = _expected(layer, h if add_residual else None, n, idx, gate)
+    diff = np.abs(out.double().cpu().numpy() - want)
+    assert out.shape == (T, m.d) and (diff <= bound).all(), (diff / bound).max()
+    return out, idx, gate
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("T", [1, 2, 3, 4, 5, 7, 8, 15, 16])
+@pytest.mark.parametrize("d,E,F,shared,F_shared,k", [(64, 4, 32, 0, 0, 2), (136, 5, 72, 2, 40, 3), (8, 1, 8, 1, 8, 1),
+                                                     (264, 20, 200, 1, 96, 4), (520, 64, 136, 3, 8, 6)])
+def test_layer(d, E, F, shared, F_shared, k, T, quant):
+    rng = np.random.default_rng(T * 1000 + d)
+    layer = _Layer(rng, d, E, F, shared, F_shared, k, max(k - 2, 0), quant, bias=T % 2 == 0)
+    is_visual = torch.from_numpy((rng.random(T) < 0.5).astype(np.uint8)).cuda() if T > 1 else None
+    x, delta, w = _bf16(rng, T, d), _bf16(rng, T, d), _bf16(rng, d)
+    _check(layer, x, is_visual=is_visual)
+    _check(layer, x, delta, (w, EPS), is_visual)
+    _check(layer, x, None, (w.float(), EPS), is_visual, add_residual=False)
+    _check(layer, x, delta, is_visual=is_visual)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("E,T,k", [(130, 3, 8), (130, 16, 8), (256, 16, 16), (256, 1, 16), (16, 16, 16)])
+def test_many_experts(E, T, k, quant):
+    rng = np.random.default_rng(E + T)
+    layer = _Layer(rng, 72, E, 40, 1, 24, k, k, quant)
+    _check(layer, _bf16(rng, T, 72), norm=(_bf16(rng, 72), EPS))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("K", [8, 24, 64, 72, 128, 192, 256, 264, 320, 448, 512, 520, 576, 768, 1032, 2064])
+def test_every_length_of_the_reductions(K, quant):
+    rng = np.random.default_rng(K)
+    layer = _Layer(rng, K, 3, 24, 1, 16, 2, 2, quant)
+    _check(layer, _bf16(rng, 5, K), norm=(_bf16(rng, K), EPS))
+    layer = _Layer(rng, 40, 3, K, 1, K, 2, 2, quant)
+    for T in (1, 6):
+        _check(layer, _bf16(rng, T, 40))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [4096, 8192, 8200, 16384])
+@pytest.mark.parametrize("T", [1, 2, 9])
+def test_long_rows(d, T):
+    rng = np.random.default_rng(d + T)
+    layer = _Layer(rng, d, 6, 24, 0, 0, 2, 2)
+    _check(layer, _bf16(rng, T, d), _bf16(rng, T, d), (_bf16(rng, d), EPS))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("T", [1, 8, 16])
+def test_at_a_layer_shape(T, quant):
+    rng = np.random.default_rng(T)
+    layer = _Layer(rng, 1280, 64, 896, 2, 896, 6, 3, quant)
+    _check(layer, _bf16(rng, T, 1280), _bf16(rng, T, 1280), (_bf16(rng, 1280), EPS))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 6, 16])
+def test_routers_by_scores_groups_and_bias(T):
+    rng = np.random.default_rng(T)
+    layer = _Layer(rng, 136, 32, 40, 1, 24, 4, 2, True)
+    x, norm = _bf16(rng, T, 136), (_bf16(rng, 136), EPS)
+    bias = torch.from_numpy((0.2 * rng.standard_normal(32)).astype(np.float32)).cuda()
+    for params in (binding.select_params("sigmoid"), binding.select_params("sigmoid", 8, 3, 1, 2.5), binding.select_params("softmax", 4, 2, 0, 0.7)):
+        for b in (None, bias):
+            _check(layer, x, norm=norm, params=params, select_bias=b)
+    masked = bias.clone()
+    masked[3:] = -math.inf       # three experts are left, fewer than are listed
+    out, idx, gate = _check(layer, x, norm=norm, params=binding.select_params("sigmoid"), select_bias=masked)
+    assert (idx[:, 3:] == -1).all()
+    layer = _Layer(rng, 136, 32, 40, 1, 24, 4, 2, True, renormalize=False)
+    _check(layer, x, params=binding.select_params(gate_scale=3.0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shared", [0, 1])
+def test_no_listed_experts(shared):
+    rng = np.random.default_rng(1)
+    layer = _Layer(rng, 72, 4, 40, shared, 24 if shared else 0, 2, 0)
+    x = _bf16(rng, 5, 72)
+    visual = torch.ones(5, dtype=torch.uint8, device="cuda")
+    _check(layer, x, is_visual=visual, norm=(_bf16(rng, 72), EPS))     # every list is empty
+    layer.m.set_topk(0, 0)
+    out, idx, _ = _check(layer, x, norm=(_bf16(rng, 72), EPS))
+    assert idx.shape == (5, 0) and (shared or torch.equal(out, x))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [False, True])
+def test_tokens_do_not_touch_each_other(quant):
+    """A token that is no ordinary number, beside others; a token alone and among others; outputs over the inputs; guards."""
+    rng = np.random.default_rng(2)
+    d = 264
+    layer = _Layer(rng, d, 12, 72, 1, 40, 3, 3, quant)
+    m, lib = layer.m, binding.load()
+    x, delta, w = _bf16(rng, 9, d), _bf16(rng, 9, d), _bf16(rng, d)
+    clean, idx, gate = m.layer_decode(x, norm=(w, EPS), delta=delta)
+    bad = x.clone()
+    bad[2, 5], bad[6, 0] = math.nan, math.inf
+    out, idx2, gate2 = m.layer_decode(bad, norm=(w, EPS), delta=delta)
+    keep = [t for t in range(9) if t not in (2, 6)]
+    assert out[[2, 6]].isnan().any(1).all()
+    assert torch.equal(idx[keep], idx2[keep]) and torch.equal(gate[keep], gate2[keep])
+    # who shares a reduction's parts with whom goes by the number of experts: equal but for the order of the additions
+    assert (out[keep].float() - clean[keep].float()).abs().max() <= 2 * HALF_BF16 * clean[keep].float().abs().max()
+    need = lib.fmoe_layer_decode_workspace_bytes(m._ctx, 9)
+    ws = torch.full((need + 512,), 0xA5, dtype=torch.uint8, device="cuda")
+    norm = binding.FmoeNormParams(w.data_ptr(), 1, EPS)
+    for over in ("x", "delta"):
+        a, b = (torch.cat([t, torch.full((1, d), 7.0, dtype=t.dtype, device="cuda")]) for t in (x, delta))
+        to = a if over == "x" else b
+        assert lib.fmoe_layer_decode(m._ctx, None, C.byref(norm), a.data_ptr(), b.data_ptr(), None, None, 9, 1, to.data_ptr(), None, None,
+                                     ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        assert torch.equal(to[:9], clean) and (to[9] == 7).all() and (ws[need:] == 0xA5).all()
+
+
+@pytest.mark.gpu
+def test_streams_and_a_graph_with_a_shared_workspace():
+    """Two contexts on two streams at once; two captured graphs that use one workspace in turn, replayed several times."""
+    rng = np.random.default_rng(3)
+    layers = [_Layer(rng, 264, 12, 72, 1, 40, 3, 3, q) for q in (False, True)]
+    xs = [_bf16(rng, T, 264) for T in (16, 3)]
+    want = [l.m.layer_decode(x) for l, x in zip(layers, xs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[], []]
+    for turn in range(6):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(layers[i].m.layer_decode(xs[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for got in outs[i]:
+            assert all(torch.equal(a, b) for a, b in zip(got, want[i]))
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    graphs, results = [], []
+    for l, x in zip(layers, xs):
+        l.m._ws = ws
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            results.append(l.m.layer_decode(x))
+        graphs.append(graph)
+    for turn in range(4):
+        for x in xs:
+            x.copy_(torch.randn(x.shape, device="cuda"))
+        ws.random_(0, 255)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        got = [[t.clone() for t in r] for r in results]
+        for i in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(got[i], layers[i].m.layer_decode(xs[i]))), (turn, i)
+
+
+@pytest.mark.gpu
+def test_decode_agrees_with_the_layer():
+    """The fused call and fmoe_layer_forward on the same tokens, away from ties."""
+    rng = np.random.default_rng(5)
+    for quant in (False, True):
+        layer = _Layer(rng, 264, 16, 72, 1, 40, 3, 3, quant)
+        x = _bf16(rng, 7, 264)
+        visual, cu = torch.zeros(7, dtype=torch.uint8, device="cuda"), torch.tensor([0, 7], dtype=torch.int32, device="cuda")
+        whole = layer.m.layer_forward(x, visual, cu, add_residual=True)[0]
+        out, idx, _ = layer.m.layer_decode(x, visual)
+        assert torch.equal(idx, layer.m.route(x, visual)[1])
+        size = (whole[:7].float() - x.float()).abs().max()
+        # h and each expert's output in bf16 on the one side: a rounding of each of five terms, and the last ones of both
+        assert ((whole[:7].float() - out.float()).abs() <= 5 * HALF_BF16 * size + 2 * HALF_BF16 * out.float().abs()).all()
+
+
+# ------------------------------------------------------------------------------------------------------------- refusals
+
+
+def test_layer_decode_refuses_bad_arguments():
+    lib = binding.load()
+
+    def ctx(**kw):
+        base = dict(d_model=64, n_experts=8, d_ffn=32, n_shared=0, d_ffn_shared=0, k_text=2, k_visual=1, renormalize=1, dtype=1)
+        base.update(kw)
+        cfg = binding.FmoeConfig(*[base[f[0]] for f in binding.FmoeConfig._fields_])
+        c = C.c_void_p()
+        assert lib.fmoe_create(C.byref(c), C.byref(cfg), 0) == 0
+        return c
+
+    c, ok = ctx(), binding.FmoeNormParams(0x1000, 1, 1e-6)
+    run = lambda c=c, p=None, n=None, x=0x1000, T=4: lib.fmoe_layer_decode(  # noqa: E731
+        c, None if p is None else C.byref(p), None if n is None else C.byref(n), x, None, None, None, T, 1, 0x2000, None, None, 0x10000,
+        1 << 30, None)
+    assert run(c=None) == -2 and run(T=-1) == -1 and run(T=17) == -5 and run(c=ctx(dtype=0)) == -5 and run(c=ctx(d_model=16392)) == -5
+    assert run(p=binding.select_params("sigmoid", 3)) == -1 and run(p=binding.select_params(gate_scale=math.nan)) == -1
+    for bad, code in ((binding.FmoeNormParams(None, 1, 1e-6), -2), (binding.FmoeNormParams(0x1008, 1, 1e-6), -1),
+                      (binding.FmoeNormParams(0x1000, 2, 1e-6), -1), (binding.FmoeNormParams(0x1000, 1, -1.0), -1)):
+        assert run(n=bad) == code
+    assert run(n=ok) == -1 and b"fmoe_set_weights" in lib.fmoe_last_error()   # nothing registered
+    assert lib.fmoe_layer_decode_workspace_bytes(c, 17) == 0 and lib.fmoe_layer_decode_workspace_bytes(None, 4) == 0
+    assert lib.fmoe_layer_decode_workspace_bytes(c, 16) >= lib.fmoe_workspace_bytes(c, 16, 1)
+
+
+@pytest.mark.gpu
+def test_layer_decode_refuses_pointers_and_tensors_that_do_not_fit():
+    rng = np.random.default_rng(6)
+    layer = _Layer(rng, 64, 4, 32)
+    lib, m = binding.load(), layer.m
+    run = lambda x=0x1000, dl=None, o=0x2000, ws=0x10000, nb=1 << 30, b=None: lib.fmoe_layer_decode(  # noqa: E731
+        m._ctx, None, None, x, dl, None, b, 4, 1, o, None, None, ws, nb, None)
+    assert run(x=None) == -2 and run(o=None) == -2 and run(x=0x1008) == -1 and run(dl=0x1008) == -1 and run(o=0x1008) == -1 and run(b=0x1008) == -1
+    assert run(ws=None) == -4 and run(ws=0x10010) == -4 and run(nb=64) == -4
+    x = _bf16(rng, 4, 64)
+    w = _bf16(rng, 64)
+    for call in (lambda: m.layer_decode(x.float()), lambda: m.layer_decode(x[:, :32]), lambda: m.layer_decode(x.cpu()),
+                 lambda: m.layer_decode(x, delta=x[:3]), lambda: m.layer_decode(x, norm=(w[:32], EPS)), lambda: m.layer_decode(x, norm=(w.cpu(), EPS)),
+                 lambda: m.layer_decode(x, is_visual=torch.zeros(3, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(binding.FmoeError):
+        m.layer_decode(_bf16(rng, 17, 64))
