@@ -37,12 +37,11 @@ SOURCES = {
 }
 
 
-HAND_PLACED = ("ffn.hip", "ffn_quant.hip")   # files whose kernels name accumulation registers themselves
-PENDING_READS = HAND_PLACED + ("ffn_rows8.hip",)   # files whose LDS reads are inline assembly, waited for later
+HAND_PLACED = ("ffn.hip", "ffn_quant.hip", "ffn_rows8.hip")   # files whose kernels name accumulation registers themselves
 
 
 def check_accumulation_registers(asm_path):
-    """The dense-shape expert GEMM kernels (ffn_dense_kernel, ffn_quant_dense_kernel) keep their accumulators in accumulation
+    """The dense-shape expert GEMM kernels (ffn_dense_kernel, ffn_quant_dense_kernel, ffn_rows8_many_kernel) keep their accumulators in accumulation
     registers that the kernel names itself, which the compiler's register allocator does not see.  This
     reads the device assembly the compiler wrote for their file and fails if, inside those kernels, the
     compiler placed anything of its own in an accumulation register (any a<N> operand outside the
@@ -52,7 +51,7 @@ def check_accumulation_registers(asm_path):
     inside = in_asm = False
     kernels = 0
     for n, line in enumerate(open(asm_path), 1):
-        if re.match(r"^_ZN\S*(ffn_dense_kernel|ffn_quant_dense_kernel)\S*:", line):
+        if re.match(r"^_ZN\S*(ffn_dense_kernel|ffn_quant_dense_kernel|ffn_rows8_many_kernel)\S*:", line):
             inside, in_asm = True, False
             kernels += 1
             name = line.split(":")[0]
@@ -111,7 +110,7 @@ def _compile(name, extra, verbose):
     src = os.path.join(CSRC, name)
     obj = os.path.join(OBJ, name.replace(".hip", ".o"))
     cmd = ["hipcc", "-c", src, "-o", obj] + COMMON + extra
-    if name in PENDING_READS:
+    if name in HAND_PLACED:
         cmd.append("-save-temps=obj")   # keeps the device assembly beside the object, for the check below
     if verbose:
         print(" ".join(cmd), flush=True)
@@ -122,10 +121,9 @@ def _compile(name, extra, verbose):
         raise RuntimeError(f"hipcc failed on {name}:\n{err}")
     if err.strip() and verbose:
         print(err, flush=True)
-    if name in PENDING_READS:
+    if name in HAND_PLACED:
         asm = os.path.join(OBJ, name.replace(".hip", "-hip-amdgcn-amd-amdhsa-gfx950.s"))
-        if name in HAND_PLACED:
-            check_accumulation_registers(asm)
+        check_accumulation_registers(asm)
         check_pending_reads(asm)
     return obj
 

@@ -25,6 +25,8 @@ namespace {
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
+#include "rows8_regs.inc"   // rows_acc<IDX>
+
 constexpr int RBK = 128;       // k per tile
 constexpr int RSTAGES = 4;     // ring of k tiles, of rows and of weights
 constexpr int RAHEAD = RSTAGES - 1;
@@ -70,13 +72,15 @@ __device__ __forceinline__ void settle_rows(u32x4_t& f0, u32x4_t& f1, uint32_t& 
   asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f0), "+v"(f1), "+v"(s) : : "memory");
 }
 
-template <int OPA, int OPB>
-__device__ __forceinline__ f32x4_t mfma_rows(u32x4_t a0, u32x4_t a1, uint32_t sa, u32x4_t b, uint32_t sb, f32x4_t c) {
-  const i32x8_t a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
+__device__ __forceinline__ i32x8_t joined(u32x4_t a0, u32x4_t a1) {
+  return i32x8_t{(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
+}
+template <int OPB>
+__device__ __forceinline__ f32x4_t mfma_rows(i32x8_t a, uint32_t sa, u32x4_t b, uint32_t sb, f32x4_t c) {
   typedef int i32x4_t __attribute__((ext_vector_type(4)));
   const i32x4_t b4 = __builtin_bit_cast(i32x4_t, b);
   const i32x8_t b8 = __builtin_shufflevector(b4, b4, 0, 1, 2, 3, -1, -1, -1, -1);   // 4-bit operands have four registers
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b8, c, 0, 4, OPA, (int)sa, OPB, (int)sb);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b8, c, 0, 4, 0, (int)sa, OPB, (int)sb);
 }
 
 // Hidden rows of a tile: silu(gate) * up, 32 columns a group, through LDS (the ring, free by now), a band of 32 rows at a time.
@@ -223,11 +227,16 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, const fmoe_tile&
   const uint32_t frag_a1 = frag_row + (uint32_t)(((lane >> 4) + 4) ^ ((lane & 15) >> 1)) * 16;
   const uint32_t frag_s = lds1 + (uint32_t)(lane & 15) * 4 + (uint32_t)(lane >> 4);
 
-  f32x4_t acc[NCB][NRB][2];
+  // Accumulators: the compiler's with one column tile, hand-placed ones with two (number (j*NRB + rb)*2 + f), which it would
+  // put in part into scratch memory
+  constexpr bool NAMED = NCB == 2;
+  f32x4_t acc[NCB][NAMED ? 1 : NRB][2];
+  if constexpr (NAMED) {
+    dense_claim_acc();
+  } else {
 #pragma unroll
-  for (int j = 0; j < NCB; ++j)
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) acc[j][rb][0] = acc[j][rb][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int rb = 0; rb < NRB; ++rb) acc[0][rb][0] = acc[0][rb][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
 
   // k tile t, U = t % RSTAGES: products, and the loads of tile t + RAHEAD; of the LAST tiles, fewer than RSTAGES, products only
   u32x4_t fa[2][2];
@@ -264,8 +273,14 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, const fmoe_tile&
       __builtin_amdgcn_sched_barrier(0);   // the next operand is on its way behind the products
       static_for<0, NCB>([&](auto jc) {
         constexpr int j = decltype(jc)::value;
-        acc[j][rb][0] = mfma_rows<0, 2 * (U & 1)>(fa[cur][0], fa[cur][1], fs[cur], breg[U][j][0], sreg[U / 2][j], acc[j][rb][0]);
-        acc[j][rb][1] = mfma_rows<0, 2 * (U & 1) + 1>(fa[cur][0], fa[cur][1], fs[cur], breg[U][j][1], sreg[U / 2][j], acc[j][rb][1]);
+        const i32x8_t a = joined(fa[cur][0], fa[cur][1]);
+        if constexpr (NAMED) {
+          rows_acc<(j * NRB + rb) * 2>::template add<2 * (U & 1)>(a, fs[cur], breg[U][j][0], sreg[U / 2][j]);
+          rows_acc<(j * NRB + rb) * 2 + 1>::template add<2 * (U & 1) + 1>(a, fs[cur], breg[U][j][1], sreg[U / 2][j]);
+        } else {
+          acc[j][rb][0] = mfma_rows<2 * (U & 1)>(a, fs[cur], breg[U][j][0], sreg[U / 2][j], acc[j][rb][0]);
+          acc[j][rb][1] = mfma_rows<2 * (U & 1) + 1>(a, fs[cur], breg[U][j][1], sreg[U / 2][j], acc[j][rb][1]);
+        }
       });
     });
     if constexpr (!LAST && (U & 1) == 1) {   // the pair is done: the next but one takes its place
@@ -280,9 +295,12 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, const fmoe_tile&
     if (t0 + decltype(uc)::value < NT) ktile(uc, std::true_type{}, t0 + decltype(uc)::value);   // uniform
   });
   FMOE_WAIT_VM(0);   // the loads issued past the end have landed before the ring is reused
+  // the last matrix instructions have retired before hand-placed accumulators are read, see ffn.hip
+  if constexpr (NAMED) asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
   auto result = [&](auto jc, auto rbc, auto fc) {
     constexpr int rb = decltype(rbc)::value;
     if constexpr (rb >= NRB) return f32x4_t{0.f, 0.f, 0.f, 0.f};   // rows that are not stored
+    else if constexpr (NAMED) return read_acc<(decltype(jc)::value * NRB + rb) * 2 + decltype(fc)::value>();
     else return acc[decltype(jc)::value][rb][decltype(fc)::value];
   };
   if constexpr (SWIGLU) {
@@ -317,7 +335,7 @@ __device__ __forceinline__ RowsProblem rows_problem(const RowsArgs& a, const Qua
   return Q;
 }
 
-constexpr int FEW_ROWS = 32, SOME_ROWS = 64;
+constexpr int FEW_ROWS = 32, SOME_ROWS = 64, MANY_ROWS = 128;
 constexpr int lds_bytes(int rows) { return RSTAGES * (rows * RBK + (rows > 64 ? rows : 64) * 4); }
 
 template <bool SWIGLU>
@@ -344,6 +362,25 @@ __global__ __launch_bounds__(256, 4) void ffn_rows8_some_kernel(RowsArgs a) {
   if (it.rows <= 32) rows_tile<SWIGLU, 1, 1, SOME_ROWS>(P, tile, it.group, it.unit, it.unit + 1, smem);
   else rows_tile<SWIGLU, 2, 1, SOME_ROWS>(P, tile, it.group, it.unit, it.unit + 1, smem);
 }
+// (The build looks at the registers of a kernel of this name.)
+template <bool SWIGLU>
+__global__ __launch_bounds__(256, 2) void ffn_rows8_many_kernel(RowsArgs a) {
+  __shared__ __align__(16) char smem[lds_bytes(MANY_ROWS)];
+  const QuantItem it = find_tile(a, (int)blockIdx.x);
+  if (it.group < 0) return;
+  const RowsProblem P = rows_problem(a, it);
+  fmoe_tile tile{};
+  tile.row0 = it.row0;
+  tile.rows = it.rows;
+  const int tiles = (P.nbw + 3) / 4, ct0 = 2 * it.unit, limit = ct0 + 2 < tiles ? ct0 + 2 : tiles;
+  switch ((tile.rows + 31) >> 5) {   // live 32-row bands of the tile, uniform
+    case 1: rows_tile<SWIGLU, 1, 2, MANY_ROWS>(P, tile, it.group, ct0, limit, smem); break;
+    case 2: rows_tile<SWIGLU, 2, 2, MANY_ROWS>(P, tile, it.group, ct0, limit, smem); break;
+    case 3: rows_tile<SWIGLU, 3, 2, MANY_ROWS>(P, tile, it.group, ct0, limit, smem); break;
+    default: rows_tile<SWIGLU, 4, 2, MANY_ROWS>(P, tile, it.group, ct0, limit, smem); break;
+  }
+}
+
 // Source rows [group][n][k]: codes two to a byte, scales one byte per 32 k.  PAIR: gate and up (fragments 0 and 1), else
 // fragment f = features 16f..16f+15 of the column block.  Past N and K the codes are 0 and the scales 1.
 template <bool PAIR>
@@ -466,13 +503,13 @@ int launch_expert_ffn_rows8(const fmoe_ctx* ctx, const uint8_t* codes, const uin
     q.C = static_cast<bf16_t*>(y_shared); q.ldc = d; q.c_group_off = (long long)n_cap * d;
   }
   const long long per_expert = row_cap / E;
-  const int form = ctx->ffn_shape ? ctx->ffn_shape - 1 : per_expert < 16 ? 0 : 1;
+  const int form = ctx->ffn_shape ? 2 * (ctx->ffn_shape - 1) : per_expert < 16 ? 0 : per_expert < 150 ? 1 : 2;
   auto launch = [&](auto swiglu, RowsArgs a) {
     constexpr bool S = decltype(swiglu)::value;
     a.expert_offsets = expert_offsets; a.n_dev = n_dev;
     a.E = E; a.n_cap = n_cap; a.row_cap = row_cap;
-    a.log2_bm = form == 0 ? 5 : 6;
-    const int per_unit = 4;   // column blocks of a unit
+    a.log2_bm = 5 + form;
+    const int per_unit = form == 2 ? 8 : 4;   // column blocks of a unit
     a.cols = (a.p0.nbw + per_unit - 1) / per_unit;
     if (Ft > 0) {
       a.shared_groups = S ? 1 : c.n_shared;
@@ -483,14 +520,15 @@ int launch_expert_ffn_rows8(const fmoe_ctx* ctx, const uint8_t* codes, const uin
     const long long items = tiles * a.cols + shared_tiles * a.shared_cols * a.shared_groups;
     const dim3 grid((unsigned)((items + 7) / 8 * 8)), block(256);
     if (form == 0) hipLaunchKernelGGL(ffn_rows8_few_kernel<S>, grid, block, 0, stream, a);
-    else hipLaunchKernelGGL(ffn_rows8_some_kernel<S>, grid, block, 0, stream, a);
+    else if (form == 1) hipLaunchKernelGGL(ffn_rows8_some_kernel<S>, grid, block, 0, stream, a);
+    else hipLaunchKernelGGL(ffn_rows8_many_kernel<S>, grid, block, 0, stream, a);
   };
   {
-    fmoe_prof_scope prof(ctx, SLOT_GEMM1, stream);
+    fmoe_prof_scope prof(ctx, form == 2 ? SLOT_GEMM1_DENSE : SLOT_GEMM1, stream);
     launch(std::true_type{}, g1);
   }
   {
-    fmoe_prof_scope prof(ctx, SLOT_GEMM2, stream);
+    fmoe_prof_scope prof(ctx, form == 2 ? SLOT_GEMM2_DENSE : SLOT_GEMM2, stream);
     launch(std::false_type{}, g2);
   }
   FMOE_HIP_CHECK(hipGetLastError());
