@@ -203,8 +203,8 @@ int fmoe_set_weights_quant(fmoe_ctx* ctx, const void* router_w, const float* rou
                            const fmoe_quant_tensor* ws_up, const fmoe_quant_tensor* ws_down, void* stream);
 
 /* Registers 4-bit expert matrices for fmoe_expert_ffn_quant_rows, beside the weights in force for the other calls, which stay (none
- * are needed).  Tensors, alignment, bf16 contexts and copies (4.25 bits a weight, the reduction padded to 128, the output columns to
- * 64 / 128) as in fmoe_set_weights_quant.  d_model, d_ffn and d_ffn_shared must be multiples of 32, and (d_model + 128) times
+ * are needed).  Tensors, alignment, bf16 contexts and copies (4.25 bits a weight, the reduction padded to 128, the output columns of the
+ * down matrices to 64) as in fmoe_set_weights_quant.  d_model, d_ffn and d_ffn_shared must be multiples of 32, and (d_model + 128) times
  * (S_m + 128), or times (N_s S_s + 128), below 2^32, else FMOE_ERR_UNSUPPORTED. */
 int fmoe_set_weights_quant_rows(fmoe_ctx* ctx, const fmoe_quant_tensor* w_gate, const fmoe_quant_tensor* w_up,
                                 const fmoe_quant_tensor* w_down, const fmoe_quant_tensor* ws_gate,

@@ -3,17 +3,19 @@
 //
 // v_mfma_scale_f32_16x16x128_f8f6f4 takes both formats as they are, and the two scales of every 32 products: nothing is converted.
 // It does in a step of 128 k what the bf16 instruction does in four of 32, in half the time.  Lane l has of a row (l % 16)
-// the 16-byte pieces l / 16 and l / 16 + 4 of a k tile of 128, of a column the 32 codes from 32 (l / 16) on; its scale operands
-// have in one of their four bytes, which the instruction names, the power of two of the l / 16-th 32 of the row and the column.
+// the 16-byte pieces l / 16 and l / 16 + 4 of a k tile of 128, of a feature the 32 codes from 32 (l / 16) on; its scale operands
+// have in one of their four bytes, which the instruction names, the power of two of the l / 16-th 32 of the row and the feature.
 // The instruction cuts the products of eight neighbouring k at 2^-13 of the largest power of two among them and adds the eights up in
 // fp32 (found on the card): nothing is lost but of products 2^8 and more below a neighbour's, and less than the rounding of the
 // rows to 8 bits has taken from them.
 //
-// Packing (fmoe_set_weights_quant_rows): of a column block (16 features, gate and up; or 32 output features), a k tile and a fragment
-// (gate / up, or features 0..15 / 16..31) lane l has one 16-byte unit, all units in one linear stream; of two k tiles the four
-// scale bytes of its column are one word.
+// The weights are the first operand, so that a lane ends up with neighbouring features of one row: four of every fragment.  A column
+// unit is four fragments, whose features are dealt so that the lane's are 8 neighbours in 32 hidden columns (gate and up of
+// either half) or 16 neighbours in 64 output columns: rows are rounded to 8 bits and stored from registers.
+// Packing (fmoe_set_weights_quant_rows): of a column unit, a k tile and a fragment lane l has one 16-byte unit, all units in one linear
+// stream; of a column unit and a k tile the four fragments' scale bytes are a word.
 //
-// A workgroup has a tile of rows and, per wavefront, one or two column blocks.  As in ffn.hip: rows global -> LDS directly, in a
+// A workgroup has a tile of rows and a column unit per wavefront.  As in ffn.hip: rows global -> LDS directly, in a
 // ring of four k tiles (128 bytes a row, pieces exchanged so that operand reads meet no bank twice); weights into registers,
 // as many tiles ahead; a barrier per k tile.  Work items are found from the experts' offsets (quant_items.h).
 
@@ -30,6 +32,7 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 constexpr int RBK = 128;       // k per tile
 constexpr int RSTAGES = 4;     // ring of k tiles, of rows and of weights
 constexpr int RAHEAD = RSTAGES - 1;
+constexpr int FRAGS = 4;       // fragments of 16 features a column unit
 
 struct RowsProblem {
   const uint8_t *A, *As;       // rows [*, lda] bytes and their scale bytes [*, ldas]
@@ -39,10 +42,10 @@ struct RowsProblem {
   const u32x4_t* Bp;
   const uint32_t* Sp;
   long long group_stride, scale_stride;   // units and words between groups
-  int nbw, N, K;
+  int units, N, K;             // column units of a group
   uint8_t *H, *Hs;             // gate/up: the hidden rows
   uint32_t ldh, ldhs;
-  int expert_cols;             // columns of one expert in H (shared experts stand side by side)
+  int expert_groups;           // groups of 32 columns of one expert in H (shared experts stand side by side)
   bf16_t* C;                   // down
   int ldc;
   int a_group_off, as_group_off;          // of a shared expert's part of the rows
@@ -60,7 +63,6 @@ struct RowsArgs {
 };
 
 __host__ __device__ inline int rows_tiles(int K) { return (K + RBK - 1) / RBK; }
-__host__ __device__ inline int rows_pairs(int K) { return (rows_tiles(K) + 1) / 2; }
 
 // Operand of a row block from LDS: the lane's two pieces and its scale byte, see lds_issue_frags_at
 template <int OFF, int OFF_S>
@@ -71,74 +73,29 @@ __device__ __forceinline__ void issue_rows(uint32_t a0, uint32_t a1, uint32_t as
 __device__ __forceinline__ void settle_rows(u32x4_t& f0, u32x4_t& f1, uint32_t& s) {
   asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f0), "+v"(f1), "+v"(s) : : "memory");
 }
-
 __device__ __forceinline__ i32x8_t joined(u32x4_t a0, u32x4_t a1) {
   return i32x8_t{(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
 }
-template <int OPB>
-__device__ __forceinline__ f32x4_t mfma_rows(i32x8_t a, uint32_t sa, u32x4_t b, uint32_t sb, f32x4_t c) {
+// c += weights (byte I of sw) x rows (byte 0 of sr)
+template <int I>
+__device__ __forceinline__ f32x4_t mfma_rows(u32x4_t w, uint32_t sw, i32x8_t r, uint32_t sr, f32x4_t c) {
   typedef int i32x4_t __attribute__((ext_vector_type(4)));
-  const i32x4_t b4 = __builtin_bit_cast(i32x4_t, b);
-  const i32x8_t b8 = __builtin_shufflevector(b4, b4, 0, 1, 2, 3, -1, -1, -1, -1);   // 4-bit operands have four registers
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b8, c, 0, 4, 0, (int)sa, OPB, (int)sb);
+  const i32x4_t w4 = __builtin_bit_cast(i32x4_t, w);
+  const i32x8_t w8 = __builtin_shufflevector(w4, w4, 0, 1, 2, 3, -1, -1, -1, -1);   // 4-bit operands have four registers
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, r, c, 4, 0, I, (int)sw, 0, (int)sr);
 }
 
-// Hidden rows of a tile: silu(gate) * up, 32 columns a group, through LDS (the ring, free by now), a band of 32 rows at a time.
-template <int NAB, int NCB, typename ACC>
-__device__ __forceinline__ void store_hidden(const RowsProblem& P, const fmoe_tile& tile, int col0, int cols, ACC acc, char* smem) {
-  constexpr int BC = 64 * NCB, CS = BC + 4;
-  float* const buf = reinterpret_cast<float*>(smem);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  static_for<0, NAB>([&](auto bandc) {
-    constexpr int band = decltype(bandc)::value;
-    __syncthreads();   // every wavefront is done with what was there
-    static_for<0, 2>([&](auto hc) {
-      static_for<0, NCB>([&](auto jc) {
-        constexpr int rb = 2 * band + decltype(hc)::value, j = decltype(jc)::value;
-        const f32x4_t g = acc(jc, std::integral_constant<int, rb>{}, std::integral_constant<int, 0>{});
-        const f32x4_t u = acc(jc, std::integral_constant<int, rb>{}, std::integral_constant<int, 1>{});
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-          buf[(decltype(hc)::value * 16 + 4 * (lane >> 4) + v) * CS + j * 64 + wave * 16 + (lane & 15)] = silu_mul_bf16(g[v], u[v]);
-      });
-    });
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < NCB; ++i) {
-      const int unit = tid + 256 * i, r = unit / (BC / 8), cu = unit % (BC / 8);
-      const int row = band * 32 + r, col = col0 + cu * 8;
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = buf[r * CS + cu * 8 + e];
-      uint32_t scale;
-      const uint2 c = rows8::quantize(v, scale);
-      if (row < tile.rows && cu * 8 < cols && col < P.N) {   // groups are whole: the same for four lanes
-        const size_t at = (size_t)(tile.row0 + row);
-        *reinterpret_cast<uint2*>(P.H + at * P.ldh + col) = c;
-        if ((cu & 3) == 0) {
-          const int expert = col / P.expert_cols, g = (col - expert * P.expert_cols) >> 5, last = (P.expert_cols >> 5) - 1;
-          uint8_t* const s = P.Hs + at * P.ldhs + expert * ((P.expert_cols + 127) / 128 * 4) + g;
-          s[0] = (uint8_t)scale;
-          if (g == last)
-            for (int k = g + 1; k & 3; ++k) s[k - g] = 127;   // the word's unused bytes
-        }
-      }
-    }
-  });
-}
-
-// One work item: NAB live bands of 32 rows, LDS stages of ROWS, NCB column tiles of 64 (gate/up) or 128 columns from ct0 on.
-// HALF: of the only band the first 16 rows.
-template <bool SWIGLU, int NAB, int NCB, int ROWS, bool HALF = false>
-__device__ __forceinline__ void rows_tile(const RowsProblem& P, const fmoe_tile& tile, int group, int ct0, int ct_limit, char* smem) {
-  static_assert(32 * NAB <= ROWS, "the rows fit in a stage");
-  constexpr int NRB = HALF ? 1 : 2 * NAB;
-  constexpr int SROWS = ROWS > 64 ? ROWS : 64;                  // scale words a stage
-  constexpr int PER_TILE = NAB + 1 + 2 * NCB;                   // loads of a k tile (without those of weight scales)
+// One work item: NRB row blocks of 16, LDS stages of ROWS rows; wavefront w has column unit cu0 + w.
+template <bool SWIGLU, int NRB, int ROWS, int WAVES, bool NAMED>
+__device__ __forceinline__ void rows_tile(const RowsProblem& P, int row0, int rows, int group, int cu0, char* smem) {
+  static_assert(16 * NRB <= ROWS && (WAVES == 1 || WAVES == 4), "the rows fit in a stage");
+  constexpr int NLA = (2 * NRB + WAVES - 1) / WAVES;           // loads of eight rows a wavefront
+  static_assert(8 * NLA * WAVES <= ROWS, "and so do the rows that are loaded");
+  constexpr int SROWS = ROWS > 64 ? ROWS : 64;                 // scale words a stage
+  constexpr int PER_TILE = NLA + 1 + FRAGS + 1;                // loads of a k tile
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int K = P.K, NT = rows_tiles(K), NP = rows_pairs(K);
-  const int col_tiles = (P.nbw + 3) / 4;
+  const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int K = P.K, NT = rows_tiles(K);
   char* const rows_lds = smem;
   char* const scales_lds = smem + RSTAGES * ROWS * RBK;
 
@@ -148,66 +105,55 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, const fmoe_tile&
       const_cast<uint32_t*>(P.Sp) + (size_t)group * P.scale_stride, 0, 0xffffffff, 0x00020000);
   const __amdgpu_buffer_rsrc_t a_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(P.A), 0, 0xffffffff, 0x00020000);
   const __amdgpu_buffer_rsrc_t as_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(P.As), 0, 0xffffffff, 0x00020000);
-  uint32_t bbase[NCB], sbase[NCB];   // scalar
-#pragma unroll
-  for (int j = 0; j < NCB; ++j) {    // column tiles past the packing: the last one again, never stored
-    const uint32_t cb = (uint32_t)(ct0 + j < col_tiles ? ct0 + j : col_tiles - 1) * 4u + (uint32_t)wave;
-    bbase[j] = cb * (uint32_t)NT * 2048u;
-    sbase[j] = cb * (uint32_t)NP * 256u;
-  }
+  const int cu = cu0 + wave < P.units ? cu0 + wave : P.units - 1;   // past the end the last one again, not stored
+  const uint32_t bbase = (uint32_t)cu * (uint32_t)NT * (FRAGS * 1024u), sbase = (uint32_t)cu * (uint32_t)NT * 256u;   // scalar
   const uint32_t lane16 = (uint32_t)lane * 16u, lane4 = (uint32_t)lane * 4u;
 
-  u32x4_t breg[RSTAGES][NCB][2];
-  uint32_t sreg[2][NCB];             // of the k tiles' pair 2i and 2i + 1
-  auto load_b = [&](int slot, int t, int j, int f) {
-    breg[slot][j][f] = __builtin_amdgcn_raw_buffer_load_b128(
-        b_rsrc, lane16, bbase[j] + (uint32_t)(t < NT ? t : NT - 1) * 2048u + (uint32_t)f * 1024u, 0);
+  u32x4_t breg[RSTAGES][FRAGS];
+  uint32_t sreg[RSTAGES];
+  auto load_b = [&](int slot, int t, int i) {
+    breg[slot][i] = __builtin_amdgcn_raw_buffer_load_b128(
+        b_rsrc, lane16, bbase + (uint32_t)(t < NT ? t : NT - 1) * (FRAGS * 1024u) + (uint32_t)i * 1024u, 0);
   };
-  auto load_s = [&](int slot, int pair, int j) {
-    sreg[slot][j] = __builtin_amdgcn_raw_buffer_load_b32(s_rsrc, lane4, sbase[j] + (uint32_t)(pair < NP ? pair : NP - 1) * 256u, 0);
+  auto load_s = [&](int slot, int t) {
+    sreg[slot] = __builtin_amdgcn_raw_buffer_load_b32(s_rsrc, lane4, sbase + (uint32_t)(t < NT ? t : NT - 1) * 256u, 0);
   };
-  // Rows this lane fetches: 32 it + 8 wave + lane / 8 of the tile; scale words of row 64 (wave % 2) + lane (or lane % 64 where the
+  // Rows this lane fetches: 8 (it * WAVES + wave) + lane / 8 of the tile; scale words of row 64 (wave % 2) + lane (or lane where the
   // stage has 64: the wavefronts then fetch the same).  Past the tile its last row.
   const uint32_t most = 0xffffffffu / P.lda - 1u;
-  const int sr = (ROWS > 64 ? 64 * (wave & 1) : 0) + lane;
-  int src[NAB + 1];
+  int src[NLA + 1];
 #pragma unroll
-  for (int it = 0; it <= NAB; ++it) {
-    const int r = it < NAB ? 32 * it + 8 * wave + (lane >> 3) : sr;
-    src[it] = tile.row0 + (r < tile.rows ? r : tile.rows - 1);
+  for (int it = 0; it <= NLA; ++it) {
+    const int r = it < NLA ? 8 * (it * WAVES + wave) + (lane >> 3) : (ROWS > 64 ? 64 * (wave & 1) : 0) + lane;
+    src[it] = row0 + (r < rows ? r : rows - 1);
     if (P.map1) src[it] = P.map1[src[it]];
   }
   order_loads();
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int t = 0; t < RAHEAD; ++t) {
+    load_s(t, t);
 #pragma unroll
-    for (int j = 0; j < NCB; ++j) load_s(i, i, j);
-#pragma unroll
-  for (int t = 0; t < RAHEAD; ++t)
-#pragma unroll
-    for (int j = 0; j < NCB; ++j) {
-      load_b(t, t, j, 0);
-      load_b(t, t, j, 1);
-    }
+    for (int i = 0; i < FRAGS; ++i) load_b(t, t, i);
+  }
   order_loads();
-  uint32_t a_src[NAB], a_last[NAB], as_src;   // of the lane's piece in k tile 0, and in the last one less its start
-  const int piece = ((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) * 16;
-  const int k_last = (NT - 1) * RBK, piece_last = k_last + piece < K ? piece : K - 16 - k_last;   // past K the row's end again
+  uint32_t a_src[NLA], a_last[NLA], as_src;   // of the lane's piece in k tile 0, and in the last one less its start
+  const int k_last = (NT - 1) * RBK;
 #pragma unroll
-  for (int it = 0; it <= NAB; ++it) {
+  for (int it = 0; it <= NLA; ++it) {
     int s = src[it];
     if (P.map1 && P.map1_limit > 0) s = s < 0 ? 0 : (s >= P.map1_limit ? P.map1_limit - 1 : s);
     if (P.map2) s = P.map2[s];
     const uint32_t at = (uint32_t)s < most ? (uint32_t)s : most;
-    if (it < NAB) {
-      a_last[it] = at * P.lda + (uint32_t)piece_last;
+    if (it < NLA) {   // row r keeps its 16-byte piece c at place c ^ (r / 2 % 8)
+      const int piece = ((lane & 7) ^ ((4 * (it * WAVES + wave) + (lane >> 4)) & 7)) * 16;
+      a_last[it] = at * P.lda + (uint32_t)(k_last + piece < K ? piece : K - 16 - k_last);   // past K the row's end again
       a_src[it] = at * P.lda + (uint32_t)piece;
     } else {
       as_src = at * P.ldas;
     }
   }
   auto load_a = [&](int stage, int t, int it) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rsrc, FMOE_LPTR(rows_lds + stage * (ROWS * RBK) + (32 * it + 8 * wave) * RBK), 16,
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rsrc, FMOE_LPTR(rows_lds + stage * (ROWS * RBK) + 8 * (it * WAVES + wave) * RBK), 16,
                                              t < NT - 1 ? a_src[it] : a_last[it], (uint32_t)(t < NT ? t : NT - 1) * RBK, 0, 0);
   };
   auto load_as = [&](int stage, int t) {
@@ -217,7 +163,7 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, const fmoe_tile&
 #pragma unroll
   for (int t = 0; t < RAHEAD; ++t) {
 #pragma unroll
-    for (int it = 0; it < NAB; ++it) load_a(t, t, it);
+    for (int it = 0; it < NLA; ++it) load_a(t, t, it);
     load_as(t, t);
     order_loads();
   }
@@ -227,15 +173,16 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, const fmoe_tile&
   const uint32_t frag_a1 = frag_row + (uint32_t)(((lane >> 4) + 4) ^ ((lane & 15) >> 1)) * 16;
   const uint32_t frag_s = lds1 + (uint32_t)(lane & 15) * 4 + (uint32_t)(lane >> 4);
 
-  // Accumulators: the compiler's with one column tile, hand-placed ones with two (number (j*NRB + rb)*2 + f), which it would
-  // put in part into scratch memory
-  constexpr bool NAMED = NCB == 2;
-  f32x4_t acc[NCB][NAMED ? 1 : NRB][2];
+  // Accumulators: hand-placed ones (number FRAGS * rb + i) for tiles of 128 rows, where the compiler would put part of them into
+  // scratch memory
+  f32x4_t acc[NAMED ? 1 : NRB][FRAGS];
   if constexpr (NAMED) {
     dense_claim_acc();
   } else {
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) acc[0][rb][0] = acc[0][rb][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+      for (int i = 0; i < FRAGS; ++i) acc[rb][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
   // k tile t, U = t % RSTAGES: products, and the loads of tile t + RAHEAD; of the LAST tiles, fewer than RSTAGES, products only
@@ -247,13 +194,14 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, const fmoe_tile&
     // loads newer than this tile's rows, see ffn_quant.hip
     constexpr int LATER = U < RAHEAD ? RAHEAD - 1 - U : 0;
     if constexpr (LAST) {
-      if (t < RAHEAD) FMOE_WAIT_VM(LATER * (NAB + 1));   // uniform
+      if (t < RAHEAD) FMOE_WAIT_VM(LATER * (NLA + 1));   // uniform
       else FMOE_WAIT_VM(LATER * PER_TILE);
     } else {
-      if (t < RAHEAD) FMOE_WAIT_VM(LATER * (NAB + 1) + U * PER_TILE);
+      if (t < RAHEAD) FMOE_WAIT_VM(LATER * (NLA + 1) + U * PER_TILE);
       else FMOE_WAIT_VM((RAHEAD - 1) * PER_TILE);
     }
-    block_barrier();   // every wavefront's share of the tile is in LDS; all are done with the tile before
+    // every wavefront's share of the tile is in LDS; all are done with the tile before (one alone has waited for its reads)
+    if constexpr (WAVES > 1) block_barrier();
     constexpr int off = U * (ROWS * RBK), off_s = U * (SROWS * 4);
     issue_rows<off, off_s>(frag_a0, frag_a1, frag_s, fa[0][0], fa[0][1], fs[0]);
     static_for<0, NRB>([&](auto rc) {
@@ -265,28 +213,20 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, const fmoe_tile&
 #pragma unroll
         for (int i = 0; i < PER_TILE; ++i) {   // load i of the tile goes out with row block i * NRB / PER_TILE
           if ((i * NRB) / PER_TILE != rb) continue;
-          if (i < NAB) load_a((U + RAHEAD) % RSTAGES, t + RAHEAD, i);
-          else if (i == NAB) load_as((U + RAHEAD) % RSTAGES, t + RAHEAD);
-          else load_b((U + RAHEAD) % RSTAGES, t + RAHEAD, (i - NAB - 1) >> 1, (i - NAB - 1) & 1);
+          if (i < NLA) load_a((U + RAHEAD) % RSTAGES, t + RAHEAD, i);
+          else if (i == NLA) load_as((U + RAHEAD) % RSTAGES, t + RAHEAD);
+          else if (i == NLA + 1) load_s((U + RAHEAD) % RSTAGES, t + RAHEAD);
+          else load_b((U + RAHEAD) % RSTAGES, t + RAHEAD, i - NLA - 2);
         }
       }
       __builtin_amdgcn_sched_barrier(0);   // the next operand is on its way behind the products
-      static_for<0, NCB>([&](auto jc) {
-        constexpr int j = decltype(jc)::value;
-        const i32x8_t a = joined(fa[cur][0], fa[cur][1]);
-        if constexpr (NAMED) {
-          rows_acc<(j * NRB + rb) * 2>::template add<2 * (U & 1)>(a, fs[cur], breg[U][j][0], sreg[U / 2][j]);
-          rows_acc<(j * NRB + rb) * 2 + 1>::template add<2 * (U & 1) + 1>(a, fs[cur], breg[U][j][1], sreg[U / 2][j]);
-        } else {
-          acc[j][rb][0] = mfma_rows<2 * (U & 1)>(a, fs[cur], breg[U][j][0], sreg[U / 2][j], acc[j][rb][0]);
-          acc[j][rb][1] = mfma_rows<2 * (U & 1) + 1>(a, fs[cur], breg[U][j][1], sreg[U / 2][j], acc[j][rb][1]);
-        }
+      const i32x8_t r = joined(fa[cur][0], fa[cur][1]);
+      static_for<0, FRAGS>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        if constexpr (NAMED) rows_acc<FRAGS * rb + i>::template add<i>(breg[U][i], sreg[U], r, fs[cur]);
+        else acc[rb][i] = mfma_rows<i>(breg[U][i], sreg[U], r, fs[cur], acc[rb][i]);
       });
     });
-    if constexpr (!LAST && (U & 1) == 1) {   // the pair is done: the next but one takes its place
-#pragma unroll
-      for (int j = 0; j < NCB; ++j) load_s(U / 2, t / 2 + 2, j);
-    }
   };
   int t0 = 0;
   for (; t0 + RSTAGES <= NT; t0 += RSTAGES)
@@ -294,28 +234,51 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, const fmoe_tile&
   static_for<0, RSTAGES - 1>([&](auto uc) {
     if (t0 + decltype(uc)::value < NT) ktile(uc, std::true_type{}, t0 + decltype(uc)::value);   // uniform
   });
-  FMOE_WAIT_VM(0);   // the loads issued past the end have landed before the ring is reused
+  FMOE_WAIT_VM(0);   // the loads issued past the end have landed before the workgroup's LDS is another's
   // the last matrix instructions have retired before hand-placed accumulators are read, see ffn.hip
   if constexpr (NAMED) asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
-  auto result = [&](auto jc, auto rbc, auto fc) {
-    constexpr int rb = decltype(rbc)::value;
-    if constexpr (rb >= NRB) return f32x4_t{0.f, 0.f, 0.f, 0.f};   // rows that are not stored
-    else if constexpr (NAMED) return read_acc<(decltype(jc)::value * NRB + rb) * 2 + decltype(fc)::value>();
-    else return acc[decltype(jc)::value][rb][decltype(fc)::value];
+  if (cu0 + wave >= P.units) return;
+  auto result = [&](auto rbc, auto ic) {
+    if constexpr (NAMED) return read_acc<FRAGS * decltype(rbc)::value + decltype(ic)::value>();
+    else return acc[decltype(rbc)::value][decltype(ic)::value];
   };
-  if constexpr (SWIGLU) {
-    store_hidden<NAB, NCB>(P, tile, ct0 * 64, (ct_limit - ct0) * 64, result, smem);
-  } else {
-    StreamProblem S{};
-    S.C = P.C;
-    S.ldc = P.ldc;
-    S.N = P.N;
-    static_for<0, NCB>([&](auto jc) {
-      if (ct0 + decltype(jc)::value < ct_limit)   // uniform
-        store_tile<false, NAB, RSTAGES>(S, tile, ct0 + decltype(jc)::value, [&](auto rbc, auto fc) { return result(jc, rbc, fc); },
-                                        reinterpret_cast<bf16_t*>(smem));
-    });
-  }
+  static_for<0, NRB>([&](auto rbc) {
+    constexpr int rb = decltype(rbc)::value;
+    const f32x4_t c0 = result(rbc, std::integral_constant<int, 0>{}), c1 = result(rbc, std::integral_constant<int, 1>{});
+    const f32x4_t c2 = result(rbc, std::integral_constant<int, 2>{}), c3 = result(rbc, std::integral_constant<int, 3>{});
+    const int r = rb * 16 + (lane & 15), g = lane >> 4;
+    const size_t at = (size_t)(row0 + r);
+    if constexpr (SWIGLU) {   // eight neighbouring columns a lane, 32 of them in the four lanes of a row
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = silu_mul_bf16(c0[e], c1[e]);
+        v[4 + e] = silu_mul_bf16(c2[e], c3[e]);
+      }
+      uint32_t scale;
+      const uint2 c = rows8::quantize(v, scale, [](uint32_t m) { return rows8::column_max(m); });
+      if (r < rows) {
+        const int col = cu * 32 + 8 * g;
+        *reinterpret_cast<uint2*>(P.H + at * P.ldh + col) = c;
+        if (g == 0) {
+          const int expert = cu / P.expert_groups, k = cu - expert * P.expert_groups;
+          uint8_t* const s = P.Hs + at * P.ldhs + expert * ((P.expert_groups + 3) / 4 * 4) + k;
+          s[0] = (uint8_t)scale;
+          if (k == P.expert_groups - 1)
+            for (int q = k + 1; q & 3; ++q) s[q - k] = 127;   // the word's unused bytes
+        }
+      }
+    } else if (r < rows) {    // sixteen neighbouring columns a lane
+      const int col = cu * 64 + 16 * g;
+      if (col < P.N) {        // (a multiple of 32)
+        auto pair = [](float a, float b) { return (uint32_t)f32_to_bf16(a) | ((uint32_t)f32_to_bf16(b) << 16); };
+        u32x4_t* const to = reinterpret_cast<u32x4_t*>(P.C + at * P.ldc + col);
+        // streaming stores: the next kernel reads the rows, this one never does
+        __builtin_nontemporal_store(u32x4_t{pair(c0[0], c0[1]), pair(c0[2], c0[3]), pair(c1[0], c1[1]), pair(c1[2], c1[3])}, to);
+        __builtin_nontemporal_store(u32x4_t{pair(c2[0], c2[1]), pair(c2[2], c2[3]), pair(c3[0], c3[1]), pair(c3[2], c3[3])}, to + 1);
+      }
+    }
+  });
 }
 
 // field by field, so that the descriptors stay in scalar registers
@@ -323,8 +286,8 @@ __device__ __forceinline__ RowsProblem rows_problem(const RowsArgs& a, const Qua
   RowsProblem Q;
 #define FMOE_SEL(f) Q.f = it.shared ? a.p1.f : a.p0.f
   FMOE_SEL(A); FMOE_SEL(As); FMOE_SEL(lda); FMOE_SEL(ldas); FMOE_SEL(map1); FMOE_SEL(map2); FMOE_SEL(map1_limit);
-  FMOE_SEL(Bp); FMOE_SEL(Sp); FMOE_SEL(group_stride); FMOE_SEL(scale_stride); FMOE_SEL(nbw); FMOE_SEL(N); FMOE_SEL(K);
-  FMOE_SEL(H); FMOE_SEL(Hs); FMOE_SEL(ldh); FMOE_SEL(ldhs); FMOE_SEL(expert_cols); FMOE_SEL(C); FMOE_SEL(ldc);
+  FMOE_SEL(Bp); FMOE_SEL(Sp); FMOE_SEL(group_stride); FMOE_SEL(scale_stride); FMOE_SEL(units); FMOE_SEL(N); FMOE_SEL(K);
+  FMOE_SEL(H); FMOE_SEL(Hs); FMOE_SEL(ldh); FMOE_SEL(ldhs); FMOE_SEL(expert_groups); FMOE_SEL(C); FMOE_SEL(ldc);
   FMOE_SEL(a_group_off); FMOE_SEL(as_group_off); FMOE_SEL(c_group_off);
 #undef FMOE_SEL
   if (it.shared) {   // a shared expert's part of the hidden rows, its output (down)
@@ -335,32 +298,34 @@ __device__ __forceinline__ RowsProblem rows_problem(const RowsArgs& a, const Qua
   return Q;
 }
 
-constexpr int FEW_ROWS = 32, SOME_ROWS = 64, MANY_ROWS = 128;
+constexpr int THIN_ROWS8 = 16, FEW_ROWS = 32, SOME_ROWS = 64, MANY_ROWS = 128;
 constexpr int lds_bytes(int rows) { return RSTAGES * (rows * RBK + (rows > 64 ? rows : 64) * 4); }
 
 template <bool SWIGLU>
-__global__ __launch_bounds__(256, 4) void ffn_rows8_few_kernel(RowsArgs a) {
+__global__ __launch_bounds__(64) void ffn_rows8_thin_kernel(RowsArgs a) {
+  __shared__ __align__(16) char smem[lds_bytes(THIN_ROWS8)];
+  const QuantItem it = find_tile(a, (int)blockIdx.x);
+  if (it.group < 0) return;
+  rows_tile<SWIGLU, 1, THIN_ROWS8, 1, false>(rows_problem(a, it), it.row0, it.rows, it.group, it.unit, smem);
+}
+template <bool SWIGLU>
+__global__ __launch_bounds__(256, 3) void ffn_rows8_few_kernel(RowsArgs a) {
   __shared__ __align__(16) char smem[lds_bytes(FEW_ROWS)];
   const QuantItem it = find_tile(a, (int)blockIdx.x);
   if (it.group < 0) return;
   const RowsProblem P = rows_problem(a, it);
-  fmoe_tile tile{};
-  tile.row0 = it.row0;
-  tile.rows = it.rows;
-  if (it.rows <= 16) rows_tile<SWIGLU, 1, 1, FEW_ROWS, true>(P, tile, it.group, it.unit, it.unit + 1, smem);   // uniform
-  else rows_tile<SWIGLU, 1, 1, FEW_ROWS>(P, tile, it.group, it.unit, it.unit + 1, smem);
+  if (it.rows <= 16) rows_tile<SWIGLU, 1, FEW_ROWS, 4, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);   // uniform
+  else rows_tile<SWIGLU, 2, FEW_ROWS, 4, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);
 }
 template <bool SWIGLU>
-__global__ __launch_bounds__(256, 4) void ffn_rows8_some_kernel(RowsArgs a) {
+__global__ __launch_bounds__(256, 2) void ffn_rows8_some_kernel(RowsArgs a) {
   __shared__ __align__(16) char smem[lds_bytes(SOME_ROWS)];
   const QuantItem it = find_tile(a, (int)blockIdx.x);
   if (it.group < 0) return;
   const RowsProblem P = rows_problem(a, it);
-  fmoe_tile tile{};
-  tile.row0 = it.row0;
-  tile.rows = it.rows;
-  if (it.rows <= 32) rows_tile<SWIGLU, 1, 1, SOME_ROWS>(P, tile, it.group, it.unit, it.unit + 1, smem);
-  else rows_tile<SWIGLU, 2, 1, SOME_ROWS>(P, tile, it.group, it.unit, it.unit + 1, smem);
+  if (it.rows <= 16) rows_tile<SWIGLU, 1, SOME_ROWS, 4, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);
+  else if (it.rows <= 32) rows_tile<SWIGLU, 2, SOME_ROWS, 4, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);
+  else rows_tile<SWIGLU, 4, SOME_ROWS, 4, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);
 }
 // (The build looks at the registers of a kernel of this name.)
 template <bool SWIGLU>
@@ -369,52 +334,50 @@ __global__ __launch_bounds__(256, 2) void ffn_rows8_many_kernel(RowsArgs a) {
   const QuantItem it = find_tile(a, (int)blockIdx.x);
   if (it.group < 0) return;
   const RowsProblem P = rows_problem(a, it);
-  fmoe_tile tile{};
-  tile.row0 = it.row0;
-  tile.rows = it.rows;
-  const int tiles = (P.nbw + 3) / 4, ct0 = 2 * it.unit, limit = ct0 + 2 < tiles ? ct0 + 2 : tiles;
-  switch ((tile.rows + 31) >> 5) {   // live 32-row bands of the tile, uniform
-    case 1: rows_tile<SWIGLU, 1, 2, MANY_ROWS>(P, tile, it.group, ct0, limit, smem); break;
-    case 2: rows_tile<SWIGLU, 2, 2, MANY_ROWS>(P, tile, it.group, ct0, limit, smem); break;
-    case 3: rows_tile<SWIGLU, 3, 2, MANY_ROWS>(P, tile, it.group, ct0, limit, smem); break;
-    default: rows_tile<SWIGLU, 4, 2, MANY_ROWS>(P, tile, it.group, ct0, limit, smem); break;
+  switch ((it.rows + 31) >> 5) {   // live 32-row bands of the tile, uniform
+    case 1: rows_tile<SWIGLU, 2, MANY_ROWS, 4, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
+    case 2: rows_tile<SWIGLU, 4, MANY_ROWS, 4, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
+    case 3: rows_tile<SWIGLU, 6, MANY_ROWS, 4, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
+    default: rows_tile<SWIGLU, 8, MANY_ROWS, 4, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
   }
 }
 
-// Source rows [group][n][k]: codes two to a byte, scales one byte per 32 k.  PAIR: gate and up (fragments 0 and 1), else
-// fragment f = features 16f..16f+15 of the column block.  Past N and K the codes are 0 and the scales 1.
+// Feature of row r of fragment i in column unit cu
+template <bool PAIR>
+__device__ __forceinline__ int unit_feature(int cu, int i, int r) {
+  return PAIR ? 32 * cu + 8 * (r >> 2) + 4 * (i >> 1) + (r & 3) : 64 * cu + 16 * (r >> 2) + 4 * i + (r & 3);
+}
+// Source rows [group][n][k]: codes two to a byte, scales one byte per 32 k.  PAIR: gate (fragments 0 and 2) and up.  Past N and K
+// the codes are 0 and the scales 1.
 template <bool PAIR>
 __global__ __launch_bounds__(256) void pack_rows8_kernel(const u32x4_t* __restrict__ codes0, const uint8_t* __restrict__ scales0,
                                                          const u32x4_t* __restrict__ codes1, const uint8_t* __restrict__ scales1,
                                                          u32x4_t* __restrict__ dst, uint32_t* __restrict__ dst_scales, int G,
-                                                         int N, int K, int nb) {
-  const int NT = rows_tiles(K), NP = rows_pairs(K), KG = K / FMOE_QUANT_GROUP;
-  const size_t total = (size_t)G * nb * NT * 128, total_scales = (size_t)G * nb * NP * 64;
+                                                         int N, int K, int units) {
+  const int NT = rows_tiles(K), KG = K / FMOE_QUANT_GROUP;
+  const size_t total = (size_t)G * units * NT * (FRAGS * 64), total_scales = (size_t)G * units * NT * 64;
   for (size_t u = (size_t)blockIdx.x * blockDim.x + threadIdx.x; u < total + total_scales; u += (size_t)gridDim.x * blockDim.x) {
     const bool scales = u >= total;
     size_t q = scales ? u - total : u;
-    const int lane = (int)(q & 63), col = lane & 15, kg = lane >> 4;
+    const int lane = (int)(q & 63), row = lane & 15;
     q >>= 6;
+    const int f = scales ? 0 : (int)(q % FRAGS);
+    if (!scales) q /= FRAGS;
+    const int k = (int)(q % NT) * 4 + (lane >> 4);   // 32 codes: a 16-byte unit of the source
+    q /= NT;
+    const int cu = (int)(q % units), g = (int)(q / units);
     if (!scales) {
-      const int f = (int)(q & 1);
-      q >>= 1;
-      const int kt = (int)(q % NT);
-      q /= NT;
-      const int b = (int)(q % nb), g = (int)(q / nb);
-      const int n = PAIR ? b * 16 + col : b * 32 + f * 16 + col, k = kt * 4 + kg;   // 32 codes: a 16-byte unit of the source
+      const int n = unit_feature<PAIR>(cu, f, row);
       u32x4_t v = {0u, 0u, 0u, 0u};
-      if (n < N && k < KG) v = (PAIR && f ? codes1 : codes0)[((size_t)g * N + n) * KG + k];
+      if (n < N && k < KG) v = (PAIR && (f & 1) ? codes1 : codes0)[((size_t)g * N + n) * KG + k];
       dst[u] = v;
     } else {
-      const int pair = (int)(q % NP);
-      q /= NP;
-      const int b = (int)(q % nb), g = (int)(q / nb);
       uint32_t v = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int f = i & 1, n = PAIR ? b * 16 + col : b * 32 + f * 16 + col, k = (2 * pair + (i >> 1)) * 4 + kg;
+      for (int i = 0; i < FRAGS; ++i) {
+        const int n = unit_feature<PAIR>(cu, i, row);
         uint32_t s = 127u;
-        if (n < N && k < KG) s = (PAIR && f ? scales1 : scales0)[((size_t)g * N + n) * KG + k];
+        if (n < N && k < KG) s = (PAIR && (i & 1) ? scales1 : scales0)[((size_t)g * N + n) * KG + k];
         v |= s << (8 * i);
       }
       dst_scales[u - total] = v;
@@ -422,16 +385,16 @@ __global__ __launch_bounds__(256) void pack_rows8_kernel(const u32x4_t* __restri
   }
 }
 
-inline int padded_blocks(const PackedMatrix& m) { return (m.nbw + 3) / 4 * 4; }
-inline size_t group_units(const PackedMatrix& m) { return (size_t)padded_blocks(m) * rows_tiles(m.K) * 128; }
-inline size_t group_words(const PackedMatrix& m) { return (size_t)padded_blocks(m) * rows_pairs(m.K) * 64; }
+inline int column_units(const PackedMatrix& m, int which) { return (which & 1) == 0 ? (m.N + 31) / 32 : (m.N + 63) / 64; }
+inline size_t group_words(const PackedMatrix& m, int which) { return (size_t)column_units(m, which) * rows_tiles(m.K) * 64; }
+inline size_t group_units(const PackedMatrix& m, int which) { return group_words(m, which) * FRAGS; }
 inline int scale_bytes(int K) { return rows_tiles(K) * 4; }   // of a row of K values
 
 }  // namespace
 
 size_t fmoe_rows8_bytes(const fmoe_ctx* ctx, int which) {
   const PackedMatrix m = packed_matrix(ctx->cfg, which);
-  return (size_t)m.groups * (group_units(m) * 16 + group_words(m) * 4);
+  return (size_t)m.groups * (group_units(m, which) * 16 + group_words(m, which) * 4);
 }
 
 int launch_pack_rows8(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStream_t stream) {
@@ -442,13 +405,14 @@ int launch_pack_rows8(fmoe_ctx* ctx, const fmoe_quant_tensor* const* w, hipStrea
     const fmoe_quant_tensor* a = w[which == 0 ? 0 : which == 1 ? 2 : which == 2 ? 3 : 5];
     const fmoe_quant_tensor* b = pair ? w[which == 0 ? 1 : 4] : nullptr;
     char* const base = static_cast<char*>(ctx->pr[which]);
-    const size_t blocks = (size_t)m.groups * (group_units(m) + group_words(m)) / 256 + 1;
+    const size_t blocks = (size_t)m.groups * (group_units(m, which) + group_words(m, which)) / 256 + 1;
     const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536)), block(256);
 #define FMOE_PACK(PAIR)                                                                                                 \
   hipLaunchKernelGGL(pack_rows8_kernel<PAIR>, grid, block, 0, stream, static_cast<const u32x4_t*>(a->codes), a->scales, \
                      PAIR ? static_cast<const u32x4_t*>(b->codes) : nullptr, PAIR ? b->scales : nullptr,                \
-                     reinterpret_cast<u32x4_t*>(base), reinterpret_cast<uint32_t*>(base + (size_t)m.groups * group_units(m) * 16), \
-                     m.groups, m.N, m.K, padded_blocks(m))
+                     reinterpret_cast<u32x4_t*>(base),                                                                  \
+                     reinterpret_cast<uint32_t*>(base + (size_t)m.groups * group_units(m, which) * 16), m.groups, m.N, m.K,  \
+                     column_units(m, which))
     if (pair) FMOE_PACK(true);
     else FMOE_PACK(false);
 #undef FMOE_PACK
@@ -471,10 +435,10 @@ int launch_expert_ffn_rows8(const fmoe_ctx* ctx, const uint8_t* codes, const uin
     if (m.groups == 0) return q;
     const char* packed = static_cast<const char*>(ctx->pr[which]);
     q.Bp = reinterpret_cast<const u32x4_t*>(packed);
-    q.Sp = reinterpret_cast<const uint32_t*>(packed + (size_t)m.groups * group_units(m) * 16);
-    q.group_stride = (long long)group_units(m);
-    q.scale_stride = (long long)group_words(m);
-    q.nbw = m.nbw; q.N = m.N; q.K = m.K;
+    q.Sp = reinterpret_cast<const uint32_t*>(packed + (size_t)m.groups * group_units(m, which) * 16);
+    q.group_stride = (long long)group_units(m, which);
+    q.scale_stride = (long long)group_words(m, which);
+    q.units = column_units(m, which); q.N = m.N; q.K = m.K;
     return q;
   };
   // hidden rows: codes, then scale bytes, in the workspace's room for bf16 ones
@@ -491,8 +455,8 @@ int launch_expert_ffn_rows8(const fmoe_ctx* ctx, const uint8_t* codes, const uin
     p.As = q.As = scales; p.ldas = q.ldas = (uint32_t)scale_bytes(d);
     p.map1 = perm_src; p.map1_limit = n_cap;
     p.map2 = q.map2 = kept_idx;
-    p.H = h; p.Hs = hs; p.ldh = (uint32_t)F; p.ldhs = (uint32_t)sF; p.expert_cols = F;
-    q.H = h_shared; q.Hs = hs_shared; q.ldh = (uint32_t)Ft; q.ldhs = (uint32_t)(c.n_shared * sFs); q.expert_cols = Fs;
+    p.H = h; p.Hs = hs; p.ldh = (uint32_t)F; p.ldhs = (uint32_t)sF; p.expert_groups = F / 32;
+    q.H = h_shared; q.Hs = hs_shared; q.ldh = (uint32_t)Ft; q.ldhs = (uint32_t)(c.n_shared * sFs); q.expert_groups = Fs / 32;
   }
   {
     RowsProblem &p = g2.p0, &q = g2.p1;
@@ -502,33 +466,35 @@ int launch_expert_ffn_rows8(const fmoe_ctx* ctx, const uint8_t* codes, const uin
     q.a_group_off = Fs; q.as_group_off = sFs;
     q.C = static_cast<bf16_t*>(y_shared); q.ldc = d; q.c_group_off = (long long)n_cap * d;
   }
+  // 0 thin, 1 few, 2 some, 3 many rows an expert
   const long long per_expert = row_cap / E;
-  const int form = ctx->ffn_shape ? 2 * (ctx->ffn_shape - 1) : per_expert < 16 ? 0 : per_expert < 150 ? 1 : 2;
+  const int form = ctx->ffn_shape ? 3 * (ctx->ffn_shape - 1) : n_cap <= 16 ? 0 : per_expert < 16 ? 1 : per_expert < 150 ? 2 : 3;
   auto launch = [&](auto swiglu, RowsArgs a) {
     constexpr bool S = decltype(swiglu)::value;
     a.expert_offsets = expert_offsets; a.n_dev = n_dev;
     a.E = E; a.n_cap = n_cap; a.row_cap = row_cap;
-    a.log2_bm = 5 + form;
-    const int per_unit = form == 2 ? 8 : 4;   // column blocks of a unit
-    a.cols = (a.p0.nbw + per_unit - 1) / per_unit;
+    a.log2_bm = 4 + form;
+    const int waves = form == 0 ? 1 : 4;   // column units of an item
+    a.cols = (a.p0.units + waves - 1) / waves;
     if (Ft > 0) {
       a.shared_groups = S ? 1 : c.n_shared;
-      a.shared_cols = (a.p1.nbw + per_unit - 1) / per_unit;
+      a.shared_cols = (a.p1.units + waves - 1) / waves;
     }
     const long long tiles = (row_cap < E ? row_cap : E) + (row_cap >> a.log2_bm);   // that the routed experts can have
     const long long shared_tiles = ((long long)n_cap + (1 << a.log2_bm) - 1) >> a.log2_bm;
     const long long items = tiles * a.cols + shared_tiles * a.shared_cols * a.shared_groups;
-    const dim3 grid((unsigned)((items + 7) / 8 * 8)), block(256);
-    if (form == 0) hipLaunchKernelGGL(ffn_rows8_few_kernel<S>, grid, block, 0, stream, a);
-    else if (form == 1) hipLaunchKernelGGL(ffn_rows8_some_kernel<S>, grid, block, 0, stream, a);
+    const dim3 grid((unsigned)((items + 7) / 8 * 8)), block(64 * waves);
+    if (form == 0) hipLaunchKernelGGL(ffn_rows8_thin_kernel<S>, grid, block, 0, stream, a);
+    else if (form == 1) hipLaunchKernelGGL(ffn_rows8_few_kernel<S>, grid, block, 0, stream, a);
+    else if (form == 2) hipLaunchKernelGGL(ffn_rows8_some_kernel<S>, grid, block, 0, stream, a);
     else hipLaunchKernelGGL(ffn_rows8_many_kernel<S>, grid, block, 0, stream, a);
   };
   {
-    fmoe_prof_scope prof(ctx, form == 2 ? SLOT_GEMM1_DENSE : SLOT_GEMM1, stream);
+    fmoe_prof_scope prof(ctx, form == 3 ? SLOT_GEMM1_DENSE : SLOT_GEMM1, stream);
     launch(std::true_type{}, g1);
   }
   {
-    fmoe_prof_scope prof(ctx, form == 2 ? SLOT_GEMM2_DENSE : SLOT_GEMM2, stream);
+    fmoe_prof_scope prof(ctx, form == 3 ? SLOT_GEMM2_DENSE : SLOT_GEMM2, stream);
     launch(std::false_type{}, g2);
   }
   FMOE_HIP_CHECK(hipGetLastError());

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
         v[e] = in ? odd(hi, lo) : 0.0f;
       }
       uint32_t scale;
-      const uint2 c = rows8::quantize(v, scale);
+      const uint2 c = rows8::quantize(v, scale, [](uint32_t m) { return rows8::quad_max(m); });
       if (in) *reinterpret_cast<uint2*>(reinterpret_cast<char*>(a.codes) + base + u * 8) = c;
       if ((u & 3) == 0 && (u >> 2) < a.scale_stride) a.scales[(size_t)row * a.scale_stride + (u >> 2)] = (uint8_t)scale;
     }

@@ -1,4 +1,4 @@
-// Rows in 8 bits: 32 neighbours share a power of two, four lanes with eight values each have a group.
+// Rows in 8 bits: 32 neighbours share a power of two; four lanes with eight values each have a group.
 #pragma once
 
 #include "common.h"
@@ -14,17 +14,26 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
   return v > o ? v : o;
 }
 
-// Eight values of a lane: their e4m3 codes; `scale` becomes the group's scale byte.  The scale is the least power of two with the
+// The same over lanes 16 apart
+__device__ __forceinline__ uint32_t column_max(uint32_t v) {
+  auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = a[0] > a[1] ? a[0] : a[1];
+  a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return a[0] > a[1] ? a[0] : a[1];
+}
+
+// Eight values of a lane: their e4m3 codes; `scale` becomes the group's scale byte; group_max: over the lanes of the group.  The scale is the least power of two with the
 // largest magnitude at most 448 = 1.75 * 2^8 of it, at least 2^-126; 1 for zeros.  The instruction divides by it and rounds to
 // the nearest code, ties to the even one.  An infinity or NaN in the group: codes 0, scale byte 255.
-__device__ __forceinline__ uint2 quantize(const float (&v)[8], uint32_t& scale) {
+template <typename MAX>
+__device__ __forceinline__ uint2 quantize(const float (&v)[8], uint32_t& scale, MAX&& group_max) {
   uint32_t big = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const uint32_t m = __float_as_uint(v[e]) & 0x7fffffffu;
     big = big > m ? big : m;
   }
-  big = quad_max(big);
+  big = group_max(big);
   int e8 = (int)(big >> 23) - 8 + ((big & 0x7fffffu) > 0x600000u ? 1 : 0);
   e8 = e8 < 1 ? 1 : e8;
   if (big == 0u) e8 = 127;
