@@ -751,7 +751,7 @@ int fmoe_layer_forward(fmoe_ctx* ctx, const fmoe_prune_params* params, const voi
 
 size_t fmoe_layer_decode_workspace_bytes(const fmoe_ctx* ctx, int32_t T) {
   if (!ctx || T < 0 || T > FMOE_DECODE_TOKENS) return 0;
-  return fmoe_layout(ctx, T, 1).total + align_up(decode_part_bytes(ctx, T > 0 ? T : 1));
+  return fmoe_layout(ctx, T, 1).total + align_up(decode_extra_bytes(ctx, T > 0 ? T : 1));
 }
 
 int fmoe_layer_decode(fmoe_ctx* ctx, const fmoe_select_params* params, const fmoe_norm_params* norm, const void* x,

@@ -227,10 +227,22 @@ int launch_combine(const fmoe_ctx* ctx, const void* y, const void* y_shared, con
                    const float* topk_gate, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,
                    int n_expected, const void* residual, void* out, hipStream_t stream);
 
-// ---- routing from logits (select.hip), weights in 4 bits (quant.hip)
+// The experts that a few tokens list, ascending: work items of a layer for a decoding step
+struct fmoe_unit {
+  int32_t expert, row0;         // row0: its first hidden row, the rows by expert and token
+  uint32_t mask;                // tokens that list it
+};
+struct fmoe_unit_list {
+  int32_t n, pad[3];
+  float gate[FMOE_MAX_EXPERTS][FMOE_DECODE_TOKENS];   // of the tokens in the mask
+  fmoe_unit unit[FMOE_MAX_EXPERTS];
+};
+
+// ---- routing from logits (select.hip), weights in 4 bits (quant.hip).  units (nullable): fp32 logits of at most
+// FMOE_DECODE_TOKENS tokens, their list is written as well
 int launch_select(const fmoe_ctx* ctx, const fmoe_select_params* p, const void* logits, int dtype,
                   const uint8_t* is_visual, const float* bias, int T, float* scores, int32_t* topk_idx,
-                  float* topk_gate, hipStream_t stream);
+                  float* topk_gate, hipStream_t stream, fmoe_unit_list* units = nullptr);
 int launch_select_backward(const fmoe_ctx* ctx, const fmoe_select_params* p, const void* logits, int dtype,
                            const int32_t* topk_idx, const float* d_gate, const float* d_scores, int T, void* d_logits,
                            hipStream_t stream);
@@ -240,7 +252,7 @@ int launch_dequantize(const void* codes, const uint8_t* scales, long long rows, 
                       hipStream_t stream);
 
 // ---- a layer for a few tokens (decode.hip)
-size_t decode_part_bytes(const fmoe_ctx* ctx, int T);
+size_t decode_extra_bytes(const fmoe_ctx* ctx, int T);   // workspace behind the layer's
 int launch_layer_decode(const fmoe_ctx* ctx, const fmoe_select_params* params, const fmoe_norm_params* norm, const void* x,
                         const void* delta, const uint8_t* is_visual, const float* select_bias, int T, int add_residual, void* out,
                         int32_t* topk_idx, float* topk_gate, void* ws, const fmoe_ws_layout& L, hipStream_t stream);

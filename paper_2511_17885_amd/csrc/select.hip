@@ -456,10 +456,10 @@ __device__ __forceinline__ int sort_entries(const SelectArgs& a, int t, int j, i
 }
 
 // KEYED: the keys are scores with a bias, or sums of scores rank the groups; else the logits are the keys.
+// ks: keys, for groups.  Returns the expert of the lane's place in the token's list, or -1 (also past T), and its gate.
 template <typename ZT, int NQ, bool KEYED, bool SIGMOID>
-__global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
-  constexpr int N = 4 * NQ, STRIDE = 64 * NQ + 4;
-  __shared__ __align__(16) float ks[ROWS][STRIDE];   // keys, for groups
+__device__ __forceinline__ int select_rows(const SelectArgs& a, float (&ks)[ROWS][64 * NQ + 4], float& gate) {
+  constexpr int N = 4 * NQ;
   const int j = threadIdx.x & 15, tok = threadIdx.x >> 4;
   const bool tv = (int)blockIdx.x * ROWS + tok < a.T;
   const int t = tv ? (int)blockIdx.x * ROWS + tok : a.T - 1;
@@ -595,10 +595,56 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
   } else {
     g = mine < 0 ? 0.0f : SIGMOID ? 1.0f / (1.0f + expf(-zl)) : expf(zl - m) * inv;
   }
+  gate = mine >= 0 ? g * a.scale : 0.0f;
   if (tv && j < a.Kmax) {
     a.idx[(size_t)t * a.Kmax + j] = mine;
-    a.gate[(size_t)t * a.Kmax + j] = mine >= 0 ? g * a.scale : 0.0f;
+    a.gate[(size_t)t * a.Kmax + j] = gate;
   }
+  return tv && j < a.Kmax ? mine : -1;
+}
+
+template <typename ZT, int NQ, bool KEYED, bool SIGMOID>
+__global__ __launch_bounds__(256) void select_kernel(SelectArgs a) {
+  __shared__ __align__(16) float ks[ROWS][64 * NQ + 4];
+  float gate;
+  (void)select_rows<ZT, NQ, KEYED, SIGMOID>(a, ks, gate);
+}
+
+// The same for tokens of one workgroup, and the experts that any of them lists, ascending, as work for the launches behind it.
+template <int NQ, bool KEYED, bool SIGMOID>
+__global__ __launch_bounds__(256) void select_units_kernel(SelectArgs a, fmoe_unit_list* list) {
+  __shared__ __align__(16) float ks[ROWS][64 * NQ + 4];
+  __shared__ uint32_t s_mask[FMOE_MAX_EXPERTS];
+  __shared__ int s_rank[FMOE_MAX_EXPERTS];
+  static_assert(ROWS >= FMOE_DECODE_TOKENS && FMOE_MAX_EXPERTS == 256, "tokens of a workgroup; four experts a lane");
+  s_mask[threadIdx.x] = 0u;
+  float gate;
+  const int mine = select_rows<float, NQ, KEYED, SIGMOID>(a, ks, gate), tok = threadIdx.x >> 4;
+  __syncthreads();
+  if (mine >= 0) atomicOr(&s_mask[mine], 1u << tok);
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    uint32_t m[4];
+    int rows = 0, some = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      m[q] = s_mask[4 * lane + q];
+      rows += __popc(m[q]);
+      some += m[q] != 0u;
+    }
+    int row = wave_scan(rows) - rows, rank = wave_scan(some) - some;
+    if (lane == 63) list->n = rank + some;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (m[q] == 0u) continue;
+      s_rank[4 * lane + q] = rank;
+      list->unit[rank++] = fmoe_unit{4 * lane + q, row, m[q]};
+      row += __popc(m[q]);
+    }
+  }
+  __syncthreads();
+  if (mine >= 0) list->gate[s_rank[mine]][tok] = gate;
 }
 
 // To the type of the logits; NaN, which an incoming gradient may hold, stays NaN.
@@ -704,6 +750,17 @@ __global__ __launch_bounds__(256) void select_backward_kernel(SelectBackwardArgs
   }
 }
 
+template <int NQ>
+void run_select_units(const SelectArgs& a, bool keyed, fmoe_unit_list* list, hipStream_t stream) {
+#define FMOE_SELECT(KEYED, SIGMOID) \
+  hipLaunchKernelGGL((select_units_kernel<NQ, KEYED, SIGMOID>), dim3(1), dim3(256), 0, stream, a, list)
+  if (keyed && a.sigmoid) FMOE_SELECT(true, true);
+  else if (keyed) FMOE_SELECT(true, false);
+  else if (a.sigmoid) FMOE_SELECT(false, true);
+  else FMOE_SELECT(false, false);
+#undef FMOE_SELECT
+}
+
 template <typename ZT, int NQ>
 void run_select(const SelectArgs& a, bool keyed, hipStream_t stream) {
   const dim3 grid((a.T + ROWS - 1) / ROWS), block(256);
@@ -739,7 +796,7 @@ void run_backward_by_size(const SelectBackwardArgs& a, bool dense, hipStream_t s
 
 int launch_select(const fmoe_ctx* ctx, const fmoe_select_params* p, const void* logits, int dtype,
                   const uint8_t* is_visual, const float* bias, int T, float* scores, int32_t* topk_idx,
-                  float* topk_gate, hipStream_t stream) {
+                  float* topk_gate, hipStream_t stream, fmoe_unit_list* units) {
   const fmoe_config& c = ctx->cfg;
   SelectArgs a{};
   a.z = logits; a.is_visual = is_visual; a.bias = bias;
@@ -751,7 +808,11 @@ int launch_select(const fmoe_ctx* ctx, const fmoe_select_params* p, const void* 
   a.scale = p->gate_scale;
   a.scores = scores; a.idx = topk_idx; a.gate = topk_gate;
   const bool keyed = bias != nullptr || (p->n_groups > 1 && p->group_score == 1);
-  if (dtype == FMOE_BF16) run_select_by_size<bf16_t>(a, keyed, stream);
+  if (units != nullptr) {   // fp32 logits of at most FMOE_DECODE_TOKENS tokens
+    if (a.E <= 64) run_select_units<1>(a, keyed, units, stream);
+    else if (a.E <= 128) run_select_units<2>(a, keyed, units, stream);
+    else run_select_units<4>(a, keyed, units, stream);
+  } else if (dtype == FMOE_BF16) run_select_by_size<bf16_t>(a, keyed, stream);
   else run_select_by_size<float>(a, keyed, stream);
   FMOE_HIP_CHECK(hipGetLastError());
   return FMOE_OK;
