@@ -2,7 +2,9 @@
 // Compiled with floating-point contraction off: the roundings that norm_dev.h relies on are written out.
 //
 // Bound: memory.  A wavefront has a row in registers (up to 4096 elements; a workgroup of four wavefronts has one of up to 16384,
-// or where there are few rows), reads it once and writes its outputs once.
+// or where there are few rows), reads it once and writes its outputs once.  22016 rows of 2048 in bf16: 73 us, 4.9 TB/s (a copy of
+// 1 GiB 5.2); gradient 72 us with the sums of the weight's; 8192 rows to 8 bits 28.8 us, 4.1 TB/s: some 25 vector instructions an
+// element for the exact rounding beside the loads.
 
 #include "norm_dev.h"
 #include "rows8_dev.h"
@@ -38,7 +40,7 @@ __device__ __forceinline__ double row_total(double v, double* s_part) {
 }
 
 // NU units of eight a lane; WPR wavefronts a row (1 or all 4).
-template <typename XT, typename WT, int NU, int WPR, bool ROWS8>
+template <typename XT, typename WT, int NU, int WPR, bool ROWS8, bool PASS>
 __global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
   __shared__ double s_part[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -53,14 +55,14 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
   for (int i = 0; i < NU; ++i) {
     const int u = first + STEP * i;
     h[i].zero();
-    if (u < units) h[i].load(static_cast<const XT*>(a.x) + base + u * 8);
+    if (u < units) h[i].template load<PASS>(static_cast<const XT*>(a.x) + base + u * 8);
   }
   if (a.delta != nullptr) {
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
       const int u = first + STEP * i;
       dl[i].zero();
-      if (u < units) dl[i].load(static_cast<const XT*>(a.delta) + base + u * 8);
+      if (u < units) dl[i].template load<PASS>(static_cast<const XT*>(a.delta) + base + u * 8);
     }
 #pragma unroll
     for (int i = 0; i < NU; ++i)
@@ -84,7 +86,7 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
     float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (in) {
       load_weights<WT>(a.w, u * 8, w);
-      if (a.h != nullptr) h[i].store(static_cast<XT*>(a.h) + base + u * 8);
+      if (a.h != nullptr) h[i].template store<PASS>(static_cast<XT*>(a.h) + base + u * 8);
     }
     if constexpr (!ROWS8) {
       Unit<XT> n;
@@ -118,7 +120,7 @@ struct NormBackwardArgs {
 };
 
 // With c = h r and g = dn w: dx = dh + r (g - c mean(g c)); a workgroup's rows add dn c up for the weight, one partial sum each.
-template <typename XT, typename WT, int NU, int WPR>
+template <typename XT, typename WT, int NU, int WPR, bool PASS>
 __global__ __launch_bounds__(256) void rms_norm_backward_kernel(NormBackwardArgs a) {
   __shared__ double s_part[4];
   __shared__ float s_dw[WPR == 1 ? 64 * NU * 8 : 1];
@@ -148,9 +150,9 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(NormBackwardArgs
       g[i].zero();
       dh[i].zero();
       if (u < units) {
-        h[i].load(static_cast<const XT*>(a.h) + base + u * 8);
-        g[i].load(static_cast<const XT*>(a.dn) + base + u * 8);
-        if (a.dh != nullptr) dh[i].load(static_cast<const XT*>(a.dh) + base + u * 8);
+        h[i].template load<PASS>(static_cast<const XT*>(a.h) + base + u * 8);
+        g[i].template load<PASS>(static_cast<const XT*>(a.dn) + base + u * 8);
+        if (a.dh != nullptr) dh[i].template load<PASS>(static_cast<const XT*>(a.dh) + base + u * 8);
       }
     }
     double sum = 0.0;
@@ -189,7 +191,7 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(NormBackwardArgs
         if constexpr (sizeof(XT) == 2) out.set2(e, nearest_bf16(v[e]), nearest_bf16(v[e + 1]));
         else out.set2(e, v[e], v[e + 1]);
       }
-      if (u < units) out.store(static_cast<XT*>(a.dx) + base + u * 8);
+      if (u < units) out.template store<PASS>(static_cast<XT*>(a.dx) + base + u * 8);
     }
   }
   if (a.part == nullptr) return;
@@ -219,34 +221,55 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(NormBackwardArgs
   }
 }
 
-// The partial sums of every column, in a fixed order: four wavefronts a quarter of them each.
+// The partial sums of every column, in a fixed order: a workgroup has 32 columns, four a lane, and takes 32 partial sums at a time.
 __global__ __launch_bounds__(256) void rms_norm_weight_kernel(const float* __restrict__ part, int parts, int d,
                                                               float* __restrict__ dw) {
-  __shared__ double s[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int k = (int)blockIdx.x * 64 + lane;
-  double sum = 0.0;
+  __shared__ double s[32][33];
+  const int c = (threadIdx.x & 7) * 4, first = threadIdx.x >> 3, k = (int)blockIdx.x * 32 + c;   // (d is a multiple of eight)
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
   if (k < d) {
 #pragma unroll 8
-    for (int p = wave; p < parts; p += 4) sum += (double)part[(size_t)p * d + k];
+    for (int p = first; p < parts; p += 32) {
+      const f32x4_t v = *reinterpret_cast<const f32x4_t*>(part + (size_t)p * d + k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += (double)v[e];
+    }
   }
-  s[wave][lane] = sum;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s[first][c + e] = sum[e];
   __syncthreads();
-  if (wave == 0 && k < d) dw[k] = (float)((s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]));
+  const int col = (int)blockIdx.x * 32 + (int)threadIdx.x;
+  if (threadIdx.x >= 32 || col >= d) return;
+  double total = 0.0;
+#pragma unroll
+  for (int p = 0; p < 32; ++p) total += s[p][threadIdx.x];
+  dw[col] = (float)total;
 }
 
-// Wavefronts a row: all four of a workgroup for rows that one cannot hold, and for few rows
-int waves_per_row(int T, int d) { return d > 4096 || T <= 1024 ? 4 : 1; }
+// Do the inputs and h, which nobody asks for again soon, pass the caches by?  (n is read by the next launch and stays.)  us with / without:
+// bf16, d 2048, 22016 rows 73 / 78, 8192 rows 31.7 / 31.8, in 8 bits 28.8 / 33.3; gradient 22016 rows 71.6 / 78.7, 8192 rows 34.0 / 36.8,
+// 4096 rows (67 MB) 24.0 / 22.9.
+bool passes(size_t bytes) { return bytes >= ((size_t)100 << 20); }
+
+// Wavefronts a row: all four of a workgroup for rows that one cannot hold, and where rows of more than 64 units are few.  us with one / four:
+// bf16, d 2048, 4096 rows 18.4 / 16.4, 2048 rows 13.0 / 11.1, 600 rows 8.1 / 5.6; d 1280 100 rows 6.4 / 4.5; d 1288 in fp32 1601 rows 6.8 / 6.4;
+// d 1024 in 8 bits 4096 rows 11.7 / 12.7, d 512 3000 rows 6.1 / 9.9.
+int waves_per_row(int T, int d) { return d > 4096 || (d > 1024 && T <= 4096) ? 4 : 1; }
+// The gradient, with two sums a row between which four wavefronts would wait for each other: d 2048 bf16 22016 rows 72 / 88, 4096 rows
+// 22.6 / 24.9, 200 rows 8.4 / 8.8; d 1280 in fp32 600 rows 10.6 / 13.6.
+int waves_per_gradient(int d) { return d > 4096 ? 4 : 1; }
 
 template <typename XT, typename WT, bool ROWS8>
 void run_norm(const NormArgs& a, hipStream_t stream) {
   const int wpr = waves_per_row(a.T, a.d);
   const int units = ROWS8 ? (a.d + 127) / 128 * 16 : a.d / 8, per_lane = (units + 64 * wpr - 1) / (64 * wpr);
   const dim3 grid(wpr == 1 ? (a.T + 3) / 4 : a.T), block(256);
-#define FMOE_NORM(NU)                                                                                     \
-  do {                                                                                                    \
-    if (wpr == 1) hipLaunchKernelGGL((rms_norm_kernel<XT, WT, NU, 1, ROWS8>), grid, block, 0, stream, a); \
-    else hipLaunchKernelGGL((rms_norm_kernel<XT, WT, NU, 4, ROWS8>), grid, block, 0, stream, a);          \
+  const bool pass = wpr == 1 && passes((size_t)a.T * a.d * sizeof(XT) * (a.delta != nullptr ? 4 : 2));
+#define FMOE_NORM(NU)                                                                                                 \
+  do {                                                                                                                \
+    if (pass) hipLaunchKernelGGL((rms_norm_kernel<XT, WT, NU, 1, ROWS8, true>), grid, block, 0, stream, a);           \
+    else if (wpr == 1) hipLaunchKernelGGL((rms_norm_kernel<XT, WT, NU, 1, ROWS8, false>), grid, block, 0, stream, a); \
+    else hipLaunchKernelGGL((rms_norm_kernel<XT, WT, NU, 4, ROWS8, false>), grid, block, 0, stream, a);               \
   } while (0)
   if (per_lane <= 1) FMOE_NORM(1);
   else if (per_lane <= 2) FMOE_NORM(2);
@@ -257,13 +280,15 @@ void run_norm(const NormArgs& a, hipStream_t stream) {
 }
 template <typename XT, typename WT>
 void run_backward(const NormBackwardArgs& a, int blocks, hipStream_t stream) {
-  const int wpr = waves_per_row(a.T, a.d);
+  const int wpr = waves_per_gradient(a.d);
   const int per_lane = (a.d / 8 + 64 * wpr - 1) / (64 * wpr);
   const dim3 grid(blocks), block(256);
-#define FMOE_NORM(NU)                                                                                       \
-  do {                                                                                                      \
-    if (wpr == 1) hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 1>), grid, block, 0, stream, a); \
-    else hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 4>), grid, block, 0, stream, a);          \
+  const bool pass = wpr == 1 && passes((size_t)a.T * a.d * sizeof(XT) * (a.dh != nullptr ? 4 : 3));
+#define FMOE_NORM(NU)                                                                                                   \
+  do {                                                                                                                  \
+    if (pass) hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 1, true>), grid, block, 0, stream, a);           \
+    else if (wpr == 1) hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 1, false>), grid, block, 0, stream, a); \
+    else hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 4, false>), grid, block, 0, stream, a);               \
   } while (0)
   if (per_lane <= 1) FMOE_NORM(1);
   else if (per_lane <= 2) FMOE_NORM(2);
@@ -277,7 +302,7 @@ void run_backward(const NormBackwardArgs& a, int blocks, hipStream_t stream) {
 
 // Workgroups of the backward kernel, and so partial sums of the weight's gradient
 int norm_backward_blocks(int T, int d) {
-  const int rows = waves_per_row(T, d) == 1 ? (T + 3) / 4 : T;
+  const int rows = waves_per_gradient(d) == 1 ? (T + 3) / 4 : T;
   return rows < 512 ? rows : 512;
 }
 
@@ -313,7 +338,7 @@ int launch_rms_norm_backward(const void* h, const void* weight, const void* d_n,
     else run_backward<float, float>(a, blocks, stream);
   }
   if (d_weight != nullptr)
-    hipLaunchKernelGGL(rms_norm_weight_kernel, dim3((d + 63) / 64), dim3(256), 0, stream, part, blocks, d, d_weight);
+    hipLaunchKernelGGL(rms_norm_weight_kernel, dim3((d + 31) / 32), dim3(256), 0, stream, part, blocks, d, d_weight);
   FMOE_HIP_CHECK(hipGetLastError());
   return FMOE_OK;
 }

@@ -90,21 +90,38 @@ template <> __device__ __forceinline__ bf16_t value_rounded<bf16_t>(float h, flo
 template <typename T> struct Unit;
 template <> struct Unit<bf16_t> {
   u32x4_t v;
-  __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const u32x4_t*>(p); }
-  __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<u32x4_t*>(p) = v; }
+  template <bool PASS = false>   // past the caches
+  __device__ __forceinline__ void load(const bf16_t* p) {
+    if constexpr (PASS) v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
+    else v = *reinterpret_cast<const u32x4_t*>(p);
+  }
+  template <bool PASS = false>
+  __device__ __forceinline__ void store(bf16_t* p) const {
+    if constexpr (PASS) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(p));
+    else *reinterpret_cast<u32x4_t*>(p) = v;
+  }
   __device__ __forceinline__ void zero() { v = u32x4_t{0u, 0u, 0u, 0u}; }
   __device__ __forceinline__ float get(int i) const { return __uint_as_float((i & 1) ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
   __device__ __forceinline__ void set2(int i, bf16_t a, bf16_t b) { v[i >> 1] = (uint32_t)a | ((uint32_t)b << 16); }   // i even
 };
 template <> struct Unit<float> {
   f32x4_t lo, hi;
+  template <bool PASS = false>
   __device__ __forceinline__ void load(const float* p) {
-    lo = reinterpret_cast<const f32x4_t*>(p)[0];
-    hi = reinterpret_cast<const f32x4_t*>(p)[1];
+    const f32x4_t* const q = reinterpret_cast<const f32x4_t*>(p);
+    lo = PASS ? __builtin_nontemporal_load(q) : q[0];
+    hi = PASS ? __builtin_nontemporal_load(q + 1) : q[1];
   }
+  template <bool PASS = false>
   __device__ __forceinline__ void store(float* p) const {
-    reinterpret_cast<f32x4_t*>(p)[0] = lo;
-    reinterpret_cast<f32x4_t*>(p)[1] = hi;
+    f32x4_t* const q = reinterpret_cast<f32x4_t*>(p);
+    if constexpr (PASS) {
+      __builtin_nontemporal_store(lo, q);
+      __builtin_nontemporal_store(hi, q + 1);
+    } else {
+      q[0] = lo;
+      q[1] = hi;
+    }
   }
   __device__ __forceinline__ void zero() { lo = hi = f32x4_t{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ float get(int i) const { return i < 4 ? lo[i] : hi[i - 4]; }
