@@ -232,13 +232,26 @@ def dequantize_weights(codes, scales, dtype=torch.bfloat16):
     return w
 
 
+_FLOAT = {torch.float32: FMOE_F32, torch.bfloat16: FMOE_BF16}
+
+
+def _differs(t, dtype, shape, index):
+    """_expect's conditions with a device index (-1: the host), in a third of its time."""
+    return t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous()
+
+
 def _norm_args(x, weight, delta):
-    d = x.shape[-1]
-    dtype = _float_type(x, "x")
-    _expect(x, "x", x.dtype, x.shape, x.device)
-    _expect(delta, "delta", x.dtype, x.shape, x.device)
-    weight_dtype = _float_type(weight, "weight")
-    _expect(weight, "weight", weight.dtype, (d,), x.device)
+    kind, weight_kind, shape, index = x.dtype, weight.dtype, x.shape, x.get_device()
+    dtype, weight_dtype, d = _FLOAT.get(kind), _FLOAT.get(weight_kind), shape[-1]
+    if dtype is None or weight_dtype is None:
+        _float_type(x, "x")
+        _float_type(weight, "weight")
+    if not x.is_contiguous():
+        _expect(x, "x", kind, shape, x.device)
+    if delta is not None and _differs(delta, kind, shape, index):
+        _expect(delta, "delta", kind, shape, x.device)
+    if _differs(weight, weight_kind, (d,), index):
+        _expect(weight, "weight", weight_kind, (d,), x.device)
     return dtype, weight_dtype, x.numel() // max(d, 1), d
 
 
@@ -247,7 +260,8 @@ def rms_norm(x, weight, eps=1e-6, delta=None):
     Returns (h, n): h = x + delta, x itself without delta.  They carry no autograd graph (rms_norm_backward)."""
     dtype, weight_dtype, T, d = _norm_args(x, weight, delta)
     h, n = (None if delta is None else torch.empty_like(x)), torch.empty_like(x)
-    _call(x.device, load().fmoe_rms_norm, _ptr(x), _ptr(delta), _ptr(weight), dtype, weight_dtype, T, d, eps, _ptr(h), _ptr(n))
+    _call(x.device, load().fmoe_rms_norm, x.data_ptr(), None if h is None else delta.data_ptr(), weight.data_ptr(), dtype, weight_dtype,
+          T, d, eps, None if h is None else h.data_ptr(), n.data_ptr())
     return (x if h is None else h), n
 
 
@@ -258,8 +272,8 @@ def rms_norm_quant(x, weight, eps=1e-6, delta=None):
     h = None if delta is None else torch.empty_like(x)
     codes = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
     scales = torch.empty(*x.shape[:-1], row_scales(d), dtype=torch.uint8, device=x.device)
-    _call(x.device, load().fmoe_rms_norm_quant, _ptr(x), _ptr(delta), _ptr(weight), dtype, weight_dtype, T, d, eps, _ptr(h),
-          _ptr(codes), _ptr(scales))
+    _call(x.device, load().fmoe_rms_norm_quant, x.data_ptr(), None if h is None else delta.data_ptr(), weight.data_ptr(), dtype,
+          weight_dtype, T, d, eps, None if h is None else h.data_ptr(), codes.data_ptr(), scales.data_ptr())
     return (x if h is None else h), codes, scales
 
 
@@ -272,8 +286,9 @@ def rms_norm_backward(h, weight, eps, d_n, d_h=None, want_weight=True):
     """fmoe_rms_norm_backward: (gradient of x, which is delta's too; gradient of the weight [d] float32 or None) from those of n and,
     if given, of h."""
     dtype, weight_dtype, T, d = _norm_args(h, weight, None)
-    _expect(d_n, "d_n", h.dtype, h.shape, h.device)
-    _expect(d_h, "d_h", h.dtype, h.shape, h.device)
+    for t, what in ((d_n, "d_n"), (d_h, "d_h")):
+        if t is not None and _differs(t, h.dtype, h.shape, h.get_device()):
+            _expect(t, what, h.dtype, h.shape, h.device)
     d_x, d_weight, ws, need = torch.empty_like(h), None, None, 0
     if want_weight:
         d_weight = torch.empty(d, dtype=torch.float32, device=h.device)
@@ -555,25 +570,30 @@ class FMoE:
         """fmoe_layer_decode: the layer for a decoding step, x [T, d] with at most 16 tokens.  norm: (weight [d], eps) or None;
         delta [T, d]: added to x first; params: select_params(...), None for a softmax router.  Returns (out [T, d], topk_idx, topk_gate)."""
         T, K = x.shape[0], max(self.kmax, 1)
-        _expect(x, "x", self.torch_dtype, (T, self.d), self.device)
-        _expect(delta, "delta", self.torch_dtype, (T, self.d), self.device)
-        _expect(is_visual, "is_visual", torch.uint8, (T,), self.device)
-        _expect(select_bias, "select_bias", torch.float32, (self.E,), self.device)
-        _expect(out, "out", self.torch_dtype, (T, self.d), self.device)
+        rows, kind, index = (T, self.d), self.torch_dtype, self.device.index
+        for t, what in ((x, "x"), (delta, "delta"), (out, "out")):
+            if t is not None and _differs(t, kind, rows, index):
+                _expect(t, what, kind, rows, self.device)
+        if is_visual is not None and _differs(is_visual, torch.uint8, (T,), index):
+            _expect(is_visual, "is_visual", torch.uint8, (T,), self.device)
+        if select_bias is not None and _differs(select_bias, torch.float32, (self.E,), index):
+            _expect(select_bias, "select_bias", torch.float32, (self.E,), self.device)
         normed = None
         if norm is not None:
             weight, eps = norm
             normed = C.byref(FmoeNormParams(weight.data_ptr(), _float_type(weight, "weight"), eps))
-            _expect(weight, "weight", weight.dtype, (self.d,), self.device)
+            if _differs(weight, weight.dtype, (self.d,), index):
+                _expect(weight, "weight", weight.dtype, (self.d,), self.device)
         if out is None:
             out = torch.empty_like(x)
         idx, gate = self._i32(T, K), self._f32(T, K)
         need = int(self.lib.fmoe_layer_decode_workspace_bytes(self._ctx, T))
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        _check(self.lib.fmoe_layer_decode(self._ctx, C.byref(params) if params is not None else None, normed, _ptr(x), _ptr(delta),
-                                          _ptr(is_visual), _ptr(select_bias), T, int(bool(add_residual)), _ptr(out), _ptr(idx),
-                                          _ptr(gate), _ptr(self._ws), self._ws.numel(), _stream()))
+        at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        _check(self.lib.fmoe_layer_decode(self._ctx, C.byref(params) if params is not None else None, normed, x.data_ptr(), at(delta),
+                                          at(is_visual), at(select_bias), T, int(bool(add_residual)), out.data_ptr(), idx.data_ptr(),
+                                          gate.data_ptr(), self._ws.data_ptr(), self._ws.numel(), _stream()))
         if self.kmax == 0:
             idx, gate = idx[:, :0], gate[:, :0]
         return out, idx, gate

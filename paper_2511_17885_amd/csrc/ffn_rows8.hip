@@ -86,15 +86,14 @@ __device__ __forceinline__ f32x4_t mfma_rows(u32x4_t w, uint32_t sw, i32x8_t r, 
 }
 
 // One work item: NRB row blocks of 16, LDS stages of ROWS rows; wavefront w has column unit cu0 + w.
-template <bool SWIGLU, int NRB, int ROWS, int WAVES, bool NAMED>
+template <bool SWIGLU, int NRB, int ROWS, bool NAMED>
 __device__ __forceinline__ void rows_tile(const RowsProblem& P, int row0, int rows, int group, int cu0, char* smem) {
-  static_assert(16 * NRB <= ROWS && (WAVES == 1 || WAVES == 4), "the rows fit in a stage");
-  constexpr int NLA = (2 * NRB + WAVES - 1) / WAVES;           // loads of eight rows a wavefront
-  static_assert(8 * NLA * WAVES <= ROWS, "and so do the rows that are loaded");
+  constexpr int NLA = (NRB + 1) / 2;                           // loads of eight rows a wavefront
+  static_assert(32 * NLA <= ROWS, "the rows fit in a stage");
   constexpr int SROWS = ROWS > 64 ? ROWS : 64;                 // scale words a stage
   constexpr int PER_TILE = NLA + 1 + FRAGS + 1;                // loads of a k tile
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int K = P.K, NT = rows_tiles(K);
   char* const rows_lds = smem;
   char* const scales_lds = smem + RSTAGES * ROWS * RBK;
@@ -118,13 +117,13 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, int row0, int ro
   auto load_s = [&](int slot, int t) {
     sreg[slot] = __builtin_amdgcn_raw_buffer_load_b32(s_rsrc, lane4, sbase + (uint32_t)(t < NT ? t : NT - 1) * 256u, 0);
   };
-  // Rows this lane fetches: 8 (it * WAVES + wave) + lane / 8 of the tile; scale words of row 64 (wave % 2) + lane (or lane where the
+  // Rows this lane fetches: 32 it + 8 wave + lane / 8 of the tile; scale words of row 64 (wave % 2) + lane (or lane where the
   // stage has 64: the wavefronts then fetch the same).  Past the tile its last row.
   const uint32_t most = 0xffffffffu / P.lda - 1u;
   int src[NLA + 1];
 #pragma unroll
   for (int it = 0; it <= NLA; ++it) {
-    const int r = it < NLA ? 8 * (it * WAVES + wave) + (lane >> 3) : (ROWS > 64 ? 64 * (wave & 1) : 0) + lane;
+    const int r = it < NLA ? 32 * it + 8 * wave + (lane >> 3) : (ROWS > 64 ? 64 * (wave & 1) : 0) + lane;
     src[it] = row0 + (r < rows ? r : rows - 1);
     if (P.map1) src[it] = P.map1[src[it]];
   }
@@ -145,7 +144,7 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, int row0, int ro
     if (P.map2) s = P.map2[s];
     const uint32_t at = (uint32_t)s < most ? (uint32_t)s : most;
     if (it < NLA) {   // row r keeps its 16-byte piece c at place c ^ (r / 2 % 8)
-      const int piece = ((lane & 7) ^ ((4 * (it * WAVES + wave) + (lane >> 4)) & 7)) * 16;
+      const int piece = ((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) * 16;
       a_last[it] = at * P.lda + (uint32_t)(k_last + piece < K ? piece : K - 16 - k_last);   // past K the row's end again
       a_src[it] = at * P.lda + (uint32_t)piece;
     } else {
@@ -153,7 +152,7 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, int row0, int ro
     }
   }
   auto load_a = [&](int stage, int t, int it) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rsrc, FMOE_LPTR(rows_lds + stage * (ROWS * RBK) + 8 * (it * WAVES + wave) * RBK), 16,
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rsrc, FMOE_LPTR(rows_lds + stage * (ROWS * RBK) + (32 * it + 8 * wave) * RBK), 16,
                                              t < NT - 1 ? a_src[it] : a_last[it], (uint32_t)(t < NT ? t : NT - 1) * RBK, 0, 0);
   };
   auto load_as = [&](int stage, int t) {
@@ -200,8 +199,7 @@ __device__ __forceinline__ void rows_tile(const RowsProblem& P, int row0, int ro
       if (t < RAHEAD) FMOE_WAIT_VM(LATER * (NLA + 1) + U * PER_TILE);
       else FMOE_WAIT_VM((RAHEAD - 1) * PER_TILE);
     }
-    // every wavefront's share of the tile is in LDS; all are done with the tile before (one alone has waited for its reads)
-    if constexpr (WAVES > 1) block_barrier();
+    block_barrier();   // every wavefront's share of the tile is in LDS; all are done with the tile before
     constexpr int off = U * (ROWS * RBK), off_s = U * (SROWS * 4);
     issue_rows<off, off_s>(frag_a0, frag_a1, frag_s, fa[0][0], fa[0][1], fs[0]);
     static_for<0, NRB>([&](auto rc) {
@@ -298,47 +296,34 @@ __device__ __forceinline__ RowsProblem rows_problem(const RowsArgs& a, const Qua
   return Q;
 }
 
-constexpr int THIN_ROWS8 = 16, FEW_ROWS = 32, SOME_ROWS = 64, MANY_ROWS = 128;
+constexpr int FEW_ROWS = 32, MANY_ROWS = 128;
 constexpr int lds_bytes(int rows) { return RSTAGES * (rows * RBK + (rows > 64 ? rows : 64) * 4); }
 
-template <bool SWIGLU>
-__global__ __launch_bounds__(64) void ffn_rows8_thin_kernel(RowsArgs a) {
-  __shared__ __align__(16) char smem[lds_bytes(THIN_ROWS8)];
-  const QuantItem it = find_tile(a, (int)blockIdx.x);
-  if (it.group < 0) return;
-  rows_tile<SWIGLU, 1, THIN_ROWS8, 1, false>(rows_problem(a, it), it.row0, it.rows, it.group, it.unit, smem);
-}
+// Bound: the weights (400 tokens, d 2048, 128 experts of 768, 12 rows an expert: 44 + 27 us with the launches, 4.9 TB/s).
 template <bool SWIGLU>
 __global__ __launch_bounds__(256, 3) void ffn_rows8_few_kernel(RowsArgs a) {
   __shared__ __align__(16) char smem[lds_bytes(FEW_ROWS)];
-  const QuantItem it = find_tile(a, (int)blockIdx.x);
+  const QuantItem it = find_tile<true>(a, (int)blockIdx.x);
   if (it.group < 0) return;
   const RowsProblem P = rows_problem(a, it);
-  if (it.rows <= 16) rows_tile<SWIGLU, 1, FEW_ROWS, 4, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);   // uniform
-  else rows_tile<SWIGLU, 2, FEW_ROWS, 4, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);
+  if (it.rows <= 16) rows_tile<SWIGLU, 1, FEW_ROWS, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);   // uniform
+  else rows_tile<SWIGLU, 2, FEW_ROWS, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);
 }
-template <bool SWIGLU>
-__global__ __launch_bounds__(256, 2) void ffn_rows8_some_kernel(RowsArgs a) {
-  __shared__ __align__(16) char smem[lds_bytes(SOME_ROWS)];
-  const QuantItem it = find_tile(a, (int)blockIdx.x);
-  if (it.group < 0) return;
-  const RowsProblem P = rows_problem(a, it);
-  if (it.rows <= 16) rows_tile<SWIGLU, 1, SOME_ROWS, 4, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);
-  else if (it.rows <= 32) rows_tile<SWIGLU, 2, SOME_ROWS, 4, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);
-  else rows_tile<SWIGLU, 4, SOME_ROWS, 4, false>(P, it.row0, it.rows, it.group, 4 * it.unit, smem);
-}
+// Bound: matrix instructions, by the power they take: 16384 tokens, two experts of 8192, d 4096 883 + 468 us, 2.4 PFLOP/s (a bf16 library
+// product of 8192^3 1.18), matrix units 70 % busy at a clock of 1.6 GHz.  With short reductions and few rows also an item's start and end:
+// 8192 tokens, d 2048, 128 experts of 768 125 + 88 us, matrix units 50 and 32 % busy.
 // (The build looks at the registers of a kernel of this name.)
 template <bool SWIGLU>
 __global__ __launch_bounds__(256, 2) void ffn_rows8_many_kernel(RowsArgs a) {
   __shared__ __align__(16) char smem[lds_bytes(MANY_ROWS)];
-  const QuantItem it = find_tile(a, (int)blockIdx.x);
+  const QuantItem it = find_tile<true>(a, (int)blockIdx.x);
   if (it.group < 0) return;
   const RowsProblem P = rows_problem(a, it);
   switch ((it.rows + 31) >> 5) {   // live 32-row bands of the tile, uniform
-    case 1: rows_tile<SWIGLU, 2, MANY_ROWS, 4, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
-    case 2: rows_tile<SWIGLU, 4, MANY_ROWS, 4, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
-    case 3: rows_tile<SWIGLU, 6, MANY_ROWS, 4, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
-    default: rows_tile<SWIGLU, 8, MANY_ROWS, 4, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
+    case 1: rows_tile<SWIGLU, 2, MANY_ROWS, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
+    case 2: rows_tile<SWIGLU, 4, MANY_ROWS, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
+    case 3: rows_tile<SWIGLU, 6, MANY_ROWS, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
+    default: rows_tile<SWIGLU, 8, MANY_ROWS, true>(P, it.row0, it.rows, it.group, 4 * it.unit, smem); break;
   }
 }
 
@@ -466,35 +451,38 @@ int launch_expert_ffn_rows8(const fmoe_ctx* ctx, const uint8_t* codes, const uin
     q.a_group_off = Fs; q.as_group_off = sFs;
     q.C = static_cast<bf16_t*>(y_shared); q.ldc = d; q.c_group_off = (long long)n_cap * d;
   }
-  // 0 thin, 1 few, 2 some, 3 many rows an expert
-  const long long per_expert = row_cap / E;
-  const int form = ctx->ffn_shape ? 3 * (ctx->ffn_shape - 1) : n_cap <= 16 ? 0 : per_expert < 16 ? 1 : per_expert < 150 ? 2 : 3;
+  // Tiles of 128 rows from so many rows an expert on, if those are items enough (tiles that the call can have times items of the narrower
+  // product).  us, tiles of 32 / 128, gate/up and down with the launches: 1280, 64 of 896, two shared 20 rows an expert 41.7 / 43.8, 75
+  // rows 63 / 62; 2048, 64 of 1408 94 rows 117 / 86, 192 rows, two shared 290 / 206; 128 of 768 256 rows 297 / 210; 512, 256 of 512
+  // 125 rows 76 / 72; few items: 4096, 8 of 1536 150 rows (204) 45 / 50, 375 rows (376) 87 / 78; 1280, 16 of 896 100 rows (140) 24 / 30, 400
+  // rows (330) 43 / 45; 512, 64 of 512 150 rows (278) 31 / 32.  (Tiles of 64 between: at best 3 % from 9 to 75 rows.)
+  const long long units1 = (g1.p0.units + 3) / 4, units2 = (g2.p0.units + 3) / 4;
+  const bool many = ctx->ffn_shape ? ctx->ffn_shape == 2
+                                   : row_cap >= 64 * E && (E + row_cap / MANY_ROWS) * (units1 < units2 ? units1 : units2) >= 300;
   auto launch = [&](auto swiglu, RowsArgs a) {
     constexpr bool S = decltype(swiglu)::value;
     a.expert_offsets = expert_offsets; a.n_dev = n_dev;
     a.E = E; a.n_cap = n_cap; a.row_cap = row_cap;
-    a.log2_bm = 4 + form;
-    const int waves = form == 0 ? 1 : 4;   // column units of an item
-    a.cols = (a.p0.units + waves - 1) / waves;
+    static_assert(FEW_ROWS == 1 << 5 && MANY_ROWS == 1 << 7, "rows of a tile");
+    a.log2_bm = many ? 7 : 5;
+    a.cols = (a.p0.units + 3) / 4;   // items of four column units
     if (Ft > 0) {
       a.shared_groups = S ? 1 : c.n_shared;
-      a.shared_cols = (a.p1.units + waves - 1) / waves;
+      a.shared_cols = (a.p1.units + 3) / 4;
     }
     const long long tiles = (row_cap < E ? row_cap : E) + (row_cap >> a.log2_bm);   // that the routed experts can have
     const long long shared_tiles = ((long long)n_cap + (1 << a.log2_bm) - 1) >> a.log2_bm;
-    const long long items = tiles * a.cols + shared_tiles * a.shared_cols * a.shared_groups;
-    const dim3 grid((unsigned)((items + 7) / 8 * 8)), block(64 * waves);
-    if (form == 0) hipLaunchKernelGGL(ffn_rows8_thin_kernel<S>, grid, block, 0, stream, a);
-    else if (form == 1) hipLaunchKernelGGL(ffn_rows8_few_kernel<S>, grid, block, 0, stream, a);
-    else if (form == 2) hipLaunchKernelGGL(ffn_rows8_some_kernel<S>, grid, block, 0, stream, a);
-    else hipLaunchKernelGGL(ffn_rows8_many_kernel<S>, grid, block, 0, stream, a);
+    const long long eighths = (tiles * a.cols + 7) / 8 + (shared_tiles * a.shared_cols * a.shared_groups + 7) / 8;
+    const dim3 grid((unsigned)(eighths * 8)), block(256);
+    if (many) hipLaunchKernelGGL(ffn_rows8_many_kernel<S>, grid, block, 0, stream, a);
+    else hipLaunchKernelGGL(ffn_rows8_few_kernel<S>, grid, block, 0, stream, a);
   };
   {
-    fmoe_prof_scope prof(ctx, form == 3 ? SLOT_GEMM1_DENSE : SLOT_GEMM1, stream);
+    fmoe_prof_scope prof(ctx, many ? SLOT_GEMM1_DENSE : SLOT_GEMM1, stream);
     launch(std::true_type{}, g1);
   }
   {
-    fmoe_prof_scope prof(ctx, form == 3 ? SLOT_GEMM2_DENSE : SLOT_GEMM2, stream);
+    fmoe_prof_scope prof(ctx, many ? SLOT_GEMM2_DENSE : SLOT_GEMM2, stream);
     launch(std::false_type{}, g2);
   }
   FMOE_HIP_CHECK(hipGetLastError());

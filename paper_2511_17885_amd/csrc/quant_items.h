@@ -22,7 +22,9 @@ struct QuantItem {
   bool shared;
 };
 // Row tiles of 1 << a.log2_bm rows.  Experts whose offsets are malformed are skipped as in fmoe_build_tiles.  Uniform.
-template <typename ARGS>
+// EVEN: an eighth of the shared groups' items and an eighth of the routed experts' for each XCD (workgroups: those of either, rounded
+// up to eights); else an eighth of the sequence, which leaves the weights of the routed experts to some of them.
+template <bool EVEN = false, typename ARGS>
 __device__ __forceinline__ QuantItem find_tile(const ARGS& a, int block) {
   constexpr int Q = FMOE_MAX_EXPERTS / 64;
   const int lane = threadIdx.x & 63, bm = 1 << a.log2_bm;
@@ -50,11 +52,25 @@ __device__ __forceinline__ QuantItem find_tile(const ARGS& a, int block) {
   const int n = resolve_count(a.n_cap, a.n_dev);
   const int shared_tiles = (n + bm - 1) >> a.log2_bm, per_group = shared_tiles * a.shared_cols;
   const int shared_items = per_group * a.shared_groups;
-  const int items = shared_items + tiles * a.cols, share = (items + 7) >> 3;
   QuantItem it{-1, 0, 0, 0, false};
-  const int place = block >> 3;
-  int g = (block & 7) * share + place;
-  if (place >= share || g >= items) return it;
+  int g;
+  if constexpr (EVEN) {
+    const int s_share = (shared_items + 7) >> 3, r_items = tiles * a.cols, r_share = (r_items + 7) >> 3, xcd = block & 7;
+    int place = block >> 3;
+    if (place < s_share) {
+      g = xcd * s_share + place;
+      if (g >= shared_items) return it;
+    } else {
+      place -= s_share;
+      g = xcd * r_share + place;
+      if (place >= r_share || g >= r_items) return it;
+      g += shared_items;
+    }
+  } else {
+    const int items = shared_items + tiles * a.cols, share = (items + 7) >> 3, place = block >> 3;
+    g = (block & 7) * share + place;
+    if (place >= share || g >= items) return it;
+  }
   if (g < shared_items) {
     it.shared = true;
     it.group = g / per_group;
