@@ -200,8 +200,10 @@ def _expect(t, what, dtype, shape, device):
 
 def _call(device, entry, *args):
     """A call without a context, on the device of its tensors, which mostly is the current one."""
-    if device.type == "cuda" and device.index == torch.cuda.current_device():
-        _check(entry(*args, torch._C._cuda_getCurrentRawStream(device.index)))
+    if device.type == "cuda" and device.index == torch._C._cuda_getDevice():
+        rc = entry(*args, torch._C._cuda_getCurrentRawStream(device.index))
+        if rc:
+            _check(rc)
     else:
         with torch.cuda.device(device):
             _check(entry(*args, _stream()))
@@ -381,8 +383,11 @@ class FMoE:
     def set_weights_quant_rows(self, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None):
         """fmoe_set_weights_quant_rows: the matrices as in set_weights_quant, for expert_ffn_quant_rows; weights registered otherwise
         stay in force for the other calls.  The context makes copies on the current stream, nothing is held on to."""
-        tensors = self._quant_tensors((w_gate, w_up, w_down, ws_gate, ws_up, ws_down))
-        _check(self.lib.fmoe_set_weights_quant_rows(self._ctx, *tensors, _stream()))
+        pairs = (w_gate, w_up, w_down, ws_gate, ws_up, ws_down)
+        _check(self.lib.fmoe_set_weights_quant_rows(self._ctx, *self._quant_tensors(pairs), _stream()))
+        for pair in pairs:
+            for t in pair or ():
+                t.record_stream(torch.cuda.current_stream())   # read until the copies are made
 
     def _quant_tensors(self, pairs):
         c = self.cfg

@@ -28,6 +28,7 @@ struct LogitArgs {
   const void* w;            // norm weight or null
   int w_bf16;
   float eps;
+  double inv_d;
   int T, d, E, groups;      // groups of 16 k in the packed router
   const float *wp, *bias;
   bf16_t *h, *n;            // [T, d] or null
@@ -49,43 +50,53 @@ __global__ __launch_bounds__(64 * LOGIT_WAVES) void decode_logits_kernel(LogitAr
   const int t0 = (int)blockIdx.y * TB, e0 = (int)blockIdx.x * LOGIT_EXPERTS, padded = a.groups * 16;
   const int quarter = (lane >> 2) & 3, g_first = wave * 4 + (lane >> 4);
   const f32x4_t* const wp = reinterpret_cast<const f32x4_t*>(a.wp) + (size_t)(e0 >> 4) * a.groups * 64 + quarter * 16 + (e0 & 15) + (lane & 3);
-  f32x4_t w[AHEAD];
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i) {                             // on their way behind the norm; past the end the last group
-    const int g = g_first + STEP * i;
-    w[i] = wp[(size_t)(g < a.groups ? g : a.groups - 1) * 64];
-  }
   // a token's row: its WPT wavefronts, units of eight
   const int tb = wave / WPT, first = (wave % WPT) * 64 + lane, t = t0 + tb < a.T ? t0 + tb : a.T - 1;
   const size_t base = (size_t)t * a.d;
   const int units = a.d >> 3;
   bf16_t* const row = rows + (size_t)tb * padded;
   constexpr int HELD = 2;                                       // units a lane holds; longer rows are read again
-  auto sum_of = [&](int u, rms::Unit<bf16_t>& h) {
+  auto load_row = [&](int u, rms::Unit<bf16_t>& h, rms::Unit<bf16_t>& dl) {
     h.load(a.x + base + u * 8);
-    if (a.delta != nullptr) {
-      rms::Unit<bf16_t> dl;
-      dl.load(a.delta + base + u * 8);
-#pragma unroll
-      for (int e = 0; e < 8; e += 2)
-        h.set2(e, rms::add_rounded<bf16_t>(h.get(e), dl.get(e)), rms::add_rounded<bf16_t>(h.get(e + 1), dl.get(e + 1)));
-    }
+    if (a.delta != nullptr) dl.load(a.delta + base + u * 8);
   };
-  rms::Unit<bf16_t> held[HELD];
-  float weight[HELD][8];                                        // of the norm, on their way behind the sum
-  double sum = 0.0;
+  auto add_delta = [&](rms::Unit<bf16_t>& h, const rms::Unit<bf16_t>& dl) {
+    if (a.delta == nullptr) return;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2)
+      h.set2(e, rms::add_rounded<bf16_t>(h.get(e), dl.get(e)), rms::add_rounded<bf16_t>(h.get(e + 1), dl.get(e + 1)));
+  };
+  auto sum_of = [&](int u, rms::Unit<bf16_t>& h) {
+    rms::Unit<bf16_t> dl;
+    load_row(u, h, dl);
+    add_delta(h, dl);
+  };
   auto load_weight = [&](int u, float (&f)[8]) {
     if (a.w_bf16) rms::load_weights<bf16_t>(a.w, u * 8, f);     // uniform
     else rms::load_weights<float>(a.w, u * 8, f);
   };
+  rms::Unit<bf16_t> held[HELD], held_delta[HELD];
+  float weight[HELD][8];                                        // of the norm
+  double sum = 0.0;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     held[i].zero();
+    held_delta[i].zero();
     if (first + 64 * WPT * i < units) {
-      sum_of(first + 64 * WPT * i, held[i]);
+      load_row(first + 64 * WPT * i, held[i], held_delta[i]);
       if (a.w != nullptr) load_weight(first + 64 * WPT * i, weight[i]);
     }
   }
+  __builtin_amdgcn_sched_barrier(0);
+  f32x4_t w[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {                             // on their way behind the norm (its rows were asked for first); past the end the last group
+    const int g = g_first + STEP * i;
+    w[i] = wp[(size_t)(g < a.groups ? g : a.groups - 1) * 64];
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) add_delta(held[i], held_delta[i]);
   rms::Scale r{1.0f, 0.0f, 0};
   if (a.w != nullptr) {
     auto add = [&](const rms::Unit<bf16_t>& h) {
@@ -108,7 +119,7 @@ __global__ __launch_bounds__(64 * LOGIT_WAVES) void decode_logits_kernel(LogitAr
     sum = 0.0;
 #pragma unroll
     for (int i = 0; i < WPT; ++i) sum += s_sum[tb * WPT + i];
-    r = rms::row_scale(sum, a.d, a.eps);
+    r = rms::row_scale(sum, a.inv_d, a.eps);
   }
   const bool mine = e0 == 0 && t0 + tb < a.T;                   // the first workgroups write the rows
   // element e of unit u: group u / 2, k = 8 (u % 2) + e of it, which lane group e % 4 wants as its number 2 (u % 2) + e / 4
@@ -489,7 +500,7 @@ int launch_layer_decode(const fmoe_ctx* ctx, const fmoe_select_params* params, c
   const bf16_t* const n = normed ? n_ws : h;
   {
     LogitArgs a{xb, static_cast<const bf16_t*>(delta), normed ? norm->weight : nullptr, normed && norm->weight_dtype == FMOE_BF16,
-                normed ? norm->eps : 0.0f, T, d, E, (d + 127) / 128 * 8, ctx->router_wp, ctx->router_bias, sum ? h_ws : nullptr,
+                normed ? norm->eps : 0.0f, 1.0 / (double)d, T, d, E, (d + 127) / 128 * 8, ctx->router_wp, ctx->router_bias, sum ? h_ws : nullptr,
                 normed ? n_ws : nullptr, logits};
     const size_t row = (size_t)a.groups * 32, room = 48 << 10;   // bytes of a token's row in LDS
     const int ebs = (E + LOGIT_EXPERTS - 1) / LOGIT_EXPERTS;

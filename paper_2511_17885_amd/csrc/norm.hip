@@ -19,6 +19,7 @@ struct NormArgs {
   const void *x, *delta, *w;
   int T, d;
   float eps;
+  double inv_d;
   void *h, *n;          // h may be null (nobody wants the sum), n with rows in 8 bits
   uint32_t* codes;      // [T, d] bytes
   uint8_t* scales;      // [T, scale_stride]
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
       const double v = (double)h[i].get(e);
       sum = fma(v, v, sum);
     }
-  const Scale r = row_scale(row_total<WPR>(sum, s_part), a.d, a.eps);
+  const Scale r = row_scale(row_total<WPR>(sum, s_part), a.inv_d, a.eps);
 #pragma unroll
   for (int i = 0; i < NU; ++i) {
     const int u = first + STEP * i;
@@ -115,6 +116,7 @@ struct NormBackwardArgs {
   const void *h, *w, *dn, *dh;
   int T, d;
   float eps;
+  double inv_d;
   void* dx;
   float* part;          // [blocks, d] or null: no gradient of the weight
 };
@@ -163,7 +165,7 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(NormBackwardArgs
         const double v = (double)h[i].get(e);
         sum = fma(v, v, sum);
       }
-    const Scale r = row_scale(row_total<WPR>(sum, s_part), a.d, a.eps);
+    const Scale r = row_scale(row_total<WPR>(sum, s_part), a.inv_d, a.eps);
     float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < NU; ++i)
@@ -174,7 +176,7 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(NormBackwardArgs
         dot = fmaf(dn * w[i].get(e), c, dot);
         dw[i][e] = fmaf(dn, c, dw[i][e]);
       }
-    const float m = (float)(row_total<WPR>((double)dot, s_part) / (double)a.d);
+    const float m = (float)(row_total<WPR>((double)dot, s_part) * a.inv_d);
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
       const int u = first + STEP * i;
@@ -309,7 +311,7 @@ int norm_backward_blocks(int T, int d) {
 int launch_rms_norm(const void* x, const void* delta, const void* weight, int dtype, int weight_dtype, int T, int d, float eps,
                     void* h, void* n, void* codes, uint8_t* scales, hipStream_t stream) {
   static_assert(MAX_D == 256 * 8 * 8, "a workgroup holds a row");
-  const NormArgs a{x, delta, weight, T, d, eps, h, n, static_cast<uint32_t*>(codes), scales, (d + 127) / 128 * 4};
+  const NormArgs a{x, delta, weight, T, d, eps, 1.0 / (double)d, h, n, static_cast<uint32_t*>(codes), scales, (d + 127) / 128 * 4};
   const bool b = dtype == FMOE_BF16, wb = weight_dtype == FMOE_BF16;
   if (codes != nullptr) {
     if (b && wb) run_norm<bf16_t, bf16_t, true>(a, stream);
@@ -329,7 +331,7 @@ int launch_rms_norm(const void* x, const void* delta, const void* weight, int dt
 int launch_rms_norm_backward(const void* h, const void* weight, const void* d_n, const void* d_h, int dtype, int weight_dtype,
                              int T, int d, float eps, void* d_x, float* d_weight, float* part, hipStream_t stream) {
   const int blocks = norm_backward_blocks(T, d);
-  const NormBackwardArgs a{h, weight, d_n, d_h, T, d, eps, d_x, d_weight != nullptr ? part : nullptr};
+  const NormBackwardArgs a{h, weight, d_n, d_h, T, d, eps, 1.0 / (double)d, d_x, d_weight != nullptr ? part : nullptr};
   if (T > 0) {
     const bool b = dtype == FMOE_BF16, wb = weight_dtype == FMOE_BF16;
     if (b && wb) run_backward<bf16_t, bf16_t>(a, blocks, stream);

@@ -23,8 +23,8 @@ struct Scale {        // r = 2^q * (hi + lo)
 };
 // The root from the hardware's estimate (some 24 bits) by one step of third order: with e = 1 - m y^2 the error of
 // y (1 + e/2 + 3 e^2/8) is of the order of e^3, far below the last bit of 64.
-__device__ __forceinline__ Scale row_scale(double sum, int d, float eps) {
-  const double m = sum / (double)d + (double)eps;
+__device__ __forceinline__ Scale row_scale(double sum, double inv_d, float eps) {
+  const double m = fma(sum, inv_d, (double)eps);
   double r = __builtin_amdgcn_rsq(m);
   Scale s{(float)r, 0.0f, 0};
   if (r > 0.0 && r < 1e300) {   // else 0 (a row with infinities), infinite (zeros without eps) or NaN as it is
