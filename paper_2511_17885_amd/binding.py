@@ -272,7 +272,7 @@ def rms_norm_quant(x, weight, eps=1e-6, delta=None):
     uint8): value k of a row is codes[k] * 2^(scales[k / 32] - 127)."""
     dtype, weight_dtype, T, d = _norm_args(x, weight, delta)
     h = None if delta is None else torch.empty_like(x)
-    codes = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    codes = torch.empty_like(x, dtype=torch.float8_e4m3fn)
     scales = torch.empty(*x.shape[:-1], row_scales(d), dtype=torch.uint8, device=x.device)
     _call(x.device, load().fmoe_rms_norm_quant, x.data_ptr(), None if h is None else delta.data_ptr(), weight.data_ptr(), dtype,
           weight_dtype, T, d, eps, None if h is None else h.data_ptr(), codes.data_ptr(), scales.data_ptr())
@@ -288,16 +288,19 @@ def rms_norm_backward(h, weight, eps, d_n, d_h=None, want_weight=True):
     """fmoe_rms_norm_backward: (gradient of x, which is delta's too; gradient of the weight [d] float32 or None) from those of n and,
     if given, of h."""
     dtype, weight_dtype, T, d = _norm_args(h, weight, None)
-    for t, what in ((d_n, "d_n"), (d_h, "d_h")):
-        if t is not None and _differs(t, h.dtype, h.shape, h.get_device()):
-            _expect(t, what, h.dtype, h.shape, h.device)
+    kind, shape, index, lib = h.dtype, h.shape, h.get_device(), load()
+    if _differs(d_n, kind, shape, index):
+        _expect(d_n, "d_n", kind, shape, h.device)
+    if d_h is not None and _differs(d_h, kind, shape, index):
+        _expect(d_h, "d_h", kind, shape, h.device)
     d_x, d_weight, ws, need = torch.empty_like(h), None, None, 0
     if want_weight:
-        d_weight = torch.empty(d, dtype=torch.float32, device=h.device)
-        need = load().fmoe_rms_norm_workspace_bytes(T, d)
+        d_weight = torch.empty_like(weight, dtype=torch.float32)
+        need = lib.fmoe_rms_norm_workspace_bytes(T, d)
         ws = torch.empty(need, dtype=torch.uint8, device=h.device)
-    _call(h.device, load().fmoe_rms_norm_backward, _ptr(h), _ptr(weight), _ptr(d_n), _ptr(d_h), dtype, weight_dtype, T, d, eps,
-          _ptr(d_x), _ptr(d_weight), _ptr(ws), need)
+    _call(h.device, lib.fmoe_rms_norm_backward, h.data_ptr(), weight.data_ptr(), d_n.data_ptr(), None if d_h is None else d_h.data_ptr(),
+          dtype, weight_dtype, T, d, eps, d_x.data_ptr(), None if ws is None else d_weight.data_ptr(), None if ws is None else ws.data_ptr(),
+          need)
     return d_x, d_weight
 
 

@@ -223,15 +223,15 @@ __global__ __launch_bounds__(256) void rms_norm_backward_kernel(NormBackwardArgs
   }
 }
 
-// The partial sums of every column, in a fixed order: a workgroup has 32 columns, four a lane, and takes 32 partial sums at a time.
+// The partial sums of every column, in a fixed order: a workgroup has 16 columns, four a lane, and takes 64 partial sums at a time.
 __global__ __launch_bounds__(256) void rms_norm_weight_kernel(const float* __restrict__ part, int parts, int d,
                                                               float* __restrict__ dw) {
-  __shared__ double s[32][33];
-  const int c = (threadIdx.x & 7) * 4, first = threadIdx.x >> 3, k = (int)blockIdx.x * 32 + c;   // (d is a multiple of eight)
+  __shared__ double s[64][17];
+  const int c = (threadIdx.x & 3) * 4, first = threadIdx.x >> 2, k = (int)blockIdx.x * 16 + c;   // (d is a multiple of eight)
   double sum[4] = {0.0, 0.0, 0.0, 0.0};
   if (k < d) {
 #pragma unroll 8
-    for (int p = first; p < parts; p += 32) {
+    for (int p = first; p < parts; p += 64) {
       const f32x4_t v = *reinterpret_cast<const f32x4_t*>(part + (size_t)p * d + k);
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] += (double)v[e];
@@ -240,11 +240,11 @@ __global__ __launch_bounds__(256) void rms_norm_weight_kernel(const float* __res
 #pragma unroll
   for (int e = 0; e < 4; ++e) s[first][c + e] = sum[e];
   __syncthreads();
-  const int col = (int)blockIdx.x * 32 + (int)threadIdx.x;
-  if (threadIdx.x >= 32 || col >= d) return;
+  const int col = (int)blockIdx.x * 16 + (int)threadIdx.x;
+  if (threadIdx.x >= 16 || col >= d) return;
   double total = 0.0;
 #pragma unroll
-  for (int p = 0; p < 32; ++p) total += s[p][threadIdx.x];
+  for (int p = 0; p < 64; ++p) total += s[p][threadIdx.x];
   dw[col] = (float)total;
 }
 
@@ -340,7 +340,7 @@ int launch_rms_norm_backward(const void* h, const void* weight, const void* d_n,
     else run_backward<float, float>(a, blocks, stream);
   }
   if (d_weight != nullptr)
-    hipLaunchKernelGGL(rms_norm_weight_kernel, dim3((d + 31) / 32), dim3(256), 0, stream, part, blocks, d, d_weight);
+    hipLaunchKernelGGL(rms_norm_weight_kernel, dim3((d + 15) / 16), dim3(256), 0, stream, part, blocks, d, d_weight);
   FMOE_HIP_CHECK(hipGetLastError());
   return FMOE_OK;
 }
