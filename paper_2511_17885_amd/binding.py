@@ -387,10 +387,10 @@ class FMoE:
         """fmoe_set_weights_quant_rows: the matrices as in set_weights_quant, for expert_ffn_quant_rows; weights registered otherwise
         stay in force for the other calls.  The context makes copies on the current stream, nothing is held on to."""
         pairs = (w_gate, w_up, w_down, ws_gate, ws_up, ws_down)
-        _check(self.lib.fmoe_set_weights_quant_rows(self._ctx, *self._quant_tensors(pairs), _stream()))
+        _call(self.device, self.lib.fmoe_set_weights_quant_rows, self._ctx, *self._quant_tensors(pairs))
         for pair in pairs:
             for t in pair or ():
-                t.record_stream(torch.cuda.current_stream())   # read until the copies are made
+                t.record_stream(torch.cuda.current_stream(self.device))   # read until the copies are made
 
     def _quant_tensors(self, pairs):
         c = self.cfg
@@ -531,6 +531,8 @@ class FMoE:
             raise TypeError(f"codes must be float8_e4m3fn or uint8, not {codes.dtype}")
         if kept_idx is None and n_kept > T:
             raise ValueError(f"{n_kept} rows of {T}")
+        if T * self.d >= 1 << 32:
+            raise ValueError(f"{T} rows of {self.d} bytes: rows are found by 32-bit offsets")
         _expect(codes, "codes", codes.dtype, (T, self.d), self.device)
         _expect(scales, "scales", torch.uint8, (T, row_scales(self.d)), self.device)
         K = max(self.kmax, 1)
@@ -539,9 +541,8 @@ class FMoE:
         if self.cfg.n_shared > 0:
             ysh = torch.empty((self.cfg.n_shared, max(n_kept, 1), self.d), dtype=torch.bfloat16, device=self.device)
         ws = self.workspace(n_kept, 1)
-        _check(self.lib.fmoe_expert_ffn_quant_rows(self._ctx, _ptr(codes), _ptr(scales), _ptr(kept_idx), n_kept, _ptr(n_kept_dev),
-                                                   _ptr(expert_offsets), _ptr(perm_src), _ptr(y), _ptr(ysh), _ptr(ws), ws.numel(),
-                                                   _stream()))
+        _call(self.device, self.lib.fmoe_expert_ffn_quant_rows, self._ctx, _ptr(codes), _ptr(scales), _ptr(kept_idx), n_kept,
+              _ptr(n_kept_dev), _ptr(expert_offsets), _ptr(perm_src), _ptr(y), _ptr(ysh), _ptr(ws), ws.numel())
         return y, ysh
 
     def combine(self, y, y_shared, inv_perm, topk_gate, kept_idx, n_kept, residual=None,
@@ -599,9 +600,9 @@ class FMoE:
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        _check(self.lib.fmoe_layer_decode(self._ctx, C.byref(params) if params is not None else None, normed, x.data_ptr(), at(delta),
-                                          at(is_visual), at(select_bias), T, int(bool(add_residual)), out.data_ptr(), idx.data_ptr(),
-                                          gate.data_ptr(), self._ws.data_ptr(), self._ws.numel(), _stream()))
+        _call(self.device, self.lib.fmoe_layer_decode, self._ctx, C.byref(params) if params is not None else None, normed, x.data_ptr(),
+              at(delta), at(is_visual), at(select_bias), T, int(bool(add_residual)), out.data_ptr(), idx.data_ptr(), gate.data_ptr(),
+              self._ws.data_ptr(), self._ws.numel())
         if self.kmax == 0:
             idx, gate = idx[:, :0], gate[:, :0]
         return out, idx, gate

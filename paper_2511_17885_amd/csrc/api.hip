@@ -879,8 +879,9 @@ int fmoe_profile_slots(void) { return SLOT_COUNT; }
 
 const char* fmoe_profile_name(int slot) {
   // kernel symbols (the two expert GEMMs: bf16 symbol; fp32 contexts run grouped_gemm_kernel, calls of at most 16
-  // tokens ffn_thin_kernel, contexts with 4-bit weights the ffn_quant kernels, the dense one in the dense slots; scan and
-  // scatter in one launch are timed as the scatter)
+  // tokens ffn_thin_kernel, contexts with 4-bit weights the ffn_quant kernels, the dense one in the dense slots, and rows in
+  // 8 bits the ffn_rows8 ones, that for many rows in the dense slots; scan and scatter in one launch are timed as the
+  // scatter; of a layer for a decoding step logits, products and join have the slots of route, the two GEMMs and combine)
   static const char* names[SLOT_COUNT] = {
       "route_kernel", "seq_ordinals_kernel", "window_score_kernel", "compact_kernel",
       "prune_dispatch_small_kernel", "permute_count_kernel", "permute_scan_kernel",

@@ -449,6 +449,13 @@ def test_set_weights_quant_rows_refuses_bad_arguments():
     assert run() == -1 and b"fmoe_set_weights_quant_rows" in lib.fmoe_last_error()   # nothing registered
 
 
+def test_rows_past_32_bit_offsets_are_refused():
+    m = binding.FMoE(d_model=64, n_experts=2, d_ffn=64, k_text=1, k_visual=1, dtype="bf16")
+    codes = torch.empty((1 << 26, 64), dtype=torch.uint8, device="meta")
+    with pytest.raises(ValueError, match="32-bit"):
+        m.expert_ffn_quant_rows(codes, codes, codes, 1, codes, codes)
+
+
 @pytest.mark.gpu
 def test_expert_ffn_quant_rows_refuses_bad_arguments():
     rng = np.random.default_rng(1)
