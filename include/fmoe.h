@@ -225,9 +225,9 @@ int fmoe_dequantize_weights(const void* codes, const uint8_t* scales, int64_t ro
 /* Root-mean-square norm of rows with the addition in front of it (no context: the current device):
  *   h = x + delta, rounded to the type;   n = h * weight / sqrt(mean over the row of h^2 + eps).
  * x, delta, h, n [T, d] of `dtype`; weight [d] of `weight_dtype` (fmoe_dtype); delta NULL: h = x; h NULL: not written.
- * n is rounded once from its exact value (the sum of squares and the root are taken in 64 bits).  A row with an infinity or
- * NaN, or of zeros with eps 0, gives what IEEE arithmetic makes of the formula.  h and n may each be x or delta, not the same
- * tensor.  d % 8 == 0, d <= 16384; eps >= 0; all pointers 16-byte aligned. */
+ * n is the fp32 number nearest to its exact value (the sum of squares and the root are taken in 64 bits), in bf16 rounded from that.
+ * A row with an infinity or NaN, or of zeros with eps 0, gives what IEEE arithmetic makes of the formula.  h and n may each be
+ * x or delta, not the same tensor.  d % 8 == 0, d <= 16384; eps >= 0; all pointers 16-byte aligned. */
 int fmoe_rms_norm(const void* x, const void* delta, const void* weight, int32_t dtype, int32_t weight_dtype, int32_t T,
                   int32_t d, float eps, void* h, void* n, void* stream);
 
@@ -236,7 +236,7 @@ int fmoe_rms_norm(const void* x, const void* delta, const void* weight, int32_t 
  * belongs to the codes 32g .. 32g+31 of it (the last group may be shorter), the bytes behind the groups are 127.
  * A group's scale is the least power of two with which its largest magnitude is at most 448 scales, at least 2^-126, and 1
  * for zeros; a code is the nearest, ties to the even one.  A group that holds an infinity or NaN gets codes 0 and scale byte 255.
- * The rounding is the only one from the exact value.  codes and scales share no memory with the inputs. */
+ * The rounding to codes is the only one from the exact value.  codes and scales share no memory with the inputs. */
 int fmoe_rms_norm_quant(const void* x, const void* delta, const void* weight, int32_t dtype, int32_t weight_dtype, int32_t T,
                         int32_t d, float eps, void* h, uint8_t* codes, uint8_t* scales, void* stream);
 

@@ -2,7 +2,7 @@
 // Compiled with floating-point contraction off: the roundings that norm_dev.h relies on are written out.
 //
 // Bound: memory.  A wavefront has a row in registers (up to 4096 elements; a workgroup of four wavefronts has one of up to 16384,
-// or where there are few rows), reads it once and writes its outputs once.  22016 rows of 2048 in bf16: 62 us, 5.8 TB/s (a copy of
+// or where there are few rows), reads it once and writes its outputs once.  22016 rows of 2048 in bf16: 58 us, 6.2 TB/s (a copy of
 // 1 GiB 5.2); gradient 68 us with the sums of the weight's; 8192 rows to 8 bits 26.8 us, 4.4 TB/s: some 25 vector instructions an
 // element for the exact rounding beside the loads.
 

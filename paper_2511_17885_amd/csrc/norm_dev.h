@@ -1,10 +1,12 @@
 // Root-mean-square norm of a row that a wavefront, or four, hold in registers: shared by norm.hip and decode.hip.
 //
-// n = h * w * r, r = 1 / sqrt(mean h^2 + eps), is rounded once from (all but) its exact value, so that it does not depend on who
-// computes it: what decides experts or falls next to a border of two codes is the same everywhere.  The sum of squares and r are
-// taken in 64 bits, once a row.  An element needs no 64-bit instruction: r = 2^q (r_hi + r_lo) with r_hi in [1, 2), the
-// products' errors come from fused multiply-adds (h is scaled by 2^q first, so that nothing overflows on the way), and the
-// sum of what they leave decides the last rounding.  (From 2^-100 down the errors underflow: nearest but for that.)
+// n = h * w * r, r = 1 / sqrt(mean h^2 + eps), is the fp32 number nearest to (all but) its exact value, or in 8 bits the code nearest to
+// that value, so that it does not depend on who computes it: what decides experts or falls next to a border of two codes is the same
+// everywhere.  bf16 is rounded from the fp32 number, as conversions from 64 bits do that go by way of it (the two roundings together
+// are off by at most half a step and 2^-17 of one).  The sum of squares and r are taken in 64 bits, once a row.  An element needs no
+// 64-bit instruction: r = 2^q (r_hi + r_lo) with r_hi in [1, 2), the products' errors come from fused multiply-adds (h is
+// scaled by 2^q first, so that nothing overflows on the way), and the sum of what they leave decides the last rounding.  (From
+// 2^-100 down the errors underflow: nearest but for that.)
 #pragma once
 
 #include "common.h"
@@ -81,9 +83,7 @@ template <> __device__ __forceinline__ float value_rounded<float>(float h, float
   return hi;
 }
 template <> __device__ __forceinline__ bf16_t value_rounded<bf16_t>(float h, float w, const Scale& r) {
-  float hi, lo;
-  value(h, w, r, hi, lo);
-  return nearest_bf16(odd(hi, lo));
+  return nearest_bf16(value_rounded<float>(h, w, r));
 }
 
 // Eight neighbouring elements
