@@ -248,17 +248,17 @@ __global__ __launch_bounds__(256) void rms_norm_weight_kernel(const float* __res
   dw[col] = (float)total;
 }
 
-// Do the inputs and h, which nobody asks for again soon, pass the caches by?  (n is read by the next launch and stays.)  us with / without:
-// bf16, d 2048, 22016 rows 73 / 78, 8192 rows 31.7 / 31.8, in 8 bits 28.8 / 33.3; gradient 22016 rows 71.6 / 78.7, 8192 rows 34.0 / 36.8,
-// 4096 rows (67 MB) 24.0 / 22.9.
+// Do the inputs and h, which nobody asks for again soon, pass the caches by?  (n is read by the next launch and stays.)  us with / without
+// (in a graph, four sets of tensors in turn): bf16, d 2048, 22016 rows 68.4 / 71.9, 8192 rows 29.0 / 30.8, in 8 bits 30.0 / 34.1; gradient
+// 22016 rows 69.8 / 76.6, 8192 rows 32.8 / 34.9, 4096 rows (67 MB) 22.8 / 20.5.
 bool passes(size_t bytes) { return bytes >= ((size_t)100 << 20); }
 
-// Wavefronts a row: all four of a workgroup for rows that one cannot hold, and where rows of more than 64 units are few.  us with one / four:
-// bf16, d 2048, 4096 rows 18.4 / 16.4, 2048 rows 13.0 / 11.1, 600 rows 8.1 / 5.6; d 1280 100 rows 6.4 / 4.5; d 1288 in fp32 1601 rows 6.8 / 6.4;
-// d 1024 in 8 bits 4096 rows 11.7 / 12.7, d 512 3000 rows 6.1 / 9.9.
+// Wavefronts a row: all four of a workgroup for rows that one cannot hold, and where rows of more than 128 units are few.  us with one / four:
+// bf16, d 2048, 4096 rows 15.5 / 14.2, in 8 bits 18.9 / 15.9, 2048 rows 11.5 / 10.2, 600 rows 6.9 / 5.4; d 1280 100 rows 5.5 / 4.4; d 1288 in
+// fp32 1601 rows 9.7 / 9.6; d 1024 4096 rows 10.3 / 11.0, in 8 bits 11.7 / 13.1; d 512 3000 rows 5.6 / 7.7.
 int waves_per_row(int T, int d) { return d > 4096 || (d > 1024 && T <= 4096) ? 4 : 1; }
-// The gradient, with two sums a row between which four wavefronts would wait for each other: d 2048 bf16 22016 rows 72 / 88, 4096 rows
-// 22.6 / 24.9, 200 rows 8.4 / 8.8; d 1280 in fp32 600 rows 10.6 / 13.6.
+// The gradient, with two sums a row between which four wavefronts would wait for each other: d 2048 bf16 22016 rows 69.8 / 86.7, 4096 rows
+// 20.5 / 21.9, 200 rows 8.3 / 8.2; d 1280 in fp32 600 rows 10.2 / 11.5.
 int waves_per_gradient(int d) { return d > 4096 ? 4 : 1; }
 
 template <typename XT, typename WT, bool ROWS8>
