@@ -106,6 +106,39 @@ def check_pending_reads(asm_path):
     return reads
 
 
+def check_matrix_operands(asm_path):
+    """A matrix instruction may read a register that a vector instruction has written only two waits later.  The compiler keeps to that with its
+    own instructions, not with those in inline assembly.  This reads the device assembly and fails where such a write is nearer."""
+    import re
+
+    def registers(text):
+        found = set()
+        for m in re.finditer(r"\bv(?:\[(\d+):(\d+)\]|(\d+)\b)", text):
+            lo = int(m.group(1) or m.group(3))
+            found.update(range(lo, int(m.group(2) or lo) + 1))
+        return found
+
+    in_asm, recent, seen = False, [], 0   # recent: registers that the last two instructions wrote
+    for n, line in enumerate(open(asm_path), 1):
+        code = line.split(";")[0].strip()
+        if "ASMSTART" in line or "ASMEND" in line:
+            in_asm = "ASMSTART" in line
+        elif not code or code.startswith((".", "#")) or code.endswith(":"):
+            continue
+        elif code.startswith("s_nop"):
+            recent = ([set()] * (int(code.split()[1]) + 1) + recent)[:2]
+        elif code.startswith("v_mfma"):
+            if in_asm:
+                seen += 1
+                if any(registers(code.split(",", 1)[1]) & r for r in recent):
+                    raise RuntimeError(f"{asm_path}:{n}: a matrix instruction reads a register that was written just before it: {code}")
+            recent = [set()] + recent[:1]
+        else:
+            vector = code.startswith("v_") and not code.startswith("v_cmp")
+            recent = [registers(code.split(",")[0]) if vector else set()] + recent[:1]
+    return seen
+
+
 def _compile(name, extra, verbose):
     src = os.path.join(CSRC, name)
     obj = os.path.join(OBJ, name.replace(".hip", ".o"))
@@ -125,6 +158,7 @@ def _compile(name, extra, verbose):
         asm = os.path.join(OBJ, name.replace(".hip", "-hip-amdgcn-amd-amdhsa-gfx950.s"))
         check_accumulation_registers(asm)
         check_pending_reads(asm)
+        check_matrix_operands(asm)
     return obj
 
 

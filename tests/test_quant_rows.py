@@ -449,6 +449,22 @@ def test_set_weights_quant_rows_refuses_bad_arguments():
     assert run() == -1 and b"fmoe_set_weights_quant_rows" in lib.fmoe_last_error()   # nothing registered
 
 
+def test_build_check_catches_operands_written_just_before(tmp_path):
+    from paper_2511_17885_amd import build
+    mfma = "\t;;#ASMSTART\n\tv_mfma_f32_16x16x32_bf16 a[0:3], v[8:11], v[4:7], a[0:3]\n\t;;#ASMEND\n"
+    good = ["\tv_mov_b32_e32 v12, v1\n", "\tv_add_u32_e32 v5, v1, v2\n\ts_nop 1\n", "\tds_read_b128 v[4:7], v1\n",
+            "\tv_mov_b32_e32 v9, v1\n\ts_nop 0\n\ts_add_i32 s1, s1, s2\n"]
+    bad = ["\tv_mov_b32_e32 v9, v1\n", "\tv_add_u32_e32 v5, v1, v2\n\ts_nop 0\n", "\tv_mov_b32_e32 v4, v1\n.LBB0_1:\n\ts_add_i32 s1, s1, s2\n"]
+    p = tmp_path / "a.s"
+    for before in good:
+        p.write_text(before + mfma)
+        assert build.check_matrix_operands(str(p)) == 1
+    for before in bad:
+        p.write_text(before + mfma)
+        with pytest.raises(RuntimeError, match="written just before"):
+            build.check_matrix_operands(str(p))
+
+
 def test_rows_past_32_bit_offsets_are_refused():
     m = binding.FMoE(d_model=64, n_experts=2, d_ffn=64, k_text=1, k_visual=1, dtype="bf16")
     codes = torch.empty((1 << 26, 64), dtype=torch.uint8, device="meta")
