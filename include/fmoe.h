@@ -410,8 +410,8 @@ int fmoe_layer_forward(fmoe_ctx* ctx, const fmoe_prune_params* params, const voi
  * x, delta, out [T, d_model] bf16; delta NULL: h = x; norm NULL: n = h.  h and n are those of fmoe_rms_norm, n rounded to bf16.
  * Logits: router_w n + router_bias, added up in 64 bits, rounded to fp32 once (so they may differ from fmoe_route's in the last
  * bits); experts and gates from them as in fmoe_select_experts with params and select_bias, params NULL: softmax over the experts.
- * is_visual [T] or NULL as there.  The activation silu(.)*(.) is rounded to bf16 between the two products; gates, experts,
- * shared experts and residual are added up in fp32 in a fixed order, with one rounding.
+ * is_visual [T] or NULL as there.  The activation silu(.)*(.) keeps 16 bits between the two products (two bf16 numbers, off by
+ * 2^-16 of its value at most); gates, experts, shared experts and residual are added up in fp32 in a fixed order, with one rounding.
  * topk_idx [T,Kmax] and topk_gate [T,Kmax] as fmoe_select_experts writes them, or NULL.  out may be x or delta.
  * ws: fmoe_layer_decode_workspace_bytes(ctx, T) bytes, 256-byte aligned.  fmoe_set_selection and fmoe_set_ffn_shape have no effect here.
  * More than 16 tokens, fp32 contexts and d_model above 16384 are FMOE_ERR_UNSUPPORTED. */

@@ -233,9 +233,10 @@ struct fmoe_unit {
   uint32_t mask;                // tokens that list it
 };
 struct fmoe_unit_list {
-  int32_t n, pad[3];
+  int32_t n, n_full, pad[2];
   float gate[FMOE_MAX_EXPERTS][FMOE_DECODE_TOKENS];   // of the tokens in the mask
   fmoe_unit unit[FMOE_MAX_EXPERTS];
+  int32_t full[FMOE_MAX_EXPERTS];   // units that two tokens eight apart list
 };
 
 // ---- routing from logits (select.hip), weights in 4 bits (quant.hip).  units (nullable): fp32 logits of at most

@@ -7,7 +7,8 @@
 //   decode_gate_up   one to four wavefronts per expert of the list and column block of 16: all tokens are the rows of the matrix
 //                    instruction, whose hidden rows are kept for those that list the expert
 //   decode_down      per 32 output columns four workgroups, whose wavefronts share the experts (and where there are fewer, their
-//                    reductions); the rows stay tokens, so that gate * product is added up in registers, then over the wavefronts
+//                    reductions); the rows stay tokens (of whose hidden rows a second plane has the other 8 bits), so that gate * product
+//                    is added up in registers, then over the wavefronts
 //                    in LDS
 //   decode_join      the four sums and the residual, in a fixed order.  (Left to the last of the four workgroups to arrive, which takes
 //                    fences between L2s that are not coherent with each other: 50 us for the down launch instead of 8.)
@@ -324,12 +325,34 @@ __device__ __forceinline__ fmoe_unit load_unit(const fmoe_unit_list* list, int u
   return r;
 }
 
+// Hidden rows h = silu(gate) * up are kept in two bf16 planes, h rounded to bf16 and what that leaves rounded again: 16 bits, 2^-16 of a
+// value at most lost, far less than the rounding of the output.  (One plane's rounding is as much as the output's; the down launch with
+// one / two, us: one token, d 2048, 64 experts of 1408, two shared, in 4 bits 6.4 / 6.9, 16 tokens 12.6 / 14.8; 8 tokens, 128 of 768 in bf16
+// 20.9 / 21.2.)  What a value too large for bf16 leaves is taken for 0.
+__device__ __forceinline__ void store_hidden(bf16_t* row, int plane, int col, float h) {
+  const bf16_t hi = f32_to_bf16(h);
+  const float top = bf16_to_f32(hi);
+  row[col] = hi;
+  row[plane + col] = rms::finite(top) ? f32_to_bf16(h - top) : 0;
+}
+
+// Entry i of the units that two tokens eight apart list, of the n in the list; how many there are
+__device__ __forceinline__ int full_unit(const fmoe_unit_list* list, int i, int n) {
+  typedef const __attribute__((address_space(4))) int32_t* const_ptr;
+  const int u = ((const_ptr)(uintptr_t)list->full)[i];
+  return u < 0 ? 0 : u < n ? u : n - 1;
+}
+__device__ __forceinline__ int full_length(const fmoe_unit_list* list, int n) {
+  const int full = list->n_full;
+  return full < 0 ? 0 : full < n ? full : n;
+}
+
 struct GateUpArgs {
   DecodeMatrix routed, shared;
   const bf16_t* n;              // [T, K]
   const fmoe_unit_list* list;   // or null: no experts are listed
   ListBounds bounds;
-  bf16_t *h, *h_shared;         // hidden rows [., routed.N] of the pairs by expert and token; [T, shared.N]
+  bf16_t *h, *h_shared;         // hidden rows [., 2, routed.N] of the pairs by expert and token; [T, 2, shared.N]
 };
 
 // NCB column blocks a wavefront: with two the rows, sixteen of them, are read half as often.
@@ -362,20 +385,26 @@ __global__ __launch_bounds__(64) void decode_gate_up_kernel(GateUpArgs a) {
   for (int v = 0; v < 4; ++v) {   // accumulator register v of lane l: row 4*(l/16) + v, column l%16
     const int t = 4 * (lane >> 4) + v;
     if (!((unit.mask >> t) & 1u)) continue;
-    bf16_t* const row = h + (size_t)(unit.row0 + __popc(unit.mask & ((1u << t) - 1u))) * M.N;
+    bf16_t* const row = h + (size_t)(unit.row0 + __popc(unit.mask & ((1u << t) - 1u))) * 2 * M.N;
 #pragma unroll
     for (int j = 0; j < NCB; ++j) {
       const int col = (cb + j) * 16 + (lane & 15);
-      if (col < M.N) row[col] = f32_to_bf16(silu_mul_bf16(acc[j][0][v], acc[j][1][v]));
+      if (col < M.N) store_hidden(row, M.N, col, silu_mul_bf16(acc[j][0][v], acc[j][1][v]));
     }
   }
+}
+
+// v plus that of the lane 32 away
+__device__ __forceinline__ float plus_32_apart(float v) {
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
 struct DownArgs {
   DecodeMatrix routed, shared;   // (a group per shared expert)
   int n_shared;
   const bf16_t *h, *h_shared;
-  int ld_shared;
+  int plane, plane_shared;       // columns of a hidden row
   const fmoe_unit_list* list;    // or null
   ListBounds bounds;
   float* part;                   // [SPLITS, T, d]
@@ -391,13 +420,19 @@ __global__ __launch_bounds__(64 * DOWN_WAVES) void decode_down_kernel(DownArgs a
   __shared__ float s_out[DOWN_WAVES][TOKENS][36];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), T = a.bounds.T;
   const int cb = (int)blockIdx.x, split = (int)blockIdx.y, d = a.routed.N;
-  const int units = (a.list != nullptr ? list_length(a.list, a.bounds) : 0) + a.n_shared, waves = DOWN_WAVES * SPLITS;
+  const int listed = a.list != nullptr ? list_length(a.list, a.bounds) : 0, units = listed + a.n_shared, waves = DOWN_WAVES * SPLITS;
   // parts of a reduction: as many as there are wavefronts for
-  const int parts = units > 0 && units < waves ? waves / units : 1;
+  const int parts = units > 0 && units < waves ? waves / units : 1, items = units * parts;
   f32x4_t total[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
-  for (int item = wave * SPLITS + split; item < units * parts; item += waves) {   // uniform
-    const int u = item / parts, part = item - u * parts;
+  // Rows are tokens, whose other plane is in the row eight away.  Where two tokens eight apart list an expert (all with a shared
+  // one), its tokens from 8 on are an item of their own, behind the others.
+  const int again = T > 8 ? a.n_shared + (listed > 0 ? full_length(a.list, listed) : 0) : 0;
+  for (int item = wave * SPLITS + split; item < items + again * parts; item += waves) {   // uniform
+    const bool second = item >= items;
+    const int place = second ? item - items : item, part = place % parts;
+    int u = place / parts;
     const bool shared = u < a.n_shared;
+    if (second && !shared) u = a.n_shared + full_unit(a.list, u - a.n_shared, listed);
     DecodeMatrix M;
 #define FMOE_SEL(f) M.f = shared ? a.shared.f : a.routed.f
     FMOE_SEL(Bp); FMOE_SEL(Sp); FMOE_SEL(group_stride); FMOE_SEL(scale_stride); FMOE_SEL(nbw); FMOE_SEL(N); FMOE_SEL(K);
@@ -408,18 +443,25 @@ __global__ __launch_bounds__(64 * DOWN_WAVES) void decode_down_kernel(DownArgs a
       unit = load_unit(a.list, u - a.n_shared, a.bounds);
       gate = *reinterpret_cast<const f32x4_t*>(&a.list->gate[u - a.n_shared][4 * (lane >> 4)]);
     }
+    const bool both = (unit.mask & (unit.mask >> 8)) != 0u;
+    const uint32_t mask = both ? unit.mask & (second ? 0xff00u : 0xffu) : unit.mask;
     const int NT = (M.K + SBK - 1) / SBK, per = ((NT + parts - 1) / parts + 3) / 4 * 4;   // whole units of scales
     const int first = part * per, last = first + per < NT ? first + per : NT;
     if (first >= last) continue;
-    // rows are tokens; one that does not list the expert takes the row of the first that does, and leaves its products out
-    const int t = lane & 15;
-    const int row = (unit.mask >> t) & 1u ? __popc(unit.mask & ((1u << t) - 1u)) : 0;
-    const bf16_t* const src = shared ? a.h_shared + (size_t)row * a.ld_shared + (size_t)u * M.K : a.h + (size_t)(unit.row0 + row) * M.K;
+    // a row with neither plane of a token takes the first row of the expert, and leaves its products out
+    const int t = lane & 15, plane = shared ? a.plane_shared : a.plane;
+    const bool own = (mask >> t) & 1u, rest = !own && ((mask >> (t ^ 8)) & 1u);
+    const int row = own || rest ? __popc(unit.mask & ((1u << (rest ? t ^ 8 : t)) - 1u)) : 0;
+    const bf16_t* const h = shared ? a.h_shared + (size_t)row * 2 * plane + (size_t)u * M.K : a.h + (size_t)(unit.row0 + row) * 2 * plane;
     f32x4_t acc[1][2] = {{f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}}};
-    accumulate<QUANT, 1>(M, unit.expert, cb, first, last, src, acc);
+    accumulate<QUANT, 1>(M, unit.expert, cb, first, last, h + (rest ? plane : 0), acc);
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) acc[0][f][v] = plus_32_apart(acc[0][f][v]);   // rows eight apart
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      if (!((unit.mask >> (4 * (lane >> 4) + v)) & 1u)) continue;
+      if (!((mask >> (4 * (lane >> 4) + v)) & 1u)) continue;
       total[0][v] = fmaf(gate[v], acc[0][0][v], total[0][v]);
       total[1][v] = fmaf(gate[v], acc[0][1][v], total[1][v]);
     }
@@ -475,11 +517,24 @@ DecodeMatrix decode_matrix(const fmoe_ctx* ctx, int which) {
   return q;
 }
 
+// Workspace behind the layer's
+struct ExtraLayout {
+  size_t list, part, h, h_shared, total;
+};
+ExtraLayout extra_layout(const fmoe_ctx* ctx, int T) {
+  const fmoe_config& c = ctx->cfg;
+  ExtraLayout L{};
+  auto take = [&](size_t bytes) { const size_t at = L.total; L.total += (bytes + 255) / 256 * 256; return at; };
+  L.list = take(sizeof(fmoe_unit_list));
+  L.part = take((size_t)SPLITS * T * c.d_model * 4);
+  L.h = take((size_t)T * ctx->kmax * c.d_ffn * 4);
+  L.h_shared = take((size_t)T * c.n_shared * c.d_ffn_shared * 4);
+  return L;
+}
+
 }  // namespace
 
-size_t decode_extra_bytes(const fmoe_ctx* ctx, int T) {
-  return (sizeof(fmoe_unit_list) + 255) / 256 * 256 + (size_t)SPLITS * T * ctx->cfg.d_model * 4;
-}
+size_t decode_extra_bytes(const fmoe_ctx* ctx, int T) { return extra_layout(ctx, T).total; }
 
 int launch_layer_decode(const fmoe_ctx* ctx, const fmoe_select_params* params, const fmoe_norm_params* norm, const void* x,
                         const void* delta, const uint8_t* is_visual, const float* select_bias, int T, int add_residual, void* out,
@@ -487,13 +542,15 @@ int launch_layer_decode(const fmoe_ctx* ctx, const fmoe_select_params* params, c
   const fmoe_config& c = ctx->cfg;
   const int d = c.d_model, E = c.n_experts, F = c.d_ffn, Ft = c.n_shared * c.d_ffn_shared;
   char* const base = static_cast<char*>(ws);
+  char* const behind = base + L.total;
+  const ExtraLayout X = extra_layout(ctx, T);
   bf16_t* const n_ws = reinterpret_cast<bf16_t*>(base + L.x_merged);
   bf16_t* const h_ws = reinterpret_cast<bf16_t*>(base + L.y);          // (T rows; y has no other use here)
   float* const logits = reinterpret_cast<float*>(base + L.probs);
   if (topk_idx == nullptr) topk_idx = reinterpret_cast<int32_t*>(base + L.topk_idx);
   if (topk_gate == nullptr) topk_gate = reinterpret_cast<float*>(base + L.topk_gate);
   const ListBounds bounds{E, T, T * ctx->kmax};
-  fmoe_unit_list* const list = reinterpret_cast<fmoe_unit_list*>(base + L.total);
+  fmoe_unit_list* const list = reinterpret_cast<fmoe_unit_list*>(behind + X.list);
   const bf16_t* const xb = static_cast<const bf16_t*>(x);
   const bool sum = delta != nullptr, normed = norm != nullptr;
   const bf16_t* const h = sum ? h_ws : xb;
@@ -521,7 +578,7 @@ int launch_layer_decode(const fmoe_ctx* ctx, const fmoe_select_params* params, c
   GateUpArgs g{};
   g.routed = decode_matrix(ctx, 0); g.shared = decode_matrix(ctx, 2);
   g.n = n; g.list = ctx->kmax > 0 ? list : nullptr; g.bounds = bounds;
-  g.h = reinterpret_cast<bf16_t*>(base + L.h); g.h_shared = reinterpret_cast<bf16_t*>(base + L.h_shared);
+  g.h = reinterpret_cast<bf16_t*>(behind + X.h); g.h_shared = reinterpret_cast<bf16_t*>(behind + X.h_shared);
   const int pairs = T * ctx->kmax, units = pairs < E ? pairs : E;
   {
     // Column blocks a wavefront.  4 bits, where sixteen rows are more to read than the weights beside them; one / two, us a call: d 2048,
@@ -541,10 +598,10 @@ int launch_layer_decode(const fmoe_ctx* ctx, const fmoe_select_params* params, c
   DownArgs a{};
   a.routed = decode_matrix(ctx, 1); a.shared = decode_matrix(ctx, 3);
   a.n_shared = c.n_shared;
-  a.h = g.h; a.h_shared = g.h_shared; a.ld_shared = Ft;
+  a.h = g.h; a.h_shared = g.h_shared; a.plane = F; a.plane_shared = Ft;
   a.list = g.list;
   a.bounds = bounds;
-  a.part = reinterpret_cast<float*>(base + L.total + (sizeof(fmoe_unit_list) + 255) / 256 * 256);
+  a.part = reinterpret_cast<float*>(behind + X.part);
   {
     fmoe_prof_scope prof(ctx, SLOT_GEMM2, stream);
     const dim3 grid(a.routed.nbw, SPLITS), block(64 * DOWN_WAVES);

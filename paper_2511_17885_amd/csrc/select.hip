@@ -626,19 +626,24 @@ __global__ __launch_bounds__(256) void select_units_kernel(SelectArgs a, fmoe_un
   if (threadIdx.x < 64) {
     const int lane = threadIdx.x;
     uint32_t m[4];
-    int rows = 0, some = 0;
+    int rows = 0, some = 0, full = 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       m[q] = s_mask[4 * lane + q];
       rows += __popc(m[q]);
       some += m[q] != 0u;
+      full += (m[q] & (m[q] >> 8)) != 0u;
     }
-    int row = wave_scan(rows) - rows, rank = wave_scan(some) - some;
-    if (lane == 63) list->n = rank + some;
+    int row = wave_scan(rows) - rows, rank = wave_scan(some) - some, at = wave_scan(full) - full;
+    if (lane == 63) {
+      list->n = rank + some;
+      list->n_full = at + full;
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (m[q] == 0u) continue;
       s_rank[4 * lane + q] = rank;
+      if ((m[q] & (m[q] >> 8)) != 0u) list->full[at++] = rank;
       list->unit[rank++] = fmoe_unit{4 * lane + q, row, m[q]};
       row += __popc(m[q]);
     }

@@ -254,6 +254,55 @@ def test_decode_agrees_with_the_layer():
         assert ((whole[:7].float() - out.float()).abs() <= 5 * HALF_BF16 * size + 2 * HALF_BF16 * out.float().abs()).all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("T,F", [(1, 64), (5, 72), (9, 136), (16, 64)])
+def test_activation_is_not_rounded_to_bf16(T, F, quant):
+    """Hidden columns in pairs that differ by a 64th and meet opposite down weights: what a rounding of the activation to bf16 leaves
+    stands out of the small difference.  Gate and up add multiples of 2^-12 below 2^10: exact in fp32."""
+    rng = np.random.default_rng(T + F)
+    d, E = 64, 2
+
+    def matrices(G):
+        gate, up, down = (rng.integers(0, 16, s).astype(np.uint8) for s in ((G, F, d), (G, F, d), (G, d, F)))
+        gate[:, 1::2], up[:, 1::2, :32], down[:, :, 1::2] = gate[:, ::2], up[:, ::2, :32], down[:, :, ::2] ^ 8
+        scale_up = np.full((G, F, 2), 127 - 3, np.uint8)
+        scale_up[:, :, 1] -= 5
+        return [(gate, np.full((G, F, 2), 127 - 3, np.uint8)), (up, scale_up), (down, np.full((G, d, -(-F // 32)), 127 - 3, np.uint8))]
+
+    host = matrices(E) + matrices(1)
+    w = [_values(*h) for h in host]
+    router = torch.from_numpy(rng.standard_normal((E, d)).astype(np.float32)).to(torch.bfloat16).cuda()
+    m = binding.FMoE(d_model=d, n_experts=E, d_ffn=F, n_shared=1, d_ffn_shared=F, k_text=1, k_visual=1, dtype="bf16")
+    if quant:
+        m.set_weights_quant(router, None, *[(torch.from_numpy(_pack(c)).cuda(), torch.from_numpy(s).cuda()) for c, s in host])
+    else:
+        m.set_weights(router, None, *[torch.from_numpy(v).to(torch.bfloat16).cuda() for v in w])
+    x = rng.integers(-8, 9, (T, d)) / 8.0
+    out, idx, gate = m.layer_decode(torch.from_numpy(x).to(torch.bfloat16).cuda(), add_residual=False)
+    idx, gate = idx.cpu().numpy(), gate.double().cpu().numpy()
+
+    def ffn(x, gate, up, down, planted=False):
+        """In 64 bits, and how far a kernel may be off that keeps 16 bits of the activation: the first eight off by half a step of bf16 at
+        most, these rounded to eight again; silu as above; sums of 2 F products in fp32."""
+        g = x @ gate.T
+        h = g / (1.0 + np.exp(-g)) * (x @ up.T)
+        eh = (HALF_BF16 ** 2 + 2.0 ** -20 * (1 + np.abs(g))) * np.abs(h) + 2.0 ** -133
+        if planted:
+            h = torch.from_numpy(h).to(torch.bfloat16).double().numpy()
+        return h @ down.T, eh @ np.abs(down).T + 2 * 2 * F * U * (np.abs(h) @ np.abs(down).T)
+
+    for planted in (False, True):
+        want, slack = ffn(x, *[v[0] for v in w[3:]], planted)
+        for t in range(T):
+            y, s = ffn(x[t:t + 1], *[v[idx[t, 0]] for v in w[:3]], planted)
+            want[t:t + 1] += gate[t, 0] * y
+            slack[t:t + 1] += gate[t, 0] * s
+        slack = slack + 24 * U * (np.abs(want) + slack)
+        wrong = np.abs(out.double().cpu().numpy() - want) > slack + HALF_BF16 * (np.abs(want) + slack)
+        assert wrong.any() == planted
+
+
 # ------------------------------------------------------------------------------------------------------------- refusals
 
 
