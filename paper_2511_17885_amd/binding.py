@@ -304,7 +304,36 @@ def rms_norm_backward(h, weight, eps, d_n, d_h=None, want_weight=True):
     return d_x, d_weight
 
 
-class FMoE:
+class _Workspace:
+    """An object's scratch memory, which grows with its calls.  All its calls have the same one: those on several streams, and the replays
+    of graphs captured from them, need an order between them (or an object each)."""
+
+    _ws = _ws_stream = None
+    _ws_kept = False     # a graph, or work on another stream than the tensor's own, may have its address
+    _outgrown = ()
+
+    def _room(self, need, device):
+        """At least `need` bytes.  A captured graph writes to the address it was captured with at every replay: what it, or another
+        stream, has seen stays when it is outgrown, as long as the object does."""
+        stream, capturing = _stream_of(device)
+        if self._ws is None or self._ws.numel() < need:
+            if self._ws is not None and (self._ws_kept or self._ws_stream is None):
+                self._outgrown = (*self._outgrown, self._ws)
+            self._ws = torch.empty(need, dtype=torch.uint8, device=device)
+            self._ws_stream, self._ws_kept = stream, capturing
+        elif capturing or stream != self._ws_stream:
+            self._ws_kept = True
+        return self._ws
+
+
+def _stream_of(device):
+    """(The device's current stream, whether it is being captured; True where that is not known.)"""
+    index = device.index
+    return (torch._C._cuda_getCurrentRawStream(index),
+            index != torch._C._cuda_getDevice() or torch._C._cuda_isCurrentStreamCapturing())
+
+
+class FMoE(_Workspace):
     """One MoE layer shape on one GPU.  Methods mirror the C entry points one to one."""
 
     def __init__(self, *, d_model, n_experts, d_ffn, k_text, k_visual, dtype, n_shared=0,
@@ -317,7 +346,6 @@ class FMoE:
         self._ctx = C.c_void_p()
         _check(self.lib.fmoe_create(C.byref(self._ctx), C.byref(self.cfg), device))
         self._weights = None
-        self._ws = None
 
     def close(self):
         if getattr(self, "_ctx", None) and self._ctx.value:
@@ -411,10 +439,7 @@ class FMoE:
         return int(self.lib.fmoe_workspace_bytes(self._ctx, max_tokens, max_seqs))
 
     def workspace(self, max_tokens, max_seqs=1):
-        need = self.workspace_bytes(max_tokens, max_seqs)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return self._ws
+        return self._room(self.workspace_bytes(max_tokens, max_seqs), self.device)
 
     def _i32(self, *shape):
         return torch.empty(*shape, dtype=torch.int32, device=self.device)
@@ -596,13 +621,11 @@ class FMoE:
         if out is None:
             out = torch.empty_like(x)
         idx, gate = self._i32(T, K), self._f32(T, K)
-        need = int(self.lib.fmoe_layer_decode_workspace_bytes(self._ctx, T))
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        ws = self._room(int(self.lib.fmoe_layer_decode_workspace_bytes(self._ctx, T)), self.device)
         at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         _call(self.device, self.lib.fmoe_layer_decode, self._ctx, C.byref(params) if params is not None else None, normed, x.data_ptr(),
               at(delta), at(is_visual), at(select_bias), T, int(bool(add_residual)), out.data_ptr(), idx.data_ptr(), gate.data_ptr(),
-              self._ws.data_ptr(), self._ws.numel())
+              ws.data_ptr(), ws.numel())
         if self.kmax == 0:
             idx, gate = idx[:, :0], gate[:, :0]
         return out, idx, gate
@@ -684,7 +707,7 @@ def stage_schedule(retention, prune_layers, window=1, alpha=1.0, gamma=0.0, sim_
             for l in prune_layers}
 
 
-class FMoEStack:
+class FMoEStack(_Workspace):
     """A stack of MoE layers with x <- x + MoE_l(x), per-layer (k_text, k_visual) (Sec. 3.1: reduced
     activation from layer l_v on) and pruning stages at chosen layers (Sec. 3.2; App. D).  One
     fmoe_stack_forward call: the sequencing, the budget bookkeeping and the index composition all
@@ -702,7 +725,6 @@ class FMoEStack:
             self.plan[l].k_text, self.plan[l].k_visual = int(kt), int(kv)
             self.plan[l].prune = sched.get(l, prune_params(retention=1.0, window=1, prune_mode=0))
         self._ctxs = (C.c_void_p * n)(*[m._ctx.value for m in self.layers])
-        self._ws = None
 
     def workspace_bytes(self, max_tokens, max_seqs):
         return int(load().fmoe_stack_workspace_bytes(self._ctxs, self.plan, len(self.layers), max_tokens, max_seqs))
@@ -715,9 +737,7 @@ class FMoEStack:
         output rows."""
         m0 = self.layers[0]
         T, B, n = x.shape[0], cu_seqlens.shape[0] - 1, len(self.layers)
-        need = self.workspace_bytes(T, B)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=m0.device)
+        ws = self._room(self.workspace_bytes(T, B), m0.device)
         if out is None:
             out = torch.empty((max(T, 1), m0.d), dtype=m0.torch_dtype, device=m0.device)
         if kept_idx is None:
@@ -734,7 +754,7 @@ class FMoEStack:
         vis_out = torch.empty(max(T, 1), dtype=torch.uint8, device=m0.device) if want_mask else None
         _check(load().fmoe_stack_forward(self._ctxs, self.plan, n, _ptr(x), _ptr(is_visual), _ptr(cu_seqlens),
                                          nv, nt, B, T, attn_ptrs, _ptr(out), _ptr(kept_idx), _ptr(new_cu),
-                                         _ptr(vis_out), C.byref(n_out), _ptr(self._ws), self._ws.numel(), _stream()))
+                                         _ptr(vis_out), C.byref(n_out), _ptr(ws), ws.numel(), _stream()))
         for l, m in enumerate(self.layers):   # the contexts' top-k now is the last layer's plan
             m.cfg.k_text, m.cfg.k_visual = self.plan[l].k_text, self.plan[l].k_visual
         if want_mask:

@@ -239,6 +239,40 @@ def test_streams_and_a_graph_with_a_shared_workspace():
 
 
 @pytest.mark.gpu
+def test_graphs_of_fewer_tokens_keep_their_workspace():
+    """A graph a batch size, each larger than the last, then a larger call: every graph still gives its outputs at each replay, and writes into
+    nothing that was allocated since."""
+    rng = np.random.default_rng(4)
+    layer = _Layer(rng, 264, 12, 72, 1, 40, 3, 3, True)
+    m, sizes = layer.m, (1, 3, 16)
+    xs = [_bf16(rng, T, 264) for T in sizes]
+    graphs, results, rooms = [], [], []
+    for x in xs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            results.append(m.layer_decode(x))
+        graphs.append(graph)
+        rooms.append((m._ws.data_ptr(), m._ws.numel()))
+    many = _bf16(rng, 300, 264)
+    visual, cu = torch.zeros(300, dtype=torch.uint8, device="cuda"), torch.tensor([0, 300], dtype=torch.int32, device="cuda")
+    whole = m.layer_forward(many, visual, cu, add_residual=True)[0].clone()
+    others = [torch.full((size,), 0x5A, dtype=torch.uint8, device="cuda") for _, size in rooms for _ in range(8)]
+    ranges = [(t.data_ptr(), t.numel()) for t in (*others, m._ws)]
+    assert not any(a < b + nb and b < a + na for a, na in rooms for b, nb in ranges)   # before anything is replayed
+    for turn in range(3):
+        for x in xs:
+            x.copy_(torch.randn(x.shape, device="cuda"))
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        got = [[t.clone() for t in r] for r in results]
+        for x, g in zip(xs, got):
+            assert all(torch.equal(a, b) for a, b in zip(g, m.layer_decode(x))), turn
+        assert all((t == 0x5A).all() for t in others)
+        assert torch.equal(m.layer_forward(many, visual, cu, add_residual=True)[0], whole)
+
+
+@pytest.mark.gpu
 def test_decode_agrees_with_the_layer():
     """The fused call and fmoe_layer_forward on the same tokens, away from ties."""
     rng = np.random.default_rng(5)

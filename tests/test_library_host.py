@@ -444,3 +444,61 @@ def test_dense_deal_meets_every_item_once(deal, n, n_several, run_len, cols):
     for tile_cap in (n, n + 71):
         assert deal.walk(n, n_several, run_len, cols, tile_cap, C.byref(singles)) == 0
         assert singles.value == (n - n_several) * cols
+
+
+def test_an_outgrown_workspace_stays_where_a_graph_or_another_stream_may_use_it(monkeypatch):
+    """Growth on the host: what a captured call or one on another stream has seen is kept, what one stream alone has used is not."""
+    import torch
+    now = {"stream": 1, "capturing": False}
+    monkeypatch.setattr(binding, "_stream_of", lambda device: (now["stream"], now["capturing"]), raising=False)
+    sizes = {1: 100, 2: 200, 3: 300, 4: 400, 5: 500}
+
+    def outgrown(cls, calls):
+        """Whether the workspace of each of the calls (stream, capturing, size) is still held after all of them."""
+        import gc
+        import weakref
+        m = object.__new__(cls)
+        m._ctx, m._ws, m.device = None, None, torch.device("cpu")
+        m.workspace_bytes = lambda tokens, seqs=1: sizes[tokens]
+        seen = []
+        for now["stream"], now["capturing"], tokens in calls:
+            ws = m.workspace(tokens) if cls is binding.FMoE else m._room(sizes[tokens], m.device)
+            assert ws.numel() >= sizes[tokens] and ws is m._ws
+            seen.append(weakref.ref(ws))
+            del ws
+        gc.collect()
+        return [r() is not None for r in seen]
+
+    for cls in (binding.FMoE, binding.FMoEStack):
+        assert outgrown(cls, [(1, False, 1), (1, False, 2), (1, False, 3)]) == [False, False, True]
+        assert outgrown(cls, [(1, True, 1), (1, False, 2), (1, False, 3)]) == [True, False, True]      # captured as it was made
+        assert outgrown(cls, [(1, False, 2), (2, True, 1), (1, False, 3)]) == [True, True, True]       # captured with one of before
+        assert outgrown(cls, [(1, False, 1), (2, False, 1), (1, False, 2), (1, False, 4)]) == [True, True, False, True]
+        assert outgrown(cls, [(1, True, t) for t in (1, 2, 3, 4, 5)]) == [True] * 5
+        assert outgrown(cls, [(1, False, 1), (2, False, 2), (2, False, 3)]) == [False, False, True]
+
+
+def test_layer_decode_uses_the_workspace_that_grows(monkeypatch):
+    """The decoding call, too, keeps a workspace that a graph holds (its own size is asked for, the memory is the object's)."""
+    import torch
+    monkeypatch.setattr(binding, "_stream_of", lambda device: (7, True), raising=False)
+    used = []
+    monkeypatch.setattr(binding, "_call", lambda device, entry, *args: used.append(args[-2]))
+
+    class Lib:
+        fmoe_layer_decode = None
+
+        @staticmethod
+        def fmoe_layer_decode_workspace_bytes(ctx, T):
+            return 1000 * T
+
+    m = object.__new__(binding.FMoE)
+    m.lib, m._ctx, m._ws, m.device, m.torch_dtype = Lib, None, None, torch.device("cpu"), torch.bfloat16
+    m.cfg = binding.FmoeConfig(64, 8, 32, 0, 0, 2, 1, 1, 1)
+    kept = []
+    for T in (1, 2, 16):
+        m.layer_decode(torch.zeros(T, 64, dtype=torch.bfloat16))
+        kept.append(m._ws)
+    held = [*m._outgrown, m._ws]
+    assert [t.data_ptr() for t in held] == used and len(held) == 3
+    assert all(a is b for a, b in zip(held, kept))
