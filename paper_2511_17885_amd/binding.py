@@ -198,6 +198,15 @@ def _expect(t, what, dtype, shape, device):
                          f"{tuple(t.shape)} on {t.device}")
 
 
+def _expect_indexes(t, what, most, device):
+    """At least `most` int32 numbers: kernels read so many, whatever the tensor has."""
+    if t is None:
+        return
+    if t.dtype != torch.int32 or t.numel() < most or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what} must be a contiguous {torch.int32} tensor of at least {most} elements on {device}, not {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+
+
 def _call(device, entry, *args):
     """A call without a context, on the device of its tensors, which mostly is the current one."""
     if device.type == "cuda" and device.index == torch._C._cuda_getDevice():
@@ -535,7 +544,16 @@ class FMoE(_Workspace):
                                              _ptr(offs), _ptr(perm), _ptr(inv), _stream()))
         return offs, perm, inv
 
+    def _expect_rows(self, kept_idx, n_kept, expert_offsets, perm_src, n_kept_dev, rows):
+        """The indexes of an expert product: kept tokens, experts' offsets, `rows` rows (these two only where tokens have experts)."""
+        _expect_indexes(kept_idx, "kept_idx", n_kept, self.device)
+        _expect_indexes(n_kept_dev, "n_kept_dev", 1, self.device)
+        if self.kmax > 0:
+            _expect_indexes(expert_offsets, "expert_offsets", self.E + 1, self.device)
+            _expect_indexes(perm_src, "perm_src", rows, self.device)
+
     def expert_ffn(self, x, kept_idx, n_kept, expert_offsets, perm_src, n_kept_dev=None):
+        self._expect_rows(kept_idx, n_kept, expert_offsets, perm_src, n_kept_dev, 0)   # (as many rows as the offsets say)
         K = max(self.kmax, 1)
         y = torch.empty((max(n_kept * K, 1), self.d), dtype=self.torch_dtype, device=self.device)
         ysh = None
@@ -560,6 +578,7 @@ class FMoE(_Workspace):
             raise ValueError(f"{T} rows of {self.d} bytes: rows are found by 32-bit offsets")
         _expect(codes, "codes", codes.dtype, (T, self.d), self.device)
         _expect(scales, "scales", torch.uint8, (T, row_scales(self.d)), self.device)
+        self._expect_rows(kept_idx, n_kept, expert_offsets, perm_src, n_kept_dev, n_kept * self.kmax)
         K = max(self.kmax, 1)
         y = torch.empty((max(n_kept * K, 1), self.d), dtype=torch.bfloat16, device=self.device)
         ysh = None

@@ -472,6 +472,37 @@ def test_rows_past_32_bit_offsets_are_refused():
         m.expert_ffn_quant_rows(codes, codes, codes, 1, codes, codes)
 
 
+def test_indexes_of_other_types_and_sizes_are_refused(monkeypatch):
+    """Offsets as cumsum gives them (int64) are not pairs of int32 numbers, and a list is not read past its end."""
+    m = object.__new__(binding.FMoE)
+    m._ctx, m.device = None, torch.device("cpu")
+    m.cfg = binding.FmoeConfig(64, 4, 32, 0, 0, 2, 1, 1, 1)
+    m.lib = type("Lib", (), {"fmoe_expert_ffn_quant_rows": None, "fmoe_expert_ffn": staticmethod(lambda *a: 0)})
+    m.workspace = lambda *a: torch.empty(256, dtype=torch.uint8)
+    calls = []
+    monkeypatch.setattr(binding, "_call", lambda *a: calls.append(a))
+    monkeypatch.setattr(binding, "_stream", lambda: None)
+    m.torch_dtype = torch.bfloat16
+    codes, scales, x = torch.zeros(8, 64, dtype=torch.uint8), torch.zeros(8, 4, dtype=torch.uint8), torch.zeros(8, 64, dtype=torch.bfloat16)
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    good = {"kept_idx": i32(6), "n_kept": 6, "expert_offsets": i32(5), "perm_src": i32(12), "n_kept_dev": i32(1)}
+    m.expert_ffn_quant_rows(codes, scales, **good)
+    m.expert_ffn_quant_rows(codes, scales, **dict(good, kept_idx=None, n_kept_dev=None))
+    m.expert_ffn(x, **good)
+    assert len(calls) == 2
+    for name, least in (("kept_idx", 6), ("expert_offsets", 5), ("perm_src", 12), ("n_kept_dev", 1)):
+        for bad in (i32(least).long(), i32(least).float(), i32(2 * least + 2)[::2], i32(least).to("meta"), i32(least - 1)):
+            with pytest.raises(ValueError, match=name):
+                m.expert_ffn_quant_rows(codes, scales, **dict(good, **{name: bad}))
+            if name != "perm_src" or bad.numel() >= least:   # (there the offsets say how many)
+                with pytest.raises(ValueError, match=name):
+                    m.expert_ffn(x, **dict(good, **{name: bad}))
+    assert len(calls) == 2
+    m.cfg.k_text = m.cfg.k_visual = 0                        # shared experts alone need no lists
+    m.expert_ffn_quant_rows(codes, scales, None, 6, None, None)
+    assert len(calls) == 3
+
+
 @pytest.mark.gpu
 def test_expert_ffn_quant_rows_refuses_bad_arguments():
     rng = np.random.default_rng(1)
