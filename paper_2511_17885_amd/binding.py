@@ -263,7 +263,10 @@ def _norm_args(x, weight, delta):
         _expect(delta, "delta", kind, shape, x.device)
     if _differs(weight, weight_kind, (d,), index):
         _expect(weight, "weight", weight_kind, (d,), x.device)
-    return dtype, weight_dtype, x.numel() // max(d, 1), d
+    T = x.numel() // max(d, 1)
+    if T >> 31 or d >> 31:   # the library's are 32-bit numbers
+        raise ValueError(f"{T} rows of {d}: more than 32 bits hold")
+    return dtype, weight_dtype, T, d
 
 
 def rms_norm(x, weight, eps=1e-6, delta=None):

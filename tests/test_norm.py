@@ -401,6 +401,16 @@ def test_norm_refuses_bad_arguments():
     assert bwd(dw=p, ws=None) == -4 and bwd(dw=p, ws=0x4010) == -4 and bwd(dw=p, nb=need - 1) == -4
 
 
+def test_norm_sizes_past_32_bits_are_refused(monkeypatch):
+    """2^32 + 4 rows are not four, nor a row of 2^32 + 8 elements one of eight."""
+    monkeypatch.setattr(binding, "_call", lambda *a: None)
+    empty = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="meta")  # noqa: E731
+    for x, w in ((empty((1 << 32) + 4, 8), empty(8)), (empty(1 << 16, (1 << 15) + 1, 16), empty(16)), (empty(1, (1 << 32) + 8), empty((1 << 32) + 8))):
+        for call in (lambda: binding.rms_norm(x, w), lambda: binding.rms_norm_quant(x, w), lambda: binding.rms_norm_backward(x, w, EPS, x)):
+            with pytest.raises(ValueError, match="32 bits"):
+                call()
+
+
 @pytest.mark.gpu
 def test_norm_binding_refuses_tensors_that_do_not_fit():
     x, w = torch.zeros(4, 64, device="cuda"), torch.ones(64, device="cuda")
