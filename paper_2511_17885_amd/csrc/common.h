@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "fmoe.h"
+#include "units.h"
 
 #define FMOE_MAX_EXPERTS 256
 #define FMOE_MAX_TOPK 16
@@ -227,12 +228,7 @@ int launch_combine(const fmoe_ctx* ctx, const void* y, const void* y_shared, con
                    const float* topk_gate, const int32_t* kept_idx, int n_cap, const int32_t* n_dev,
                    int n_expected, const void* residual, void* out, hipStream_t stream);
 
-// The experts that a few tokens list, ascending: work items of a layer for a decoding step
-struct fmoe_unit {
-  int32_t expert, row0;         // row0: its first hidden row, the rows by expert and token
-  uint32_t mask;                // tokens that list it
-};
-struct fmoe_unit_list {
+struct fmoe_unit_list {           // (units.h)
   int32_t n, n_full, pad[2];
   float gate[FMOE_MAX_EXPERTS][FMOE_DECODE_TOKENS];   // of the tokens in the mask
   fmoe_unit unit[FMOE_MAX_EXPERTS];

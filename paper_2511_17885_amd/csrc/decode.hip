@@ -304,26 +304,19 @@ __device__ __forceinline__ void accumulate(const DecodeMatrix& M, int group, int
   }
 }
 
-// The list of experts is a workspace's content: whatever is read there (two calls that share a workspace without an order, say)
-// is kept within the layer's experts and the call's rows.
-struct ListBounds {
-  int E, T, pairs;              // pairs: hidden rows
-};
-__device__ __forceinline__ int list_length(const fmoe_unit_list* list, const ListBounds& b) {
-  const int most = b.pairs < b.E ? b.pairs : b.E, n = list->n;
-  return n < 0 ? 0 : n < most ? n : most;
-}
-// Unit u, in scalar registers (an entry behind the last is not used)
+// The list's length and unit u (which may be behind the last), held within bounds (units.h), in scalar registers
+__device__ __forceinline__ int list_length(const fmoe_unit_list* list, const ListBounds& b) { return units_within(list->n, b); }
 __device__ __forceinline__ fmoe_unit load_unit(const fmoe_unit_list* list, int u, const ListBounds& b) {
   typedef const __attribute__((address_space(4))) int32_t* const_ptr;
   const const_ptr p = (const_ptr)(uintptr_t)(list->unit + u);
-  fmoe_unit r{p[0], p[1], (uint32_t)p[2] & ((1u << b.T) - 1u)};
-  const int last = b.pairs - (r.mask != 0u ? __popc(r.mask) : 1);
-  r.expert = r.expert < 0 ? 0 : r.expert < b.E ? r.expert : b.E - 1;
-  r.row0 = r.row0 < last ? r.row0 : last;
-  r.row0 = r.row0 < 0 ? 0 : r.row0;
-  return r;
+  return unit_within(fmoe_unit{p[0], p[1], (uint32_t)p[2]}, b);
 }
+// Of the n units those that two tokens eight apart list: number i, how many there are
+__device__ __forceinline__ int full_unit(const fmoe_unit_list* list, int i, int n) {
+  typedef const __attribute__((address_space(4))) int32_t* const_ptr;
+  return full_unit_within(((const_ptr)(uintptr_t)list->full)[i], n);
+}
+__device__ __forceinline__ int full_length(const fmoe_unit_list* list, int n) { return full_units_within(list->n_full, n); }
 
 // Hidden rows h = silu(gate) * up are kept in two bf16 planes, h rounded to bf16 and what that leaves rounded again: 16 bits, 2^-16 of a
 // value at most lost, far less than the rounding of the output.  (One plane's rounding is as much as the output's; the down launch with
@@ -334,17 +327,6 @@ __device__ __forceinline__ void store_hidden(bf16_t* row, int plane, int col, fl
   const float top = bf16_to_f32(hi);
   row[col] = hi;
   row[plane + col] = rms::finite(top) ? f32_to_bf16(h - top) : 0;
-}
-
-// Entry i of the units that two tokens eight apart list, of the n in the list; how many there are
-__device__ __forceinline__ int full_unit(const fmoe_unit_list* list, int i, int n) {
-  typedef const __attribute__((address_space(4))) int32_t* const_ptr;
-  const int u = ((const_ptr)(uintptr_t)list->full)[i];
-  return u < 0 ? 0 : u < n ? u : n - 1;
-}
-__device__ __forceinline__ int full_length(const fmoe_unit_list* list, int n) {
-  const int full = list->n_full;
-  return full < 0 ? 0 : full < n ? full : n;
 }
 
 struct GateUpArgs {

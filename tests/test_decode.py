@@ -340,6 +340,59 @@ def test_activation_is_not_rounded_to_bf16(T, F, quant):
 # ------------------------------------------------------------------------------------------------------------- refusals
 
 
+UNITS = r"""
+#include "units.h"
+extern "C" int units_(int n, int E, int T, int pairs) { return units_within(n, ListBounds{E, T, pairs}); }
+extern "C" void unit_(const int* in, int E, int T, int pairs, int* out) {
+  const fmoe_unit u = unit_within(fmoe_unit{in[0], in[1], (uint32_t)in[2]}, ListBounds{E, T, pairs});
+  out[0] = u.expert, out[1] = u.row0, out[2] = (int)u.mask;
+}
+extern "C" int full_units_(int n_full, int n) { return full_units_within(n_full, n); }
+extern "C" int full_unit_(int u, int n) { return full_unit_within(u, n); }
+"""
+
+
+@pytest.fixture(scope="module")
+def units(tmp_path_factory):
+    import os
+    import subprocess
+    d = tmp_path_factory.mktemp("units")
+    (d / "units.cpp").write_text(UNITS)
+    csrc = os.path.join(os.path.dirname(binding.__file__), "csrc")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", csrc, str(d / "units.cpp"), "-o", str(d / "units.so")], check=True)
+    return C.CDLL(str(d / "units.so"))
+
+
+@pytest.mark.parametrize("E,T,k", [(1, 1, 1), (4, 1, 4), (4, 16, 1), (64, 16, 6), (256, 1, 16), (256, 16, 16), (20, 9, 3)])
+def test_any_list_in_the_workspace_stays_within_the_layer(units, E, T, k):
+    """What a call takes from the list of experts, whatever stands there: experts of the layer, rows of the call, no more units than either."""
+    rng = np.random.default_rng(E + T)
+    pairs = T * k
+    ends = [0, 1, -1, 2, E - 1, E, E + 1, T, pairs - 1, pairs, pairs + 1, 255, 256, 0x5a5a5a5a, -0x5a5a5a5b, 2 ** 31 - 1, -2 ** 31]
+    any32 = lambda size: np.where(rng.random(size) < 0.5, rng.choice(ends, size), rng.integers(-2 ** 31, 2 ** 31, size)).astype(np.int32)  # noqa: E731
+    for n in [*ends, *any32(50).tolist()]:
+        units_of = units.units_(C.c_int(n), E, T, pairs)
+        assert 0 <= units_of <= min(pairs, E) and (units_of == n or not 0 <= n <= min(pairs, E))
+        for least in {1, min(pairs, E)}:
+            full, at = units.full_units_(C.c_int(n), least), units.full_unit_(C.c_int(n), least)
+            assert 0 <= full <= least and 0 <= at < least
+            assert (full == n or not 0 <= n <= least) and (at == n or not 0 <= n < least)
+    out = (C.c_int * 3)()
+    for entry in any32((4000, 3)):
+        units.unit_((C.c_int * 3)(*entry.tolist()), E, T, pairs, out)
+        expert, row0, mask = out
+        rows = bin(mask).count("1")
+        assert 0 <= expert < E and 0 <= mask < 1 << T and 0 <= row0 and row0 + max(rows, 1) <= pairs
+    # a list as a call writes it comes through as it is
+    listed = np.sort(rng.choice(E, size=min(E, pairs), replace=False))
+    row = 0
+    for i, e in enumerate(listed.tolist()):
+        mask = int(rng.integers(1, 1 << T)) if pairs - row - (len(listed) - i - 1) >= T else 1 << int(rng.integers(0, T))
+        units.unit_((C.c_int * 3)(e, row, mask), E, T, pairs, out)
+        assert tuple(out) == (e, row, mask)
+        row += bin(mask).count("1")
+
+
 def test_layer_decode_refuses_bad_arguments():
     lib = binding.load()
 
