@@ -569,12 +569,10 @@ int launch_layer_decode(const fmoe_ctx* ctx, const fmoe_select_params* params, c
     const int blocks = g.shared.nbw + units * g.routed.nbw, ncb = ctx->quant && T > 4 ? 2 : 1;
     const dim3 grid((g.shared.nbw + ncb - 1) / ncb + units * ((g.routed.nbw + ncb - 1) / ncb));
     fmoe_prof_scope prof(ctx, SLOT_GEMM1, stream);
-    if (blocks > 0 && ncb == 1) {
-      if (ctx->quant) hipLaunchKernelGGL((decode_gate_up_kernel<true, 1>), grid, dim3(64), 0, stream, g);
-      else hipLaunchKernelGGL((decode_gate_up_kernel<false, 1>), grid, dim3(64), 0, stream, g);
-    } else if (blocks > 0) {
-      if (ctx->quant) hipLaunchKernelGGL((decode_gate_up_kernel<true, 2>), grid, dim3(64), 0, stream, g);
-      else hipLaunchKernelGGL((decode_gate_up_kernel<false, 2>), grid, dim3(64), 0, stream, g);
+    if (blocks > 0) {
+      if (!ctx->quant) hipLaunchKernelGGL((decode_gate_up_kernel<false, 1>), grid, dim3(64), 0, stream, g);
+      else if (ncb == 1) hipLaunchKernelGGL((decode_gate_up_kernel<true, 1>), grid, dim3(64), 0, stream, g);
+      else hipLaunchKernelGGL((decode_gate_up_kernel<true, 2>), grid, dim3(64), 0, stream, g);
     }
   }
   DownArgs a{};

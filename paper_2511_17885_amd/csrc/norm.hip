@@ -290,7 +290,8 @@ void run_backward(const NormBackwardArgs& a, int blocks, hipStream_t stream) {
   do {                                                                                                                  \
     if (pass) hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 1, true>), grid, block, 0, stream, a);           \
     else if (wpr == 1) hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 1, false>), grid, block, 0, stream, a); \
-    else hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 4, false>), grid, block, 0, stream, a);               \
+    else if constexpr (NU > 2) /* four wavefronts: rows of more than 512 units */                                       \
+      hipLaunchKernelGGL((rms_norm_backward_kernel<XT, WT, NU, 4, false>), grid, block, 0, stream, a);                  \
   } while (0)
   if (per_lane <= 1) FMOE_NORM(1);
   else if (per_lane <= 2) FMOE_NORM(2);
