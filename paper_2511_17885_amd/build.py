@@ -108,7 +108,8 @@ def check_pending_reads(asm_path):
 
 def check_matrix_operands(asm_path):
     """A matrix instruction may read a register that a vector instruction has written only two waits later.  The compiler keeps to that with its
-    own instructions, not with those in inline assembly.  This reads the device assembly and fails where such a write is nearer."""
+    own instructions, not with those in inline assembly.  This reads the device assembly and fails where such a write is nearer, on the way
+    down or by a branch.  Exchanges (v_swap, v_permlane*_swap) write both of their operands."""
     import re
 
     def registers(text):
@@ -116,26 +117,44 @@ def check_matrix_operands(asm_path):
         for m in re.finditer(r"\bv(?:\[(\d+):(\d+)\]|(\d+)\b)", text):
             lo = int(m.group(1) or m.group(3))
             found.update(range(lo, int(m.group(2) or lo) + 1))
-        return found
+        return frozenset(found)
 
-    in_asm, recent, seen = False, [], 0   # recent: registers that the last two instructions wrote
+    lines, in_asm = [], False   # (number, code, within inline assembly)
     for n, line in enumerate(open(asm_path), 1):
         code = line.split(";")[0].strip()
         if "ASMSTART" in line or "ASMEND" in line:
             in_asm = "ASMSTART" in line
-        elif not code or code.startswith((".", "#")) or code.endswith(":"):
-            continue
-        elif code.startswith("s_nop"):
-            recent = ([set()] * (int(code.split()[1]) + 1) + recent)[:2]
-        elif code.startswith("v_mfma"):
-            if in_asm:
-                seen += 1
-                if any(registers(code.split(",", 1)[1]) & r for r in recent):
-                    raise RuntimeError(f"{asm_path}:{n}: a matrix instruction reads a register that was written just before it: {code}")
-            recent = [set()] + recent[:1]
-        else:
-            vector = code.startswith("v_") and not code.startswith("v_cmp")
-            recent = [registers(code.split(",")[0]) if vector else set()] + recent[:1]
+        elif code.endswith(":") or (code and not code.startswith((".", "#"))):
+            lines.append((n, code, in_asm))
+    none = frozenset()
+    entered, before = {}, None  # label -> what the last two instructions wrote, over the branches that lead there
+    while entered != before:    # twice or three times: two instructions reach over two branches at most
+        before, entered, seen, recent = entered, dict(entered), 0, (none, none)
+        for n, code, in_asm in lines:
+            word = code.split()[0]
+            if code.endswith(":"):
+                recent = tuple(a | b for a, b in zip(recent, before.get(code[:-1], (none, none))))
+            elif word == "s_nop":
+                recent = ((none,) * (int(code.split()[1], 0) + 1) + recent)[:2]
+            elif word.startswith("v_mfma"):
+                if in_asm:
+                    seen += 1
+                    if any(registers(code.split(",", 1)[1]) & r for r in recent):
+                        raise RuntimeError(f"{asm_path}:{n}: a matrix instruction reads a register that was written just before it: {code}")
+                recent = (none, recent[0])
+            elif word.startswith(("s_branch", "s_cbranch")):
+                recent, label = (none, recent[0]), code.split()[-1]
+                entered[label] = tuple(a | b for a, b in zip(recent, entered.get(label, (none, none))))
+                if word == "s_branch":
+                    recent = (none, none)
+            elif word in ("s_endpgm", "s_setpc_b64"):
+                recent = (none, none)
+            else:
+                operands = code[len(word):].split(",")
+                written = none
+                if word.startswith("v_") and not word.startswith("v_cmp"):
+                    written = registers(",".join(operands[:2 if "swap" in word else 1]))
+                recent = (written, recent[0])
     return seen
 
 

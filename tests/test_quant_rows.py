@@ -465,6 +465,30 @@ def test_build_check_catches_operands_written_just_before(tmp_path):
             build.check_matrix_operands(str(p))
 
 
+def test_build_check_follows_branches_and_exchanges(tmp_path):
+    """Both operands of an exchange are written; what a block is entered with by a branch counts, over one or two of them."""
+    from paper_2511_17885_amd import build
+    mfma = ("\t;;#ASMSTART\n\tv_mfma_scale_f32_16x16x128_f8f6f4 a[0:3], v[4:7], v[8:15], a[0:3], v16, v17 cbsz:4\n\t;;#ASMEND\n\ts_endpgm\n")
+    good = ["\tv_permlane32_swap_b32_e32 v1, v2\n", "\tv_permlane32_swap_b32_e32 v1, v9\n\ts_nop 1\n",
+            "\tv_mov_b32_e32 v9, v1\n\ts_nop 0\n\ts_cbranch_scc0 .L1\n\ts_nop 1\n.L1:\n",
+            "\tv_mov_b32_e32 v9, v1\n\ts_branch .L2\n.L1:\n",                 # leads elsewhere
+            "\tv_mov_b32_e32 v9, v1\n\ts_endpgm\n.L1:\n",
+            ".L1:\n\tv_mov_b32_e32 v9, v1\n\ts_nop 1\n"]
+    bad = ["\tv_permlane32_swap_b32_e32 v1, v9\n", "\tv_permlane16_swap_b32_e32 v9, v1\n\ts_nop 0\n", "\tv_swap_b32 v1, v17\n",
+           "\tv_mov_b32_e32 v9, v1\n\ts_cbranch_scc0 .L1\n\ts_nop 1\n.L1:\n",
+           "\tv_mov_b32_e32 v9, v1\n\ts_branch .L1\n\ts_nop 1\n.L1:\n",
+           "\ts_branch .L3\n.L1:\n\ts_branch .L2\n.L3:\n\tv_mov_b32_e32 v16, v1\n.L4:\n\ts_branch .L2\n\ts_nop 1\n.L2:\n",
+           "\ts_cbranch_vccnz .L1\n\ts_nop 1\n.L2:\n" + mfma + ".L1:\n\tv_mov_b32_e32 v9, v1\n\ts_branch .L2\n"]   # backwards
+    p = tmp_path / "a.s"
+    for before in good:
+        p.write_text(before + mfma)
+        assert build.check_matrix_operands(str(p)) == 1
+    for before in bad:
+        p.write_text(before + mfma)
+        with pytest.raises(RuntimeError, match="written just before"):
+            build.check_matrix_operands(str(p))
+
+
 def test_rows_past_32_bit_offsets_are_refused():
     m = binding.FMoE(d_model=64, n_experts=2, d_ffn=64, k_text=1, k_visual=1, dtype="bf16")
     codes = torch.empty((1 << 26, 64), dtype=torch.uint8, device="meta")
