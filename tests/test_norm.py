@@ -341,6 +341,119 @@ def test_backward_of_rows_far_from_one_and_in_place():
         assert (np.abs(_np(dw) - want_w) <= U * 9 * size_w).all()
 
 
+# Up to 4096 rows of more than 1024 elements have four wavefronts a row, from 4097 on one (up to 4096 elements).  From 100 MB of tensors
+# on, one wavefront's rows pass the caches by.
+TYPES = [(torch.bfloat16, torch.bfloat16, True), (torch.bfloat16, torch.float32, False), (torch.float32, torch.float32, True),
+         (torch.float32, torch.bfloat16, False)]
+ONE_WAVEFRONT = [(4097, 1032), (4098, 1288), (4097, 1544), (4099, 2048), (4097, 2056), (4098, 2568), (4097, 4096)]
+PAST_CACHES = [(6401, 2048, torch.bfloat16), (4097, 4096, torch.bfloat16), (6403, 1024, torch.float32), (4097, 2048, torch.float32),
+               (52001, 256, torch.bfloat16)]
+
+
+def _sample(T):
+    return np.unique(np.r_[0:4, 62:66, T // 2 + np.arange(8), T - 5:T])
+
+
+def _check_norms(T, d, dtype, weight_dtype, delta, seed):
+    x, dl, w = _inputs(T, d, dtype, weight_dtype, delta, seed=seed)
+    rows = _sample(T)
+    h, n = binding.rms_norm(x.cuda(), w.cuda(), EPS, delta=_cuda(dl))
+    h8, codes, scales = binding.rms_norm_quant(x.cuda(), w.cuda(), EPS, delta=_cuda(dl))
+    want_h, want_n = _norm(_np(x[rows]), None if dl is None else _np(dl[rows]), _np(w), EPS, dtype)
+    assert np.array_equal(_np(h[rows]), want_h) and torch.equal(h8, h)
+    _assert_norm(n[rows], want_n, dtype)
+    want_c, want_s = _quantize(want_n)
+    assert np.array_equal(codes.view(torch.uint8)[rows].cpu().numpy(), want_c) and np.array_equal(scales[rows].cpu().numpy(), want_s)
+    # and rows here and there as in calls of 64, which pass no cache by and have four wavefronts a row of more than 1024
+    for i in range(0, T, 997):
+        part = slice(i, i + 64)
+        h1, n1 = binding.rms_norm(x[part].cuda(), w.cuda(), EPS, delta=_cuda(None if dl is None else dl[part]))
+        _, c1, s1 = binding.rms_norm_quant(x[part].cuda(), w.cuda(), EPS, delta=_cuda(None if dl is None else dl[part]))
+        assert torch.equal(n[part], n1) and torch.equal(h[part], h1)
+        assert torch.equal(codes[part].view(torch.uint8), c1.view(torch.uint8)) and torch.equal(scales[part], s1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,weight_dtype,delta", TYPES)
+@pytest.mark.parametrize("T,d", ONE_WAVEFRONT)
+def test_norms_of_many_rows_with_one_wavefront_each(T, d, dtype, weight_dtype, delta):
+    _check_norms(T, d, dtype, weight_dtype, delta, 20)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,dtype", PAST_CACHES)
+def test_norms_whose_rows_pass_the_caches(T, d, dtype):
+    _check_norms(T, d, dtype, dtype, True, 21)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,dtype", PAST_CACHES + [(3203, 2048, torch.float32), (700, 8200, torch.bfloat16)])
+def test_backward_whose_rows_pass_the_caches(T, d, dtype):
+    """Gradients of rows as in calls of 64, the weight's against 64 bits."""
+    h, dh, w = _inputs(T, d, dtype, dtype, True, seed=22)
+    dn = _inputs(T, d, dtype, dtype, False, seed=23)[0]
+    dx, dw = binding.rms_norm_backward(h.cuda(), w.cuda(), EPS, dn.cuda(), d_h=dh.cuda())
+    rows = _sample(T)
+    want, size, _, _, _ = _backward(_np(h[rows]), _np(w), EPS, _np(dn[rows]), _np(dh[rows]))
+    assert (np.abs(_np(dx[rows]) - want) <= HALF[dtype] * (np.abs(want) + U * size) + U * size).all()
+    for i in range(0, T, 997):
+        part = slice(i, i + 64)
+        assert torch.equal(dx[part], binding.rms_norm_backward(h[part].cuda(), w.cuda(), EPS, dn[part].cuda(), d_h=dh[part].cuda())[0])
+    want_w, size_w = 0.0, 0.0
+    for i in range(0, T, 4096):
+        part = slice(i, i + 4096)
+        _, _, a, b, _ = _backward(_np(h[part]), _np(w), EPS, _np(dn[part]), None)
+        want_w, size_w = want_w + a, size_w + b
+    in_a_row = -(-T // 2048) if d <= 4096 else -(-T // 512)   # that a wavefront, or four, add up in fp32, then three sums, then 64 bits
+    assert (np.abs(_np(dw) - want_w) <= U * (in_a_row + 3 + 5) * size_w).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d", [(4096, 1288), (4097, 1288), (4096, 4096), (4097, 4096), (4097, 8192)])
+def test_a_row_is_the_same_on_both_sides_of_the_line(T, d):
+    x, dl, w = (t.cuda() for t in _inputs(4097, d, torch.bfloat16, torch.bfloat16, True, seed=24))
+    h, n = binding.rms_norm(x[:T], w, EPS, delta=dl[:T])
+    _, c, s = binding.rms_norm_quant(x[:T], w, EPS, delta=dl[:T])
+    for part in (slice(0, 1), slice(2000, 2009), slice(4095, 4096)):
+        h1, n1 = binding.rms_norm(x[part], w, EPS, delta=dl[part])
+        _, c1, s1 = binding.rms_norm_quant(x[part], w, EPS, delta=dl[part])
+        assert torch.equal(h[part], h1) and torch.equal(n[part], n1)
+        assert torch.equal(c[part].view(torch.uint8), c1.view(torch.uint8)) and torch.equal(s[part], s1)
+
+
+@pytest.mark.gpu
+def test_8_bits_at_the_borders_of_codes_and_scales_with_one_wavefront_a_row():
+    test_8_bits_at_the_borders_of_codes_and_scales(4097)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d", [(8, 1288), (8, 4104), (4097, 1288), (4097, 2056)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_that_are_no_ordinary_numbers_in_either_form(T, d, dtype):
+    x, dl, w = _inputs(T, d, dtype, torch.float32, True, seed=25)
+    x[0], dl[0] = 0.0, 0.0
+    x[1, 5] = -math.inf
+    x[2, 7], dl[2, 7] = math.inf, -math.inf
+    x[3, d - 1] = math.nan
+    x[4] *= 2.0 ** 120
+    x[5] *= 2.0 ** -80
+    dl[5] *= 2.0 ** -80
+    x[6], dl[6] = torch.finfo(dtype).max, 0.0
+    with np.errstate(all="ignore"):
+        for eps in (EPS, 0.0):
+            h, n = binding.rms_norm(x.cuda(), w.cuda(), eps, delta=dl.cuda())
+            want_h, want_n = _norm(_np(x[:8]), _np(dl[:8]), _np(w), eps, dtype)
+            got, odd = _np(n[:8]), ~np.isfinite(want_n)
+            assert np.array_equal(_np(h[:8]), want_h, equal_nan=True) and np.array_equal(np.isnan(got), np.isnan(want_n))
+            _assert_norm(torch.where(torch.from_numpy(odd), 0.0, n[:8].cpu()), np.where(odd, 0.0, want_n), dtype)
+            assert np.isfinite(got[4:]).all() and np.isnan(got[1:4]).any(1).all()
+            _, codes, scales = binding.rms_norm_quant(x.cuda(), w.cuda(), eps, delta=dl.cuda())
+            want_c, want_s = _quantize(want_n)
+            assert np.array_equal(scales.cpu().numpy()[:8], want_s)
+            got_c = codes.view(torch.uint8).cpu().numpy()[:8]
+            assert ((got_c == want_c) | ((got_c & 0x7f) + (want_c & 0x7f) == 0)).all()
+
+
 # -------------------------------------------------------------------------------------------------- streams and graphs
 
 

@@ -266,6 +266,113 @@ def test_nan_reaches_its_own_rows_and_experts_only(T):
     assert nan[expert == 2].all() and not nan[expert != 2].any() and not ysh.isnan().any()
 
 
+# The first product of the form for many rows an expert takes each code in one piece, and cuts (see _products)
+
+
+def _real_layer(rng, d, E, F, shared, F_shared, k):
+    """Random weights of the usual sizes: what they and the rows add up to, and what is cut, is not exact."""
+    shapes = [(E, F, d), (E, F, d), (E, d, F)] + ([(shared, F_shared, d)] * 2 + [(shared, d, F_shared)] if shared else [])
+    host = [(rng.integers(0, 16, s).astype(np.uint8), (125 - int(round(np.log2(s[2]) / 2)) + rng.integers(-1, 2, (*s[:2], -(-s[2] // 32)))).astype(np.uint8))
+            for s in shapes]
+    m = binding.FMoE(d_model=d, n_experts=E, d_ffn=F, n_shared=shared, d_ffn_shared=F_shared, k_text=k, k_visual=k, dtype="bf16")
+    m.set_weights_quant_rows(*[(_gpu(_pack(c)), _gpu(s)) for c, s in host])
+    return m, [[_matrix(c[g], s[g]) for g in range(len(c))] for c, s in host]
+
+
+def _check_real(m, w, rng, T, E, k, codes, scales, skew=0.0, most=24):
+    x, xs = _as_rows(codes, scales)
+    offsets, src = _rows(rng, T, E, k, skew)
+    y, ysh = m.expert_ffn_quant_rows(_gpu(codes).view(torch.float8_e4m3fn), _gpu(scales), None, T, _gpu(offsets), _gpu(src))
+    torch.cuda.synchronize()
+    pick = lambda n: np.arange(n) if n <= most else np.unique(np.r_[:2, rng.choice(n, most - 4, replace=False), n - 2:n])  # noqa: E731
+    for e in range(E):
+        r = offsets[e] + pick(offsets[e + 1] - offsets[e])
+        want, bound = _ffn(x[src[r]], xs[src[r]], *[v[e] for v in w[:3]])
+        assert (np.abs(y[r].double().cpu().numpy() - want) <= bound).all(), e
+    for i in range(len(w[3]) if len(w) > 3 else 0):
+        r = pick(T)
+        want, bound = _ffn(x[r], xs[r], *[v[i] for v in w[3:]])
+        assert (np.abs(ysh[i][r].double().cpu().numpy() - want) <= bound).all(), i
+
+
+def _force(monkeypatch, shape):
+    """Every layer that is made from now on takes the form for few (1) or for many rows an expert (2)."""
+    made = binding.FMoE
+
+    def of_shape(**kw):
+        m = made(**kw)
+        m.set_ffn_shape(shape)
+        return m
+
+    monkeypatch.setattr(binding, "FMoE", of_shape)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [1, 2])
+@pytest.mark.parametrize("T,d,F", [(3, 64, 32), (130, 288, 96), (40, 1056, 224), (300, 512, 160)])
+def test_rows_of_all_sizes_in_either_form(T, d, F, shape):
+    """Rows as the norm rounds them, with groups and elements of very different sizes among neighbours, so that products are cut."""
+    rng = np.random.default_rng(T + d + shape)
+    m, w = _real_layer(rng, d, 3, F, 1, 64, 2)
+    m.set_ffn_shape(shape)
+    v = rng.standard_normal((T, d)) * np.exp(0.5 * rng.standard_normal((T, 1))) * np.exp2(-rng.integers(0, 12, (T, d)) * (rng.random((T, d)) < 0.5))
+    _check_real(m, w, rng, T, 3, 2, *_quantize(v))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [1, 2])
+def test_every_code_and_scale_in_either_form(shape, monkeypatch):
+    _force(monkeypatch, shape)
+    test_every_code_and_scale()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [1, 2])
+@pytest.mark.parametrize("T", [5, 300])
+def test_nan_reaches_its_own_rows_and_experts_only_in_either_form(T, shape, monkeypatch):
+    _force(monkeypatch, shape)
+    test_nan_reaches_its_own_rows_and_experts_only(T)
+
+
+@pytest.mark.gpu
+def test_many_rows_reach_their_form_unforced():
+    """Sizes that the rule gives to the form for many rows: 300 items of 128 rows and more, 64 rows an expert and more."""
+    rng = np.random.default_rng(77)
+    T, d, E, F, k = 9000, 512, 24, 1408, 2
+    assert T * k >= 64 * E and (E + T * k // 128) * min(-(-F // 128), -(-d // 256)) >= 300
+    m, w = _real_layer(rng, d, E, F, 1, 96, k)
+    codes, scales = _quantize(rng.standard_normal((T, d)))
+    _check_real(m, w, rng, T, E, k, codes, scales, skew=0.5, most=8)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [0, 1, 2])
+@pytest.mark.parametrize("T,k", [(700, 0), (1500, 1)])
+def test_shared_experts_see_far_more_rows_than_the_others(T, k, shape):
+    """Shared experts alone, and beside 64 experts that have a few rows each."""
+    rng = np.random.default_rng(T + shape)
+    m, w = _real_layer(rng, 160, 64, 64, 2, 96, max(k, 1))
+    m.set_ffn_shape(shape)
+    codes, scales = _quantize(rng.standard_normal((T, 160)))
+    if k:
+        _check_real(m, w, rng, T, 64, k, codes, scales, most=6)
+        return
+    m.set_topk(0, 0)
+    x, xs = _as_rows(codes, scales)
+    _, ysh = m.expert_ffn_quant_rows(_gpu(codes), _gpu(scales), None, T, None, None)
+    r = np.r_[0:10, T // 2:T // 2 + 10, T - 10:T]
+    for i in range(2):
+        want, bound = _ffn(x[r], xs[r], *[v[i] for v in w[3:]])
+        assert (np.abs(ysh[i][r].double().cpu().numpy() - want) <= bound).all(), i
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [1, 2])
+def test_norm_router_experts_and_combine_together_in_either_form(shape, monkeypatch):
+    _force(monkeypatch, shape)
+    test_norm_router_experts_and_combine_together(300)
+
+
 @pytest.mark.gpu
 def test_indexes_counts_and_rows_behind():
     """Kept tokens by index, a device count below the capacity, experts without rows, and rows behind the last left alone."""
