@@ -366,9 +366,11 @@ int fmoe_expert_ffn(fmoe_ctx* ctx, const void* x, const int32_t* kept_idx, int32
  * [T, 4 * ceil(d_model / 128)] as fmoe_rms_norm_quant writes them (16- and 4-byte aligned; the bytes behind a row's groups 127).
  * The activation silu(.)*(.) is rounded to 8 bits in the same way (32 neighbouring columns a power of two) between the two
  * products; y and y_shared are bf16, rounded once.  Sums are fp32's.  fmoe_set_ffn_shape chooses between the forms for few (1) and for
- * many rows an expert (2; unforced from 64 on, if the call is large enough) here too.  In the form for few nothing else is lost before the
- * activation is rounded; in the form for many, and in both forms' second product, a product loses what lies below 2^-13 of the largest
- * power of two among eight neighbours', so that hidden values next to a border of two codes may fall to the other one.  A row whose input or activation holds an infinity or
+ * many rows an expert (2; unforced where n_kept * Kmax / E, the room for rows and not their number, is 64 or more and the call is large
+ * enough; shared experts go with the others) here too.  In the form for few no product is cut before the activation is rounded, which is off
+ * by the sums' roundings in fp32 and 2^-20 (1 + |gate|) of its size there; in the form for many, and in both forms' second product, a
+ * product loses what lies below 2^-13 of the largest power of two among eight neighbours'.  So hidden values next to a border of two
+ * codes may fall to the other one.  A row whose input or activation holds an infinity or
  * NaN gives NaN.  Every other argument as in fmoe_expert_ffn; the row limit of kept_idx is 2^32 / d_model tokens. */
 int fmoe_expert_ffn_quant_rows(fmoe_ctx* ctx, const uint8_t* codes, const uint8_t* scales, const int32_t* kept_idx,
                                int32_t n_kept, const int32_t* n_kept_dev, const int32_t* expert_offsets,

@@ -393,8 +393,8 @@ struct DownArgs {
 };
 
 // Workgroups that share 32 output columns.  us a call, 1 / 2 / 4 / 8 of them (in a graph, weights from memory): one token, d 1280, 64 experts
-// of 896, two shared, 4 bits 20.4 / 21.5 / 20.5; d 2048, 64 of 1408, two shared, 4 bits 2 tokens 28.6 / 27.6 / 26.3, 8 tokens
-// 59 / 51 / 47; 16 tokens 79 / 68 / 62 / 64; 128 of 768, bf16 one token 35.7 / 34.9 / 33.3, 8 tokens 94 / 81 / 74 / 76.
+// of 896, two shared, 4 bits 22.2 / 21.7 / 20.4 / 20.5; d 2048, 64 of 1408, two shared, 4 bits 2 tokens 31.3 / 28.0 / 26.8 / 29.3, 8 tokens
+// 59 / 48 / 43 / 46; 16 tokens 84 / 66 / 58 / 60; 128 of 768, bf16 one token 36.8 / 35.1 / 33.6 / 33.7, 8 tokens 100 / 84 / 78 / 81.
 constexpr int SPLITS = 4, DOWN_WAVES = 8;
 
 template <bool QUANT>
@@ -564,8 +564,8 @@ int launch_layer_decode(const fmoe_ctx* ctx, const fmoe_select_params* params, c
   const int pairs = T * ctx->kmax, units = pairs < E ? pairs : E;
   {
     // Column blocks a wavefront.  4 bits, where sixteen rows are more to read than the weights beside them; one / two, us a call: d 2048,
-    // 64 experts of 1408, two shared 4 tokens 32.6 / 33.0, 8 tokens 47.1 / 43.3, 16 tokens 62 / 53; d 1280, 64 of 896 12 tokens
-    // 33.4 / 31.5; 2 tokens 26.3 / 29.7; bf16 weights (four times the bytes): 128 of 768 2 tokens 41.1 / 44.2, 8 tokens 73.6 / 75.0
+    // 64 experts of 1408, two shared 2 tokens 26.6 / 30.1, 4 tokens 32.3 / 33.5, 8 tokens 47.0 / 43.3, 16 tokens 72 / 58; d 1280, 64
+    // of 896 12 tokens 34.6 / 32.7; bf16 weights (four times the bytes): 128 of 768 2 tokens 42.9 / 46.2, 8 tokens 78.2 / 78.4
     const int blocks = g.shared.nbw + units * g.routed.nbw, ncb = ctx->quant && T > 4 ? 2 : 1;
     const dim3 grid((g.shared.nbw + ncb - 1) / ncb + units * ((g.routed.nbw + ncb - 1) / ncb));
     fmoe_prof_scope prof(ctx, SLOT_GEMM1, stream);

@@ -14,8 +14,9 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));   // one 16-byte chunk
 
-// silu(g) * u for values that are rounded to bf16 next: the hardware reciprocal (1 ulp of fp32) instead of
-// the correctly rounded one, a third of the instructions (1.7 % of the gate/up kernel at 2064 rows per expert).
+// silu(g) * u for values that are rounded next, to bf16, 16 or 8 bits: the hardware reciprocal (1 ulp of fp32) instead of
+// the correctly rounded one, a third of the instructions (1.7 % of the gate/up kernel at 2064 rows per expert).  With the
+// hardware's exponential off by 2^-20 (1 + |g|) of its size at most.
 __device__ __forceinline__ float silu_mul_bf16(float g, float u) {
   return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
 }

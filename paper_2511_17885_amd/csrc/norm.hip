@@ -4,7 +4,8 @@
 // Bound: memory.  A wavefront has a row in registers (up to 4096 elements; a workgroup of four wavefronts has one of up to 16384,
 // or where there are few rows), reads it once and writes its outputs once.  22016 rows of 2048 in bf16: 58 us, 6.2 TB/s (a copy of
 // 1 GiB 5.2); gradient 68 us with the sums of the weight's; 8192 rows to 8 bits 26.8 us, 4.4 TB/s: some 25 vector instructions an
-// element for the exact rounding beside the loads.
+// element for the exact rounding beside the loads.  (Called again and again, so that outputs are where the last call's were, which the
+// memory-side cache still has in part; four sets of inputs and outputs in turn, as below: 68 us for the first of these.)
 
 #include "norm_dev.h"
 #include "rows8_dev.h"
@@ -255,10 +256,10 @@ bool passes(size_t bytes) { return bytes >= ((size_t)100 << 20); }
 
 // Wavefronts a row: all four of a workgroup for rows that one cannot hold, and where rows of more than 128 units are few.  us with one / four:
 // bf16, d 2048, 4096 rows 15.5 / 14.2, in 8 bits 18.9 / 15.9, 2048 rows 11.5 / 10.2, 600 rows 6.9 / 5.4; d 1280 100 rows 5.5 / 4.4; d 1288 in
-// fp32 1601 rows 9.7 / 9.6; d 1024 4096 rows 10.3 / 11.0, in 8 bits 11.7 / 13.1; d 512 3000 rows 5.6 / 7.7.
+// fp32 1601 rows 9.7 / 9.6; d 1024 4096 rows 10.3 / 11.0, in 8 bits 11.7 / 13.1; d 512 3000 rows 5.6 / 7.7.  (The figures end at d 2048.)
 int waves_per_row(int T, int d) { return d > 4096 || (d > 1024 && T <= 4096) ? 4 : 1; }
 // The gradient, with two sums a row between which four wavefronts would wait for each other: d 2048 bf16 22016 rows 69.8 / 86.7, 4096 rows
-// 20.5 / 21.9, 200 rows 8.3 / 8.2; d 1280 in fp32 600 rows 10.2 / 11.5.
+// 20.5 / 21.9, 200 rows 8.3 / 8.2; d 1280 in fp32 600 rows 10.2 / 11.5, 1600 rows 14.6 / 13.9.  (The figures end at d 2048.)
 int waves_per_gradient(int d) { return d > 4096 ? 4 : 1; }
 
 template <typename XT, typename WT, bool ROWS8>
