@@ -321,21 +321,30 @@ class _Workspace:
     of graphs captured from them, need an order between them (or an object each)."""
 
     _ws = _ws_stream = None
-    _ws_kept = False     # a graph, or work on another stream than the tensor's own, may have its address
-    _outgrown = ()
+    _ws_captured = False   # a graph has its address
+    _ws_streams = _outgrown = ()
 
     def _room(self, need, device):
-        """At least `need` bytes.  A captured graph writes to the address it was captured with at every replay: what it, or another
-        stream, has seen stays when it is outgrown, as long as the object does."""
+        """At least `need` bytes.  A captured graph writes to the address it was captured with at every replay: what a capture has seen
+        stays when it is outgrown, as long as the object does.  Else it is freed behind the work of every stream that has used it."""
         stream, capturing = _stream_of(device)
         if self._ws is None or self._ws.numel() < need:
-            if self._ws is not None and (self._ws_kept or self._ws_stream is None):
+            if self._ws is not None and (self._ws_captured or self._ws_stream is None):
                 self._outgrown = (*self._outgrown, self._ws)
+            for other in self._ws_streams:
+                _used_by(self._ws, other, device)
             self._ws = torch.empty(need, dtype=torch.uint8, device=device)
-            self._ws_stream, self._ws_kept = stream, capturing
-        elif capturing or stream != self._ws_stream:
-            self._ws_kept = True
+            self._ws_stream, self._ws_captured, self._ws_streams = stream, capturing, ()
+        else:
+            self._ws_captured |= capturing
+            if stream != self._ws_stream and stream not in self._ws_streams:
+                self._ws_streams = (*self._ws_streams, stream)
         return self._ws
+
+
+def _used_by(t, stream, device):
+    """The tensor's memory is not given to others before the work that the stream has now is done."""
+    t.record_stream(torch.cuda.ExternalStream(stream, device=device))
 
 
 def _stream_of(device):

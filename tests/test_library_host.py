@@ -446,21 +446,25 @@ def test_dense_deal_meets_every_item_once(deal, n, n_several, run_len, cols):
         assert singles.value == (n - n_several) * cols
 
 
-def test_an_outgrown_workspace_stays_where_a_graph_or_another_stream_may_use_it(monkeypatch):
-    """Growth on the host: what a captured call or one on another stream has seen is kept, what one stream alone has used is not."""
+def test_an_outgrown_workspace_stays_where_a_graph_may_use_it_and_waits_for_other_streams(monkeypatch):
+    """Growth on the host: what a captured call has seen is kept, what another stream has used is freed behind that stream's work."""
     import torch
     now = {"stream": 1, "capturing": False}
     monkeypatch.setattr(binding, "_stream_of", lambda device: (now["stream"], now["capturing"]), raising=False)
+    waits = []
+    monkeypatch.setattr(binding, "_used_by", lambda t, stream, device: waits.append((t.numel(), stream)), raising=False)
     sizes = {1: 100, 2: 200, 3: 300, 4: 400, 5: 500}
 
     def outgrown(cls, calls):
-        """Whether the workspace of each of the calls (stream, capturing, size) is still held after all of them."""
+        """Whether the workspace of each of the calls (stream, capturing, size) is still held after all of them; which wait for which
+        stream before they are freed."""
         import gc
         import weakref
         m = object.__new__(cls)
         m._ctx, m._ws, m.device = None, None, torch.device("cpu")
         m.workspace_bytes = lambda tokens, seqs=1: sizes[tokens]
         seen = []
+        waits.clear()
         for now["stream"], now["capturing"], tokens in calls:
             ws = m.workspace(tokens) if cls is binding.FMoE else m._room(sizes[tokens], m.device)
             assert ws.numel() >= sizes[tokens] and ws is m._ws
@@ -473,9 +477,11 @@ def test_an_outgrown_workspace_stays_where_a_graph_or_another_stream_may_use_it(
         assert outgrown(cls, [(1, False, 1), (1, False, 2), (1, False, 3)]) == [False, False, True]
         assert outgrown(cls, [(1, True, 1), (1, False, 2), (1, False, 3)]) == [True, False, True]      # captured as it was made
         assert outgrown(cls, [(1, False, 2), (2, True, 1), (1, False, 3)]) == [True, True, True]       # captured with one of before
-        assert outgrown(cls, [(1, False, 1), (2, False, 1), (1, False, 2), (1, False, 4)]) == [True, True, False, True]
+        assert waits == [(200, 2)]
+        assert outgrown(cls, [(1, False, 1), (2, False, 1), (3, False, 1), (2, False, 1), (1, False, 2), (1, False, 4)]) == [False] * 5 + [True]
+        assert waits == [(100, 2), (100, 3)]
         assert outgrown(cls, [(1, True, t) for t in (1, 2, 3, 4, 5)]) == [True] * 5
-        assert outgrown(cls, [(1, False, 1), (2, False, 2), (2, False, 3)]) == [False, False, True]
+        assert outgrown(cls, [(1, False, 1), (2, False, 2), (2, False, 3)]) == [False, False, True] and waits == []
 
 
 def test_layer_decode_uses_the_workspace_that_grows(monkeypatch):
