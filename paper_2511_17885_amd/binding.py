@@ -344,7 +344,8 @@ class _Workspace:
 
 def _used_by(t, stream, device):
     """The tensor's memory is not given to others before the work that the stream has now is done."""
-    t.record_stream(torch.cuda.ExternalStream(stream, device=device))
+    # (a null handle given to ExternalStream is none to it: it makes another stream)
+    t.record_stream(torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device))
 
 
 def _stream_of(device):
